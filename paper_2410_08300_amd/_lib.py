@@ -47,6 +47,47 @@ class Desc(ctypes.Structure):
                 ("has_bias", ctypes.c_int32), ("fuse_relu", ctypes.c_int32)]
 
 
+EXPORTED_LM = ("convsel_linear_workspace_bytes", "convsel_linear", "convsel_linear_describe", "convsel_qk_norm_rope",
+               "convsel_kv_cache_bytes", "convsel_kv_write", "convsel_kv_read", "convsel_attention_workspace_bytes",
+               "convsel_attention", "convsel_attention_describe")
+
+
+class LinearDesc(ctypes.Structure):
+    """convsel_linear_desc_t."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("m", "in_features", "out_features", "ldx", "ldr", "ldy")]
+                + [(n, ctypes.c_int32) for n in ("dtype", "act", "has_bias", "has_residual")])
+
+
+class QkDesc(ctypes.Structure):
+    """convsel_qk_desc_t."""
+    _fields_ = ([("tokens", ctypes.c_int64)]
+                + [(n, ctypes.c_int32) for n in ("q_heads", "k_heads", "head_dim", "rotary_dim")]
+                + [(n, ctypes.c_int64) for n in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                                                 "q_out_token_stride", "q_out_head_stride", "k_out_token_stride",
+                                                 "k_out_head_stride", "max_position")]
+                + [(n, ctypes.c_int32) for n in ("dtype", "norm", "interleaved")] + [("eps", ctypes.c_float)])
+
+
+class KvCacheDesc(ctypes.Structure):
+    """convsel_kv_cache_t."""
+    _fields_ = ([("pages", ctypes.c_int64)]
+                + [(n, ctypes.c_int32) for n in ("kv_heads", "head_dim", "page_size", "format")]
+                + [(n, ctypes.c_void_p) for n in ("k_codes", "v_codes", "k_scales", "v_scales")])
+
+
+class KvBatchDesc(ctypes.Structure):
+    """convsel_kv_batch_t."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("seqs", "tokens", "table_width")]
+                + [(n, ctypes.c_void_p) for n in ("table", "lengths", "offsets")])
+
+
+class AttentionDesc(ctypes.Structure):
+    """convsel_attention_desc_t."""
+    _fields_ = ([(n, ctypes.c_int32) for n in ("q_heads", "dtype", "causal", "window")] + [("scale", ctypes.c_float)]
+                + [(n, ctypes.c_int64) for n in ("q_token_stride", "q_head_stride", "y_token_stride",
+                                                 "y_head_stride")])
+
+
 class Conv2dError(RuntimeError):
     """A non-OK status from the library; ``status`` holds the code."""
 
@@ -135,6 +176,22 @@ def lib():
         for n in EXPORTED_MODEL:
             if n != "convsel_model_destroy":
                 getattr(L, n).restype = i32
+        # decoder operators (include/convsel_lm.h)
+        lp, qp, cp, bp, ap = (ctypes.POINTER(t) for t in (LinearDesc, QkDesc, KvCacheDesc, KvBatchDesc,
+                                                          AttentionDesc))
+        sp = ctypes.POINTER(ctypes.c_size_t)
+        L.convsel_linear_workspace_bytes.argtypes = [lp, sp]
+        L.convsel_linear.argtypes = [vp, vp, vp, vp, vp, lp, vp, ctypes.c_size_t, vp]
+        L.convsel_linear_describe.argtypes = [lp, ctypes.c_char_p, ctypes.c_size_t]
+        L.convsel_qk_norm_rope.argtypes = [vp] * 9 + [qp, vp]
+        L.convsel_kv_cache_bytes.argtypes = [cp, sp]
+        L.convsel_kv_write.argtypes = [cp, bp, vp, vp, i64, i64, i64, i64, ctypes.c_int32, vp]
+        L.convsel_kv_read.argtypes = [cp, bp, vp, vp, ctypes.c_int32, vp]
+        L.convsel_attention_workspace_bytes.argtypes = [cp, bp, ap, sp]
+        L.convsel_attention.argtypes = [vp, cp, bp, vp, ap, vp, ctypes.c_size_t, vp]
+        L.convsel_attention_describe.argtypes = [cp, bp, ap, ctypes.c_char_p, ctypes.c_size_t]
+        for n in EXPORTED_LM:
+            getattr(L, n).restype = i32
         _lib = L
     return _lib
 

@@ -696,4 +696,7 @@ conv_status_t conv2d_prepacked_residual(const void* x, const void* packed, const
   return from_hip(launch_implicit_main(s, x, packed, b, y, workspace, (hipStream_t)stream, res));
 }
 
+// For the decoder operators' entry points: a current device that is gfx950.
+conv_status_t device_ready() { return ensure_device(); }
+
 }  // namespace convsel

@@ -1,0 +1,70 @@
+// Device-side helpers of the decoder operators: 8-bit codes, the sequences of
+// a call and cache addresses.
+#pragma once
+
+#include "../../include/convsel_lm.h"
+#include "common.hpp"
+
+namespace convsel {
+namespace lm {
+
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr float kMinScale = 7.888609052210118e-31f;  // 2^-100
+
+__device__ __forceinline__ int clampi(int v, int lo, int hi) { return v < lo ? lo : (v > hi ? hi : v); }
+
+// A sequence's packed tokens, bounded by the call's.
+struct Span {
+  int first, count;
+};
+__device__ __forceinline__ Span span_of(const int32_t* offsets, int64_t b, int tokens) {
+  const int lo = clampi(offsets[b], 0, tokens);
+  const int hi = clampi(offsets[b + 1], lo, tokens);
+  return {lo, hi - lo};
+}
+
+// Value that a code stands for, before its scale.
+__device__ __forceinline__ float decode(uint32_t byte, int format) {
+  if (format == CONVSEL_KV_INT8) return static_cast<float>(static_cast<int8_t>(byte));
+  return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(byte), 0);
+}
+
+// Code of x in a block of scale s: the fp32 quotient, rounded to nearest even.
+__device__ __forceinline__ uint32_t encode(float x, float s, int format) {
+  float t = x / s;
+  t = t != t ? 0.f : t;
+  if (format == CONVSEL_KV_INT8) {
+    t = fminf(fmaxf(t, -127.f), 127.f);
+    return static_cast<uint32_t>(static_cast<int>(rintf(t))) & 0xffu;
+  }
+  t = fminf(fmaxf(t, -448.f), 448.f);
+  return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(t, t, 0, false)) & 0xffu;
+}
+
+__device__ __forceinline__ float qmax_of(int format) { return format == CONVSEL_KV_INT8 ? 127.f : 448.f; }
+
+// Byte of value code (t, d) within a page and head.
+__device__ __forceinline__ int v_byte(int t, int d, int dp) {
+  return (t & ~15) * dp + (((t & 15) >> 2) * 16 + (d & 15)) * (dp >> 2) + (d >> 4) * 4 + (t & 3);
+}
+
+template <typename T>
+__device__ __forceinline__ float activate(float z, int act) {
+  constexpr bool exact = sizeof(T) == 4;  // fp32 outputs show the last bits of exp and the quotient
+  switch (act) {
+    case CONVSEL_ACT_RELU: return z < 0.f ? 0.f : z;  // NaN stays
+    case CONVSEL_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case CONVSEL_ACT_GELU_TANH: {
+      // (1 + tanh u) / 2 = 1 / (1 + exp(-2u))
+      const float u2 = -1.5957691216057308f * (z + 0.044715f * z * z * z);
+      return exact ? z / (1.f + expf(u2)) : z * __frcp_rn(1.f + __expf(u2));
+    }
+    case CONVSEL_ACT_SILU: return exact ? z / (1.f + expf(-z)) : z * __frcp_rn(1.f + __expf(-z));
+    default: return z;
+  }
+}
+
+}  // namespace lm
+}  // namespace convsel
