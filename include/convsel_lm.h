@@ -143,7 +143,7 @@ typedef struct convsel_kv_cache {
 typedef struct convsel_kv_batch {
   int64_t seqs;
   int64_t tokens;          /* packed tokens of the call */
-  int64_t table_width;     /* pages a sequence may have; * page_size < 2^31 */
+  int64_t table_width;     /* pages a sequence may have; * page_size <= 2^30 */
   const int32_t* table;    /* seqs x table_width */
   const int32_t* lengths;  /* seqs: what it means is said at each call */
   const int32_t* offsets;  /* seqs + 1 */
@@ -187,7 +187,7 @@ conv_status_t convsel_kv_read(const convsel_kv_cache_t* cache, const convsel_kv_
  * nothing is zero.  What lies in masked places (rows never written, pages
  * handed back) has no influence, whatever bits it holds. */
 typedef struct convsel_attention_desc {
-  int32_t q_heads;
+  int32_t q_heads; /* tokens * q_heads < 2^31 */
   int32_t dtype;   /* of q and y */
   int32_t causal;
   int32_t window;  /* 0: none */

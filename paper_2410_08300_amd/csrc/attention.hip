@@ -1,4 +1,20 @@
 // Attention of new queries over the 8-bit paged cache.
+//
+// Mathematics.  With codes K, V and one scale a block of tokens, a query's score
+// is s_j = scale * ks * (q . K_j) and its result sum_j e^(s_j) vs V_j / sum_j
+// e^(s_j).  Everything runs in powers of two (scale carries log2 e).  vs = vf *
+// 2^ve; the running maximum M is a whole number of at least s_j + ve (so that
+// M - ve is exact), and
+//   u_j = 2^(s_j + ve - M)
+//   result = sum_j (u_j vf) V_j / sum_j u_j 2^-ve
+// holds the largest weight times its value scale near one: a page of small
+// values may hold the weight, and no scale overflows.  Scales reach from 2^-100
+// to 2^121, so a change of M is an exponent added, and where u would leave fp32
+// (scales 2^100 apart within a row) the sum's terms are formed without it.
+// Weights go to the matrix cores in 11 bits, 2^15 times as large (their
+// steps are then 2^-39 of the largest); codes are exact in them.  fp32 calls hold queries and weights as
+// two such numbers, 22 bits.  Queries are brought to [2^14, 2^15) by a power of
+// two, which bf16 survives exactly.  Sums and statistics are fp32.
 #include <stdio.h>
 
 #include "lm_common.hpp"
@@ -9,85 +25,517 @@ namespace {
 
 using namespace lm;
 
-// One wave per (query, head): the running maximum and sum of the softmax over
-// the keys one by one, four head columns a lane.
-template <typename T>
-__global__ __launch_bounds__(64) void attention_row_kernel(const T* q, convsel_kv_cache_t c, convsel_kv_batch_t b,
-                                                           T* y, convsel_attention_desc_t a) {
-  const int lane = threadIdx.x, seq = blockIdx.z, hq = blockIdx.y;
-  const int head = hq / (a.q_heads / c.kv_heads);
-  const Span sp = span_of(b.offsets, seq, static_cast<int>(b.tokens));
-  const int ps = c.page_size, D = c.head_dim, dp = kv_row_bytes(D);
-  const int64_t len = b.lengths[seq];
-  const int64_t limit = min(len, b.table_width * ps);
-  for (int i = blockIdx.x; i < sp.count; i += gridDim.x) {
-    const int64_t p = len - sp.count + i;
-    int64_t lo = 0, hi = limit;
-    if (a.causal) hi = min(hi, p + 1);
-    if (a.window > 0) lo = max(lo, p - a.window + 1);
-    float qv[4], o[4] = {0.f, 0.f, 0.f, 0.f};
-    const T* qr = q + static_cast<int64_t>(sp.first + i) * a.q_token_stride + hq * a.q_head_stride;
-    for (int u = 0; u < 4; ++u) qv[u] = lane + 64 * u < D ? elem<T>::load(qr + lane + 64 * u) : 0.f;
-    float m = -__builtin_inff(), l = 0.f;
-    for (int64_t j = lo; j < hi; ++j) {
-      const int64_t page = b.table[seq * b.table_width + j / ps];
-      if (page < 0 || page >= c.pages) continue;
-      const int t = static_cast<int>(j % ps);
-      const int64_t ph = page * c.kv_heads + head;
-      const uint8_t* kc = reinterpret_cast<const uint8_t*>(c.k_codes) + ph * (ps * dp);
-      const uint8_t* vc = reinterpret_cast<const uint8_t*>(c.v_codes) + ph * (ps * dp);
-      float s = 0.f;
-      for (int u = 0; u < 4; ++u)
-        if (lane + 64 * u < D) s += qv[u] * decode(kc[t * dp + lane + 64 * u], c.format);
+typedef float f32x4v_t __attribute__((ext_vector_type(4)));
+
+struct AttnArgs {
+  int64_t pages, table_width;
+  int64_t q_token, q_head, y_token, y_head;
+  int tokens, kv_heads, group, dim, ps_shift, causal, window, nsplit, tiles;
+  float scale;  // times log2 e
+};
+
+// Rows of keys a query sees: [lo, hi).
+struct Range {
+  int lo, hi;
+};
+
+// Sixteen tokens of one page: a lane's part of their key and value codes.
+template <int NC>
+struct Block {
+  uint32_t k[2 * NC], v[2 * NC];
+  float ks, vs;
+};
+
+template <int NC>
+__device__ __forceinline__ void load_codes(uint32_t* dst, const uint8_t* src) {
+  if constexpr (NC % 2 == 0) {
 #pragma unroll
-      for (int x = 32; x > 0; x >>= 1) s += __shfl_xor(s, x);
-      // The maximum runs over weight times value scale, so that a page of small values may hold the weight.  It and
-      // the scale's exponent are whole numbers: their difference is exact, and the fused product rounds once.
-      int ve;
-      const float vf = frexpf(c.v_scales[ph], &ve);
-      const float sk = s * c.k_scales[ph], c2 = a.scale * 1.4426950408889634f;
-      const float mn = fmaxf(m, ceilf(sk * c2) + ve);
-      const float f = exp2f(m - mn), u2 = exp2f(fmaf(sk, c2, ve - mn)), ev = u2 * vf;
-      l = l * f + ldexpf(u2, -ve);
-      m = mn;
-      for (int u = 0; u < 4; ++u)
-        if (lane + 64 * u < D) o[u] = o[u] * f + ev * decode(vc[v_byte(t, lane + 64 * u, dp)], c.format);
+    for (int i = 0; i < NC / 2; ++i) {
+      const uint4 u = reinterpret_cast<const uint4*>(src)[i];
+      dst[4 * i] = u.x; dst[4 * i + 1] = u.y; dst[4 * i + 2] = u.z; dst[4 * i + 3] = u.w;
     }
-    T* yr = y + static_cast<int64_t>(sp.first + i) * a.y_token_stride + hq * a.y_head_stride;
-    const float inv = l != 0.f ? 1.f / l : 0.f;
-    for (int u = 0; u < 4; ++u)
-      if (lane + 64 * u < D) elem<T>::store(yr + lane + 64 * u, o[u] * inv);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const uint2 u = reinterpret_cast<const uint2*>(src)[i];
+      dst[2 * i] = u.x; dst[2 * i + 1] = u.y;
+    }
+  }
+}
+
+// Four codes as 16-bit floats, exactly.
+template <int FMT>
+__device__ __forceinline__ void widen4(uint32_t w, f16x2_t& lo, f16x2_t& hi) {
+  if constexpr (FMT == CONVSEL_KV_INT8) {
+    // 1024 + (code + 128) has the code's byte as its lowest bits.
+    const uint32_t u = w ^ 0x80808080u;
+    const f16x2_t off = {static_cast<_Float16>(-1152.f), static_cast<_Float16>(-1152.f)};
+    lo = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + off;
+    hi = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + off;
+  } else {
+    lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false);
+    hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true);
+  }
+}
+
+template <int FMT>
+__device__ __forceinline__ f16x8_t widen8(uint32_t a, uint32_t b) {
+  f16x2_t p[4];
+  widen4<FMT>(a, p[0], p[1]);
+  widen4<FMT>(b, p[2], p[3]);
+  f16x8_t r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[2 * i] = p[i][0];
+    r[2 * i + 1] = p[i][1];
+  }
+  return r;
+}
+
+__device__ __forceinline__ f32x4v_t mfma16(const f16x8_t& a, const f16x8_t& b, const f32x4v_t& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+constexpr float kWeight = 0x1p15f;  // weights as the matrix cores take them, and back
+constexpr float kResult = 0x1p-15f;
+constexpr float kFar = -100.f;      // exponents of u below this are near the end of fp32
+
+// Exponent to add to what was kept at maximum `from`, now at `to` >= from.
+__device__ __forceinline__ int shift_of(float from, float to) {
+  return from == to ? 0 : static_cast<int>(fmaxf(from - to, -300.f));
+}
+
+// Power of two that brings magnitudes up to amax under 2^15.
+__device__ __forceinline__ int query_exponent(float amax) {
+  int e = 0;
+  if (amax > 0.f && amax < __builtin_inff()) frexpf(amax, &e);
+  return e - 15;
+}
+
+// ---------------------------------------------------------------------------
+// Few query rows: one workgroup of four waves per (16 rows, key head, part of
+// the keys).  A row is a query of the sequence and one of the heads that share
+// the key head.  Wave w takes every fourth pair of 16-token blocks, keeps its
+// own maximum, sums and result, and the four are joined in LDS at the end; the
+// parts of a split axis are joined by attention_join_kernel.
+//
+// Scores are computed as K q^T: a lane of the 16 x 16 x 32 product then holds
+// four neighbouring tokens of one query, and in the order in which V lies in
+// the cache those are the weights that the second product wants from it: no
+// value is moved between lanes, and codes go from memory to the matrix cores
+// through registers alone.
+// ---------------------------------------------------------------------------
+template <typename T, int FMT, int NC>
+__global__ __launch_bounds__(256) void attention_rows_kernel(
+    const T* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
+    const float* __restrict__ ks, const float* __restrict__ vs, const int32_t* __restrict__ table,
+    const int32_t* __restrict__ lengths, const int32_t* __restrict__ offsets, T* __restrict__ y,
+    float* __restrict__ part, float* __restrict__ stat, AttnArgs a) {
+  constexpr bool TWO = sizeof(T) == 4;
+  constexpr int DP = 32 * NC, DT = 2 * NC, LB = DP / 4;  // row bytes, 16-column tiles, bytes of a lane
+  __shared__ float so[4][16][DP + 4];
+  __shared__ float sm[4][16], sl[4][16];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, g = lane >> 4;
+  const int seq = blockIdx.z, head = blockIdx.y;
+  const Span sp = span_of(offsets, seq, a.tokens);
+  const int rows = sp.count * a.group;
+  const int split = blockIdx.x % a.nsplit;
+  const int64_t len = lengths[seq];
+  const int limit = static_cast<int>(max((int64_t)0, min(len, a.table_width << a.ps_shift)));
+  const int32_t* my_table = table + seq * a.table_width;
+
+  for (int tile = blockIdx.x / a.nsplit; tile * 16 < rows; tile += a.tiles) {
+    // This lane's query row, and what the tile's rows see between them.
+    const int row = min(tile * 16 + col, rows - 1);
+    const int tok = row / a.group;
+    const int64_t first = len - sp.count;  // position of the sequence's first query
+    int lo = 0, hi = limit;
+    {
+      const int tok0 = tile * 16 / a.group, tok1 = min(tile * 16 + 15, rows - 1) / a.group;
+      if (a.causal) hi = static_cast<int>(max((int64_t)0, min((int64_t)hi, first + tok1 + 1)));
+      if (a.window > 0) lo = static_cast<int>(max((int64_t)0, first + tok0 - a.window + 1));
+    }
+    const int64_t p = first + tok;
+    const int row_hi = a.causal ? static_cast<int>(max((int64_t)0, min((int64_t)hi, p + 1))) : hi;
+    const int row_lo = a.window > 0 ? static_cast<int>(max((int64_t)0, min((int64_t)hi, p - a.window + 1))) : 0;
+    const int b0 = lo >> 4, b1 = hi > lo ? (hi + 15) >> 4 : b0;
+    const int pairs = (b1 - b0 + 1) >> 1;
+    const int per = (pairs + a.nsplit - 1) / a.nsplit;
+    const int pair0 = split * per, pair1 = min(pairs, pair0 + per);
+
+    // The query row, as the second operand: lane (row, g) holds columns
+    // g * LB + 8 c + 0..7, the columns that lane (token, g) loads of a key.
+    f16x8_t qh[NC], ql[TWO ? NC : 1];
+    float cs;
+    {
+      const T* src = q + (sp.first + tok) * a.q_token +
+                     (static_cast<int64_t>(head) * a.group + row % a.group) * a.q_head;
+      float qv[NC][8], amax = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int d = g * LB + 8 * c + j;
+          qv[c][j] = d < a.dim ? elem<T>::load(src + (d < a.dim ? d : 0)) : 0.f;
+          amax = fmaxf(amax, fabsf(qv[c][j]));
+        }
+      amax = fmaxf(amax, __shfl_xor(amax, 16));
+      amax = fmaxf(amax, __shfl_xor(amax, 32));
+      const int e = query_exponent(amax);
+      cs = ldexpf(a.scale, e);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float v = ldexpf(qv[c][j], -e);
+          qh[c][j] = static_cast<_Float16>(v);
+          if constexpr (TWO) ql[c][j] = static_cast<_Float16>(v - static_cast<float>(qh[c][j]));
+        }
+    }
+
+    f32x4v_t o[DT];
+#pragma unroll
+    for (int i = 0; i < DT; ++i) o[i] = f32x4v_t{0.f, 0.f, 0.f, 0.f};
+    float m = -__builtin_inff(), l = 0.f;
+
+    // Page of block b, -1 where there is none.
+    auto page_of = [&](int b) -> int {
+      if (b >= b1) return -1;
+      const int pg = my_table[b >> (a.ps_shift - 4)];
+      return pg >= 0 && pg < a.pages ? pg : -1;
+    };
+    auto load = [&](Block<NC>& r, int b, int pg) {
+      const int64_t ph = static_cast<int64_t>(pg < 0 ? 0 : pg) * a.kv_heads + head;
+      const int t0 = (b & ((1 << (a.ps_shift - 4)) - 1)) << 4;
+      const int64_t at = ((ph << a.ps_shift) + t0) * DP;
+      load_codes<NC>(r.k, kc + at + col * DP + g * LB);
+      load_codes<NC>(r.v, vc + at + lane * LB);
+      r.ks = ks[ph];
+      r.vs = vs[ph];
+    };
+    auto compute = [&](Block<NC> (&r)[2], int pair, int pg0, int pg1) {
+      const int pgs[2] = {pg0, pg1};
+      float sc[2][4];
+      float top = -__builtin_inff();
+      int ve[2];
+      float vf[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int j0 = (b0 + 2 * pair + i) << 4;
+        const bool there = pgs[i] >= 0;
+        f32x4v_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const f16x8_t kf = widen8<FMT>(r[i].k[2 * c], r[i].k[2 * c + 1]);
+          acc = mfma16(kf, qh[c], acc);
+          if constexpr (TWO) acc = mfma16(kf, ql[c], acc);
+        }
+        vf[i] = frexpf(there ? r[i].vs : 1.f, &ve[i]);
+        const float f = (there ? r[i].ks : 0.f) * cs;
+        const bool whole = there && j0 >= lo && j0 + 16 <= hi && (!a.causal || j0 + 15 <= first + tile * 16 / a.group) &&
+                           a.window == 0;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int j = j0 + 4 * g + x;
+          const float s = acc[x] * f;
+          sc[i][x] = whole || (there && j >= row_lo && j < row_hi) ? s : -__builtin_inff();
+          top = fmaxf(top, ceilf(sc[i][x]) + ve[i]);
+        }
+        // Rows never written may hold any bits; a weight of zero does not silence a NaN code.
+        if (!there || j0 + 16 > limit) {
+          const int n = there ? clampi(limit - j0 - 4 * g, 0, 4) : 0;
+          const uint32_t keep = n >= 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
+#pragma unroll
+          for (int d = 0; d < DT; ++d) r[i].v[d] &= keep;
+        }
+      }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (__any(top > m)) {
+        const float mn = fmaxf(m, top);
+        const int dm = shift_of(m, mn);
+        m = mn;
+        l = ldexpf(l, dm);
+        const float f = ldexpf(1.f, dm);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] *= f;
+      }
+      f16x8_t wh, wl;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float sum = 0.f;
+        const float vd = vf[i] * kWeight, up = ve[i] - m;
+        float tmax = -__builtin_inff();
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          // Scores are finite or -inf here (or NaN, which stays); m is finite once any score is.
+          const float t = sc[i][x] == -__builtin_inff() ? -__builtin_inff() : sc[i][x] + up;
+          tmax = fmaxf(tmax, t);
+          const float u = __builtin_amdgcn_exp2f(t);
+          sum += u;
+          float w = u * vd;
+          // One rounded w: the compiler would fuse the product into one of the two conversions below only, and
+          // the second would then miss by a step where the first fell the other way.
+          if constexpr (TWO) asm volatile("" : "+v"(w));
+          wh[4 * i + x] = static_cast<_Float16>(w);
+          if constexpr (TWO) wl[4 * i + x] = static_cast<_Float16>(w - static_cast<float>(wh[4 * i + x]));
+        }
+        if (__any(tmax < kFar && tmax > -__builtin_inff())) {
+          sum = 0.f;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const float n = rintf(sc[i][x]);
+            if (sc[i][x] > -__builtin_inff())
+              sum += ldexpf(__builtin_amdgcn_exp2f(sc[i][x] - n), static_cast<int>(fmaxf(n - m, -300.f)));
+          }
+          l += sum;
+        } else {
+          l += ldexpf(sum, -ve[i]);
+        }
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const f16x8_t vf8 = widen8<FMT>(r[0].v[d], r[1].v[d]);
+        o[d] = mfma16(vf8, wh, o[d]);
+        if constexpr (TWO) o[d] = mfma16(vf8, wl, o[d]);
+      }
+    };
+
+    {
+      Block<NC> ra[2], rb[2];
+      int pa[2], pb[2];
+      auto fetch = [&](Block<NC> (&r)[2], int (&pg)[2], int pair) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) load(r[i], b0 + 2 * pair + i, pg[i]);
+      };
+      auto look = [&](int (&pg)[2], int pair) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) pg[i] = pair < pair1 ? page_of(b0 + 2 * pair + i) : -1;
+      };
+      int pair = pair0 + wave;
+      if (pair < pair1) {
+        look(pa, pair);
+        look(pb, pair + 4);
+        fetch(ra, pa, pair);
+        for (; pair < pair1; pair += 8) {
+          int pn[2];
+          if (pair + 4 < pair1) fetch(rb, pb, pair + 4);
+          look(pn, pair + 8);
+          compute(ra, pair, pa[0], pa[1]);
+          pa[0] = pn[0]; pa[1] = pn[1];
+          if (pair + 4 >= pair1) break;
+          if (pair + 8 < pair1) fetch(ra, pa, pair + 8);
+          look(pn, pair + 12);
+          compute(rb, pair + 4, pb[0], pb[1]);
+          pb[0] = pn[0]; pb[1] = pn[1];
+        }
+      }
+    }
+
+    // Join the four waves.
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) {
+      sm[wave][col] = m;
+      sl[wave][col] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4v_t*>(&so[wave][col][16 * d + 4 * g]) = o[d];
+    __syncthreads();
+    const int r = threadIdx.x >> 4, d0 = threadIdx.x & 15;  // 16 threads a row
+    float mt = sm[0][r];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) mt = fmaxf(mt, sm[w][r]);
+    float f[4], lt = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int dm = shift_of(sm[w][r], mt);
+      f[w] = ldexpf(1.f, dm);
+      lt += ldexpf(sl[w][r], dm);
+    }
+    if (tile * 16 + r < rows) {
+      const int rt = (tile * 16 + r) / a.group, rh = (tile * 16 + r) % a.group;
+      const int64_t h = static_cast<int64_t>(head) * a.group + rh;
+      if (a.nsplit == 1) {
+        T* dst = y + (sp.first + rt) * a.y_token + h * a.y_head;
+        const float inv = lt == 0.f ? 0.f : kResult / lt;
+        for (int d = d0; d < a.dim; d += 16) {
+          float v = 0.f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) v += so[w][r][d] * f[w];
+          elem<T>::store(dst + d, v * inv);
+        }
+      } else {
+        const int64_t at = ((sp.first + rt) * static_cast<int64_t>(a.kv_heads) * a.group + h) * a.nsplit + split;
+        for (int d = d0; d < a.dim; d += 16) {
+          float v = 0.f;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) v += so[w][r][d] * f[w];
+          part[at * a.dim + d] = v;
+        }
+        if (d0 == 0) {
+          stat[2 * at] = mt;
+          stat[2 * at + 1] = lt;
+        }
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the parts of a split axis: one wave per (token, head) that a sequence owns.
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join_kernel(const float* __restrict__ part,
+                                                             const float* __restrict__ stat,
+                                                             const int32_t* __restrict__ offsets, int seqs,
+                                                             T* __restrict__ y, AttnArgs a) {
+  const int heads = a.kv_heads * a.group;
+  const int lane = threadIdx.x & 63;
+  const int64_t it = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  const int64_t t = it / heads;
+  // Rising offsets from 0: the tokens behind the last one belong to nobody.
+  if (t >= clampi(offsets[seqs], 0, a.tokens)) return;
+  const int64_t h = it % heads;
+  float m = -__builtin_inff();
+  for (int s = lane; s < a.nsplit; s += 64) m = fmaxf(m, stat[2 * (it * a.nsplit + s)]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.nsplit; ++s) {
+    const float ms = stat[2 * (it * a.nsplit + s)];
+    const int dm = shift_of(ms, m);
+    const float f = ldexpf(1.f, dm);
+    l += ldexpf(stat[2 * (it * a.nsplit + s) + 1], dm);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int d = lane + 64 * u;
+      if (d < a.dim) v[u] += part[(it * a.nsplit + s) * a.dim + d] * f;
+    }
+  }
+  const float inv = l == 0.f ? 0.f : kResult / l;
+  T* dst = y + t * a.y_token + h * a.y_head;
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int d = lane + 64 * u;
+    if (d < a.dim) elem<T>::store(dst + d, v[u] * inv);
+  }
+}
+
+// How a call is cut: rows of 16, and parts of the keys.  The host knows how
+// many tokens the call has and how many a sequence may hold, not how they are
+// spread; every count below only sets the grid, kernels walk what there is.
+struct Plan {
+  int tiles, nsplit;
+};
+
+Plan plan(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convsel_attention_desc_t& d) {
+  const int64_t group = d.q_heads / c.kv_heads;
+  const int64_t avg = (b.tokens + b.seqs - 1) / b.seqs;
+  Plan p;
+  const int64_t tiles = (avg * group + 15) / 16;
+  p.tiles = (int)(tiles < 65536 ? tiles : 65536);
+  int64_t keys = b.table_width * c.page_size;
+  if (d.window > 0 && d.window + avg < keys) keys = d.window + avg;
+  const int64_t groups = p.tiles * c.kv_heads * b.seqs;
+  int64_t n = (1024 + groups - 1) / groups;
+  if (n > keys / 256) n = keys / 256;
+  if (n > 128) n = 128;
+  p.nsplit = (int)(n < 1 ? 1 : n);
+  return p;
+}
+
+size_t part_floats(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convsel_attention_desc_t& d,
+                   const Plan& p) {
+  const size_t n = (size_t)b.tokens * d.q_heads * p.nsplit * c.head_dim;
+  return (n + 63) / 64 * 64;
+}
+
+template <typename T, int FMT, int NC>
+void launch_rows(dim3 grid, const void* q, const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, void* y,
+                 float* part, float* stat, const AttnArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((attention_rows_kernel<T, FMT, NC>), grid, dim3(256), 0, st, (const T*)q,
+                     (const uint8_t*)c.k_codes, (const uint8_t*)c.v_codes, c.k_scales, c.v_scales, b.table, b.lengths,
+                     b.offsets, (T*)y, part, stat, a);
+}
+
+template <typename T, int FMT>
+void launch_rows_nc(int nc, dim3 grid, const void* q, const convsel_kv_cache_t& c, const convsel_kv_batch_t& b,
+                    void* y, float* part, float* stat, const AttnArgs& a, hipStream_t st) {
+  switch (nc) {
+    case 1: return launch_rows<T, FMT, 1>(grid, q, c, b, y, part, stat, a, st);
+    case 2: return launch_rows<T, FMT, 2>(grid, q, c, b, y, part, stat, a, st);
+    case 3: return launch_rows<T, FMT, 3>(grid, q, c, b, y, part, stat, a, st);
+    case 4: return launch_rows<T, FMT, 4>(grid, q, c, b, y, part, stat, a, st);
+    case 5: return launch_rows<T, FMT, 5>(grid, q, c, b, y, part, stat, a, st);
+    case 6: return launch_rows<T, FMT, 6>(grid, q, c, b, y, part, stat, a, st);
+    case 7: return launch_rows<T, FMT, 7>(grid, q, c, b, y, part, stat, a, st);
+    default: return launch_rows<T, FMT, 8>(grid, q, c, b, y, part, stat, a, st);
   }
 }
 
 }  // namespace
 
-size_t attention_workspace(const convsel_kv_cache_t&, const convsel_kv_batch_t&, const convsel_attention_desc_t&) {
-  return 0;
+size_t attention_workspace(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b,
+                           const convsel_attention_desc_t& d) {
+  const Plan p = plan(c, b, d);
+  if (p.nsplit == 1) return 0;
+  return (part_floats(c, b, d, p) + (size_t)b.tokens * d.q_heads * p.nsplit * 2) * 4;
 }
 
 hipError_t launch_attention(const void* q, const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, void* y,
-                            const convsel_attention_desc_t& d, void*, hipStream_t stream) {
+                            const convsel_attention_desc_t& d, void* workspace, hipStream_t stream) {
+  const Plan p = plan(c, b, d);
+  AttnArgs a;
+  a.pages = c.pages;
+  a.table_width = b.table_width;
+  a.q_token = d.q_token_stride; a.q_head = d.q_head_stride;
+  a.y_token = d.y_token_stride; a.y_head = d.y_head_stride;
+  a.tokens = (int)b.tokens; a.kv_heads = c.kv_heads; a.group = d.q_heads / c.kv_heads; a.dim = c.head_dim;
+  a.ps_shift = c.page_size == 16 ? 4 : c.page_size == 32 ? 5 : c.page_size == 64 ? 6 : 7;
+  a.causal = d.causal; a.window = d.window; a.nsplit = p.nsplit; a.tiles = p.tiles;
+  a.scale = d.scale * 1.4426950408889634f;
+  float* part = (float*)workspace;
+  float* stat = part ? part + part_floats(c, b, d, p) : nullptr;
+  const int nc = kv_row_bytes(c.head_dim) / 32;
   for (int64_t s0 = 0; s0 < b.seqs; s0 += 65535) {
-    convsel_kv_batch_t p = b;
-    p.seqs = b.seqs - s0 < 65535 ? b.seqs - s0 : 65535;
-    p.table += s0 * b.table_width;
-    p.lengths += s0;
-    p.offsets += s0;
-    const int64_t rows = (b.tokens + b.seqs - 1) / b.seqs;
-    const dim3 grid((unsigned)(rows < 65536 ? rows : 65536), d.q_heads, (unsigned)p.seqs);
+    convsel_kv_batch_t pb = b;
+    pb.seqs = b.seqs - s0 < 65535 ? b.seqs - s0 : 65535;
+    pb.table += s0 * b.table_width;
+    pb.lengths += s0;
+    pb.offsets += s0;
+    const dim3 grid((unsigned)p.tiles * p.nsplit, c.kv_heads, (unsigned)pb.seqs);
+    if (d.dtype == CONV_F32) {
+      if (c.format == CONVSEL_KV_INT8)
+        launch_rows_nc<float, CONVSEL_KV_INT8>(nc, grid, q, c, pb, y, part, stat, a, stream);
+      else
+        launch_rows_nc<float, CONVSEL_KV_FP8>(nc, grid, q, c, pb, y, part, stat, a, stream);
+    } else {
+      if (c.format == CONVSEL_KV_INT8)
+        launch_rows_nc<bf16_t, CONVSEL_KV_INT8>(nc, grid, q, c, pb, y, part, stat, a, stream);
+      else
+        launch_rows_nc<bf16_t, CONVSEL_KV_FP8>(nc, grid, q, c, pb, y, part, stat, a, stream);
+    }
+  }
+  if (p.nsplit > 1) {
+    const int64_t rows = b.tokens * d.q_heads;
+    const dim3 grid((unsigned)((rows + 3) / 4));
     if (d.dtype == CONV_F32)
-      hipLaunchKernelGGL(attention_row_kernel<float>, grid, dim3(64), 0, stream, (const float*)q, c, p, (float*)y, d);
+      hipLaunchKernelGGL(attention_join_kernel<float>, grid, dim3(256), 0, stream, part, stat, b.offsets, (int)b.seqs,
+                         (float*)y, a);
     else
-      hipLaunchKernelGGL(attention_row_kernel<bf16_t>, grid, dim3(64), 0, stream, (const bf16_t*)q, c, p, (bf16_t*)y,
-                         d);
+      hipLaunchKernelGGL(attention_join_kernel<bf16_t>, grid, dim3(256), 0, stream, part, stat, b.offsets,
+                         (int)b.seqs, (bf16_t*)y, a);
   }
   return hipGetLastError();
 }
 
-void attention_describe(const convsel_kv_cache_t&, const convsel_kv_batch_t&, const convsel_attention_desc_t&,
+void attention_describe(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convsel_attention_desc_t& d,
                         char* buf, size_t len) {
-  snprintf(buf, len, "attention kernels=attention_row_kernel workspace=0");
+  const Plan p = plan(c, b, d);
+  snprintf(buf, len, "attention kernels=attention_rows_kernel%s rows=16 tiles=%d split=%d workspace=%zu",
+           p.nsplit > 1 ? ";attention_join_kernel" : "", p.tiles, p.nsplit, attention_workspace(c, b, d));
 }
 
 }  // namespace convsel

@@ -97,7 +97,7 @@ conv_status_t cache_pointers(const convsel_kv_cache_t* c) {
 
 conv_status_t batch_sizes(const convsel_kv_cache_t* c, const convsel_kv_batch_t* b) {
   if (!b || b->seqs < 0 || b->seqs > kInt31 || b->tokens < 0 || b->tokens > kInt31) return CONV_ERR_INVALID_ARG;
-  if (b->table_width < 0 || b->table_width > kInt31 / c->page_size) return CONV_ERR_INVALID_ARG;
+  if (b->table_width < 0 || b->table_width > ((int64_t)1 << 30) / c->page_size) return CONV_ERR_INVALID_ARG;
   return CONV_OK;
 }
 
@@ -119,6 +119,7 @@ conv_status_t attention_sizes(const convsel_kv_cache_t* c, const convsel_kv_batc
   if (st == CONV_OK) st = batch_sizes(c, b);
   if (st != CONV_OK) return st;
   if (!d || d->q_heads < 1 || d->q_heads > 65535 || d->q_heads % c->kv_heads != 0) return CONV_ERR_INVALID_ARG;
+  if (b->tokens > kInt31 / d->q_heads) return CONV_ERR_INVALID_ARG;  // rows are counted in 32 bits
   if (!dtype_ok(d->dtype) || !flag_ok(d->causal) || d->window < 0 || !isfinite(d->scale)) return CONV_ERR_INVALID_ARG;
   if (!stride_ok(d->q_token_stride) || !stride_ok(d->q_head_stride) || !stride_ok(d->y_token_stride) ||
       !stride_ok(d->y_head_stride))

@@ -136,11 +136,11 @@ class Cache:
 
 
 def attention(q, cache, table, lengths, offsets, causal, window, scale):
-    """(y, p|v|, |s|): the result, the weights' sum over the values' magnitudes, and the largest
-    sum of magnitudes behind a row's scores."""
+    """(y, p|v|, |s|, p scale): the result, the weights' sum over the values' magnitudes, the largest
+    sum of magnitudes behind a row's scores, and a row's largest weight times its block's value scale."""
     q = f64(q).numpy()
     t, hq, dim = q.shape
-    y, mag, smag = np.zeros(q.shape), np.zeros(q.shape), np.zeros((t, hq, 1))
+    y, mag, smag, top = np.zeros(q.shape), np.zeros(q.shape), np.zeros((t, hq, 1)), np.zeros((t, hq, 1))
     for b in range(len(lengths)):
         n = offsets[b + 1] - offsets[b]
         keys = [(j, cache.value("k", table, b, j), cache.value("v", table, b, j)) for j in range(lengths[b])]
@@ -149,6 +149,7 @@ def attention(q, cache, table, lengths, offsets, causal, window, scale):
             continue
         pos = np.array([e[0] for e in keys])
         k, v = np.stack([e[1] for e in keys]), np.stack([e[2] for e in keys])
+        vs = np.stack([cache.scales["v"][table[b][j // cache.page]] for j in pos]).astype(np.float64)
         group = hq // k.shape[1]
         for i in range(n):
             p = lengths[b] - n + i
@@ -167,20 +168,19 @@ def attention(q, cache, table, lengths, offsets, causal, window, scale):
                 w /= w.sum()
                 y[offsets[b] + i, h] = w @ vv
                 mag[offsets[b] + i, h] = w @ np.abs(vv)
+                top[offsets[b] + i, h] = (w * vs[seen][:, h // group]).max()
                 smag[offsets[b] + i, h] = (np.abs(kk) @ np.abs(row)).max() * abs(scale)
-    return y, mag, smag
+    return y, mag, smag, top
 
 
-def attention_bound(y, mag, smag, dim, dtype):
+def attention_bound(y, mag, smag, top, dim, dtype):
     """Error that a kernel of the stated precision stays within: its output's
     rounding; weights held in 11 bits (bf16 outputs) or 22 (fp32); the roundings
     of the scores' sums (dim + 8 of them, and an exponential good to a few
     units of its argument), which move every weight by twice as much; and the
-    smallest step of a weight, 2^-40 of the row's largest weight times its
-    values' scale, for each of up to 2^10 keys and codes up to 2^9: 2^-21 of
-    that weight and scale, which the row's widest column shows at least 2^3
-    times over (its codes reach that far)."""
+    smallest step of a weight, 2^-39 of the row's largest weight times its
+    block's value scale (`top`): half of it for each of up to 2^10 keys with
+    codes up to 2^9, 2^-21 of `top`."""
     weight = 2.0 ** -11 if dtype == torch.bfloat16 else 2.0 ** -22
     score = (dim + 16) * 2.0 ** -24 * smag
-    widest = np.max(mag, axis=-1, keepdims=True) if mag.size else mag
-    return half_ulp(dtype) * np.abs(y) + (weight + 2 * score + 2.0 ** -20) * mag + 2.0 ** -24 * widest + 1e-37
+    return half_ulp(dtype) * np.abs(y) + (weight + 2 * score + 2.0 ** -20) * mag + 2.0 ** -21 * top + 1e-37

@@ -394,8 +394,8 @@ def test_attention(case, fmt, dtype):
     whole = torch.full((q.shape[0] + 2, hq, dim + 4), 7.0, device=DEV, dtype=q.dtype)
     out = whole[1:-1, :, :dim]
     y = cs.cached_attention(q, cache, ints(table), ints(lengths), ints(off), causal=causal, window=window, out=out)
-    exact, mag, smag = ref.attention(q, want, table, lengths, off, causal, window, scale)
-    within(y, exact, ref.attention_bound(exact, mag, smag, dim, q.dtype), "attention %s" % (case,))
+    exact, mag, smag, top = ref.attention(q, want, table, lengths, off, causal, window, scale)
+    within(y, exact, ref.attention_bound(exact, mag, smag, top, dim, q.dtype), "attention %s" % (case,))
     assert bool((whole[0] == 7).all()) and bool((whole[-1] == 7).all()) and bool((whole[..., dim:] == 7).all())
 
 
@@ -452,8 +452,8 @@ def test_attention_scores_far_apart_and_scales_of_extreme_size(dtype):
         q = (q.float() * qgain).to(DT[dtype])
         off = offsets_of([2, 60])
         y = cs.cached_attention(q, cache, ints(table), ints([150, 90]), ints(off), scale=scale)
-        exact, mag, smag = ref.attention(q, want, table, [150, 90], off, True, 0, scale)
-        within(y, exact, ref.attention_bound(exact, mag, smag, 64, q.dtype),
+        exact, mag, smag, top = ref.attention(q, want, table, [150, 90], off, True, 0, scale)
+        within(y, exact, ref.attention_bound(exact, mag, smag, top, 64, q.dtype),
                "extremes %g %g" % (qgain, scale))
 
 
@@ -500,7 +500,7 @@ def test_attention_long(length, new, fmt):
     cache, table, q, exact, mag = long_case(length, new, fmt)
     y = cs.cached_attention(q, cache, table, ints([length]), ints([0, new]))
     # Scores here have magnitudes' sums under 128 * 4.5 * 4.5 / sqrt(128).
-    bound = ref.attention_bound(exact.cpu().numpy(), mag.cpu().numpy(), 230.0, 128, torch.bfloat16)
+    bound = ref.attention_bound(exact.cpu().numpy(), mag.cpu().numpy(), 230.0, 0.0, 128, torch.bfloat16)
     within(y, exact, bound, "long")
     for _ in range(3):
         assert torch.equal(cs.cached_attention(q, cache, table, ints([length]), ints([0, new])), y)
