@@ -1,24 +1,9 @@
 // Attention of new queries over the 8-bit paged cache.
-//
-// Mathematics.  With codes K, V and one scale a block of tokens, a query's score
-// is s_j = scale * ks * (q . K_j) and its result sum_j e^(s_j) vs V_j / sum_j
-// e^(s_j).  Everything runs in powers of two (scale carries log2 e).  vs = vf *
-// 2^ve; the running maximum M is a whole number of at least s_j + ve (so that
-// M - ve is exact), and
-//   u_j = 2^(s_j + ve - M)
-//   result = sum_j (u_j vf) V_j / sum_j u_j 2^-ve
-// holds the largest weight times its value scale near one: a page of small
-// values may hold the weight, and no scale overflows.  Scales reach from 2^-100
-// to 2^121, so a change of M is an exponent added, and where u would leave fp32
-// (scales 2^100 apart within a row) the sum's terms are formed without it.
-// Weights go to the matrix cores in 11 bits, 2^15 times as large (their
-// steps are then 2^-39 of the largest); codes are exact in them.  fp32 calls hold queries and weights as
-// two such numbers, 22 bits.  Queries are brought to [2^14, 2^15) by a power of
-// two, which bf16 survives exactly.  Sums and statistics are fp32.
+#include <math.h>
 #include <stdio.h>
 
-#include "lm_common.hpp"
-#include "lm_kernels.hpp"
+
+#include "attention_common.hpp"
 
 namespace convsel {
 namespace {
@@ -26,18 +11,6 @@ namespace {
 using namespace lm;
 
 typedef float f32x4v_t __attribute__((ext_vector_type(4)));
-
-struct AttnArgs {
-  int64_t pages, table_width;
-  int64_t q_token, q_head, y_token, y_head;
-  int tokens, kv_heads, group, dim, ps_shift, causal, window, nsplit, tiles;
-  float scale;  // times log2 e
-};
-
-// Rows of keys a query sees: [lo, hi).
-struct Range {
-  int lo, hi;
-};
 
 // Sixteen tokens of one page: a lane's part of their key and value codes.
 template <int NC>
@@ -63,53 +36,8 @@ __device__ __forceinline__ void load_codes(uint32_t* dst, const uint8_t* src) {
   }
 }
 
-// Four codes as 16-bit floats, exactly.
-template <int FMT>
-__device__ __forceinline__ void widen4(uint32_t w, f16x2_t& lo, f16x2_t& hi) {
-  if constexpr (FMT == CONVSEL_KV_INT8) {
-    // 1024 + (code + 128) has the code's byte as its lowest bits.
-    const uint32_t u = w ^ 0x80808080u;
-    const f16x2_t off = {static_cast<_Float16>(-1152.f), static_cast<_Float16>(-1152.f)};
-    lo = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04010400u)) + off;
-    hi = __builtin_bit_cast(f16x2_t, __builtin_amdgcn_perm(0x64646464u, u, 0x04030402u)) + off;
-  } else {
-    lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, false);
-    hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.f, true);
-  }
-}
-
-template <int FMT>
-__device__ __forceinline__ f16x8_t widen8(uint32_t a, uint32_t b) {
-  f16x2_t p[4];
-  widen4<FMT>(a, p[0], p[1]);
-  widen4<FMT>(b, p[2], p[3]);
-  f16x8_t r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    r[2 * i] = p[i][0];
-    r[2 * i + 1] = p[i][1];
-  }
-  return r;
-}
-
 __device__ __forceinline__ f32x4v_t mfma16(const f16x8_t& a, const f16x8_t& b, const f32x4v_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-
-constexpr float kWeight = 0x1p15f;  // weights as the matrix cores take them, and back
-constexpr float kResult = 0x1p-15f;
-constexpr float kFar = -100.f;      // exponents of u below this are near the end of fp32
-
-// Exponent to add to what was kept at maximum `from`, now at `to` >= from.
-__device__ __forceinline__ int shift_of(float from, float to) {
-  return from == to ? 0 : static_cast<int>(fmaxf(from - to, -300.f));
-}
-
-// Power of two that brings magnitudes up to amax under 2^15.
-__device__ __forceinline__ int query_exponent(float amax) {
-  int e = 0;
-  if (amax > 0.f && amax < __builtin_inff()) frexpf(amax, &e);
-  return e - 15;
 }
 
 // ---------------------------------------------------------------------------
@@ -167,32 +95,28 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(
 
     // The query row, as the second operand: lane (row, g) holds columns
     // g * LB + 8 c + 0..7, the columns that lane (token, g) loads of a key.
-    f16x8_t qh[NC], ql[TWO ? NC : 1];
-    float cs;
+    float qv[NC][8];
     {
       const T* src = q + (sp.first + tok) * a.q_token +
-                     (static_cast<int64_t>(head) * a.group + row % a.group) * a.q_head;
-      float qv[NC][8], amax = 0.f;
+                     (static_cast<int64_t>(head) * a.group + row % a.group) * a.q_head + g * LB;
+      if (a.q_vec) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NC; ++c)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int d = g * LB + 8 * c + j;
-          qv[c][j] = d < a.dim ? elem<T>::load(src + (d < a.dim ? d : 0)) : 0.f;
-          amax = fmaxf(amax, fabsf(qv[c][j]));
-        }
-      amax = fmaxf(amax, __shfl_xor(amax, 16));
-      amax = fmaxf(amax, __shfl_xor(amax, 32));
-      const int e = query_exponent(amax);
-      cs = ldexpf(a.scale, e);
+          for (int j = 0; j < 8; j += elem<T>::per16) {
+            const vec16 v = load16(src + 8 * c + j);
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+            for (int x = 0; x < elem<T>::per16; ++x) qv[c][j + x] = elem<T>::to_f32(vec16_get<T>(v, x));
+          }
+      } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float v = ldexpf(qv[c][j], -e);
-          qh[c][j] = static_cast<_Float16>(v);
-          if constexpr (TWO) ql[c][j] = static_cast<_Float16>(v - static_cast<float>(qh[c][j]));
-        }
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int d = g * LB + 8 * c + j;
+            qv[c][j] = d < a.dim ? elem<T>::load(src + 8 * c + j) : 0.f;
+          }
+      }
     }
 
     f32x4v_t o[DT];
@@ -214,6 +138,27 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(
       load_codes<NC>(r.v, vc + at + lane * LB);
       r.ks = ks[ph];
       r.vs = vs[ph];
+    };
+    f16x8_t qh[NC], ql[TWO ? NC : 1];
+    float cs = 0.f;
+    auto prepare_query = [&]() {
+      float amax = 0.f;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) amax = fmaxf(amax, fabsf(qv[c][j]));
+      amax = fmaxf(amax, __shfl_xor(amax, 16));
+      amax = fmaxf(amax, __shfl_xor(amax, 32));
+      const int e = query_exponent(amax);
+      cs = ldexpf(a.scale, e);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float v = ldexpf(qv[c][j], -e);
+          qh[c][j] = static_cast<_Float16>(v);
+          if constexpr (TWO) ql[c][j] = static_cast<_Float16>(v - static_cast<float>(qh[c][j]));
+        }
     };
     auto compute = [&](Block<NC> (&r)[2], int pair, int pg0, int pg1) {
       const int pgs[2] = {pg0, pg1};
@@ -319,6 +264,7 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(
         look(pa, pair);
         look(pb, pair + 4);
         fetch(ra, pa, pair);
+        prepare_query();  // the first codes are on their way
         for (; pair < pair1; pair += 8) {
           int pn[2];
           if (pair + 4 < pair1) fetch(rb, pb, pair + 4);
@@ -373,7 +319,7 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(
           float v = 0.f;
 #pragma unroll
           for (int w = 0; w < 4; ++w) v += so[w][r][d] * f[w];
-          part[at * a.dim + d] = v;
+          part[at * ((a.dim + 3) & ~3) + d] = v;
         }
         if (d0 == 0) {
           stat[2 * at] = mt;
@@ -385,93 +331,137 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(
   }
 }
 
-// Joins the parts of a split axis: one wave per (token, head) that a sequence owns.
+// Joins the parts of a split axis: one workgroup per (token, head) that a
+// sequence owns.  Partial results are rows of whole 16-byte units.
+constexpr int kMaxSplit = 128;
+
 template <typename T>
 __global__ __launch_bounds__(256) void attention_join_kernel(const float* __restrict__ part,
                                                              const float* __restrict__ stat,
                                                              const int32_t* __restrict__ offsets, int seqs,
                                                              T* __restrict__ y, AttnArgs a) {
-  const int heads = a.kv_heads * a.group;
-  const int lane = threadIdx.x & 63;
-  const int64_t it = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
-  const int64_t t = it / heads;
-  // Rising offsets from 0: the tokens behind the last one belong to nobody.
-  if (t >= clampi(offsets[seqs], 0, a.tokens)) return;
-  const int64_t h = it % heads;
-  float m = -__builtin_inff();
-  for (int s = lane; s < a.nsplit; s += 64) m = fmaxf(m, stat[2 * (it * a.nsplit + s)]);
+  __shared__ float sf[kMaxSplit];
+  __shared__ float4 sv[256];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t heads = static_cast<int64_t>(a.kv_heads) * a.group;
+  const int64_t it = blockIdx.x, t = it / heads, h = it - t * heads;
+  const int owned = clampi(offsets[seqs], 0, a.tokens);
+  const int n = a.nsplit;
+  // Offsets rise from 0: the tokens behind the last one belong to nobody.
+  if (t >= owned) return;
+  // Each wave reads all statistics; lane s holds those of parts s and s + 64.
+  float ms[2], ls[2], m = -__builtin_inff(), l = 0.f;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int s = lane + 64 * i;
+    const float2 v = s < n ? reinterpret_cast<const float2*>(stat)[it * n + s] : make_float2(-__builtin_inff(), 0.f);
+    ms[i] = v.x;
+    ls[i] = v.y;
+    m = fmaxf(m, v.x);
+  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  float l = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < a.nsplit; ++s) {
-    const float ms = stat[2 * (it * a.nsplit + s)];
-    const int dm = shift_of(ms, m);
-    const float f = ldexpf(1.f, dm);
-    l += ldexpf(stat[2 * (it * a.nsplit + s) + 1], dm);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int d = lane + 64 * u;
-      if (d < a.dim) v[u] += part[(it * a.nsplit + s) * a.dim + d] * f;
+  for (int i = 0; i < 2; ++i) {
+    const int dm = shift_of(ms[i], m);
+    if (wave == 0) sf[lane + 64 * i] = ldexpf(1.f, dm);
+    l += ldexpf(ls[i], dm);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o);
+  __syncthreads();
+  // Four columns a thread, the parts dealt to as many groups as the workgroup holds.
+  const int c4 = (a.dim + 3) / 4, groups = 256 / c4;
+  const int col = threadIdx.x % c4, group = threadIdx.x / c4;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (group < groups) {
+    const float4* src = reinterpret_cast<const float4*>(part) + it * n * c4 + col;
+#pragma unroll 4
+    for (int s = group; s < n; s += groups) {
+      const float4 p = src[s * c4];
+      const float f = sf[s];
+      v.x += p.x * f; v.y += p.y * f; v.z += p.z * f; v.w += p.w * f;
     }
   }
-  const float inv = l == 0.f ? 0.f : kResult / l;
-  T* dst = y + t * a.y_token + h * a.y_head;
-#pragma unroll
-  for (int u = 0; u < 4; ++u) {
-    const int d = lane + 64 * u;
-    if (d < a.dim) elem<T>::store(dst + d, v[u] * inv);
+  sv[threadIdx.x] = v;
+  __syncthreads();
+  const int d = threadIdx.x;
+  if (d < a.dim) {
+    float r = 0.f;
+    for (int i = 0; i < groups; ++i) r += reinterpret_cast<const float*>(&sv[i * c4])[d];
+    const float inv = l == 0.f ? 0.f : kResult / l;
+    elem<T>::store(y + t * a.y_token + h * a.y_head + d, r * inv);
   }
 }
 
-// How a call is cut: rows of 16, and parts of the keys.  The host knows how
-// many tokens the call has and how many a sequence may hold, not how they are
-// spread; every count below only sets the grid, kernels walk what there is.
+// How a call is cut: rows, in 16s or 128s, and parts of the keys.  The host
+// knows how many tokens the call has and how many a sequence may hold, not how
+// they are spread; every count only sets the grid, and kernels walk what there
+// is.
 struct Plan {
+  bool tiles128;
   int tiles, nsplit;
 };
 
 Plan plan(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convsel_attention_desc_t& d) {
   const int64_t group = d.q_heads / c.kv_heads;
   const int64_t avg = (b.tokens + b.seqs - 1) / b.seqs;
-  Plan p;
-  const int64_t tiles = (avg * group + 15) / 16;
-  p.tiles = (int)(tiles < 65536 ? tiles : 65536);
   int64_t keys = b.table_width * c.page_size;
   if (d.window > 0 && d.window + avg < keys) keys = d.window + avg;
+  Plan p;
+  // The 128-row kernel widens codes once for 128 rows but takes some 15 us for
+  // its first keys; the 16-row kernel is through them in 8.  Measured with
+  // heads of 128 and 64, they cross where rows x keys x width reach 1.6e9 in
+  // bf16 and 4e9 in fp32 (one sequence, 32 query heads of 128 on 8, bf16: 128
+  // new tokens on 4000, 40 against 53 us; 64 on 1000, 26 against 18; 2048 on
+  // none 92 against 186), provided that its tiles are at least half full.
+  const double work = (double)avg * d.q_heads * b.seqs * keys * kv_row_bytes(c.head_dim);
+  p.tiles128 = avg * group >= 64 && work >= (d.dtype == CONV_F32 ? 4e9 : 1.6e9);
+  const int64_t rows = p.tiles128 ? 128 : 16;
+  const int64_t tiles = (avg * group + rows - 1) / rows;
+  p.tiles = (int)(tiles < 32768 ? tiles : 32768);
   const int64_t groups = p.tiles * c.kv_heads * b.seqs;
-  int64_t n = (1024 + groups - 1) / groups;
+  // Two workgroups a CU, with 256 keys at least in each part.
+  int64_t n = (512 + groups - 1) / groups;
   if (n > keys / 256) n = keys / 256;
-  if (n > 128) n = 128;
+  if (p.tiles128) {
+    // A tile of 64 keys takes 2.3 us where nothing else runs on the CU, a part's results 2e-6 us a value to write
+    // and join: the sum is least at the root of their ratio.
+    const double walk = keys / 64 * 2.3, join = (double)b.tokens * d.q_heads * c.head_dim * 2e-6;
+    const int64_t best = (int64_t)sqrt(walk / join);
+    if (n > best) n = best;
+  } else if (n < 4 && groups < 4096) {
+    // Sequences of unlike lengths end together where each is cut (64 of 2048 .. 8192 tokens: 145 -> 134 us).
+    n = keys / 2048 < 4 ? keys / 2048 : 4;
+  }
+  if (n > kMaxSplit) n = kMaxSplit;
   p.nsplit = (int)(n < 1 ? 1 : n);
   return p;
 }
 
 size_t part_floats(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convsel_attention_desc_t& d,
                    const Plan& p) {
-  const size_t n = (size_t)b.tokens * d.q_heads * p.nsplit * c.head_dim;
+  const size_t n = (size_t)b.tokens * d.q_heads * p.nsplit * ((c.head_dim + 3) / 4 * 4);
   return (n + 63) / 64 * 64;
 }
 
 template <typename T, int FMT, int NC>
-void launch_rows(dim3 grid, const void* q, const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, void* y,
-                 float* part, float* stat, const AttnArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((attention_rows_kernel<T, FMT, NC>), grid, dim3(256), 0, st, (const T*)q,
-                     (const uint8_t*)c.k_codes, (const uint8_t*)c.v_codes, c.k_scales, c.v_scales, b.table, b.lengths,
-                     b.offsets, (T*)y, part, stat, a);
+void launch_rows(dim3 grid, const AttnPointers& p, const AttnArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((attention_rows_kernel<T, FMT, NC>), grid, dim3(256), 0, st, (const T*)p.q, p.k_codes, p.v_codes,
+                     p.k_scales, p.v_scales, p.table, p.lengths, p.offsets, (T*)p.y, p.part, p.stat, a);
 }
 
 template <typename T, int FMT>
-void launch_rows_nc(int nc, dim3 grid, const void* q, const convsel_kv_cache_t& c, const convsel_kv_batch_t& b,
-                    void* y, float* part, float* stat, const AttnArgs& a, hipStream_t st) {
-  switch (nc) {
-    case 1: return launch_rows<T, FMT, 1>(grid, q, c, b, y, part, stat, a, st);
-    case 2: return launch_rows<T, FMT, 2>(grid, q, c, b, y, part, stat, a, st);
-    case 3: return launch_rows<T, FMT, 3>(grid, q, c, b, y, part, stat, a, st);
-    case 4: return launch_rows<T, FMT, 4>(grid, q, c, b, y, part, stat, a, st);
-    case 5: return launch_rows<T, FMT, 5>(grid, q, c, b, y, part, stat, a, st);
-    case 6: return launch_rows<T, FMT, 6>(grid, q, c, b, y, part, stat, a, st);
-    case 7: return launch_rows<T, FMT, 7>(grid, q, c, b, y, part, stat, a, st);
-    default: return launch_rows<T, FMT, 8>(grid, q, c, b, y, part, stat, a, st);
+void launch_rows_nc(dim3 grid, const AttnPointers& p, const AttnArgs& a, hipStream_t st) {
+  switch ((a.dim + 31) / 32) {
+    case 1: return launch_rows<T, FMT, 1>(grid, p, a, st);
+    case 2: return launch_rows<T, FMT, 2>(grid, p, a, st);
+    case 3: return launch_rows<T, FMT, 3>(grid, p, a, st);
+    case 4: return launch_rows<T, FMT, 4>(grid, p, a, st);
+    case 5: return launch_rows<T, FMT, 5>(grid, p, a, st);
+    case 6: return launch_rows<T, FMT, 6>(grid, p, a, st);
+    case 7: return launch_rows<T, FMT, 7>(grid, p, a, st);
+    default: return launch_rows<T, FMT, 8>(grid, p, a, st);
   }
 }
 
@@ -496,36 +486,44 @@ hipError_t launch_attention(const void* q, const convsel_kv_cache_t& c, const co
   a.ps_shift = c.page_size == 16 ? 4 : c.page_size == 32 ? 5 : c.page_size == 64 ? 6 : 7;
   a.causal = d.causal; a.window = d.window; a.nsplit = p.nsplit; a.tiles = p.tiles;
   a.scale = d.scale * 1.4426950408889634f;
-  float* part = (float*)workspace;
-  float* stat = part ? part + part_floats(c, b, d, p) : nullptr;
-  const int nc = kv_row_bytes(c.head_dim) / 32;
+  // Queries are read and results written in 16-byte (results: four-value) units where every row starts on one and
+  // has no padding.
+  const int64_t unit = d.dtype == CONV_F32 ? 4 : 8, es = 16 / unit;
+  a.q_vec = c.head_dim % 32 == 0 && a.q_token % unit == 0 && a.q_head % unit == 0 && (uintptr_t)q % 16 == 0;
+  a.y_vec = c.head_dim % 4 == 0 && a.y_token % 4 == 0 && a.y_head % 4 == 0 && (uintptr_t)y % (4 * es) == 0;
+  AttnPointers ptr;
+  ptr.q = q;
+  ptr.k_codes = (const uint8_t*)c.k_codes; ptr.v_codes = (const uint8_t*)c.v_codes;
+  ptr.k_scales = c.k_scales; ptr.v_scales = c.v_scales;
+  ptr.y = y;
+  ptr.part = (float*)workspace;
+  ptr.stat = p.nsplit > 1 ? ptr.part + part_floats(c, b, d, p) : nullptr;
   for (int64_t s0 = 0; s0 < b.seqs; s0 += 65535) {
-    convsel_kv_batch_t pb = b;
-    pb.seqs = b.seqs - s0 < 65535 ? b.seqs - s0 : 65535;
-    pb.table += s0 * b.table_width;
-    pb.lengths += s0;
-    pb.offsets += s0;
-    const dim3 grid((unsigned)p.tiles * p.nsplit, c.kv_heads, (unsigned)pb.seqs);
+    const int64_t seqs = b.seqs - s0 < 65535 ? b.seqs - s0 : 65535;
+    ptr.table = b.table + s0 * b.table_width;
+    ptr.lengths = b.lengths + s0;
+    ptr.offsets = b.offsets + s0;
+    if (p.tiles128) {
+      const hipError_t e = launch_attention_tiles(ptr, a, d.dtype, c.format, seqs, stream);
+      if (e != hipSuccess) return e;
+      continue;
+    }
+    const dim3 grid((unsigned)p.tiles * p.nsplit, c.kv_heads, (unsigned)seqs);
     if (d.dtype == CONV_F32) {
-      if (c.format == CONVSEL_KV_INT8)
-        launch_rows_nc<float, CONVSEL_KV_INT8>(nc, grid, q, c, pb, y, part, stat, a, stream);
-      else
-        launch_rows_nc<float, CONVSEL_KV_FP8>(nc, grid, q, c, pb, y, part, stat, a, stream);
+      if (c.format == CONVSEL_KV_INT8) launch_rows_nc<float, CONVSEL_KV_INT8>(grid, ptr, a, stream);
+      else launch_rows_nc<float, CONVSEL_KV_FP8>(grid, ptr, a, stream);
     } else {
-      if (c.format == CONVSEL_KV_INT8)
-        launch_rows_nc<bf16_t, CONVSEL_KV_INT8>(nc, grid, q, c, pb, y, part, stat, a, stream);
-      else
-        launch_rows_nc<bf16_t, CONVSEL_KV_FP8>(nc, grid, q, c, pb, y, part, stat, a, stream);
+      if (c.format == CONVSEL_KV_INT8) launch_rows_nc<bf16_t, CONVSEL_KV_INT8>(grid, ptr, a, stream);
+      else launch_rows_nc<bf16_t, CONVSEL_KV_FP8>(grid, ptr, a, stream);
     }
   }
   if (p.nsplit > 1) {
-    const int64_t rows = b.tokens * d.q_heads;
-    const dim3 grid((unsigned)((rows + 3) / 4));
+    const dim3 grid((unsigned)(b.tokens * d.q_heads));
     if (d.dtype == CONV_F32)
-      hipLaunchKernelGGL(attention_join_kernel<float>, grid, dim3(256), 0, stream, part, stat, b.offsets, (int)b.seqs,
-                         (float*)y, a);
+      hipLaunchKernelGGL(attention_join_kernel<float>, grid, dim3(256), 0, stream, ptr.part, ptr.stat, b.offsets,
+                         (int)b.seqs, (float*)y, a);
     else
-      hipLaunchKernelGGL(attention_join_kernel<bf16_t>, grid, dim3(256), 0, stream, part, stat, b.offsets,
+      hipLaunchKernelGGL(attention_join_kernel<bf16_t>, grid, dim3(256), 0, stream, ptr.part, ptr.stat, b.offsets,
                          (int)b.seqs, (bf16_t*)y, a);
   }
   return hipGetLastError();
@@ -534,8 +532,9 @@ hipError_t launch_attention(const void* q, const convsel_kv_cache_t& c, const co
 void attention_describe(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convsel_attention_desc_t& d,
                         char* buf, size_t len) {
   const Plan p = plan(c, b, d);
-  snprintf(buf, len, "attention kernels=attention_rows_kernel%s rows=16 tiles=%d split=%d workspace=%zu",
-           p.nsplit > 1 ? ";attention_join_kernel" : "", p.tiles, p.nsplit, attention_workspace(c, b, d));
+  snprintf(buf, len, "attention kernels=attention_%s_kernel%s rows=%d tiles=%d split=%d workspace=%zu",
+           p.tiles128 ? "tiles" : "rows", p.nsplit > 1 ? ";attention_join_kernel" : "", p.tiles128 ? 128 : 16, p.tiles,
+           p.nsplit, attention_workspace(c, b, d));
 }
 
 }  // namespace convsel

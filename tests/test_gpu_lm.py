@@ -399,6 +399,125 @@ def test_attention(case, fmt, dtype):
     assert bool((whole[0] == 7).all()) and bool((whole[-1] == 7).all()) and bool((whole[..., dim:] == 7).all())
 
 
+def wide(table, case, work=6e9):
+    """The table with room for so many pages (it has none there) that the host, which sees the width alone, plans
+    for long sequences: 128-row tiles where a key head has 64 rows, and keys cut into parts."""
+    hq, hk, dim, page, lengths, new = case[:6]
+    keys = work / (max(1, sum(new) // len(new)) * hq * len(new) * ((dim + 31) // 32 * 32))
+    width = max(len(table[0]), min(int(keys) // page + 1, 1 << 20))
+    t = torch.full((len(table), width), -1, dtype=torch.int32, device=DEV)
+    t[:, :len(table[0])] = ints(table)
+    return t
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("case", ATTENTION_CASES, ids=lambda c: "h%d-%d-d%d-p%d-n%s" % (c[:4] + (sum(c[5]),)))
+def test_attention_planned_for_long_sequences(case, fmt, dtype):
+    hq, hk, dim, page, lengths, new, causal, window = case
+    say("case attention planned long", case, fmt, dtype)
+    cache, want, table, q = build(case, fmt, dtype, seed=2)
+    scale = -0.8 / math.sqrt(dim)
+    off = offsets_of(new)
+    t = wide(table, case)
+    tiles = "attention_tiles_kernel" in cs.describe_attention(cache, len(new), sum(new), t.shape[1], hq, DT[dtype], causal, window)
+    assert tiles == (sum(new) // len(new) * hq // hk >= 64 and not window), "another kernel than the case is for"
+    whole = torch.full((q.shape[0] + 2, hq, dim + 4), 7.0, device=DEV, dtype=q.dtype)
+    out = whole[1:-1, :, :dim]
+    y = cs.cached_attention(q, cache, t, ints(lengths), ints(off), causal=causal, window=window, scale=scale, out=out)
+    exact, mag, smag, top = ref.attention(q, want, table, lengths, off, causal, window, scale)
+    within(y, exact, ref.attention_bound(exact, mag, smag, top, dim, q.dtype), "attention %s" % (case,))
+    assert bool((whole[0] == 7).all()) and bool((whole[-1] == 7).all()) and bool((whole[..., dim:] == 7).all())
+
+
+# More of the 128-row kernel: windows, ragged ends, empty rows and idle waves, every width it is built for.
+TILE_CASES = [
+    (6, 2, 128, 16, [400, 63], [130, 40], True, 90), (8, 1, 64, 64, [500], [33], True, 17),
+    (4, 4, 32, 16, [129, 1], [129, 1], True, 0), (4, 2, 96, 32, [65, 190], [100, 190], True, 0),
+    (2, 1, 160, 16, [270], [70], False, 0), (2, 1, 192, 128, [260], [90], True, 0), (2, 1, 224, 16, [140], [100], True, 50),
+    (2, 1, 256, 64, [300, 90], [64, 64], True, 0), (3, 1, 100, 16, [90], [50], False, 30), (1, 1, 5, 16, [200], [129], True, 0),
+    (16, 1, 128, 128, [128], [8], True, 0), (2, 2, 128, 16, [40, 300], [150, 150], True, 0)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("fmt", ["int8", "fp8"])
+@pytest.mark.parametrize("case", TILE_CASES, ids=lambda c: "h%d-%d-d%d-p%d-n%s" % (c[:4] + (sum(c[5]),)))
+def test_attention_in_tiles_of_128_rows(case, fmt, dtype):
+    hq, hk, dim, page, lengths, new, causal, window = case
+    say("case attention tiles", case, fmt, dtype)
+    cache, want, table, q = build(case, fmt, dtype, seed=4)
+    off, scale = offsets_of(new), 1.0 / math.sqrt(dim)
+    exact, mag, smag, top = ref.attention(q, want, table, lengths, off, causal, window, scale)
+    # With a window the host plans for no more keys than it leaves: the kernel is reached where many sequences share it.
+    n = len(new)
+    if window:
+        rep = int(6e9 / (sum(new) // n * n * hq * (window + sum(new) // n) * ((dim + 31) // 32 * 32))) + 1
+        rep = min(rep, 8192)
+    else:
+        rep = 1
+    t = wide(table, case) if not window else wide(table, case, 0)
+    if window and t.shape[1] * page < window + sum(new) // n:
+        t = torch.nn.functional.pad(t, (0, (window + sum(new) // n) // page + 1 - t.shape[1]), value=-1)
+    assert "attention_tiles_kernel" in cs.describe_attention(cache, n * rep, sum(new) * rep, t.shape[1], hq, DT[dtype], causal, window)
+    offs = [0]
+    for _ in range(rep):
+        offs += [offs[-1] + o for o in off[1:]]
+    y = cs.cached_attention(q.repeat(rep, 1, 1), cache, t.repeat(rep, 1), ints(lengths * rep), ints(offs), causal=causal,
+                            window=window)
+    y = y.view(rep, sum(new), hq, dim)
+    within(y[0], exact, ref.attention_bound(exact, mag, smag, top, dim, q.dtype), "tiles %s" % (case,))
+    assert bool((y == y[0]).all()), "the same sequence gave two results"
+
+
+@pytest.mark.parametrize("new", [40, 150])
+def test_tiles_of_128_rows_ignore_what_lies_behind_masks(new):
+    case = (4, 2, 64, 16, [200, 170], [new, new], True, 0)
+    cache, want, table, q = build(case, "fp8", "bf16")
+    off, lens = ints([0, new, 2 * new]), ints([200, 170])
+    t = wide(table, case)
+    assert "attention_tiles_kernel" in cs.describe_attention(cache, 2, 2 * new, t.shape[1], 4)
+    y = cs.cached_attention(q, cache, t, lens, off)
+    k, v = cache.k_codes.view(cache.pages, 2, 16, 64), cache.v_codes.view(cache.pages, 2, 4, 16, 4, 4)
+    for bits in (0, 0x7F, 0x80):
+        k[table[0][12], :, 8:] = bits
+        v[table[0][12], :, 2:] = bits
+        assert torch.equal(cs.cached_attention(q, cache, t, lens, off), y)
+    # A page in the middle that is not there, a row of NaN, lengths of nothing, and no pages at all.
+    hole = t.clone()
+    hole[0, 3] = 2 ** 31 - 1
+    want.codes["k"] = want.codes["k"].copy()
+    rows = [r[:] for r in table]
+    rows[0][3] = -1
+    exact, mag, smag, top = ref.attention(q, want, rows, [200, 170], [0, new, 2 * new], True, 0, 0.125)
+    within(cs.cached_attention(q, cache, hole, lens, off), exact,
+           ref.attention_bound(exact, mag, smag, top, 64, q.dtype), "hole")
+    bad = q.clone()
+    bad[new, 1, 3] = float("nan")
+    z = cs.cached_attention(bad, cache, t, lens, off)
+    assert bool(z[new, 1].isnan().all())
+    clean = y.clone()
+    clean[new, 1] = z[new, 1] = 0
+    assert torch.equal(z, clean)
+    assert bool((cs.cached_attention(q, cache, t, ints([0, -7]), off) == 0).all())
+    assert bool((cs.cached_attention(q, cache, torch.full_like(t, -1), lens, off) == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tiles_of_128_rows_with_scales_of_extreme_size(dtype):
+    case = (4, 2, 64, 16, [150, 90], [40, 60], True, 0)
+    for qgain, scale in ((1.0, 30.0), (1e20, 1e-20), (1e-20, 1e20), (0.0, 1.0), (1.0, 0.0), (3.0, -0.7)):
+        cache, want, table, q = build(case, "int8", dtype, seed=5)
+        spread = 10.0 ** torch.randint(-20, 21, (cache.pages, 2), device=DEV, generator=gen(9)).float()
+        cache.v_scales.mul_(spread)
+        want.scales["v"] *= spread.cpu().numpy()
+        q = (q.float() * qgain).to(DT[dtype])
+        t = wide(table, case)
+        assert "attention_tiles_kernel" in cs.describe_attention(cache, 2, 100, t.shape[1], 4, DT[dtype])
+        y = cs.cached_attention(q, cache, t, ints([150, 90]), ints([0, 40, 100]), scale=scale)
+        exact, mag, smag, top = ref.attention(q, want, table, [150, 90], [0, 40, 100], True, 0, scale)
+        within(y, exact, ref.attention_bound(exact, mag, smag, top, 64, q.dtype), "extremes %g %g" % (qgain, scale))
+
+
 @pytest.mark.parametrize("fmt", ["int8", "fp8"])
 @pytest.mark.parametrize("new", [1, 3, 150])
 def test_attention_ignores_what_lies_behind_masks(fmt, new):
