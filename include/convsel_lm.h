@@ -45,7 +45,7 @@ typedef enum convsel_act {
 } convsel_act_t;
 
 typedef struct convsel_linear_desc {
-  int64_t m, in_features, out_features;
+  int64_t m, in_features, out_features;  /* out_features < 2^26, m * out_features <= 2^35 */
   int64_t ldx, ldr, ldy;  /* ldr is read only with a residual */
   int32_t dtype;          /* conv_dtype_t of x, w, b, r and y */
   int32_t act;            /* convsel_act_t */

@@ -1,98 +1,200 @@
-// Linear layers: y = act(x W^T + b) + r.
+// Linear layers: y = act(x W^T + b) + r.  Few rows stream the weights through
+// registers (here); more rows go in tiles (linear_tiles.hip).
 #include <stdio.h>
 
-#include "lm_common.hpp"
-#include "lm_kernels.hpp"
+#include "linear_common.hpp"
 
 namespace convsel {
 namespace {
 
 using namespace lm;
 
-// Any sizes, strides and alignment.  256 threads = 4 waves in a 2 x 2 grid
-// own a 64 x 64 tile of y; rows of x and w are staged in LDS in k-tiles of
-// 64 bytes, element by element where a 16-byte load could be misaligned or
-// leave the row.  The matrix product's rows are w's and its columns x's, so a
-// lane ends with four consecutive outputs of one token.
-template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void linear_tile_kernel(LinearArgs g, int tiles_o) {
+typedef float f32x4v_t __attribute__((ext_vector_type(4)));
+
+// One 16-byte unit of a 16 x 16 product's operands: 8 bf16 or 4 fp32 of a lane.
+__device__ __forceinline__ f32x4v_t mac16(bf16_t, const vec16& a, const vec16& b, f32x4v_t c) {
+  bf16x8_t av, bv;
+  __builtin_memcpy(&av, &a, 16);
+  __builtin_memcpy(&bv, &b, 16);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bv, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4v_t mac16(float, const vec16& a, const vec16& b, f32x4v_t c) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.d[i]), __uint_as_float(b.d[i]), c, 0, 0, 0);
+  return c;
+}
+
+// Few rows: a workgroup owns 16 outputs and NT tiles of 16 rows of x, and its
+// waves share out the reduction, whose sums meet in LDS.  A lane holds 32
+// neighbouring bytes of one weight row (four lanes read a whole 128-byte line)
+// and the same columns of one row of x; which column a product takes at which
+// step does not matter while both operands agree.
+//
+// What bounds it: the weights' way from memory.  A step of a wave is 2 KiB of
+// them; steps are fetched kDepth ahead, and as many waves as leave each of them
+// a few steps keep a CU's share of the weights on their way at once.
+constexpr int kDepth = 4;
+
+template <typename T, bool VEC, int NT>
+__global__ __launch_bounds__(1024) void linear_rows_kernel(LinearArgs g, int waves, int vec_out) {
   constexpr int UE = elem<T>::per16;
-  constexpr int BK = 4 * UE, KP = BK + UE;
-  __shared__ __align__(16) T Ws[64 * KP];
-  __shared__ __align__(16) T Xs[64 * KP];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int wo = wave >> 1, wx = wave & 1;
-  const int64_t o0 = static_cast<int64_t>(blockIdx.x % tiles_o) * 64, m0 = static_cast<int64_t>(blockIdx.x / tiles_o) * 64;
-  const int row = tid >> 2, kc = (tid & 3) * UE;
-  const T* X = reinterpret_cast<const T*>(g.x) + (m0 + row) * g.ldx;
-  const T* W = reinterpret_cast<const T*>(g.w) + (o0 + row) * g.in;
-  const bool xok = m0 + row < g.m, wok = o0 + row < g.out;
-  auto fetch = [&](const T* base, bool ok, int64_t k) -> vec16 {
-    if (VEC) return ok && k < g.in ? load16(base + k) : vec16_zero();
-    uint32_t e[UE];
+  constexpr int SK = 8 * UE;  // columns of a step: two units of each of four lanes
+  __shared__ f32x4v_t part[16][NT][64];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r16 = lane & 15, q = lane >> 4;
+  const int64_t o0 = static_cast<int64_t>(blockIdx.x) * 16, m0 = static_cast<int64_t>(blockIdx.y) * (16 * NT);
+  // Rows past the last one read the last one's values; their results go nowhere.
+  const T* W = reinterpret_cast<const T*>(g.w) + min(o0 + r16, g.out - 1) * g.in;
+  const T* X[NT];
 #pragma unroll
-    for (int i = 0; i < UE; ++i) e[i] = ok && k + i < g.in ? load_bits(base + k + i) : 0u;
-    vec16 r;
-    pack16<T>(r, e);
-    return r;
-  };
-  f32x16_t acc = zero16();
-  vec16 rx = fetch(X, xok, kc), rw = fetch(W, wok, kc);
-  const int half = lane >> 5, l32 = lane & 31;
-  for (int64_t k0 = 0; k0 < g.in; k0 += BK) {
-    store16(&Xs[row * KP + kc], rx);
-    store16(&Ws[row * KP + kc], rw);
-    lds_sync();
-    rx = fetch(X, xok, k0 + BK + kc);
-    rw = fetch(W, wok, k0 + BK + kc);
+  for (int n = 0; n < NT; ++n)
+    X[n] = reinterpret_cast<const T*>(g.x) + min(m0 + 16 * n + r16, g.m - 1) * g.ldx;
+  auto unit = [&](const T* row, int64_t k) -> vec16 {
+    if constexpr (VEC) {
+      // Whole units: none straddles the end of the reduction.
+      const vec16 v = load16(row + (k < g.in ? k : 0));
+      vec16 r;
 #pragma unroll
-    for (int st = 0; st < 2; ++st) {
-      const int kofs = st * 2 * UE + half * UE;
-      mfma_32x32<T>(acc, load16(&Ws[(wo * 32 + l32) * KP + kofs]), load16(&Xs[(wx * 32 + l32) * KP + kofs]));
+      for (int i = 0; i < 4; ++i) r.d[i] = k < g.in ? v.d[i] : 0u;
+      return r;
+    } else {
+      uint32_t e[UE];
+#pragma unroll
+      for (int i = 0; i < UE; ++i) {
+        const uint32_t bits = load_bits(row + (k + i < g.in ? k + i : 0));
+        e[i] = k + i < g.in ? bits : 0u;
+      }
+      vec16 r;
+      pack16<T>(r, e);
+      return r;
     }
-    lds_sync();
-  }
-  const int64_t m = m0 + wx * 32 + l32;
-  if (m >= g.m) return;
-  const T* B = reinterpret_cast<const T*>(g.b);
-  const T* R = reinterpret_cast<const T*>(g.r);
+  };
+  const int64_t steps = (g.in + SK - 1) / SK;
+  f32x4v_t acc[NT];
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    const int64_t o = o0 + wo * 32 + mfma_row(v, lane);
-    if (o >= g.out) continue;
-    float z = acc[v];
-    if (B) z += elem<T>::load(B + o);
-    z = activate<T>(z, g.act);
-    if (R) z += elem<T>::load(R + m * g.ldr + o);
-    elem<T>::store(reinterpret_cast<T*>(g.y) + m * g.ldy + o, z);
+  for (int n = 0; n < NT; ++n) acc[n] = f32x4v_t{0.f, 0.f, 0.f, 0.f};
+  vec16 wv[kDepth][2], xv[kDepth][NT][2];
+  auto fetch = [&](int d, int64_t s) {
+    const int64_t k = s * SK + q * 2 * UE;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) wv[d][u] = unit(W, k + u * UE);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) xv[d][n][u] = unit(X[n], k + u * UE);
+  };
+  for (int64_t s0 = wave; s0 < steps; s0 += static_cast<int64_t>(waves) * kDepth) {
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) fetch(d, s0 + static_cast<int64_t>(d) * waves);
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) acc[n] = mac16(T{}, wv[d][u], xv[d][n][u], acc[n]);
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) part[wave][n][lane] = acc[n];
+  __syncthreads();
+  // Lane (row of x, q) of a tile holds outputs 4 q .. 4 q + 3: one thread finishes each of them.
+  for (int i = threadIdx.x; i < NT * 64; i += blockDim.x) {
+    const int n = i >> 6, l = i & 63;
+    const int64_t m = m0 + 16 * n + (l & 15), o = o0 + 4 * (l >> 4);
+    if (m >= g.m || o >= g.out) continue;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int w = 0; w < waves; ++w) {
+      const f32x4v_t v = part[w][n][l];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) sum[x] += v[x];
+    }
+    finish4<T>(g, m, o, sum, vec_out);
   }
 }
 
-}  // namespace
+// Which kernel: up to kFewRows rows, or operands the tiles cannot address.
+constexpr int64_t kFewRows = 16;
 
-size_t linear_workspace(const LinearArgs&) { return 0; }
+struct RowsPlan {
+  int waves, nt;
+  bool vec;
+};
 
-hipError_t launch_linear(const LinearArgs& a, void*, hipStream_t stream) {
+RowsPlan rows_plan(const LinearArgs& a) {
   const int64_t per = a.dtype == CONV_F32 ? 4 : 8;
-  const bool vec = a.in % per == 0 && a.ldx % per == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.w % 16 == 0;
-  const int64_t to = (a.out + 63) / 64, tm = (a.m + 63) / 64;
-  const dim3 grid((unsigned)(to * tm));
-  if (a.dtype == CONV_F32) {
-    if (vec)
-      hipLaunchKernelGGL((linear_tile_kernel<float, true>), grid, dim3(256), 0, stream, a, (int)to);
-    else
-      hipLaunchKernelGGL((linear_tile_kernel<float, false>), grid, dim3(256), 0, stream, a, (int)to);
-  } else {
-    if (vec)
-      hipLaunchKernelGGL((linear_tile_kernel<bf16_t, true>), grid, dim3(256), 0, stream, a, (int)to);
-    else
-      hipLaunchKernelGGL((linear_tile_kernel<bf16_t, false>), grid, dim3(256), 0, stream, a, (int)to);
+  RowsPlan p;
+  p.vec = a.in % per == 0 && a.ldx % per == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.w % 16 == 0;
+  p.nt = a.m <= 16 ? 1 : 2;
+  // Each wave has kDepth steps at least where the reduction is that long.
+  const int64_t steps = (a.in + 8 * per - 1) / (8 * per);
+  int64_t w = steps / kDepth;
+  p.waves = (int)(w < 1 ? 1 : w > 16 ? 16 : w);
+  return p;
+}
+
+template <typename T, bool VEC, int NT>
+hipError_t launch_rows(const LinearArgs& a, const RowsPlan& p, int vec_out, hipStream_t st) {
+  const int64_t groups = (a.m + 16 * NT - 1) / (16 * NT);
+  for (int64_t g0 = 0; g0 < groups; g0 += 65535) {
+    LinearArgs b = a;
+    const int64_t es = sizeof(T), m0 = g0 * 16 * NT;
+    b.x = (const char*)a.x + m0 * a.ldx * es;
+    b.y = (char*)a.y + m0 * a.ldy * es;
+    if (a.r) b.r = (const char*)a.r + m0 * a.ldr * es;
+    b.m = a.m - m0;
+    const int64_t n = groups - g0 < 65535 ? groups - g0 : 65535;
+    if (n * 16 * NT < b.m) b.m = n * 16 * NT;
+    hipLaunchKernelGGL((linear_rows_kernel<T, VEC, NT>), dim3((unsigned)((a.out + 15) / 16), (unsigned)n),
+                       dim3(64 * p.waves), 0, st, b, p.waves, vec_out);
   }
   return hipGetLastError();
 }
 
-void linear_describe(const LinearArgs&, char* buf, size_t len) {
-  snprintf(buf, len, "linear kernels=linear_tile_kernel tile=64x64 workspace=0");
+template <typename T>
+hipError_t launch_rows_t(const LinearArgs& a, const RowsPlan& p, int vec_out, hipStream_t st) {
+  if (p.nt == 1)
+    return p.vec ? launch_rows<T, true, 1>(a, p, vec_out, st) : launch_rows<T, false, 1>(a, p, vec_out, st);
+  return p.vec ? launch_rows<T, true, 2>(a, p, vec_out, st) : launch_rows<T, false, 2>(a, p, vec_out, st);
+}
+
+// Whether outputs may be read and written four at a time.
+int outputs_vec(const LinearArgs& a) {
+  const uintptr_t unit = a.dtype == CONV_F32 ? 16 : 8;
+  return a.ldy % 4 == 0 && (uintptr_t)a.y % unit == 0 && (!a.r || (a.ldr % 4 == 0 && (uintptr_t)a.r % unit == 0));
+}
+
+bool in_rows(const LinearArgs& a, LinearTiles* t) {
+  *t = linear_tiles_plan(a);
+  return a.m <= kFewRows || t->config < 0;
+}
+
+}  // namespace
+
+size_t linear_workspace(const LinearArgs& a) {
+  LinearTiles t;
+  if (in_rows(a, &t)) return 0;
+  return t.pack_bytes + t.part_bytes;
+}
+
+hipError_t launch_linear(const LinearArgs& a, void* workspace, hipStream_t stream) {
+  LinearTiles t;
+  if (!in_rows(a, &t)) return launch_linear_tiles(a, t, workspace, stream);
+  const RowsPlan p = rows_plan(a);
+  return a.dtype == CONV_F32 ? launch_rows_t<float>(a, p, outputs_vec(a), stream)
+                             : launch_rows_t<bf16_t>(a, p, outputs_vec(a), stream);
+}
+
+void linear_describe(const LinearArgs& a, char* buf, size_t len) {
+  LinearTiles t;
+  if (in_rows(a, &t)) {
+    const RowsPlan p = rows_plan(a);
+    snprintf(buf, len, "linear kernels=linear_rows_kernel tile=%dx16 waves=%d workspace=0", 16 * p.nt, p.waves);
+    return;
+  }
+  snprintf(buf, len, "linear kernels=%slinear_tiles_kernel%s tile=%s split=%d workspace=%zu",
+           t.pack ? "linear_pack_kernel;" : "", t.splits > 1 ? ";linear_join_kernel" : "", linear_tiles_name(t.config),
+           t.splits, linear_workspace(a));
 }
 
 }  // namespace convsel

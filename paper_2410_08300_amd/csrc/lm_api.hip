@@ -53,7 +53,7 @@ bool rows_apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t inner) {
 
 conv_status_t linear_sizes(const convsel_linear_desc_t* d) {
   if (!d || d->m < 0 || d->in_features < 1 || d->out_features < 1) return CONV_ERR_INVALID_ARG;
-  if (d->m > kInt31 || d->in_features > kInt31 || d->out_features > kInt31) return CONV_ERR_INVALID_ARG;
+  if (d->m > kInt31 || d->in_features > kInt31 || d->out_features >= ((int64_t)1 << 26)) return CONV_ERR_INVALID_ARG;
   if (d->m > 0 && d->out_features > kOutputsMax / d->m) return CONV_ERR_INVALID_ARG;
   if (!dtype_ok(d->dtype) || d->act < CONVSEL_ACT_NONE || d->act > CONVSEL_ACT_SILU) return CONV_ERR_INVALID_ARG;
   if (!flag_ok(d->has_bias) || !flag_ok(d->has_residual)) return CONV_ERR_INVALID_ARG;
