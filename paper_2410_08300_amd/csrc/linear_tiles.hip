@@ -1,20 +1,21 @@
 // Linear layers in tiles: both operands through LDS DMA.
 //
 // A workgroup owns TM rows of x and TO outputs and walks the reduction in
-// k-tiles of 64 bytes (32 bf16, 16 fp32).  A k-tile of 16 operand rows is 1 KiB
-// of LDS, one DMA instruction: its 16-byte units lie unit by unit, 16 rows of
-// each in a row, so the 16 rows that a quarter wave reads of one unit are 256
-// consecutive bytes.  Rows past the operand and columns past the reduction read
-// zeros through the buffer's range.  Four stages form a ring with three k-tiles
-// on their way.  A wave multiplies FO x FM blocks of 32 x 32; the operands of a
-// k-tile's second half are read while its first half multiplies, and the next
-// k-tile's first half (behind the tile's one barrier) while the second does.
+// k-tiles of 128 bytes (64 bf16, 32 fp32), so that every DMA instruction reads
+// whole cache lines: eight operand rows of 128 bytes.  In LDS two rows share a
+// 256-byte line, with the 16-byte unit u of row r at place 8 (r % 2) + (u ^ (r /
+// 2 % 8)): the 16 rows that a quarter wave reads of one unit lie on different
+// banks.  Rows past the operand and columns past the reduction read zeros
+// through the buffer's range.  NST stages form a ring; a stage is filled again
+// as soon as its last unit is read.  A wave multiplies FO x FM blocks of 32 x 32
+// in four steps a k-tile; the operands of a step are read while the step before
+// it multiplies, those of the next k-tile's first step behind the tile's one
+// barrier.
 //
 // The products' rows are w's and their columns x's.  Sums leave through LDS,
 // each wave in a place of its own, so that every row of y is read (residual)
 // and written along its outputs.
 #include <stdio.h>
-#include <stdlib.h>
 
 #include <type_traits>
 
@@ -27,18 +28,17 @@ namespace {
 using namespace igemm;
 using namespace lm;
 
-constexpr int kStages = 4;
-
-template <int FO_, int FM_, int WO_, int WM_>
+template <int FO_, int FM_, int WO_, int WM_, int NST_>
 struct Tile {
-  static constexpr int FO = FO_, FM = FM_, WO = WO_, WM = WM_;
+  static constexpr int FO = FO_, FM = FM_, WO = WO_, WM = WM_, NST = NST_;
   static constexpr int TO = FO * 32 * WO, TM = FM * 32 * WM, WAVES = WO * WM;
-  static constexpr int STAGE = (TO + TM) * 64;
-  static constexpr int NDMA = (TO + TM) / 16 / WAVES;  // DMA instructions of a wave and stage
-  static constexpr int OUT_ROW = FO * 32 + 4;          // floats: rows 16 bytes apart in the banks
+  static constexpr int STAGE = (TO + TM) * 128;
+  static constexpr int NDMA = (TO + TM) / 8 / WAVES;  // DMA instructions of a wave and stage
+  static constexpr int OUT_ROW = FO * 32 + 4;         // floats: rows 16 bytes apart in the banks
   static constexpr int OUT = WAVES * 32 * OUT_ROW * 4;
-  static constexpr int LDS = kStages * STAGE > OUT ? kStages * STAGE : OUT;
-  static_assert((TO + TM) % (16 * WAVES) == 0 && LDS <= 160 * 1024 && NDMA * (kStages - 1) <= 63, "tile");
+  static constexpr int LDS = NST * STAGE > OUT ? NST * STAGE : OUT;
+  static_assert((TO + TM) % (8 * WAVES) == 0 && LDS <= 160 * 1024 && NST >= 2 && NST <= 4 && NDMA * (NST - 1) <= 63,
+                "tile");
 };
 
 struct TileArgs {
@@ -52,7 +52,7 @@ struct TileArgs {
 template <typename T, typename S>
 __global__ __launch_bounds__(S::WAVES * 64, S::WAVES == 8 ? 2 : 1) void linear_tiles_kernel(TileArgs a) {
   constexpr int FO = S::FO, FM = S::FM, NDMA = S::NDMA, STAGE = S::STAGE;
-  constexpr int ES = elem<T>::bytes, UE = elem<T>::per16, BK = 64 / ES;
+  constexpr int NST = S::NST, ES = elem<T>::bytes, UE = elem<T>::per16, BK = 128 / ES;
   __shared__ __align__(16) char lds[S::LDS];
   const LinearArgs& g = a.g;
   const int lane = threadIdx.x & 63;
@@ -77,39 +77,40 @@ __global__ __launch_bounds__(S::WAVES * 64, S::WAVES == 8 ? 2 : 1) void linear_t
   const u32x4_t xr = dma_rsrc(reinterpret_cast<const T*>(g.x) + m0 * g.ldx, xbytes);
   const uint32_t lds0 = lds_address(lds);
 
-  // Instruction J = wave * NDMA + d of a stage fills rows 16 J .. 16 J + 15: w's rows first, then x's.
+  // Instruction J = wave * NDMA + d of a stage fills rows 8 J .. 8 J + 7: w's rows first, then x's.
   uint32_t dvo[NDMA];
-  const int dku = (lane >> 4) * UE;  // this lane's column within a k-tile
+  int dku[NDMA];  // this lane's column within a k-tile
 #pragma unroll
   for (int d = 0; d < NDMA; ++d) {
-    const int row = (wave * NDMA + d) * 16 + (lane & 15);
+    const int U = (wave * NDMA + d) * 64 + lane;
+    const int line = U >> 4, pos = U & 15;
+    const int row = 2 * line + (pos >> 3);
+    dku[d] = ((pos & 7) ^ (line & 7)) * UE;
     const bool isw = row < S::TO;
     const int64_t r = isw ? row : row - S::TO;
     const bool ok = r < (isw ? wrows : xrows);
-    dvo[d] = ok ? static_cast<uint32_t>((r * (isw ? g.in : g.ldx) + dku) * ES) : (isw ? wbytes : xbytes);
+    dvo[d] = ok ? static_cast<uint32_t>((r * (isw ? g.in : g.ldx) + dku[d]) * ES) : (isw ? wbytes : xbytes);
   }
   const int k0 = split * a.per, all = static_cast<int>((g.in + BK - 1) / BK);
   const int nk = min(all, k0 + a.per) - k0;
-  auto issue = [&](int kt) {
-    const uint32_t st = lds0 + (kt % kStages) * STAGE;
-    const uint32_t so = static_cast<uint32_t>(k0 + kt) * 64;
-    const bool past = static_cast<int64_t>(k0 + kt) * BK + dku >= g.in;
-#pragma unroll
-    for (int d = 0; d < NDMA; ++d) {
-      const int J = wave * NDMA + d;
-      const bool isw = J < S::TO / 16;
-      dma16(isw ? wr : xr, st + J * 1024, past ? (isw ? wbytes : xbytes) : dvo[d], so);
-    }
+  // DMA instruction d of stage kt.  Past the last k-tile it fills the stage with zeros that nobody reads: the loop
+  // below has no branch, and the same number is always on its way.
+  auto issue = [&](int kt, int d) {
+    const uint32_t st = lds0 + (kt % NST) * STAGE;
+    const int at = k0 + min(kt, nk - 1);
+    const int64_t left = kt < nk ? g.in - static_cast<int64_t>(at) * BK : 0;
+    const int J = wave * NDMA + d;
+    const bool isw = J < S::TO / 8;
+    dma16(isw ? wr : xr, st + J * 1024, dku[d] < left ? dvo[d] : (isw ? wbytes : xbytes),
+          static_cast<uint32_t>(at) * 128);
   };
 
+  // Unit 2 t + half of row l32 of a block of 32 rows.
   const int half = lane >> 5, l32 = lane & 31;
-  // Unit 2 t + half of row r of a stage.
-  auto place = [&](int r, int t) { return (r >> 4) * 1024 + (2 * t + half) * 256 + (r & 15) * 16; };
-  int woff[FO], xoff[FM];
+  int off[4];
 #pragma unroll
-  for (int i = 0; i < FO; ++i) woff[i] = place((wo * FO + i) * 32 + l32, 0);
-#pragma unroll
-  for (int i = 0; i < FM; ++i) xoff[i] = place(S::TO + (wm * FM + i) * 32 + l32, 0);
+  for (int t = 0; t < 4; ++t)
+    off[t] = (l32 >> 1) * 256 + ((8 * (l32 & 1) + ((2 * t + half) ^ ((l32 >> 1) & 7))) << 4);
 
   f32x16_t acc[FO][FM];
 #pragma unroll
@@ -119,49 +120,72 @@ __global__ __launch_bounds__(S::WAVES * 64, S::WAVES == 8 ? 2 : 1) void linear_t
   vec16 fw[2][FO], fx[2][FM];
   auto read = [&](int kt, auto t_c) {
     constexpr int t = decltype(t_c)::value;
-    const char* st = lds + (kt % kStages) * STAGE + t * 512;
+    const char* st = lds + (kt % NST) * STAGE + off[t];
 #pragma unroll
-    for (int i = 0; i < FO; ++i) fw[t][i] = *reinterpret_cast<const vec16*>(st + woff[i]);
+    for (int i = 0; i < FM; ++i) fx[t & 1][i] = *reinterpret_cast<const vec16*>(st + S::TO * 128 + (wm * FM + i) * 4096);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) fx[t][i] = *reinterpret_cast<const vec16*>(st + xoff[i]);
-    __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < FO; ++i) fw[t & 1][i] = *reinterpret_cast<const vec16*>(st + (wo * FO + i) * 4096);
   };
   auto multiply = [&](auto t_c) {
     constexpr int t = decltype(t_c)::value;
 #pragma unroll
     for (int i = 0; i < FO; ++i)
 #pragma unroll
-      for (int j = 0; j < FM; ++j) mfma_32x32<T>(acc[i][j], fw[t][i], fx[t][j]);
+      for (int j = 0; j < FM; ++j) mfma_32x32<T>(acc[i][j], fw[t & 1][i], fx[t & 1][j]);
+  };
+  // One step: the reads of the next one between the products of this.
+  auto interleave = [&]() {
+    constexpr int M = FO * FM * (ES == 4 ? 4 : 1), R = FO + FM;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, M >= 2 * R ? 2 : 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
     __builtin_amdgcn_sched_barrier(0);
   };
-  // Stage kt is in once no DMAs but those of later stages are pending: two of them at the start, one from then on
-  // (the third is issued behind the barrier).  Behind it every wave is also done with stage kt - 2.
-  auto arrive = [&](int kt) {
-    const int later = min(nk - 1, kt == 0 ? kStages - 2 : kt + 1) - kt;
-    if (later >= 2) CONVSEL_WAIT_VMCNT(2 * NDMA);
-    else if (later == 1) CONVSEL_WAIT_VMCNT(NDMA);
-    else CONVSEL_WAIT_VMCNT(0);
-    asm volatile("" ::: "memory");
+  // A stage is in once no DMAs but those of the `later` stages issued after it are pending.  This wave's reads of the
+  // stage before it have arrived too, so behind the barrier that stage may be filled again.
+  auto arrive = [&](auto later_c) {
+    CONVSEL_WAIT_VMCNT(decltype(later_c)::value * NDMA);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  const std::integral_constant<int, 0> first{};
-  const std::integral_constant<int, 1> second{};
+  const std::integral_constant<int, 0> t0{};
+  const std::integral_constant<int, 1> t1{};
+  const std::integral_constant<int, 2> t2{};
+  const std::integral_constant<int, 3> t3{};
 #pragma unroll
-  for (int p = 0; p < kStages - 1; ++p)
-    if (p < nk) issue(p);
-  arrive(0);
-  read(0, first);
+  for (int p = 0; p < NST; ++p)
+#pragma unroll
+    for (int d = 0; d < NDMA; ++d) issue(p, d);
+  arrive(std::integral_constant<int, NST - 1>{});
+  read(0, t0);
+  __builtin_amdgcn_sched_barrier(0);
   for (int kt = 0; kt < nk; ++kt) {
-    read(kt, second);
-    multiply(first);
-    if (kt + 1 < nk) {
-      arrive(kt + 1);
-      if (kt + kStages - 1 < nk) issue(kt + kStages - 1);
-      read(kt + 1, first);
+    read(kt, t1);
+    multiply(t0);
+    interleave();
+    read(kt, t2);
+    multiply(t1);
+    interleave();
+    read(kt, t3);
+    multiply(t2);
+    interleave();
+    arrive(std::integral_constant<int, NST - 2>{});
+    read(kt + 1, t0);
+    __builtin_amdgcn_sched_barrier(0);
+    // The stage just read is filled again, an instruction behind each product: a burst of them would leave the matrix
+    // cores idle.
+#pragma unroll
+    for (int q = 0; q < FO * FM || q < NDMA; ++q) {
+      if (q < FO * FM) mfma_32x32<T>(acc[q / FM][q % FM], fw[1][q / FM], fx[1][q % FM]);
+      __builtin_amdgcn_sched_barrier(0);
+      if (q < NDMA) issue(kt + NST, q);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    multiply(second);
   }
+  CONVSEL_WAIT_VMCNT(0);  // the zeros behind the last k-tile too
 
   lds_sync();  // every wave is done with the stages
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * S::OUT_ROW;
@@ -233,10 +257,11 @@ __global__ __launch_bounds__(256) void linear_pack_kernel(LinearArgs g, T* dst, 
   }
 }
 
-typedef Tile<4, 2, 2, 4> Tile256;
-typedef Tile<2, 2, 2, 2> Tile128;
-typedef Tile<1, 1, 2, 2> Tile64;
-constexpr int kTileSide[3] = {256, 128, 64};
+// A wave's block is 128 x 64, 64 x 64 and 32 x 32 (outputs x rows).
+typedef Tile<4, 2, 2, 4, 2> Tile256;
+typedef Tile<2, 2, 2, 2, 2> Tile128;
+typedef Tile<1, 1, 2, 2, 4> Tile64;
+constexpr int kSide[3] = {256, 128, 64};
 
 template <typename T, typename S>
 hipError_t launch(const TileArgs& a, hipStream_t st) {
@@ -262,10 +287,10 @@ hipError_t launch_all(const LinearArgs& a0, const LinearTiles& p, void* workspac
     a.g.in = a.g.ldx = padded;
     ws += p.pack_bytes;
   }
-  const int side = kTileSide[p.config];
+  const int side = kSide[p.config];
   a.to = (int)((a0.out + side - 1) / side);
   a.tm = (int)((a0.m + side - 1) / side);
-  const int64_t bk = 64 / sizeof(T), all = (a.g.in + bk - 1) / bk;
+  const int64_t bk = 128 / sizeof(T), all = (a.g.in + bk - 1) / bk;
   a.splits = p.splits;
   a.per = (int)((all + p.splits - 1) / p.splits);
   a.part = (float*)ws;
@@ -292,6 +317,7 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
   const int64_t padded = (a.in + per - 1) / per * per;
   p.pack_bytes = p.pack ? align256((size_t)(a.m + a.out) * padded * es) : 0;
   p.part_bytes = 0;
+  p.config = 0;
   p.splits = 1;
   // A tile's rows are addressed in 32 bits from its first one.
   const int64_t ld = p.pack || a.in > a.ldx ? padded : a.ldx;
@@ -299,20 +325,32 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
     p.config = -1;
     return p;
   }
-  auto tiles = [&](int side) { return ((a.out + side - 1) / side) * ((a.m + side - 1) / side); };
-  const int64_t all = (a.in + 64 / es - 1) / (64 / es);
-  const char* force = getenv("LCFG");
-  if (force) { p.config = atoi(force); } else {
-  p.config = tiles(256) >= 256 ? 0 : tiles(128) >= 256 ? 1 : 2; }
-  const int64_t n = tiles(kTileSide[p.config]);
-  int64_t want = getenv("LWANT") ? atoi(getenv("LWANT")) : 512;
-  int64_t s = want / n;
-  int64_t least = getenv("LLEAST") ? atoi(getenv("LLEAST")) : 16;
-  if (s > all / least) s = all / least;
-  if (s > 16) s = 16;
-  if (s < 1) s = 1;
-  if (n * s >= ((int64_t)1 << 22)) { /* grids stay in range: one part */ s = 1; }
-  p.splits = (int)((all + (all + s - 1) / s - 1) / ((all + s - 1) / s));
+  auto tiles = [&](int c) { return ((a.out + kSide[c] - 1) / kSide[c]) * ((a.m + kSide[c] - 1) / kSide[c]); };
+  const int64_t all = (a.in + 128 / es - 1) / (128 / es);
+  // The tile and the parts that take the least time by what was measured: a k-tile takes a CU with one workgroup
+  // `one` us and a CU with k of them (one after the other or side by side) k * `each`, whichever is more; a call
+  // some 4 us around that, joining parts 2.5 and their way through the caches at 8 TB/s.  At 4096 -> 4096 in bf16:
+  // 4096 rows 130 us in 256s, 155 in 128s, 258 in 64s; 2048 rows 109, 79, 124; 256 rows 95, 25 (4 parts), 24 (2).
+  static const double kOne[2][3] = {{7.4, 2.1, 0.66}, {1.55, 0.83, 0.36}};
+  static const double kEach[2][3] = {{7.6, 2.05, 0.645}, {2.05, 0.61, 0.25}};
+  const int ty = a.dtype == CONV_F32 ? 0 : 1;
+  double best = 0.;
+  for (int c = 0; c < 3; ++c) {
+    const int64_t n = tiles(c);
+    for (int64_t s = 1; s <= 16; ++s) {
+      if (s > 1 && (s > all / 4 || n * s > 2048)) break;
+      const int64_t per_part = (all + s - 1) / s, parts = (all + per_part - 1) / per_part;
+      if (parts != s) continue;
+      const double k = (double)((n * s + 255) / 256);
+      double t = per_part * (kOne[ty][c] > k * kEach[ty][c] ? kOne[ty][c] : k * kEach[ty][c]);
+      if (s > 1) t += 2.5 + (double)s * a.m * a.out * 8 / 8e6;
+      if ((c == 0 && s == 1) || t < best) {
+        best = t;
+        p.config = c;
+        p.splits = (int)s;
+      }
+    }
+  }
   if (p.splits > 1) p.part_bytes = (size_t)p.splits * a.m * ((a.out + 3) / 4 * 4) * 4;
   return p;
 }

@@ -95,6 +95,10 @@ def linear(x, w, b=None, act="none", residual=None, out=None):
     r2, ldr = (None, 0) if residual is None else _rows(residual)
     w = w.contiguous()
     b = None if b is None else b.contiguous()
+    if x2.shape[0] > 16:
+        # The library's tiles read operands that start on 16 bytes; a view that does not is copied first.
+        x2, ldx = (x2, ldx) if x2.data_ptr() % 16 == 0 else (x2.clone(memory_format=torch.contiguous_format), i)
+        w = w if w.data_ptr() % 16 == 0 else w.clone()
     d = _linear_desc(x2.shape[0], i, o, ldx, ldr, ldy, dt, act, b is not None, r2 is not None)
     L = _lib.lib()
     n = ctypes.c_size_t()

@@ -65,6 +65,44 @@ def test_linear_sizes(size, dtype):
         within(y, want, bound + ref.half_ulp(dt) * want.abs() * 1.01, "linear %s %s" % (size, activation))
 
 
+# One case for each tile and way of cutting it, with the kernels that it must reach.
+TILE_SIZES = [(4000, 72, 4001, "tile=256x256 split=1"), (3999, 200, 4000, "tile=256x256 split=1"),
+              (2000, 136, 2100, "tile=128x128 split=1"), (2050, 1030, 2048, "linear_pack_kernel;linear_tiles_kernel tile=128x128 split=1"),
+              (1030, 8200, 2052, "tile=128x128 split=5"), (100, 2056, 130, "tile=64x64 split="),
+              (500, 260, 1000, "linear_pack_kernel;linear_tiles_kernel tile=64x64 split=1"), (1111, 100, 999, "tile=64x64 split=1")]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("size", TILE_SIZES, ids=lambda s: "x".join(map(str, s[:3])))
+def test_linear_in_every_tile(size, dtype):
+    m, i, o, runs = size
+    dt = DT[dtype]
+    say("case linear tile", size, dtype, cs.describe_linear(m, i, o, dt))
+    if dtype == "bf16":
+        assert runs in cs.describe_linear(m, i, o, dt)
+    g = gen(m + i)
+    x = torch.randn(m, i, generator=g, device=DEV).to(dt)
+    w = (torch.randn(o, i, generator=g, device=DEV) / i ** 0.5).to(dt)
+    b = torch.randn(o, generator=g, device=DEV).to(dt)
+    r = torch.randn(m, o, generator=g, device=DEV).to(dt)
+    whole = torch.full((m + 2, o + 6), 7.0, device=DEV, dtype=dt)
+    y = whole[1:-1, 2:o + 2]
+    cs.linear(x, w, b, act="silu", residual=r, out=y)
+    # The reference on the GPU in 64 bits: its own roundings are nothing here.
+    xd, wd = x.double(), w.double()
+    z = xd @ wd.T.contiguous() + b.double()
+    mag = xd.abs() @ wd.abs().T.contiguous() + b.double().abs()
+    want = z / (1 + torch.exp(-z))
+    bound = (i + 8) * 2.0 ** -24 * 1.13 * mag + 16 * 2.0 ** -24 * want.abs()
+    want = want + r.double()
+    bound = bound + (2.0 ** -24 + ref.half_ulp(dt) * 1.01) * want.abs()
+    assert bool(((y.double() - want).abs() <= bound).all())
+    inside = torch.zeros_like(whole, dtype=torch.bool)
+    inside[1:-1, 2:o + 2] = True
+    assert bool((whole[~inside] == 7.0).all())
+    assert torch.equal(cs.linear(x, w, b, act="silu", residual=r), y)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("activation", list(cs.ACTIVATIONS))
 def test_linear_activations_over_their_range(activation, dtype):
