@@ -9,6 +9,7 @@ Calls are asynchronous, and like every PyTorch operation they take tensors of
 another stream only after the caller has made the current one wait for it.
 """
 import ctypes
+import functools
 import math
 
 import torch
@@ -22,28 +23,21 @@ ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 FORMATS = {"int8": 0, "fp8": 1}
 
 
-def _dtype_of(what, *tensors):
-    dt = tensors[0].dtype
+def _dtype_of(what, first, *others):
+    dt, dev = first.dtype, first.device
     if dt not in _DTYPES:
         raise ValueError("%s: unsupported dtype %s (float32 or bfloat16)" % (what, dt))
-    dev = tensors[0].device
-    for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("%s runs on the GPU only: move its tensors to a HIP device" % what)
-        if t.dtype != dt or t.device != dev:
-            raise ValueError("%s: tensors must share one dtype and device" % what)
+    if dev.type != "cuda":
+        raise ValueError("%s runs on the GPU only: move its tensors to a HIP device" % what)
+    for t in others:
+        if t is not None and (t.dtype is not dt or t.device != dev):
+            raise ValueError("%s: tensors must share one dtype and one HIP device" % what)
     return _DTYPES[dt]
 
 
 def _raise(st, what):
-    if st != _lib.CONV_OK:
+    if st:
         raise _lib.Conv2dError(st, what)
-
-
-def _workspace(nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
 # ---- linear -------------------------------------------------------------------
@@ -51,6 +45,8 @@ def _workspace(nbytes, device):
 def _rows(t):
     """t as a matrix of rows with a dense last dimension (a view where it can
     be one), and its row stride."""
+    if t.dim() == 2 and t.is_contiguous():
+        return t, t.shape[1]
     m = t.reshape(-1, t.shape[-1])
     if m.stride(1) != 1 and m.shape[1] > 1 or m.stride(0) < m.shape[1] and m.shape[0] > 1:
         m = m.contiguous()
@@ -61,6 +57,15 @@ def _linear_desc(m, i, o, ldx, ldr, ldy, dtype, act, bias, residual):
     if act not in ACTIVATIONS:
         raise ValueError("unknown activation %r (one of %s)" % (act, ", ".join(ACTIVATIONS)))
     return _lib.LinearDesc(m, i, o, ldx, ldr, ldy, dtype, ACTIVATIONS[act], bias, residual)
+
+
+@functools.lru_cache(maxsize=1024)
+def _linear_plan(*sizes):
+    """(descriptor by reference, workspace bytes) of a call of these sizes."""
+    d = ctypes.byref(_linear_desc(*sizes))
+    n = ctypes.c_size_t()
+    _raise(_lib.lib().convsel_linear_workspace_bytes(d, ctypes.byref(n)), "linear")
+    return d, n.value
 
 
 def linear(x, w, b=None, act="none", residual=None, out=None):
@@ -99,15 +104,13 @@ def linear(x, w, b=None, act="none", residual=None, out=None):
         # The library's tiles read operands that start on 16 bytes; a view that does not is copied first.
         x2, ldx = (x2, ldx) if x2.data_ptr() % 16 == 0 else (x2.clone(memory_format=torch.contiguous_format), i)
         w = w if w.data_ptr() % 16 == 0 else w.clone()
-    d = _linear_desc(x2.shape[0], i, o, ldx, ldr, ldy, dt, act, b is not None, r2 is not None)
-    L = _lib.lib()
-    n = ctypes.c_size_t()
-    _raise(L.convsel_linear_workspace_bytes(ctypes.byref(d), ctypes.byref(n)), "linear")
-    with _on(x.device):
-        ws = _workspace(n.value, x.device)
-        st = L.convsel_linear(x2.data_ptr(), w.data_ptr(), None if b is None else b.data_ptr(),
-                              None if r2 is None else r2.data_ptr(), y2.data_ptr(), ctypes.byref(d),
-                              None if ws is None else ws.data_ptr(), n.value, _stream_of(x.device))
+    d, n = _linear_plan(x2.shape[0], i, o, ldx, ldr, ldy, dt, act, b is not None, r2 is not None)
+    dev = x.device
+    with _on(dev):
+        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+        st = _lib.lib().convsel_linear(x2.data_ptr(), w.data_ptr(), None if b is None else b.data_ptr(),
+                                       None if r2 is None else r2.data_ptr(), y2.data_ptr(), d,
+                                       None if ws is None else ws.data_ptr(), n, _stream_of(dev))
     _raise(st, "linear")
     return out
 
@@ -131,9 +134,14 @@ def _heads(t, what):
 
 
 def _ints(t, n, what, device):
-    if t.dtype != torch.int32 or tuple(t.shape) != n or t.device != device:
-        raise ValueError("%s must be an int32 tensor of shape %s on %s" % (what, n, device))
-    return t.contiguous()
+    if t.dtype is not torch.int32 or t.shape != n or t.device != device:
+        raise ValueError("%s must be an int32 tensor of shape %s on %s" % (what, tuple(n), device))
+    return t if t.is_contiguous() else t.contiguous()
+
+
+@functools.lru_cache(maxsize=1024)
+def _qk_plan(*sizes):
+    return ctypes.byref(_lib.QkDesc(*sizes))
 
 
 def qk_norm_rope(q, k, positions, cos, sin, q_weight=None, k_weight=None, eps=1e-6, norm="rms", interleaved=False,
@@ -181,14 +189,14 @@ def qk_norm_rope(q, k, positions, cos, sin, q_weight=None, k_weight=None, eps=1e
     if dim == 0:
         raise ValueError("qk_norm_rope: empty heads")
     qs, ks, qo, ko = q.stride(), k.stride(), q_out.stride(), k_out.stride()
-    d = _lib.QkDesc(t, hq, hk, dim, rotary, qs[0], qs[1], ks[0], ks[1], qo[0], qo[1], ko[0], ko[1], rows, dt,
-                    1 if norm == "rms" else 0, bool(interleaved), eps)
+    d = _qk_plan(t, hq, hk, dim, rotary, qs[0], qs[1], ks[0], ks[1], qo[0], qo[1], ko[0], ko[1], rows, dt,
+                 1 if norm == "rms" else 0, bool(interleaved), eps)
     with _on(q.device):
         st = _lib.lib().convsel_qk_norm_rope(
             q.data_ptr(), k.data_ptr(), None if q_weight is None else q_weight.data_ptr(),
             None if k_weight is None else k_weight.data_ptr(), positions.data_ptr() if rotary else None,
             cos.data_ptr() if rotary else None, sin.data_ptr() if rotary else None, q_out.data_ptr(),
-            k_out.data_ptr(), ctypes.byref(d), _stream_of(q.device))
+            k_out.data_ptr(), d, _stream_of(q.device))
     _raise(st, "qk_norm_rope")
     return q_out, k_out
 
@@ -227,23 +235,21 @@ class KVCache:
         self.k_scales = torch.zeros(self.pages, self.kv_heads, device=device)
         self.v_scales = torch.zeros(self.pages, self.kv_heads, device=device)
         self.device = self.k_codes.device
+        # The cache as the library takes it; its buffers stay for the object's life.
+        self._desc = ctypes.byref(_lib.KvCacheDesc(
+            self.pages, self.kv_heads, self.head_dim, self.page_size, FORMATS[fmt], self.k_codes.data_ptr(),
+            self.v_codes.data_ptr(), self.k_scales.data_ptr(), self.v_scales.data_ptr()))
 
-    def desc(self):
-        """The cache as the library takes it."""
-        return _lib.KvCacheDesc(self.pages, self.kv_heads, self.head_dim, self.page_size, FORMATS[self.fmt],
-                                self.k_codes.data_ptr(), self.v_codes.data_ptr(), self.k_scales.data_ptr(),
-                                self.v_scales.data_ptr())
-
-    def batch(self, what, table, lengths, offsets, tokens):
+    def _batch(self, what, table, lengths, offsets, tokens):
         """(descriptor, tensors it points into) of a call's sequences."""
         if table.dim() != 2:
             raise ValueError("%s: the block table must be [sequences][pages]" % what)
         n = table.shape[0]
-        table = _ints(table, tuple(table.shape), "%s: the block table" % what, self.device)
-        lengths = _ints(lengths, (n,), "%s: lengths" % what, self.device)
-        offsets = _ints(offsets, (n + 1,), "%s: offsets" % what, self.device)
-        return _lib.KvBatchDesc(n, tokens, table.shape[1], table.data_ptr(), lengths.data_ptr(),
-                                offsets.data_ptr()), (table, lengths, offsets)
+        table = _ints(table, table.shape, what + ": the block table", self.device)
+        lengths = _ints(lengths, (n,), what + ": lengths", self.device)
+        offsets = _ints(offsets, (n + 1,), what + ": offsets", self.device)
+        return ctypes.byref(_lib.KvBatchDesc(n, tokens, table.shape[1], table.data_ptr(), lengths.data_ptr(),
+                                             offsets.data_ptr())), (table, lengths, offsets)
 
     def write(self, k, v, table, starts, offsets):
         """Quantises the packed tokens ``k`` and ``v`` ([tokens][kv_heads]
@@ -253,10 +259,10 @@ class KVCache:
         if k.shape != v.shape or k.shape[1:] != (self.kv_heads, self.head_dim) or k.device != self.device:
             raise ValueError("KVCache.write: k and v must be [tokens][%d][%d] on %s"
                              % (self.kv_heads, self.head_dim, self.device))
-        b, keep = self.batch("KVCache.write", table, starts, offsets, k.shape[0])
-        c, ks, vs = self.desc(), k.stride(), v.stride()
+        b, keep = self._batch("KVCache.write", table, starts, offsets, k.shape[0])
+        ks, vs = k.stride(), v.stride()
         with _on(self.device):
-            st = _lib.lib().convsel_kv_write(ctypes.byref(c), ctypes.byref(b), k.data_ptr(), v.data_ptr(), ks[0],
+            st = _lib.lib().convsel_kv_write(self._desc, b, k.data_ptr(), v.data_ptr(), ks[0],
                                              ks[1], vs[0], vs[1], dt, _stream_of(self.device))
         _raise(st, "KVCache.write")
 
@@ -266,18 +272,28 @@ class KVCache:
         ``tokens`` is their total, offsets[-1]."""
         if dtype not in _DTYPES:
             raise ValueError("KVCache.read: unsupported dtype %s (float32 or bfloat16)" % dtype)
-        b, keep = self.batch("KVCache.read", table, starts, offsets, int(tokens))
-        c = self.desc()
+        b, keep = self._batch("KVCache.read", table, starts, offsets, int(tokens))
         with _on(self.device):
             k = torch.empty((tokens, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
             v = torch.empty_like(k)
-            st = _lib.lib().convsel_kv_read(ctypes.byref(c), ctypes.byref(b), k.data_ptr(), v.data_ptr(),
+            st = _lib.lib().convsel_kv_read(self._desc, b, k.data_ptr(), v.data_ptr(),
                                             _DTYPES[dtype], _stream_of(self.device))
         _raise(st, "KVCache.read")
         return k, v
 
 
 # ---- attention ------------------------------------------------------------------
+
+@functools.lru_cache(maxsize=1024)
+def _attention_plan(pages, kv_heads, head_dim, page_size, fmt, seqs, tokens, width, *sizes):
+    """(descriptor by reference, workspace bytes) of a call of these sizes."""
+    c = _lib.KvCacheDesc(pages, kv_heads, head_dim, page_size, fmt, None, None, None, None)
+    b = _lib.KvBatchDesc(seqs, tokens, width, None, None, None)
+    d, n = ctypes.byref(_lib.AttentionDesc(*sizes)), ctypes.c_size_t()
+    _raise(_lib.lib().convsel_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(b), d, ctypes.byref(n)),
+           "cached_attention")
+    return d, n.value
+
 
 def cached_attention(q, cache, table, lengths, offsets, causal=True, window=0, scale=None, out=None):
     """Attention of the packed queries ``q`` ([tokens][q_heads][head_dim]) over
@@ -298,30 +314,27 @@ def cached_attention(q, cache, table, lengths, offsets, causal=True, window=0, s
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     elif out.shape != q.shape or (out.stride(2) != 1 and q.shape[2] > 1):
         raise ValueError("cached_attention: out must have q's shape and a dense last dimension")
-    b, keep = cache.batch("cached_attention", table, lengths, offsets, q.shape[0])
-    c, qs, ys = cache.desc(), q.stride(), out.stride()
-    d = _lib.AttentionDesc(q.shape[1], dt, bool(causal), int(window),
-                           1.0 / math.sqrt(cache.head_dim) if scale is None else scale, qs[0], qs[1], ys[0], ys[1])
-    L = _lib.lib()
-    n = ctypes.c_size_t()
-    _raise(L.convsel_attention_workspace_bytes(ctypes.byref(c), ctypes.byref(b), ctypes.byref(d), ctypes.byref(n)),
-           "cached_attention")
+    b, keep = cache._batch("cached_attention", table, lengths, offsets, q.shape[0])
+    qs, ys, c = q.stride(), out.stride(), cache._desc
+    d, n = _attention_plan(cache.pages, cache.kv_heads, cache.head_dim, cache.page_size, FORMATS[cache.fmt],
+                           table.shape[0], q.shape[0], table.shape[1], q.shape[1], dt, bool(causal), int(window),
+                           1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), qs[0], qs[1], ys[0],
+                           ys[1])
     with _on(q.device):
-        ws = _workspace(n.value, q.device)
-        st = L.convsel_attention(q.data_ptr(), ctypes.byref(c), ctypes.byref(b), out.data_ptr(), ctypes.byref(d),
-                                 None if ws is None else ws.data_ptr(), n.value, _stream_of(q.device))
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+        st = _lib.lib().convsel_attention(q.data_ptr(), c, b, out.data_ptr(), d, None if ws is None else ws.data_ptr(),
+                                          n, _stream_of(q.device))
     _raise(st, "cached_attention")
     return out
 
 
 def describe_attention(cache, seqs, tokens, table_width, q_heads, dtype=torch.bfloat16, causal=True, window=0):
     """How the library runs cached_attention at these sizes, as one line."""
-    c = cache.desc()
     b = _lib.KvBatchDesc(seqs, tokens, table_width, None, None, None)
     dim = cache.head_dim
     d = _lib.AttentionDesc(q_heads, _DTYPES[dtype], bool(causal), int(window), 1.0, q_heads * dim, dim, q_heads * dim,
                            dim)
     buf = ctypes.create_string_buffer(512)
-    _raise(_lib.lib().convsel_attention_describe(ctypes.byref(c), ctypes.byref(b), ctypes.byref(d), buf, len(buf)),
+    _raise(_lib.lib().convsel_attention_describe(cache._desc, ctypes.byref(b), ctypes.byref(d), buf, len(buf)),
            "cached_attention")
     return buf.value.decode()

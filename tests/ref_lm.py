@@ -56,19 +56,15 @@ def norm_rope(x, weight, positions, cos, sin, eps, rms, interleaved):
         return z, z.abs()
     half = cos.shape[1]
     out, mag = z.clone(), z.abs()
-    for t in range(x.shape[0]):
-        p = int(positions[t])
-        if p < 0 or p >= cos.shape[0]:
-            out[t] = float("nan")
-            continue
-        for i in range(half):
-            a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + half)
-            c, s = float(cos[p, i]), float(sin[p, i])
-            out[t, :, a] = z[t, :, a] * c - z[t, :, b] * s
-            out[t, :, b] = z[t, :, b] * c + z[t, :, a] * s
-            both = z[t, :, a].abs() + z[t, :, b].abs()
-            mag[t, :, a] = both
-            mag[t, :, b] = both
+    p = torch.tensor(positions, dtype=torch.int64)
+    there = (p >= 0) & (p < cos.shape[0])
+    c, s = (f64(t)[torch.where(there, p, 0)][:, None, :] for t in (cos, sin))
+    first = slice(0, 2 * half, 2) if interleaved else slice(0, half)
+    second = slice(1, 2 * half, 2) if interleaved else slice(half, 2 * half)
+    a, b = z[..., first], z[..., second]
+    out[..., first], out[..., second] = a * c - b * s, b * c + a * s
+    mag[..., first] = mag[..., second] = a.abs() + b.abs()
+    out[~there] = float("nan")
     return out, mag
 
 

@@ -190,7 +190,10 @@ ROPE_CASES = [  # tokens, q heads, k heads, dim, rotary, interleaved, norm, weig
     (33, 2, 2, 96, 96, True, "none", True), (3, 1, 1, 2, 2, False, "rms", True), (9, 5, 0, 256, 64, False, "rms", True),
     (4, 0, 3, 192, 96, True, "none", False), (6, 2, 1, 7, 4, False, "rms", True), (2, 2, 2, 1024, 1024, False, "rms", True),
     (65, 6, 3, 32, 0, False, "rms", True), (3, 2, 2, 100, 50, False, "rms", True), (257, 2, 1, 128, 64, True, "rms", True),
-    (4, 3, 2, 512, 512, True, "rms", True), (2, 1, 1, 1, 0, False, "rms", True)]
+    (4, 3, 2, 512, 512, True, "rms", True), (2, 1, 1, 1, 0, False, "rms", True), (6, 33, 5, 128, 128, False, "rms", True),
+    (4, 40, 1, 64, 32, False, "rms", True), (2, 9, 9, 72, 16, False, "none", True), (8, 2, 17, 256, 256, True, "rms", False),
+    (4, 7, 3, 1024, 512, False, "rms", True), (2, 3, 3, 8, 8, True, "rms", True), (130, 5, 2, 96, 0, False, "none", False),
+    (2050, 3, 1, 64, 64, True, "rms", True), (2051, 9, 2, 128, 64, False, "rms", True)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -232,6 +235,25 @@ def test_positions_outside_the_tables_are_nan_and_read_nothing(dim, rot):
     qo, ko = cs.qk_norm_rope(q, q[:, :1], pos, cos, sin)
     for o in (qo, ko):
         assert bool(o[:2].isfinite().all()) and bool(o[2:].isnan().all())
+
+
+@pytest.mark.parametrize("dim,rot,inter", [(128, 64, False), (128, 32, True), (80, 16, False), (7, 4, False)])
+def test_infinities_stay_where_nothing_turns_and_with_their_partners(dim, rot, inter):
+    cos, sin = rope_tables(64, rot)
+    pos = ints([3, 5])
+    for dt in (torch.float32, torch.bfloat16):
+        x = torch.randn(2, 3, dim, device=DEV).to(dt)
+        bad = x.clone()
+        bad[0, 1, dim - 1] = float("inf")
+        bad[1, 2, 0] = float("inf")
+        want, _ = cs.qk_norm_rope(x, x[:, :1], pos, cos, sin, norm="none", interleaved=inter)
+        got, _ = cs.qk_norm_rope(bad, x[:, :1], pos, cos, sin, norm="none", interleaved=inter)
+        assert float(got[0, 1, dim - 1]) == float("inf")
+        other = 1 if inter else rot // 2
+        assert not bool(got[1, 2, [0, other]].isfinite().any())
+        same = torch.ones_like(x, dtype=torch.bool)
+        same[0, 1, dim - 1] = same[1, 2, 0] = same[1, 2, other] = False
+        assert torch.equal(got[same], want[same])
 
 
 def test_heads_of_zeros_and_head_major_strides():
