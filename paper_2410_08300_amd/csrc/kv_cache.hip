@@ -7,12 +7,50 @@ namespace {
 
 using namespace lm;
 
-// One workgroup per (page of a sequence, head, keys or values): the largest
-// magnitude of the page's new tokens, the scale, then the codes.  Every
-// 4-byte word of codes belongs to one thread, which keeps the bytes that the
-// call does not write.
-template <typename T>
-__global__ __launch_bounds__(256) void kv_write_kernel(convsel_kv_cache_t c, convsel_kv_batch_t b, KvTokens in) {
+// Writing: one workgroup per (page of a sequence, head, keys or values).  The
+// page's new tokens are read twice, 16 bytes a lane: for the largest magnitude,
+// and, from the CU's own cache now, for the codes.  Keys leave as they lie;
+// values, whose layout puts four tokens of a column side by side, are taken four
+// tokens at a time and change places in LDS.  A page that already holds tokens,
+// or ends inside a block, goes the general way: every 4-byte word of codes
+// belongs to one thread, which keeps the bytes that the call does not write.
+//
+// What bounds it: traffic, two or four bytes in and one out for each value, and
+// for a few tokens the way from the lengths to the table to the page.
+
+// The fp32 quotient x / s of finite numbers, correctly rounded, from r = 1 / s
+// (correctly rounded): x r is within two units of it, one step with the exact
+// remainder brings that within one, and from there a second step rounds right
+// (Markstein 1990).  Five operations; the general quotient takes some twelve.
+__device__ __forceinline__ float quotient(float x, float s, float r) {
+  float q = x * r;
+  q = fmaf(fmaf(-q, s, x), r, q);
+  return fmaf(fmaf(-q, s, x), r, q);
+}
+
+// Codes of four finite numbers of magnitudes up to the block's largest: no
+// quotient is more than a rounding beyond the largest code.
+template <int FMT>
+__device__ __forceinline__ uint32_t four_codes(float x0, float x1, float x2, float x3, float s, float r) {
+  const float q0 = quotient(x0, s, r), q1 = quotient(x1, s, r), q2 = quotient(x2, s, r), q3 = quotient(x3, s, r);
+  if constexpr (FMT == CONVSEL_KV_INT8) {
+    // 1.5 * 2^23 + q holds q, rounded to nearest even, in its lowest byte.
+    const uint32_t a = __float_as_uint(q0 + 12582912.f), b = __float_as_uint(q1 + 12582912.f);
+    const uint32_t c = __float_as_uint(q2 + 12582912.f), d = __float_as_uint(q3 + 12582912.f);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u),
+                                 0x05040100u);
+  } else {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(q0, q1, 0, false);
+    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(q2, q3, lo, true));
+  }
+}
+
+template <typename T, int FMT>
+__global__ __launch_bounds__(256) void kv_write_kernel(convsel_kv_cache_t c, convsel_kv_batch_t b, KvTokens in,
+                                                       int vec) {
+  constexpr int UE = elem<T>::per16;
+  extern __shared__ __align__(16) uint8_t turn[];  // a page's value codes
+  __shared__ float red[4];
   const int seq = blockIdx.z;
   const bool values = blockIdx.y >= static_cast<unsigned>(c.kv_heads);
   const int head = values ? blockIdx.y - c.kv_heads : blockIdx.y;
@@ -24,74 +62,114 @@ __global__ __launch_bounds__(256) void kv_write_kernel(convsel_kv_cache_t c, con
   const int64_t token = values ? in.v_token : in.k_token;
   const T* src0 = reinterpret_cast<const T*>(values ? in.v : in.k) +
                   head * (values ? in.v_head : in.k_head) + sp.first * token;
-  __shared__ float red[4];
   for (int64_t pg = start / ps + blockIdx.x; pg * ps < end; pg += gridDim.x) {
     const int64_t page = b.table[seq * b.table_width + pg];
     if (page < 0 || page >= c.pages) continue;
     const int r0 = static_cast<int>(max(start - pg * ps, (int64_t)0));
     const int r1 = static_cast<int>(min(end - pg * ps, (int64_t)ps));
     const T* src = src0 + (pg * ps - start) * token;  // row r of the page is src + r * token
+    const int64_t ph = page * c.kv_heads + head;
+    float* scale_at = (values ? c.v_scales : c.k_scales) + ph;
+    const float old = *scale_at;
     float amax = 0.f;
-    for (int i = threadIdx.x; i < (r1 - r0) * D; i += 256) {
-      const float v = fabsf(elem<T>::load(src + (r0 + i / D) * token + i % D));
-      if (v < __builtin_inff()) amax = fmaxf(amax, v);
+    bool wild = false;  // infinities or NaN among them
+    auto see = [&](float x) {
+      const float v = fabsf(x);
+      const bool finite = v < __builtin_inff();
+      wild |= !finite;
+      amax = fmaxf(amax, finite ? v : 0.f);
+    };
+    const int upr = vec ? D / UE : 0;  // units of a token's row, where rows are whole units
+    if (vec) {
+#pragma unroll 4
+      for (int u = threadIdx.x; u < (r1 - r0) * upr; u += 256) {
+        const vec16 v = load16(src + (r0 + u / upr) * token + u % upr * UE);
+#pragma unroll
+        for (int x = 0; x < UE; ++x) see(elem<T>::to_f32(vec16_get<T>(v, x)));
+      }
+    } else {
+      for (int i = threadIdx.x; i < (r1 - r0) * D; i += 256) see(elem<T>::load(src + (r0 + i / D) * token + i % D));
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-    __syncthreads();
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = amax;
-    __syncthreads();
+    wild = __syncthreads_or(wild);
     amax = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    float* scale_at = (values ? c.v_scales : c.k_scales) + page * c.kv_heads + head;
-    const float old = *scale_at;
-    float scale = fmaxf(amax / qmax_of(c.format), kMinScale);
+    __syncthreads();  // every thread has `old` and red before either is written again
+    float scale = fmaxf(amax / qmax_of(FMT), kMinScale);
     if (r0 > 0) scale = fmaxf(scale, old);
     const bool grown = r0 > 0 && scale != old;
-    __syncthreads();
     if (threadIdx.x == 0) *scale_at = scale;
-    uint8_t* codes = reinterpret_cast<uint8_t*>(values ? c.v_codes : c.k_codes) +
-                     (page * c.kv_heads + head) * static_cast<int64_t>(ps * dp);
-    auto code_at = [&](int t, int d, uint32_t held) -> uint32_t {
-      if (t >= r1 || (t < r0 && !grown)) return held;
-      if (t < r0) return encode(decode(held, c.format) * old, scale, c.format);
-      return d < D ? encode(elem<T>::load(src + t * token + d), scale, c.format) : 0u;
-    };
-    const int from = grown ? 0 : r0;
-    if (!values) {
-      const int words = dp / 4;
-      for (int i = threadIdx.x; i < (r1 - from) * words; i += 256) {
-        const int t = from + i / words, d = i % words * 4;
-        uint32_t* at = reinterpret_cast<uint32_t*>(codes + t * dp + d);
-        const uint32_t held = t < r0 ? *at : 0u;
-        uint32_t w = 0;
+    uint8_t* codes = reinterpret_cast<uint8_t*>(values ? c.v_codes : c.k_codes) + ph * static_cast<int64_t>(ps * dp);
+    const float inv = 1.f / scale;
+    const bool whole = vec && D == dp && r0 == 0 && !wild && (!values || (r1 & 15) == 0);
+    if (whole && !values) {
+#pragma unroll 2
+      for (int u = threadIdx.x; u < r1 * upr; u += 256) {
+        const vec16 v = load16(src + (u / upr) * token + u % upr * UE);
+        uint32_t w[UE / 4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w |= code_at(t, d + j, (held >> (8 * j)) & 0xffu) << (8 * j);
-        *at = w;
+        for (int x = 0; x < UE; x += 4)
+          w[x / 4] = four_codes<FMT>(elem<T>::to_f32(vec16_get<T>(v, x)), elem<T>::to_f32(vec16_get<T>(v, x + 1)),
+                                     elem<T>::to_f32(vec16_get<T>(v, x + 2)), elem<T>::to_f32(vec16_get<T>(v, x + 3)),
+                                     scale, inv);
+        uint8_t* at = codes + u * UE;  // rows lie one behind the other
+        if constexpr (UE == 8) *reinterpret_cast<uint2*>(at) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t*>(at) = w[0];
       }
+    } else if (whole) {
+      for (int u = threadIdx.x; u < (r1 >> 2) * upr; u += 256) {
+        const int t = u / upr * 4, d = u % upr * UE;
+        vec16 v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = load16(src + (t + j) * token + d);
+#pragma unroll
+        for (int x = 0; x < UE; ++x)
+          *reinterpret_cast<uint32_t*>(turn + v_byte(t, d + x, dp)) =
+              four_codes<FMT>(elem<T>::to_f32(vec16_get<T>(v[0], x)), elem<T>::to_f32(vec16_get<T>(v[1], x)),
+                              elem<T>::to_f32(vec16_get<T>(v[2], x)), elem<T>::to_f32(vec16_get<T>(v[3], x)), scale,
+                              inv);
+      }
+      __syncthreads();
+      for (int i = threadIdx.x; i < r1 * dp / 16; i += 256) store16(codes + i * 16, load16(turn + i * 16));
+      __syncthreads();
     } else {
-      const int t4 = from >> 2;
-      for (int i = threadIdx.x; i < ((r1 + 3) / 4 - t4) * dp; i += 256) {
-        const int t = (t4 + i / dp) * 4, d = i % dp;
-        uint32_t* at = reinterpret_cast<uint32_t*>(codes + v_byte(t, d, dp));
-        const uint32_t held = t < r0 || t + 4 > r1 ? *at : 0u;
+      auto code_at = [&](int t, int d, uint32_t was) -> uint32_t {
+        if (t >= r1 || (t < r0 && !grown)) return was;
+        if (t >= r0 && d >= D) return 0u;
+        return encode(t < r0 ? decode(was, FMT) * old : elem<T>::load(src + t * token + d), scale, FMT);
+      };
+      // Keys: a word is four columns of a token.  Values: four tokens of a column.
+      const int from = grown ? 0 : r0;
+      const int i0 = values ? (from >> 2) * dp : from * (dp / 4), i1 = values ? ((r1 + 3) >> 2) * dp : r1 * (dp / 4);
+      for (int i = i0 + threadIdx.x; i < i1; i += 256) {
+        const int t = values ? i / dp * 4 : i / (dp / 4), d = values ? i % dp : i % (dp / 4) * 4;
+        uint32_t* at = reinterpret_cast<uint32_t*>(codes + (values ? v_byte(t, d, dp) : t * dp + d));
+        const uint32_t was = t < r0 || (values && t + 4 > r1) ? *at : 0u;
         uint32_t w = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w |= code_at(t + j, d, (held >> (8 * j)) & 0xffu) << (8 * j);
+        for (int j = 0; j < 4; ++j)
+          w |= code_at(values ? t + j : t, values ? d : d + j, (was >> (8 * j)) & 0xffu) << (8 * j);
         *at = w;
       }
     }
   }
 }
 
-// One workgroup per (16 positions of a sequence, head), positions aligned to
-// the cache's 16-token blocks.
+// Reading: one workgroup per (16 positions of a sequence, head), positions
+// aligned to the cache's 16-token blocks.  A thread takes four codes at a time,
+// neighbours in the cache: four columns of a key, four tokens of a value, whose
+// codes reach their rows through LDS.
 template <typename T>
-__global__ __launch_bounds__(256) void kv_read_kernel(convsel_kv_cache_t c, convsel_kv_batch_t b, T* k, T* v) {
+__global__ __launch_bounds__(256) void kv_read_kernel(convsel_kv_cache_t c, convsel_kv_batch_t b, T* k, T* v,
+                                                      int vec) {
+  constexpr int UE = elem<T>::per16;
   const int seq = blockIdx.z, head = blockIdx.y;
   const Span sp = span_of(b.offsets, seq, static_cast<int>(b.tokens));
   const int ps = c.page_size, D = c.head_dim, dp = kv_row_bytes(D);
   const int64_t start = b.lengths[seq], end = start + sp.count;  // 64-bit: bounded below
   const int64_t row = static_cast<int64_t>(c.kv_heads) * D;
+  __shared__ __align__(16) uint8_t turn[16 * 256];
   // Floor division: a negative start names positions before the sequence.
   const int64_t first = start >= 0 ? start / 16 : -((-start + 15) / 16);
   for (int64_t blk = first + blockIdx.x; blk * 16 < end; blk += gridDim.x) {
@@ -104,13 +182,48 @@ __global__ __launch_bounds__(256) void kv_read_kernel(convsel_kv_cache_t c, conv
     const uint8_t* kc = reinterpret_cast<const uint8_t*>(c.k_codes) + ph * (ps * dp) + t0 * dp;
     const uint8_t* vc = reinterpret_cast<const uint8_t*>(c.v_codes) + ph * (ps * dp) + t0 * dp;
     const float ks = there ? c.k_scales[ph] : 0.f, vs = there ? c.v_scales[ph] : 0.f;
-    for (int i = threadIdx.x; i < 16 * D; i += 256) {
-      const int t = i / D, d = i % D;
-      const int64_t p = p0 + t;
-      if (p < start || p >= end) continue;
-      const int64_t at = (sp.first + (p - start)) * row + static_cast<int64_t>(head) * D + d;
-      elem<T>::store(k + at, there ? decode(kc[t * dp + d], c.format) * ks : 0.f);
-      elem<T>::store(v + at, there ? decode(vc[v_byte(t, d, dp)], c.format) * vs : 0.f);
+    // Value codes to token rows: word (g, column) holds tokens 4 g .. 4 g + 3.
+    __syncthreads();
+    for (int i = threadIdx.x; i < 4 * dp; i += 256) {
+      const uint32_t w = reinterpret_cast<const uint32_t*>(vc)[i];
+      const int unit = i / (dp / 16), dt = i % (dp / 16);
+      const int d = dt * 16 + (unit & 15), t = unit / 16 * 4;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) turn[(t + x) * dp + d] = static_cast<uint8_t>(w >> (8 * x));
+    }
+    __syncthreads();
+    auto one = [&](uint32_t code, float s) { return there ? decode(code, c.format) * s : 0.f; };
+    if (vec) {
+      const int upr = D / UE;
+      for (int i = threadIdx.x; i < 16 * upr; i += 256) {
+        const int t = i / upr, d = i % upr * UE;
+        const int64_t p = p0 + t;
+        if (p < start || p >= end) continue;
+        const int64_t at = (sp.first + (p - start)) * row + static_cast<int64_t>(head) * D + d;
+        uint32_t kw[UE / 4], vw[UE / 4];
+#pragma unroll
+        for (int x = 0; x < UE / 4; ++x) {
+          kw[x] = *reinterpret_cast<const uint32_t*>(kc + t * dp + d + 4 * x);
+          vw[x] = *reinterpret_cast<const uint32_t*>(turn + t * dp + d + 4 * x);
+        }
+        vec16 ko, vo;
+#pragma unroll
+        for (int x = 0; x < UE; ++x) {
+          vec16_set<T>(ko, x, elem<T>::from_f32(one(kw[x / 4] >> (8 * (x % 4)) & 0xffu, ks)));
+          vec16_set<T>(vo, x, elem<T>::from_f32(one(vw[x / 4] >> (8 * (x % 4)) & 0xffu, vs)));
+        }
+        store16(k + at, ko);
+        store16(v + at, vo);
+      }
+    } else {
+      for (int i = threadIdx.x; i < 16 * D; i += 256) {
+        const int t = i / D, d = i % D;
+        const int64_t p = p0 + t;
+        if (p < start || p >= end) continue;
+        const int64_t at = (sp.first + (p - start)) * row + static_cast<int64_t>(head) * D + d;
+        elem<T>::store(k + at, one(kc[t * dp + d], ks));
+        elem<T>::store(v + at, one(turn[t * dp + d], vs));
+      }
     }
   }
 }
@@ -128,10 +241,22 @@ hipError_t launch_kv_write(const convsel_kv_cache_t& c, const convsel_kv_batch_t
     p.offsets += s0;
     const int64_t pages = (b.tokens + b.seqs - 1) / b.seqs / c.page_size + 2;
     const dim3 grid((unsigned)(pages < 65536 ? pages : 65536), 2 * c.kv_heads, (unsigned)p.seqs);
-    if (t.dtype == CONV_F32)
-      hipLaunchKernelGGL(kv_write_kernel<float>, grid, dim3(256), 0, stream, c, p, t);
-    else
-      hipLaunchKernelGGL(kv_write_kernel<bf16_t>, grid, dim3(256), 0, stream, c, p, t);
+    // Rows of whole 16-byte units that start on one.
+    const int64_t ue = t.dtype == CONV_F32 ? 4 : 8;
+    const int vec = c.head_dim % ue == 0 && t.k_token % ue == 0 && t.k_head % ue == 0 && t.v_token % ue == 0 &&
+                    t.v_head % ue == 0 && (uintptr_t)t.k % 16 == 0 && (uintptr_t)t.v % 16 == 0;
+    const size_t lds = (size_t)c.page_size * kv_row_bytes(c.head_dim);  // at most 32 KiB
+    if (t.dtype == CONV_F32) {
+      if (c.format == CONVSEL_KV_INT8)
+        hipLaunchKernelGGL((kv_write_kernel<float, CONVSEL_KV_INT8>), grid, dim3(256), lds, stream, c, p, t, vec);
+      else
+        hipLaunchKernelGGL((kv_write_kernel<float, CONVSEL_KV_FP8>), grid, dim3(256), lds, stream, c, p, t, vec);
+    } else {
+      if (c.format == CONVSEL_KV_INT8)
+        hipLaunchKernelGGL((kv_write_kernel<bf16_t, CONVSEL_KV_INT8>), grid, dim3(256), lds, stream, c, p, t, vec);
+      else
+        hipLaunchKernelGGL((kv_write_kernel<bf16_t, CONVSEL_KV_FP8>), grid, dim3(256), lds, stream, c, p, t, vec);
+    }
   }
   return hipGetLastError();
 }
@@ -146,10 +271,12 @@ hipError_t launch_kv_read(const convsel_kv_cache_t& c, const convsel_kv_batch_t&
     p.offsets += s0;
     const int64_t blocks = (b.tokens + b.seqs - 1) / b.seqs / 16 + 2;
     const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536), c.kv_heads, (unsigned)p.seqs);
+    const int64_t ue = t.dtype == CONV_F32 ? 4 : 8;
+    const int vec = c.head_dim % ue == 0 && (uintptr_t)t.k % 16 == 0 && (uintptr_t)t.v % 16 == 0;
     if (t.dtype == CONV_F32)
-      hipLaunchKernelGGL(kv_read_kernel<float>, grid, dim3(256), 0, stream, c, p, (float*)t.k, (float*)t.v);
+      hipLaunchKernelGGL(kv_read_kernel<float>, grid, dim3(256), 0, stream, c, p, (float*)t.k, (float*)t.v, vec);
     else
-      hipLaunchKernelGGL(kv_read_kernel<bf16_t>, grid, dim3(256), 0, stream, c, p, (bf16_t*)t.k, (bf16_t*)t.v);
+      hipLaunchKernelGGL(kv_read_kernel<bf16_t>, grid, dim3(256), 0, stream, c, p, (bf16_t*)t.k, (bf16_t*)t.v, vec);
   }
   return hipGetLastError();
 }
