@@ -169,16 +169,19 @@ __global__ __launch_bounds__(256, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void atte
             widen8<FMT>(kr[j].x, kr[j].y);
       }
       // Values: a unit is four tokens of two columns 16 apart; rows never written are silenced.
-      const bool cut = pg < 0 || blk * 16 + 16 > limit;
+      if (pg < 0 || blk * 16 + 16 > limit) {
 #pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        const int i = lane + 64 * j, L = i / NC, d32 = i % NC, g = L >> 4, dl = L & 15;
-        if (cut) {
+        for (int j = 0; j < NC; ++j) {
+          const int g = (lane + 64 * j) / NC >> 4;
           const int n = pg < 0 ? 0 : clampi(limit - blk * 16 - 4 * g, 0, 4);
           const uint32_t keep = n >= 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
           vr[j].x &= keep;
           vr[j].y &= keep;
         }
+      }
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        const int i = lane + 64 * j, L = i / NC, d32 = i % NC, g = L >> 4, dl = L & 15;
         const f16x8_t w = widen8<FMT>(vr[j].x, vr[j].y);
         char* at = &vt_lds[buf][((wave * NC + d32) * 64 + (g & 1) * 32 + dl) * 16 + (g >> 1) * 8];
         uint4 u;
@@ -192,8 +195,8 @@ __global__ __launch_bounds__(256, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void atte
         BlockMeta m;
         m.ks = pg < 0 ? -1.f : ksr;
         m.ve = e;
-        m.up = TWO ? 0.f : 15.f + log2f(f);
-        m.scale = TWO ? kWeight * f : kResult / f;
+        m.up = TWO ? 0.f : 15.f + __builtin_amdgcn_logf(f);
+        m.scale = TWO ? kWeight * f : kResult * __builtin_amdgcn_rcpf(f);
         meta[buf][wave] = m;
       }
     };
