@@ -394,12 +394,47 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const float* __rest
   }
 }
 
+// The same for few parts: four columns of a row a thread, whole rows a workgroup.
+// (32768 rows of 128 columns in 2 parts: a workgroup a row took 43 us.)
+constexpr int kFewParts = 16;
+
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join_few_kernel(const float* __restrict__ part,
+                                                                 const float* __restrict__ stat,
+                                                                 const int32_t* __restrict__ offsets, int seqs,
+                                                                 T* __restrict__ y, AttnArgs a) {
+  const int64_t heads = static_cast<int64_t>(a.kv_heads) * a.group;
+  const int c4 = (a.dim + 3) / 4, n = a.nsplit;
+  const int in_wg = threadIdx.x / c4, col = threadIdx.x % c4;
+  const int64_t it = static_cast<int64_t>(blockIdx.x) * (256 / c4) + in_wg, t = it / heads, h = it - t * heads;
+  if (in_wg >= 256 / c4 || t >= clampi(offsets[seqs], 0, a.tokens)) return;
+  const float2* st = reinterpret_cast<const float2*>(stat) + it * n;
+  const float4* src = reinterpret_cast<const float4*>(part) + it * n * c4 + col;
+  float m = -__builtin_inff(), l = 0.f;
+  for (int s = 0; s < n; ++s) m = fmaxf(m, st[s].x);
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int s = 0; s < n; ++s) {
+    const float2 ms = st[s];
+    const float4 p = src[s * c4];
+    const int dm = shift_of(ms.x, m);
+    const float f = ldexpf(1.f, dm);
+    l += ldexpf(ms.y, dm);
+    v.x += p.x * f; v.y += p.y * f; v.z += p.z * f; v.w += p.w * f;
+  }
+  const float inv = l == 0.f ? 0.f : kResult / l;
+  T* dst = y + t * a.y_token + h * a.y_head + 4 * col;
+  const float r[4] = {v.x * inv, v.y * inv, v.z * inv, v.w * inv};
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+    if (4 * col + x < a.dim) elem<T>::store(dst + x, r[x]);
+}
+
 // How a call is cut: rows, in 16s or 128s, and parts of the keys.  The host
 // knows how many tokens the call has and how many a sequence may hold, not how
 // they are spread; every count only sets the grid, and kernels walk what there
 // is.
 struct Plan {
-  bool tiles128;
+  int rows;  // of a workgroup: 16, 128 or 256
   int tiles, nsplit;
 };
 
@@ -416,26 +451,38 @@ Plan plan(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convse
   // new tokens on 4000, 40 against 53 us; 64 on 1000, 26 against 18; 2048 on
   // none 92 against 186), provided that its tiles are at least half full.
   const double work = (double)avg * d.q_heads * b.seqs * keys * kv_row_bytes(c.head_dim);
-  p.tiles128 = avg * group >= 64 && work >= (d.dtype == CONV_F32 ? 4e9 : 1.6e9);
-  const int64_t rows = p.tiles128 ? 128 : 16;
-  const int64_t tiles = (avg * group + rows - 1) / rows;
-  p.tiles = (int)(tiles < 32768 ? tiles : 32768);
-  const int64_t groups = p.tiles * c.kv_heads * b.seqs;
-  // Two workgroups a CU, with 256 keys at least in each part.
-  int64_t n = (512 + groups - 1) / groups;
-  if (n > keys / 256) n = keys / 256;
-  if (p.tiles128) {
-    // A tile of 64 keys takes 2.3 us where nothing else runs on the CU, a part's results 2e-6 us a value to write
-    // and join: the sum is least at the root of their ratio.
-    const double walk = keys / 64 * 2.3, join = (double)b.tokens * d.q_heads * c.head_dim * 2e-6;
-    const int64_t best = (int64_t)sqrt(walk / join);
-    if (n > best) n = best;
-  } else if (n < 4 && groups < 4096) {
-    // Sequences of unlike lengths end together where each is cut (64 of 2048 .. 8192 tokens: 145 -> 134 us).
-    n = keys / 2048 < 4 ? keys / 2048 : 4;
+  const bool many = avg * group >= 64 && work >= (d.dtype == CONV_F32 ? 4e9 : 1.6e9);
+  auto cut = [&](int rows) {
+    const int64_t tiles = (avg * group + rows - 1) / rows;
+    p.rows = rows;
+    p.tiles = (int)(tiles < 32768 ? tiles : 32768);
+    const int64_t groups = p.tiles * c.kv_heads * b.seqs;
+    // Two workgroups a CU (one of 256 rows), with 256 keys at least in each part.
+    const int64_t want = rows == 256 ? 256 : 512;
+    int64_t n = (want + groups - 1) / groups;
+    if (n > keys / 256) n = keys / 256;
+    if (rows > 16) {
+      // 64 keys take 2.3 us where nothing else runs on the CU, a part's results 2e-6 us a value to write and join: the
+      // sum is least at the root of their ratio.
+      const double walk = keys / 64 * 2.3, join = (double)b.tokens * d.q_heads * c.head_dim * 2e-6;
+      const int64_t best = (int64_t)sqrt(walk / join);
+      if (n > best) n = best;
+    } else if (n < 4 && groups < 4096) {
+      // Sequences of unlike lengths end together where each is cut (64 of 2048 .. 8192 tokens: 145 -> 134 us).
+      n = keys / 2048 < 4 ? keys / 2048 : 4;
+    }
+    if (n > kMaxSplit) n = kMaxSplit;
+    p.nsplit = (int)(n < 1 ? 1 : n);
+    return groups * p.nsplit;
+  };
+  // 256 rows share codes and barriers among twice as many, and pay where every CU has work for long: long sequences,
+  // and either a second workgroup a CU to even out what a causal mask leaves, or a prefix that makes all alike (32 query
+  // heads of 128 on 8: 4096 new tokens 244 -> 223 us, 512 on 8000 136 -> 126; but 2048 new ones 93 -> 100).
+  if (many && attention_tiles_wide(d.dtype, c.head_dim) && keys >= 2048) {
+    const int64_t wgs = cut(256);
+    if (wgs >= 512 || (wgs >= 256 && keys >= 4 * avg)) return p;
   }
-  if (n > kMaxSplit) n = kMaxSplit;
-  p.nsplit = (int)(n < 1 ? 1 : n);
+  cut(many ? 128 : 16);
   return p;
 }
 
@@ -503,8 +550,8 @@ hipError_t launch_attention(const void* q, const convsel_kv_cache_t& c, const co
     ptr.table = b.table + s0 * b.table_width;
     ptr.lengths = b.lengths + s0;
     ptr.offsets = b.offsets + s0;
-    if (p.tiles128) {
-      const hipError_t e = launch_attention_tiles(ptr, a, d.dtype, c.format, seqs, stream);
+    if (p.rows > 16) {
+      const hipError_t e = launch_attention_tiles(ptr, a, d.dtype, c.format, p.rows, seqs, stream);
       if (e != hipSuccess) return e;
       continue;
     }
@@ -518,13 +565,24 @@ hipError_t launch_attention(const void* q, const convsel_kv_cache_t& c, const co
     }
   }
   if (p.nsplit > 1) {
-    const dim3 grid((unsigned)(b.tokens * d.q_heads));
-    if (d.dtype == CONV_F32)
-      hipLaunchKernelGGL(attention_join_kernel<float>, grid, dim3(256), 0, stream, ptr.part, ptr.stat, b.offsets,
-                         (int)b.seqs, (float*)y, a);
-    else
-      hipLaunchKernelGGL(attention_join_kernel<bf16_t>, grid, dim3(256), 0, stream, ptr.part, ptr.stat, b.offsets,
-                         (int)b.seqs, (bf16_t*)y, a);
+    const int64_t rows = b.tokens * d.q_heads, in_wg = p.nsplit <= kFewParts ? 256 / ((c.head_dim + 3) / 4) : 1;
+    const dim3 grid((unsigned)((rows + in_wg - 1) / in_wg));
+    const int seqs = (int)b.seqs;
+    if (p.nsplit <= kFewParts) {
+      if (d.dtype == CONV_F32)
+        hipLaunchKernelGGL(attention_join_few_kernel<float>, grid, dim3(256), 0, stream, ptr.part, ptr.stat, b.offsets,
+                           seqs, (float*)y, a);
+      else
+        hipLaunchKernelGGL(attention_join_few_kernel<bf16_t>, grid, dim3(256), 0, stream, ptr.part, ptr.stat, b.offsets,
+                           seqs, (bf16_t*)y, a);
+    } else {
+      if (d.dtype == CONV_F32)
+        hipLaunchKernelGGL(attention_join_kernel<float>, grid, dim3(256), 0, stream, ptr.part, ptr.stat, b.offsets, seqs,
+                           (float*)y, a);
+      else
+        hipLaunchKernelGGL(attention_join_kernel<bf16_t>, grid, dim3(256), 0, stream, ptr.part, ptr.stat, b.offsets,
+                           seqs, (bf16_t*)y, a);
+    }
   }
   return hipGetLastError();
 }
@@ -533,7 +591,8 @@ void attention_describe(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b
                         char* buf, size_t len) {
   const Plan p = plan(c, b, d);
   snprintf(buf, len, "attention kernels=attention_%s_kernel%s rows=%d tiles=%d split=%d workspace=%zu",
-           p.tiles128 ? "tiles" : "rows", p.nsplit > 1 ? ";attention_join_kernel" : "", p.tiles128 ? 128 : 16, p.tiles,
+           p.rows > 16 ? "tiles" : "rows",
+           p.nsplit <= 1 ? "" : p.nsplit <= kFewParts ? ";attention_join_few_kernel" : ";attention_join_kernel", p.rows, p.tiles,
            p.nsplit, attention_workspace(c, b, d));
 }
 

@@ -94,8 +94,10 @@ __device__ __forceinline__ int query_exponent(float amax) {
 
 }  // namespace lm
 
-// Many query rows (attention_tiles.hip): grid of rows in 128s.
-hipError_t launch_attention_tiles(const lm::AttnPointers& p, const lm::AttnArgs& a, int dtype, int format,
+// Many query rows (attention_tiles.hip): 128 of them a workgroup, or 256 where
+// attention_tiles_wide() has them.
+bool attention_tiles_wide(int dtype, int head_dim);
+hipError_t launch_attention_tiles(const lm::AttnPointers& p, const lm::AttnArgs& a, int dtype, int format, int rows,
                                   int64_t seqs, hipStream_t stream);
 
 }  // namespace convsel

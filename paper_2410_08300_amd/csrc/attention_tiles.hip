@@ -1,22 +1,24 @@
 // Attention over the 8-bit paged cache for many query rows.
 //
-// One workgroup of four waves per 128 rows of a key head (a row is a query of
-// the sequence and one of the heads that share the key head), 32 rows a wave.
-// Keys pass in tiles of 64 tokens, four 16-token blocks: wave w loads block w's
-// codes one tile ahead, widens them to 16-bit floats once for all 128 rows, and
-// stores them in LDS in the order in which lanes read them back: every read of
-// an operand is 1 KiB in a row.  Two tiles fit in LDS, so there is one barrier a
-// tile, and two workgroups share a CU up to head widths of 128 in bf16.
+// One workgroup of W = 4 or 8 waves per 32 W rows of a key head (a row is a query
+// of the sequence and one of the heads that share the key head), 32 rows a wave.
+// Keys pass in tiles of W 16-token blocks: wave w loads block w's codes one tile
+// ahead, widens them to 16-bit floats once for all rows, and stores them in LDS
+// in the order in which lanes read them back: every read of an operand is 1 KiB
+// in a row.  Two tiles fit in LDS, so there is one barrier a tile; up to head
+// widths of 128 in bf16 a CU has eight waves, of two workgroups or one.
 //
 // Scores are K q^T in 32 x 32 x 16 products: a lane ends with 16 tokens of one
 // query, in runs of four as the cache's blocks hold them, and feeds its weights
 // to the second product, V^T P^T, without moving them.  A row's statistics need
 // one exchange, with the lane that holds the other tokens.
 //
-// What bounds it: the vector unit.  A weight costs a fused product, a
-// transcendental (four slots), an addition to the sum, half a conversion and
-// half a maximum; 32 of them a lane and tile stand beside 32 products of 32
-// cycles each.
+// What bounds it: the vector unit, with the waits between its phases.  A weight
+// costs a fused product, a transcendental (four slots), an addition to the sum,
+// half a conversion and half a maximum; 16 of them a lane and 32 keys stand
+// beside 16 products of 32 cycles each.  4096 new tokens of 32 heads of 128 on 8,
+// causal, int8: 195 us, 705 TFLOP/s; the products alone would take 90 at the
+// rate of a large product.
 #include "attention_common.hpp"
 #include "lm_common.hpp"
 
@@ -74,19 +76,20 @@ __device__ __forceinline__ void use_groups(f16x8_t (&first)[kAhead], const Load&
   }
 }
 
-template <typename T, int FMT, int NC>
-__global__ __launch_bounds__(256, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void attention_tiles_kernel(
+template <typename T, int FMT, int NC, int W>
+__global__ __launch_bounds__(64 * W, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void attention_tiles_kernel(
     const T* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
     const float* __restrict__ ks, const float* __restrict__ vs, const int32_t* __restrict__ table,
     const int32_t* __restrict__ lengths, const int32_t* __restrict__ offsets, T* __restrict__ y,
     float* __restrict__ part, float* __restrict__ stat, AttnArgs a) {
   constexpr bool TWO = sizeof(T) == 4;
   constexpr int DP = 32 * NC, QC = 2 * NC;  // row bytes, 16-column chunks
-  constexpr int KB = 2 * QC * 1024, VB = 4 * NC * 1024;  // bytes of a tile's keys and values in LDS
+  constexpr int ROWS = 32 * W;  // a wave has 32 query rows and stages one block of keys
+  constexpr int KB = W / 2 * QC * 1024, VB = W * NC * 1024;  // bytes of a tile's keys and values in LDS
   __shared__ __align__(16) char lds[2 * (KB + VB)];
   char(*const kt_lds)[KB] = reinterpret_cast<char(*)[KB]>(lds);
   char(*const vt_lds)[VB] = reinterpret_cast<char(*)[VB]>(lds + 2 * KB);
-  __shared__ BlockMeta meta[2][4];
+  __shared__ BlockMeta meta[2][W];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, half = lane >> 5;
@@ -99,11 +102,11 @@ __global__ __launch_bounds__(256, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void atte
   const int limit = static_cast<int>(max((int64_t)0, min(len, a.table_width << a.ps_shift)));
   const int64_t first = len - sp.count;  // position of the sequence's first query
   const int32_t* my_table = table + seq * a.table_width;
-  const int ntile = (rows + 127) >> 7;
+  const int ntile = (rows + ROWS - 1) / ROWS;
 
   for (int nt = blockIdx.y; nt < ntile; nt += a.tiles) {
     const int tile = ntile - 1 - nt;  // under a causal mask the last rows have the most keys: they start first
-    const int r0 = tile * 128;
+    const int r0 = tile * ROWS;
     // Keys that tokens t0..t1 see between them, and that every one of them sees.
     auto seen_by = [&](int t0, int t1, int& lo, int& hi, int& in_lo, int& in_hi) {
       lo = 0; hi = limit; in_lo = 0; in_hi = limit;
@@ -117,9 +120,9 @@ __global__ __launch_bounds__(256, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void atte
       }
     };
     int lo, hi, in_lo, in_hi;
-    seen_by(r0 / a.group, min(r0 + 127, rows - 1) / a.group, lo, hi, in_lo, in_hi);
+    seen_by(r0 / a.group, min(r0 + ROWS - 1, rows - 1) / a.group, lo, hi, in_lo, in_hi);
     const int b0 = lo >> 4, b1 = hi > lo ? (hi + 15) >> 4 : b0;
-    const int steps = (b1 - b0 + 3) >> 2;
+    const int steps = (b1 - b0 + W - 1) / W;
     const int per = (steps + a.nsplit - 1) / a.nsplit;
     const int k0 = split * per, k1 = min(steps, k0 + per);
     // This wave's rows and this lane's.
@@ -139,12 +142,12 @@ __global__ __launch_bounds__(256, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void atte
     int pg = -1, blk = 0;
     // The page of a tile's block is looked up a tile before its codes are.
     auto look = [&](int kt) {
-      const int b = b0 + 4 * kt + wave;
+      const int b = b0 + W * kt + wave;
       return b < b1 ? my_table[b >> (a.ps_shift - 4)] : -1;
     };
     int entry = -1;
     auto fetch = [&](int kt) {
-      blk = b0 + 4 * kt + wave;
+      blk = b0 + W * kt + wave;
       pg = entry >= 0 && entry < a.pages ? entry : -1;
       const int64_t ph = static_cast<int64_t>(pg < 0 ? 0 : pg) * a.kv_heads + head;
       const int t0 = (blk & ((1 << (a.ps_shift - 4)) - 1)) << 4;
@@ -264,8 +267,8 @@ __global__ __launch_bounds__(256, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void atte
     for (int i = 0; i < NC; ++i) o[i] = zero16();
     float m = -kInf, l = 0.f;
 
-    // 32 of the tile's tokens: half a tile's scores and weights fit beside the results without spilling.
-    auto compute = [&](int buf, int tt, int j0, bool masked) {
+    // 32 of the tile's tokens, from position j1 on: their scores and weights fit beside the results without spilling.
+    auto compute = [&](int buf, int tt, int j1, bool masked) {
       BlockMeta bm[2];
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
@@ -292,7 +295,7 @@ __global__ __launch_bounds__(256, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void atte
       if (masked) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          const int j = j0 + 32 * tt + 8 * (v >> 2) + 4 * half + (v & 3);
+          const int j = j1 + 8 * (v >> 2) + 4 * half + (v & 3);
           if (!(bm[v >> 3].ks >= 0.f && j >= row_lo && j < row_hi)) sc[v] = -kInf;
         }
       }
@@ -357,12 +360,15 @@ __global__ __launch_bounds__(256, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void atte
       for (int kt = k0; kt < k1; ++kt) {
         const int buf = (kt - k0) & 1;
         if (kt + 1 < k1) fetch(kt + 1);
-        const int j0 = (b0 + 4 * kt) * 16;
-        if (!idle && j0 < whi && j0 + 64 > wlo) {
-          const float worst = fminf(fminf(meta[buf][0].ks, meta[buf][1].ks), fminf(meta[buf][2].ks, meta[buf][3].ks));
-          const bool masked = !(uniform(worst) >= 0.f && j0 >= in_lo && j0 + 64 <= in_hi);
+        const int j0 = (b0 + W * kt) * 16;
+        if (!idle) {
 #pragma unroll 1
-          for (int tt = 0; tt < 2; ++tt) compute(buf, tt, j0, masked);
+          for (int tt = 0; tt < W / 2; ++tt) {
+            const int j1 = j0 + 32 * tt;
+            if (j1 >= whi || j1 + 32 <= wlo) continue;
+            const float worst = fminf(meta[buf][2 * tt].ks, meta[buf][2 * tt + 1].ks);
+            compute(buf, tt, j1, !(uniform(worst) >= 0.f && j1 >= in_lo && j1 + 32 <= in_hi));
+          }
         }
         if (kt + 1 < k1) stash(buf ^ 1);
         lds_sync();
@@ -419,37 +425,52 @@ __global__ __launch_bounds__(256, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void atte
   }
 }
 
-template <typename T, int FMT, int NC>
-hipError_t launch(const AttnPointers& p, const AttnArgs& a, int64_t seqs, hipStream_t st) {
+// Eight waves' tiles of 128 keys fit in LDS, twice, up to head widths of 128,
+// and their registers do in bf16.
+template <typename T, int NC>
+constexpr bool kWide = sizeof(T) == 2 && NC <= 4;
+
+template <typename T, int FMT, int NC, int W>
+hipError_t launch_waves(const AttnPointers& p, const AttnArgs& a, int64_t seqs, hipStream_t st) {
   const dim3 grid((unsigned)(a.kv_heads * a.nsplit), (unsigned)a.tiles, (unsigned)seqs);
-  hipLaunchKernelGGL((attention_tiles_kernel<T, FMT, NC>), grid, dim3(256), 0, st, (const T*)p.q, p.k_codes, p.v_codes,
-                     p.k_scales, p.v_scales, p.table, p.lengths, p.offsets, (T*)p.y, p.part, p.stat, a);
+  hipLaunchKernelGGL((attention_tiles_kernel<T, FMT, NC, W>), grid, dim3(64 * W), 0, st, (const T*)p.q, p.k_codes,
+                     p.v_codes, p.k_scales, p.v_scales, p.table, p.lengths, p.offsets, (T*)p.y, p.part, p.stat, a);
   return hipGetLastError();
 }
 
+template <typename T, int FMT, int NC>
+hipError_t launch(const AttnPointers& p, const AttnArgs& a, int rows, int64_t seqs, hipStream_t st) {
+  if constexpr (kWide<T, NC>) {
+    if (rows == 256) return launch_waves<T, FMT, NC, 8>(p, a, seqs, st);
+  }
+  return launch_waves<T, FMT, NC, 4>(p, a, seqs, st);
+}
+
 template <typename T, int FMT>
-hipError_t launch_nc(const AttnPointers& p, const AttnArgs& a, int64_t seqs, hipStream_t st) {
+hipError_t launch_nc(const AttnPointers& p, const AttnArgs& a, int rows, int64_t seqs, hipStream_t st) {
   switch ((a.dim + 31) / 32) {
-    case 1: return launch<T, FMT, 1>(p, a, seqs, st);
-    case 2: return launch<T, FMT, 2>(p, a, seqs, st);
-    case 3: return launch<T, FMT, 3>(p, a, seqs, st);
-    case 4: return launch<T, FMT, 4>(p, a, seqs, st);
-    case 5: return launch<T, FMT, 5>(p, a, seqs, st);
-    case 6: return launch<T, FMT, 6>(p, a, seqs, st);
-    case 7: return launch<T, FMT, 7>(p, a, seqs, st);
-    default: return launch<T, FMT, 8>(p, a, seqs, st);
+    case 1: return launch<T, FMT, 1>(p, a, rows, seqs, st);
+    case 2: return launch<T, FMT, 2>(p, a, rows, seqs, st);
+    case 3: return launch<T, FMT, 3>(p, a, rows, seqs, st);
+    case 4: return launch<T, FMT, 4>(p, a, rows, seqs, st);
+    case 5: return launch<T, FMT, 5>(p, a, rows, seqs, st);
+    case 6: return launch<T, FMT, 6>(p, a, rows, seqs, st);
+    case 7: return launch<T, FMT, 7>(p, a, rows, seqs, st);
+    default: return launch<T, FMT, 8>(p, a, rows, seqs, st);
   }
 }
 
 }  // namespace
 
-hipError_t launch_attention_tiles(const AttnPointers& p, const AttnArgs& a, int dtype, int format, int64_t seqs,
-                                  hipStream_t st) {
+bool attention_tiles_wide(int dtype, int head_dim) { return dtype == CONV_BF16 && head_dim <= 128; }
+
+hipError_t launch_attention_tiles(const AttnPointers& p, const AttnArgs& a, int dtype, int format, int rows,
+                                  int64_t seqs, hipStream_t st) {
   if (dtype == CONV_F32)
-    return format == CONVSEL_KV_INT8 ? launch_nc<float, CONVSEL_KV_INT8>(p, a, seqs, st)
-                                     : launch_nc<float, CONVSEL_KV_FP8>(p, a, seqs, st);
-  return format == CONVSEL_KV_INT8 ? launch_nc<bf16_t, CONVSEL_KV_INT8>(p, a, seqs, st)
-                                   : launch_nc<bf16_t, CONVSEL_KV_FP8>(p, a, seqs, st);
+    return format == CONVSEL_KV_INT8 ? launch_nc<float, CONVSEL_KV_INT8>(p, a, rows, seqs, st)
+                                     : launch_nc<float, CONVSEL_KV_FP8>(p, a, rows, seqs, st);
+  return format == CONVSEL_KV_INT8 ? launch_nc<bf16_t, CONVSEL_KV_INT8>(p, a, rows, seqs, st)
+                                   : launch_nc<bf16_t, CONVSEL_KV_FP8>(p, a, rows, seqs, st);
 }
 
 }  // namespace convsel

@@ -529,6 +529,33 @@ def test_attention_in_tiles_of_128_rows(case, fmt, dtype):
     assert bool((y == y[0]).all()), "the same sequence gave two results"
 
 
+@pytest.mark.parametrize("rows,fmt,dtype", [(128, "int8", "bf16"), (256, "int8", "bf16"), (256, "fp8", "bf16"), (128, "fp8", "f32")])
+@pytest.mark.parametrize("dim", [128, 64, 72, 20])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_in_tiles_of_either_height(rows, fmt, dtype, dim, causal):
+    """Sequences of unlike lengths in one call, planned for short and for long ones: the tile's height differs, and in
+    the higher one waves past the rows, tiles past the keys and blocks past the tokens all occur."""
+    case = (4, 1, dim, 16, [400, 63, 200, 17], [130, 40, 200, 20], causal, 0)
+    say("case attention heights", rows, fmt, dtype, dim, causal)
+    cache, want, table, q = build(case, fmt, dtype, seed=6)
+    off, scale = offsets_of(case[5]), 1.0 / math.sqrt(dim)
+    exact, mag, smag, top = ref.attention(q, want, table, case[4], off, causal, 0, scale)
+    bound = ref.attention_bound(exact, mag, smag, top, dim, q.dtype)
+    # High tiles are for 2048 keys and more; below, many sequences have to share the call.
+    rep = 1 if rows == 256 or dtype == "f32" else int(2e9 / (sum(case[5]) * 4 * 416 * ((dim + 31) // 32 * 32))) + 1
+    t = wide(table, case) if rep == 1 else ints(table)
+    t = t.repeat(rep, 1)
+    text = cs.describe_attention(cache, 4 * rep, sum(case[5]) * rep, t.shape[1], 4, DT[dtype], causal)
+    assert "attention_tiles_kernel" in text and " rows=%d " % rows in text, text
+    offs = [0]
+    for _ in range(rep):
+        offs += [offs[-1] + o for o in off[1:]]
+    y = cs.cached_attention(q.repeat(rep, 1, 1), cache, t, ints(case[4] * rep), ints(offs), causal=causal)
+    y = y.view(rep, -1, 4, dim)
+    within(y[0], exact, bound, "heights")
+    assert bool((y == y[0]).all()), "the same sequence gave two results"
+
+
 @pytest.mark.parametrize("new", [40, 150])
 def test_tiles_of_128_rows_ignore_what_lies_behind_masks(new):
     case = (4, 2, 64, 16, [200, 170], [new, new], True, 0)
