@@ -57,11 +57,11 @@ typedef struct convsel_linear_desc {
 conv_status_t convsel_linear_workspace_bytes(const convsel_linear_desc_t* desc, size_t* bytes);
 
 /* Any alignment of elements is served; more than 16 rows run fastest where x
- * and w start on 16 bytes.  y may be r itself (same address and stride: the residual is updated in
- * place); otherwise the span of y, first to last element, must not overlap
- * that of x, w, b or r.  INVALID_ARG for a malformed descriptor, a NULL or
- * overlapping pointer, a pointer not aligned to its element; WORKSPACE for too
- * little of it. */
+ * and w start on 16 bytes.  y may be r itself (same address and stride: the
+ * residual is updated in place); otherwise the span of y, first to last
+ * element, must not overlap that of x, w, b or r.  INVALID_ARG for a malformed
+ * descriptor, a NULL or overlapping pointer, a pointer not aligned to its
+ * element; WORKSPACE for too little of it. */
 conv_status_t convsel_linear(const void* x, const void* w, const void* b, const void* r, void* y,
                              const convsel_linear_desc_t* desc, void* workspace, size_t workspace_bytes,
                              void* stream);

@@ -144,6 +144,34 @@ def test_linear_strided_rows_leading_dims_and_guards(m, dtype):
     assert cs.linear(x[:0], w).shape == (0, o)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linear_many_rows_that_tiles_cannot_address(dtype):
+    """Rows further apart than a tile's offsets reach, and operands that start on no 16 bytes, through the C entry."""
+    dt, m, i, o = DT[dtype], 37, 96, 50
+    say("case linear rows", dtype)
+    far = (1 << 31) // 256 // dt.itemsize + 8
+    g = gen(9)
+    base = torch.empty(m * far + 64, device=DEV, dtype=dt)
+    x = base.as_strided((m, i), (far, 1), 16)
+    x.copy_(torch.randn(m, i, generator=g, device=DEV))
+    w = torch.randn(o, i, generator=g, device=DEV).to(dt)
+    r = torch.randn(m, o, generator=g, device=DEV).to(dt)
+    want, bound = ref.linear(x, w, None, "relu", r)
+    bound = bound + ref.half_ulp(dt) * want.abs() * 1.01
+    within(cs.linear(x, w, act="relu", residual=r), want, bound, "far rows")
+    lib = cs._lib.lib()
+    for shift in (1, 3):
+        xs = torch.empty(m * i + shift, device=DEV, dtype=dt)[shift:].view(m, i).copy_(x)
+        ws = torch.empty(o * i + shift, device=DEV, dtype=dt)[shift:].view(o, i).copy_(w)
+        y = torch.empty(m, o, device=DEV, dtype=dt)
+        d, n = cs.lm._linear_plan(m, i, o, i, o, o, cs.lm._DTYPES[dt], "relu", False, True)
+        space = torch.empty(max(n, 1), device=DEV, dtype=torch.uint8)
+        st = lib.convsel_linear(xs.data_ptr(), ws.data_ptr(), None, r.data_ptr(), y.data_ptr(), d, space.data_ptr(), n,
+                                torch.cuda.current_stream().cuda_stream)
+        assert st == 0
+        within(y, want, bound, "shifted by %d" % shift)
+
+
 def test_linear_updates_its_residual_in_place():
     for m in (1, 9, 70, 300):
         x, w = torch.randn(m, 256, device=DEV).bfloat16(), torch.randn(192, 256, device=DEV).bfloat16()
