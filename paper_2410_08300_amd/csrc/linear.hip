@@ -94,13 +94,14 @@ __global__ __launch_bounds__(1024) void linear_rows_kernel(LinearArgs g, int wav
   // Lane (row of x, q) holds outputs 4 q .. 4 q + 3: the first wave finishes them.
   const int64_t m = m0 + r16, o = o0 + 4 * q;
   if (wave != 0 || m >= g.m || o >= g.out) return;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+  float sum[1][4] = {}, bias[4];
+  load_bias4<T>(g, o, bias);
   for (int w = 0; w < waves; ++w) {
     const f32x4v_t v = part[w][lane];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) sum[x] += v[x];
+    for (int x = 0; x < 4; ++x) sum[0][x] += v[x];
   }
-  finish4<T>(g, m, o, sum, vec_out);
+  finish4<T, 1>(g, m, 0, o, sum, bias, vec_out);
 }
 
 // Which kernel: up to kFewRows rows, or operands the tiles cannot address.
@@ -179,8 +180,8 @@ void linear_describe(const LinearArgs& a, char* buf, size_t len) {
     snprintf(buf, len, "linear kernels=linear_rows_kernel tile=16x16 waves=%d workspace=0", p.waves);
     return;
   }
-  snprintf(buf, len, "linear kernels=%slinear_tiles_kernel%s tile=%s split=%d workspace=%zu",
-           t.pack ? "linear_pack_kernel;" : "", t.splits > 1 ? ";linear_join_kernel" : "", linear_tiles_name(t.config),
+  snprintf(buf, len, "linear kernels=%slinear_tiles%s_kernel%s tile=%s split=%d workspace=%zu",
+           t.pack ? "linear_pack_kernel;" : "", t.config == 0 ? "256" : "", t.splits > 1 ? ";linear_join_kernel" : "", linear_tiles_name(t.config),
            t.splits, linear_workspace(a));
 }
 

@@ -7,43 +7,68 @@
 namespace convsel {
 namespace lm {
 
-// Four neighbouring outputs o .. o + 3 of row m from their sums: bias,
+// The biases of outputs o .. o + 3.
+template <typename T>
+__device__ __forceinline__ void load_bias4(const LinearArgs& g, int64_t o, float (&b)[4]) {
+  const T* B = reinterpret_cast<const T*>(g.b);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) b[i] = B && o + i < g.out ? elem<T>::load(B + o + i) : 0.f;
+}
+
+// Outputs o .. o + 3 of N rows m, m + step ... from their sums z: bias,
 // activation, residual, one rounding.  `vec`: every row of y and r starts on a
 // whole unit of four.
-template <typename T>
-__device__ __forceinline__ void finish4(const LinearArgs& g, int64_t m, int64_t o, const float (&sum)[4], bool vec) {
-  const T* B = reinterpret_cast<const T*>(g.b);
+template <typename T, int N>
+__device__ __forceinline__ void finish4(const LinearArgs& g, int64_t m, int step, int64_t o, float (&z)[N][4],
+                                        const float (&bias)[4], bool vec) {
   const T* R = reinterpret_cast<const T*>(g.r);
   T* Y = reinterpret_cast<T*>(g.y) + m * g.ldy + o;
-  if (R) R += m * g.ldr + o;
-  const bool whole = o + 4 <= g.out;
-  float z[4];
+  const int64_t left = g.m - m, ldy = step * g.ldy, ldr = step * g.ldr;
+  const bool whole = vec && o + 4 <= g.out;
+  float r[N][4];
+  if (R) {
+    R += m * g.ldr + o;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    z[i] = sum[i];
-    if (B) z[i] += elem<T>::load(B + (whole || o + i < g.out ? o + i : o));
-    z[i] = activate<T>(z[i], g.act);
-  }
-  if (vec && whole) {
-    if constexpr (sizeof(T) == 4) {
-      float4 v = make_float4(z[0], z[1], z[2], z[3]);
-      if (R) {
-        const float4 r = *reinterpret_cast<const float4*>(R);
-        v.x += r.x; v.y += r.y; v.z += r.z; v.w += r.w;
+    for (int n = 0; n < N; ++n) {
+      const T* p = n * step < left ? R + n * ldr : R;
+      if (whole) {
+        if constexpr (sizeof(T) == 4) {
+          const float4 v = *reinterpret_cast<const float4*>(p);
+          r[n][0] = v.x; r[n][1] = v.y; r[n][2] = v.z; r[n][3] = v.w;
+        } else {
+          const uint2 v = *reinterpret_cast<const uint2*>(p);
+          r[n][0] = bf16_to_f32(v.x & 0xffffu); r[n][1] = bf16_to_f32(v.x >> 16);
+          r[n][2] = bf16_to_f32(v.y & 0xffffu); r[n][3] = bf16_to_f32(v.y >> 16);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[n][i] = elem<T>::load(p + (o + i < g.out ? i : 0));
       }
-      *reinterpret_cast<float4*>(Y) = v;
-    } else {
-      if (R) {
-        const uint2 r = *reinterpret_cast<const uint2*>(R);
-        z[0] += bf16_to_f32(r.x & 0xffffu); z[1] += bf16_to_f32(r.x >> 16);
-        z[2] += bf16_to_f32(r.y & 0xffffu); z[3] += bf16_to_f32(r.y >> 16);
-      }
-      *reinterpret_cast<uint2*>(Y) = make_uint2(f32x2_to_bf16x2(z[0], z[1]), f32x2_to_bf16x2(z[2], z[3]));
     }
-  } else {
+  }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (o + i < g.out) elem<T>::store(Y + i, R ? z[i] + elem<T>::load(R + i) : z[i]);
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[n][i] += bias[i];
+  activate_all<T, N>(z, g.act);
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    if (n * step >= left) break;
+    if (R) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[n][i] += r[n][i];
+    }
+    T* p = Y + n * ldy;
+    if (whole) {
+      if constexpr (sizeof(T) == 4)
+        *reinterpret_cast<float4*>(p) = make_float4(z[n][0], z[n][1], z[n][2], z[n][3]);
+      else
+        *reinterpret_cast<uint2*>(p) = make_uint2(f32x2_to_bf16x2(z[n][0], z[n][1]), f32x2_to_bf16x2(z[n][2], z[n][3]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (o + i < g.out) elem<T>::store(p + i, z[n][i]);
+    }
   }
 }
 

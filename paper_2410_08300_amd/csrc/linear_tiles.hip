@@ -6,18 +6,25 @@
 // 256-byte line, with the 16-byte unit u of row r at place 8 (r % 2) + (u ^ (r /
 // 2 % 8)): the 16 rows that a quarter wave reads of one unit lie on different
 // banks.  Rows past the operand and columns past the reduction read zeros
-// through the buffer's range.  NST stages form a ring; a stage is filled again
-// as soon as its last unit is read.  A wave multiplies FO x FM blocks of 32 x 32
-// in four steps a k-tile; the operands of a step are read while the step before
-// it multiplies, those of the next k-tile's first step behind the tile's one
-// barrier.
+// through the buffer's range.  The products' rows are w's and their columns x's.
+// Sums leave through LDS, each wave in a place of its own, so that every row of
+// y is read (residual) and written along its outputs.
 //
-// The products' rows are w's and their columns x's.  Sums leave through LDS,
-// each wave in a place of its own, so that every row of y is read (residual)
-// and written along its outputs.
+// Tiles of 64 and 128 (linear_tiles_kernel): NST stages form a ring; a stage is
+// filled again as soon as its last unit is read.  A wave multiplies FO x FM
+// blocks of 32 x 32 in four steps a k-tile; the operands of a step are read
+// while the step before it multiplies, those of the next k-tile's first step
+// behind the tile's one barrier.  Two workgroups share a CU and fill each
+// other's waits.  Tiles of 256: linear_tiles256_kernel.
+//
+// What bounds them: few tiles, the way of a k-tile from memory, once a k-tile;
+// many, the matrix cores at the clock that the card's power leaves them (bf16
+// 4096 rows, 4096 -> 16384: 455 us, 1210 TFLOP/s, 84 % of the kernel's cycles in
+// products, at 1.6 GHz; fp32 4096 rows, 2048 -> 4096: 138 TFLOP/s of 149).
 #include <stdio.h>
 
 #include <type_traits>
+#include <utility>
 
 #include "igemm_common.hpp"
 #include "linear_common.hpp"
@@ -49,8 +56,83 @@ struct TileArgs {
   float* part;         // [split][m][out rounded up to 4]
 };
 
+// The workgroup's part of the reduction and tile.  Workgroup w runs on XCD w % 8: each XCD has a contiguous run of tiles,
+// eight rows of tiles deep before the next outputs, so that the workgroups of one L2 share both operands.  False for a
+// workgroup without work.
+__device__ __forceinline__ bool place(const TileArgs& a, int& split, int& tm, int& to) {
+  const int units = a.to * a.tm * a.splits;
+  const int per_xcd = (units + 7) >> 3;
+  const int unit = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= per_xcd || unit >= units) return false;
+  const int tile = unit / a.splits;
+  split = unit % a.splits;
+  const int band = tile / (8 * a.to), in_band = tile - band * 8 * a.to;
+  const int deep = min(8, a.tm - band * 8);
+  tm = band * 8 + in_band % deep;
+  to = in_band / deep;
+  return true;
+}
+
+// Writes a wave's FO x FM blocks, whose first row and output are m0 and o0: through its own place in LDS, so that every
+// row of y is read (residual) and written along its outputs.
 template <typename T, typename S>
-__global__ __launch_bounds__(S::WAVES * 64, S::WAVES == 8 ? 2 : 1) void linear_tiles_kernel(TileArgs a) {
+__device__ __forceinline__ void store_blocks(const TileArgs& a, const f32x16_t (&acc)[S::FO][S::FM], char* lds, int wave,
+                                             int lane, int64_t m0, int64_t o0, int split) {
+  constexpr int FO = S::FO, FM = S::FM;
+  const LinearArgs& g = a.g;
+  const int half = lane >> 5, l32 = lane & 31;
+  float* mine = reinterpret_cast<float*>(lds) + wave * 32 * S::OUT_ROW;
+  const int64_t opad = (g.out + 3) & ~static_cast<int64_t>(3);
+  // A lane has the same four outputs of all its rows.  Rows go in fours, so that what they read is on its way together;
+  // one copy of the code for all, as five activations unrolled over a tile do not stay in the instruction cache (37 us
+  // a tile of 256, with the products 143).
+  constexpr int PER = FO * 8, STEP = 64 / PER, N = 4;
+  const int row = lane / PER, col = 4 * (lane % PER);
+  const int64_t o = o0 + col;
+  const bool there = o < g.out;
+  float bias[4];
+  load_bias4<T>(g, o, bias);
+#pragma unroll 1
+  for (int j = 0; j < FM; ++j) {
+#pragma unroll
+    for (int jj = 0; jj < FM; ++jj)
+      if (jj == j) {
+#pragma unroll
+        for (int i = 0; i < FO; ++i)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            *reinterpret_cast<float4*>(mine + l32 * S::OUT_ROW + 32 * i + 8 * v + 4 * half) =
+                make_float4(acc[i][jj][4 * v], acc[i][jj][4 * v + 1], acc[i][jj][4 * v + 2], acc[i][jj][4 * v + 3]);
+      }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int r0 = 0; r0 < 32; r0 += N * STEP) {
+      float z[N][4];
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const float4 v = *reinterpret_cast<const float4*>(mine + (r0 + n * STEP + row) * S::OUT_ROW + col);
+        z[n][0] = v.x; z[n][1] = v.y; z[n][2] = v.z; z[n][3] = v.w;
+      }
+      const int64_t m = m0 + j * 32 + r0 + row;
+      if (!there || m >= g.m) continue;
+      if (a.splits > 1) {
+        float* dst = a.part + (split * g.m + m) * opad + o;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          if (m + n * STEP < g.m)
+            *reinterpret_cast<float4*>(dst + n * STEP * opad) = make_float4(z[n][0], z[n][1], z[n][2], z[n][3]);
+      } else {
+        finish4<T, N>(g, m, STEP, o, z, bias, a.vec_out);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+template <typename T, typename S>
+__global__ __launch_bounds__(S::WAVES * 64, 1) void linear_tiles_kernel(TileArgs a) {
   constexpr int FO = S::FO, FM = S::FM, NDMA = S::NDMA, STAGE = S::STAGE;
   constexpr int NST = S::NST, ES = elem<T>::bytes, UE = elem<T>::per16, BK = 128 / ES;
   __shared__ __align__(16) char lds[S::LDS];
@@ -58,17 +140,9 @@ __global__ __launch_bounds__(S::WAVES * 64, S::WAVES == 8 ? 2 : 1) void linear_t
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wo = wave % S::WO, wm = wave / S::WO;
-  // Workgroup w runs on XCD w % 8: each XCD has a contiguous run of tiles, eight rows of tiles deep before the next
-  // outputs, so that the workgroups of one L2 share both operands.
-  const int units = a.to * a.tm * a.splits;
-  const int per_xcd = (units + 7) >> 3;
-  const int unit = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if ((blockIdx.x >> 3) >= per_xcd || unit >= units) return;  // uniform
-  const int split = unit % a.splits, tile = unit / a.splits;
-  const int band = tile / (8 * a.to), in_band = tile - band * 8 * a.to;
-  const int deep = min(8, a.tm - band * 8);
-  const int64_t m0 = static_cast<int64_t>(band * 8 + in_band % deep) * S::TM;
-  const int64_t o0 = static_cast<int64_t>(in_band / deep) * S::TO;
+  int split, tm, to;
+  if (!place(a, split, tm, to)) return;  // uniform
+  const int64_t m0 = static_cast<int64_t>(tm) * S::TM, o0 = static_cast<int64_t>(to) * S::TO;
 
   const int64_t wrows = min(g.out - o0, static_cast<int64_t>(S::TO)), xrows = min(g.m - m0, static_cast<int64_t>(S::TM));
   const uint32_t wbytes = static_cast<uint32_t>(((wrows - 1) * g.in + g.in) * ES);
@@ -186,39 +260,195 @@ __global__ __launch_bounds__(S::WAVES * 64, S::WAVES == 8 ? 2 : 1) void linear_t
     }
   }
   CONVSEL_WAIT_VMCNT(0);  // the zeros behind the last k-tile too
-
-  lds_sync();  // every wave is done with the stages
-  float* mine = reinterpret_cast<float*>(lds) + wave * 32 * S::OUT_ROW;
-  const int64_t opad = (g.out + 3) & ~static_cast<int64_t>(3);
-#pragma unroll
-  for (int j = 0; j < FM; ++j) {
-#pragma unroll
-    for (int i = 0; i < FO; ++i)
-#pragma unroll
-      for (int v = 0; v < 4; ++v)
-        *reinterpret_cast<float4*>(mine + l32 * S::OUT_ROW + 32 * i + 8 * v + 4 * half) =
-            make_float4(acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
-    constexpr int PER = FO * 8;  // units of four of a row
-#pragma unroll 4
-    for (int u = lane; u < 32 * PER; u += 64) {
-      const int r = u / PER, c = u % PER;
-      const int64_t m = m0 + (wm * FM + j) * 32 + r, o = o0 + wo * FO * 32 + 4 * c;
-      const float4 z = *reinterpret_cast<const float4*>(mine + r * S::OUT_ROW + 4 * c);
-      if (m >= g.m || o >= g.out) continue;
-      if (a.splits > 1) {
-        *reinterpret_cast<float4*>(a.part + (split * g.m + m) * opad + o) = z;
-      } else {
-        const float s[4] = {z.x, z.y, z.z, z.w};
-        finish4<T>(g, m, o, s, a.vec_out);
-      }
-    }
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
-    __builtin_amdgcn_wave_barrier();
-  }
+  lds_sync();             // every wave is done with the stages
+  store_blocks<T, S>(a, acc, lds, wave, lane, m0 + wm * FM * 32, o0 + wo * FO * 32, split);
 }
 
+// f(0), f(1) ... with constants.
+template <int... I, typename F>
+__device__ __forceinline__ void times(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
+// Tiles of 256: four waves, one to each SIMD, of 4 x 4 blocks.  (Eight waves of 4 x 2 read half as much again from LDS:
+// 540 us where this kernel takes 455.)  The ring holds five units of one operand's 256 rows and one k-tile, in the
+// order w, x, w, x ...; a wave reads all of a k-tile's operands by the middle of its products, so that a unit is on its
+// way for a whole k-tile at least.
+typedef Tile<4, 4, 2, 2, 2> Tile256;
+
+template <typename T>
+__global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
+  typedef Tile256 S;
+  constexpr int ES = elem<T>::bytes, UE = elem<T>::per16, BK = 128 / ES, UNIT = 256 * 128, RING = 5;
+  static_assert(S::OUT <= RING * UNIT, "epilogue");
+  __shared__ __align__(16) char lds[RING * UNIT];
+  const LinearArgs& g = a.g;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wo = wave & 1, wm = wave >> 1;
+  int split, tm, to;
+  if (!place(a, split, tm, to)) return;  // uniform
+  const int64_t m0 = static_cast<int64_t>(tm) * 256, o0 = static_cast<int64_t>(to) * 256;
+  const int wrows = static_cast<int>(min(g.out - o0, static_cast<int64_t>(256)));
+  const int xrows = static_cast<int>(min(g.m - m0, static_cast<int64_t>(256)));
+  const uint32_t wbytes = static_cast<uint32_t>(wrows * g.in * ES);
+  const uint32_t xbytes = static_cast<uint32_t>(((xrows - 1) * g.ldx + g.in) * ES);
+  u32x4_t wr = dma_rsrc(reinterpret_cast<const T*>(g.w) + o0 * g.in, wbytes);
+  u32x4_t xr = dma_rsrc(reinterpret_cast<const T*>(g.x) + m0 * g.ldx, xbytes);
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(lds) + wave * 8192);
+  const int all = static_cast<int>((g.in + BK - 1) / BK);
+  const int k0 = __builtin_amdgcn_readfirstlane(split * a.per);
+  const int nk = __builtin_amdgcn_readfirstlane(min(all, k0 + a.per) - k0);
+  // Columns of the last k-tile, where it is cut off.
+  const int ragged = k0 + nk == all ? static_cast<int>(g.in - static_cast<int64_t>(all - 1) * BK) : BK;
+
+  // Instruction d of this wave fills rows 8 (8 wave + d) .. of a unit; the unit of a row that a lane fetches depends on
+  // d's parity only.
+  uint32_t wvo[8], xvo[8];
+  int col[2];
+#pragma unroll
+  for (int d = 0; d < 8; ++d) {
+    const int U = (wave * 8 + d) * 64 + lane;
+    const int line = U >> 4, pos = U & 15;
+    const int row = 2 * line + (pos >> 3), c = ((pos & 7) ^ (line & 7)) * UE;
+    if (d < 2) col[d] = c;
+    wvo[d] = row < wrows ? static_cast<uint32_t>((row * g.in + c) * ES) : wbytes;
+    xvo[d] = row < xrows ? static_cast<uint32_t>((row * g.ldx + c) * ES) : xbytes;
+  }
+  // Before k-tile kt is fetched: columns past the reduction, in its last k-tile, and k-tiles past the last lie beyond
+  // the buffers and read zeros (which nobody reads, in the latter), so that the loop has no branch around its products
+  // and the same number of DMAs is always on its way.
+  uint32_t at = 0;
+  auto next = [&](int kt) {
+    at = static_cast<uint32_t>(k0 + kt) * 128;
+    if (kt == nk - 1 && ragged < BK) {
+#pragma unroll
+      for (int d = 0; d < 8; ++d) {
+        wvo[d] = col[d & 1] < ragged ? wvo[d] : wbytes;
+        xvo[d] = col[d & 1] < ragged ? xvo[d] : xbytes;
+      }
+    }
+    wr[2] = __builtin_amdgcn_readfirstlane(kt < nk ? wr[2] : 0u);
+    xr[2] = __builtin_amdgcn_readfirstlane(kt < nk ? xr[2] : 0u);
+  };
+  // Few instructions between two products: the address goes straight into m0.
+  auto issue = [&](const u32x4_t& r, int slot, uint32_t vo, auto d_c) {
+    const uint32_t st = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(lds0 + slot * UNIT)));
+    const uint32_t so = static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(static_cast<int>(at)));
+    asm volatile("s_add_u32 m0, %0, %4\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(st), "v"(vo), "s"(r), "s"(so), "n"(decltype(d_c)::value * 1024)
+                 : "memory", "scc");
+  };
+  auto issue_w = [&](int slot, auto d_c) { issue(wr, slot, wvo[decltype(d_c)::value], d_c); };
+  auto issue_x = [&](int slot, auto d_c) { issue(xr, slot, xvo[decltype(d_c)::value], d_c); };
+
+  const int half = lane >> 5, l32 = lane & 31;
+  int off[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+    off[t] = (l32 >> 1) * 256 + ((8 * (l32 & 1) + ((2 * t + half) ^ ((l32 >> 1) & 7))) << 4);
+  f32x16_t acc[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i][j] = zero16();
+  vec16 f[4][8];  // step, w's blocks and x's
+  // Operand n of step t: in the order in which the products want them.
+  auto read = [&](int sw, int sx, int t, int n) {
+    const int i = n >> 1;
+    const char* st = lds + ((n & 1) ? sx * UNIT + wm * 16384 : sw * UNIT + wo * 16384) + off[t] + i * 4096;
+    f[t][(n & 1) * 4 + i] = *reinterpret_cast<const vec16*>(st);
+  };
+  auto multiply = [&](int t, int q) {
+    // Blocks in the order in which their operands come: (0,0) (1,0) (0,1) (1,1) (2,0) ...
+    constexpr int O[16] = {0, 1, 0, 1, 2, 2, 0, 1, 2, 3, 3, 3, 0, 1, 2, 3}, M[16] = {0, 0, 1, 1, 0, 1, 2, 2, 2, 0, 1, 2, 3, 3, 3, 3};
+    mfma_32x32<T>(acc[O[q]][M[q]], f[t][O[q]], f[t][4 + M[q]]);
+  };
+  auto fix = [] { __builtin_amdgcn_sched_barrier(0); };
+
+  const std::make_integer_sequence<int, 8> eight{};
+  const std::make_integer_sequence<int, 16> sixteen{};
+
+  for (int kt = 0; kt < 2; ++kt) {
+    next(kt);
+    times(eight, [&](auto d) { issue_w(2 * kt, d); });
+    times(eight, [&](auto d) { issue_x(2 * kt + 1, d); });
+  }
+  CONVSEL_WAIT_VMCNT(16);
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+#pragma unroll
+  for (int n = 0; n < 8; ++n) read(0, 1, 0, n);
+  fix();
+  // A CU takes 64 bytes of a DMA a cycle, and a wave that finds it busy stops, its products too: behind every product
+  // just one of the four waves issues, so each has code of its own.
+  auto walk = [&](auto role_c) {
+    int sw = 0;  // the slot of w's unit of k-tile kt; x's is the next one
+    for (int kt = 0; kt < nk; ++kt) {
+      const int sx = sw == 4 ? 0 : sw + 1, before = sw == 0 ? 4 : sw - 1;
+      const int nw = sw >= 3 ? sw - 3 : sw + 2, nx = nw == 4 ? 0 : nw + 1;
+      next(kt + 2);
+      auto refill = [&](auto q_c) {
+        constexpr int q = decltype(q_c)::value, d = q / 4;
+        if constexpr (q % 4 == decltype(role_c)::value) {
+          if constexpr (d < 8) issue_w(before, std::integral_constant<int, d>{});
+          else issue_x(sw, std::integral_constant<int, d - 8>{});
+        }
+        fix();
+      };
+      times(sixteen, [&](auto q_c) {
+        constexpr int q = decltype(q_c)::value;
+        multiply(0, q);
+        fix();
+        read(sw, sx, 1 + (q >> 3), q & 7);
+        refill(std::integral_constant<int, q>{});
+      });
+      times(sixteen, [&](auto q_c) {
+        constexpr int q = decltype(q_c)::value;
+        multiply(1, q);
+        fix();
+        if constexpr (q < 8) read(sw, sx, 3, q);
+        refill(std::integral_constant<int, 16 + q>{});
+      });
+      // All of the k-tile's operands are in registers: behind the barrier its two units may be filled again.
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      times(sixteen, [&](auto q_c) {
+        constexpr int q = decltype(q_c)::value;
+        multiply(2, q);
+        fix();
+        refill(std::integral_constant<int, 32 + q>{});
+      });
+      times(sixteen, [&](auto q_c) {
+        constexpr int q = decltype(q_c)::value;
+        multiply(3, q);
+        fix();
+        refill(std::integral_constant<int, 48 + q>{});
+        if constexpr (q == 7) {
+          // The next k-tile's units are in once no DMAs but those issued after them are on their way: all of w's in
+          // this k-tile, and x's but two.
+          CONVSEL_WAIT_VMCNT(14);
+          __builtin_amdgcn_s_barrier();
+          asm volatile("" ::: "memory");
+        }
+        if constexpr (q >= 8) read(nw, nx, 0, q - 8);
+        fix();
+      });
+      sw = nw;
+    }
+  };
+  switch (wave) {
+    case 0: walk(std::integral_constant<int, 0>{}); break;
+    case 1: walk(std::integral_constant<int, 1>{}); break;
+    case 2: walk(std::integral_constant<int, 2>{}); break;
+    default: walk(std::integral_constant<int, 3>{}); break;
+  }
+  CONVSEL_WAIT_VMCNT(0);  // the zeros behind the last k-tile too
+  lds_sync();             // every wave is done with the ring
+  store_blocks<T, S>(a, acc, lds, wave, lane, m0 + wm * 128, o0 + wo * 128, split);
+}
 // Sums the parts of a split reduction, in their order, four outputs a thread.
 template <typename T>
 __global__ __launch_bounds__(256) void linear_join_kernel(TileArgs a) {
@@ -226,13 +456,14 @@ __global__ __launch_bounds__(256) void linear_join_kernel(TileArgs a) {
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (i >= quads * a.g.m) return;
   const int64_t m = i / quads, o = (i - m * quads) * 4;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  float s[1][4] = {}, bias[4];
+  load_bias4<T>(a.g, o, bias);
 #pragma unroll 4
   for (int p = 0; p < a.splits; ++p) {
     const float4 z = reinterpret_cast<const float4*>(a.part)[p * quads * a.g.m + i];
-    s[0] += z.x; s[1] += z.y; s[2] += z.z; s[3] += z.w;
+    s[0][0] += z.x; s[0][1] += z.y; s[0][2] += z.z; s[0][3] += z.w;
   }
-  finish4<T>(a.g, m, o, s, a.vec_out);
+  finish4<T, 1>(a.g, m, 0, o, s, bias, a.vec_out);
 }
 
 // Rows of x and w, one after the other, copied to rows of whole 16-byte units.
@@ -258,7 +489,6 @@ __global__ __launch_bounds__(256) void linear_pack_kernel(LinearArgs g, T* dst, 
 }
 
 // A wave's block is 128 x 64, 64 x 64 and 32 x 32 (outputs x rows).
-typedef Tile<4, 2, 2, 4, 2> Tile256;
 typedef Tile<2, 2, 2, 2, 2> Tile128;
 typedef Tile<1, 1, 2, 2, 4> Tile64;
 constexpr int kSide[3] = {256, 128, 64};
@@ -298,9 +528,13 @@ hipError_t launch_all(const LinearArgs& a0, const LinearTiles& p, void* workspac
   a.vec_out = a0.ldy % 4 == 0 && (uintptr_t)a0.y % unit == 0 &&
               (!a0.r || (a0.ldr % 4 == 0 && (uintptr_t)a0.r % unit == 0));
   hipError_t e = hipSuccess;
-  if (p.config == 0) e = launch<T, Tile256>(a, st);
-  else if (p.config == 1) e = launch<T, Tile128>(a, st);
-  else e = launch<T, Tile64>(a, st);
+  if (p.config == 0) {
+    const int units = a.to * a.tm * a.splits;
+    hipLaunchKernelGGL(linear_tiles256_kernel<T>, dim3((unsigned)(8 * ((units + 7) / 8))), dim3(256), 0, st, a);
+    e = hipGetLastError();
+  } else {
+    e = p.config == 1 ? launch<T, Tile128>(a, st) : launch<T, Tile64>(a, st);
+  }
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t quads = (a0.out + 3) / 4 * a0.m;
   hipLaunchKernelGGL(linear_join_kernel<T>, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a);
@@ -327,12 +561,14 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
   }
   auto tiles = [&](int c) { return ((a.out + kSide[c] - 1) / kSide[c]) * ((a.m + kSide[c] - 1) / kSide[c]); };
   const int64_t all = (a.in + 128 / es - 1) / (128 / es);
-  // The tile and the parts that take the least time by what was measured: a k-tile takes a CU with one workgroup
-  // `one` us and a CU with k of them (one after the other or side by side) k * `each`, whichever is more; a call
-  // some 4 us around that, joining parts 2.5 and their way through the caches at 8 TB/s.  At 4096 -> 4096 in bf16:
-  // 4096 rows 130 us in 256s, 155 in 128s, 258 in 64s; 2048 rows 109, 79, 124; 256 rows 95, 25 (4 parts), 24 (2).
-  static const double kOne[2][3] = {{7.4, 2.1, 0.66}, {1.55, 0.83, 0.36}};
-  static const double kEach[2][3] = {{7.6, 2.05, 0.645}, {2.05, 0.61, 0.25}};
+  // The tile and the parts that take the least time by what was measured, in us.  A k-tile takes a CU with one workgroup
+  // `one`, and with k of them k * `each`, or `one` for the last of an odd number of 128s, which two share a CU; tiles of
+  // 256, one a CU, add `alone` for their first loads and last stores.  Joining parts adds 2.5 and their way through the
+  // caches at 8 TB/s.  At 4096 -> 4096 in bf16: 4096 rows 125 us in 256s, 171 in 128s, 271 in 64s; 2048 rows 81 (2
+  // parts), 80, 138; 700 rows 46 (5), 56 (4), 56; 256 rows 32 (11), 27 (4), 25 (2).
+  static const double kOne[2][3] = {{8.3, 2.35, 0.7}, {1.72, 0.83, 0.36}};
+  static const double kEach[2][3] = {{8.3, 2.15, 0.625}, {1.72, 0.61, 0.25}};
+  static const double kAlone[3] = {6., 0., 0.};
   const int ty = a.dtype == CONV_F32 ? 0 : 1;
   double best = 0.;
   for (int c = 0; c < 3; ++c) {
@@ -341,8 +577,10 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
       if (s > 1 && (s > all / 4 || n * s > 2048)) break;
       const int64_t per_part = (all + s - 1) / s, parts = (all + per_part - 1) / per_part;
       if (parts != s) continue;
-      const double k = (double)((n * s + 255) / 256);
-      double t = per_part * (kOne[ty][c] > k * kEach[ty][c] ? kOne[ty][c] : k * kEach[ty][c]);
+      const int64_t k = (n * s + 255) / 256;
+      double step = k * kEach[ty][c];
+      if (k == 1 || (c == 1 && k % 2)) step += kOne[ty][c] - kEach[ty][c];
+      double t = per_part * step + k * kAlone[c];
       if (s > 1) t += 2.5 + (double)s * a.m * a.out * 8 / 8e6;
       if ((c == 0 && s == 1) || t < best) {
         best = t;

@@ -50,19 +50,38 @@ __device__ __forceinline__ int v_byte(int t, int d, int dp) {
   return (t & ~15) * dp + (((t & 15) >> 2) * 16 + (d & 15)) * (dp >> 2) + (d >> 4) * 4 + (t & 3);
 }
 
-template <typename T>
-__device__ __forceinline__ float activate(float z, int act) {
+template <typename T, int ACT>
+__device__ __forceinline__ float activate(float z) {
   constexpr bool exact = sizeof(T) == 4;  // fp32 outputs show the last bits of exp and the quotient
+  if constexpr (ACT == CONVSEL_ACT_RELU) return z < 0.f ? 0.f : z;  // NaN stays
+  if constexpr (ACT == CONVSEL_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+  if constexpr (ACT == CONVSEL_ACT_GELU_TANH) {
+    // (1 + tanh u) / 2 = 1 / (1 + exp(-2u))
+    const float u2 = -1.5957691216057308f * (z + 0.044715f * z * z * z);
+    return exact ? z / (1.f + expf(u2)) : z * __builtin_amdgcn_rcpf(1.f + __expf(u2));
+  }
+  if constexpr (ACT == CONVSEL_ACT_SILU)
+    return exact ? z / (1.f + expf(-z)) : z * __builtin_amdgcn_rcpf(1.f + __expf(-z));
+  return z;
+}
+
+template <typename T, int ACT, int N>
+__device__ __forceinline__ void activate_all(float (&z)[N][4]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[n][i] = activate<T, ACT>(z[n][i]);
+}
+
+// One choice for all of the values.
+template <typename T, int N>
+__device__ __forceinline__ void activate_all(float (&z)[N][4], int act) {
   switch (act) {
-    case CONVSEL_ACT_RELU: return z < 0.f ? 0.f : z;  // NaN stays
-    case CONVSEL_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-    case CONVSEL_ACT_GELU_TANH: {
-      // (1 + tanh u) / 2 = 1 / (1 + exp(-2u))
-      const float u2 = -1.5957691216057308f * (z + 0.044715f * z * z * z);
-      return exact ? z / (1.f + expf(u2)) : z * __frcp_rn(1.f + __expf(u2));
-    }
-    case CONVSEL_ACT_SILU: return exact ? z / (1.f + expf(-z)) : z * __frcp_rn(1.f + __expf(-z));
-    default: return z;
+    case CONVSEL_ACT_RELU: return activate_all<T, CONVSEL_ACT_RELU>(z);
+    case CONVSEL_ACT_GELU: return activate_all<T, CONVSEL_ACT_GELU>(z);
+    case CONVSEL_ACT_GELU_TANH: return activate_all<T, CONVSEL_ACT_GELU_TANH>(z);
+    case CONVSEL_ACT_SILU: return activate_all<T, CONVSEL_ACT_SILU>(z);
+    default: return;
   }
 }
 

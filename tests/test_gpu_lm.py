@@ -66,9 +66,9 @@ def test_linear_sizes(size, dtype):
 
 
 # One case for each tile and way of cutting it, with the kernels that it must reach.
-TILE_SIZES = [(4000, 72, 4001, "tile=256x256 split=1"), (3999, 200, 4000, "tile=256x256 split=1"),
+TILE_SIZES = [(4000, 72, 4001, "tile=128x128 split=1"), (3999, 200, 4000, "tile=128x128 split=1"),
               (2000, 136, 2100, "tile=128x128 split=1"), (2050, 1030, 2048, "linear_pack_kernel;linear_tiles_kernel tile=128x128 split=1"),
-              (1030, 8200, 2052, "tile=128x128 split=5"), (100, 2056, 130, "tile=64x64 split="),
+              (1030, 8200, 2052, "tile=128x128 split="), (100, 2056, 130, "tile=64x64 split="),
               (500, 260, 1000, "linear_pack_kernel;linear_tiles_kernel tile=64x64 split=1"), (1111, 100, 999, "tile=64x64 split=1")]
 
 
@@ -101,6 +101,33 @@ def test_linear_in_every_tile(size, dtype):
     inside[1:-1, 2:o + 2] = True
     assert bool((whole[~inside] == 7.0).all())
     assert torch.equal(cs.linear(x, w, b, act="silu", residual=r), y)
+
+
+# The kernel for tiles of 256: a cut last k-tile and none, rows and outputs that end inside a tile, copied operands, parts.
+BIG_TILES = [("bf16", 3999, 720, 4000, "linear_tiles256_kernel tile=256x256 split=1"),
+             ("f32", 3999, 720, 4000, "linear_tiles256_kernel tile=256x256 split=1"),
+             ("bf16", 3850, 1030, 4001, "linear_pack_kernel;linear_tiles256_kernel tile=256x256 split=1"),
+             ("f32", 3850, 1023, 4001, "linear_pack_kernel;linear_tiles256_kernel tile=256x256 split=1"),
+             ("bf16", 700, 4096, 4096, "tile=256x256 split=5"), ("bf16", 1500, 4104, 4096, "tile=256x256 split=2")]
+
+
+@pytest.mark.parametrize("size", BIG_TILES, ids=lambda s: "%s-%dx%dx%d" % s[:4])
+def test_linear_in_tiles_of_256(size):
+    dtype, m, i, o, runs = size
+    dt = DT[dtype]
+    say("case linear tile 256", size, cs.describe_linear(m, i, o, dt))
+    assert runs in cs.describe_linear(m, i, o, dt)
+    g = gen(m + i)
+    x, w = torch.randn(m, i, generator=g, device=DEV).to(dt), torch.randn(o, i, generator=g, device=DEV).to(dt)
+    b, r = torch.randn(o, generator=g, device=DEV).to(dt), torch.randn(m, o, generator=g, device=DEV).to(dt)
+    y = cs.linear(x, w, b, act="silu", residual=r)
+    # Rows from the first, middle and last tiles, and the outputs of all.
+    rows = torch.tensor(sorted({0, 1, 31, 127, 128, 255, 256, 300, 511, m // 2, m - 2, m - 1}), device=DEV)
+    want, bound = ref.linear(x[rows], w, b, "silu", r[rows])
+    within(y[rows], want, bound + ref.half_ulp(dt) * want.abs() * 1.01, "linear 256 %s" % (size,))
+    # Every other row against the same sums in fp32 by torch's own order: no row may be another's.
+    near = torch.nn.functional.silu(x.float() @ w.float().T + b.float()) + r.float()
+    assert float((y.float() - near).abs().max()) <= 2.0 ** -6 * float(near.abs().max())
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
