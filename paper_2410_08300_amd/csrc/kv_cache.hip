@@ -15,8 +15,9 @@ using namespace lm;
 // or ends inside a block, goes the general way: every 4-byte word of codes
 // belongs to one thread, which keeps the bytes that the call does not write.
 //
-// What bounds it: traffic, two or four bytes in and one out for each value, and
-// for a few tokens the way from the lengths to the table to the page.
+// What bounds it: traffic, two or four bytes in and one out for each value, at
+// 3.8 to 4.3 TB/s for prompts in bf16, and for a few tokens (64 sequences of one:
+// 6.4 us) the way from the lengths to the table to the page.
 
 // The fp32 quotient x / s of finite numbers, correctly rounded, from r = 1 / s
 // (correctly rounded): x r is within two units of it, one step with the exact
@@ -45,12 +46,12 @@ __device__ __forceinline__ uint32_t four_codes(float x0, float x1, float x2, flo
   }
 }
 
-template <typename T, int FMT>
-__global__ __launch_bounds__(256) void kv_write_kernel(convsel_kv_cache_t c, convsel_kv_batch_t b, KvTokens in,
+template <typename T, int FMT, int NT>
+__global__ __launch_bounds__(NT) void kv_write_kernel(convsel_kv_cache_t c, convsel_kv_batch_t b, KvTokens in,
                                                        int vec) {
   constexpr int UE = elem<T>::per16;
   extern __shared__ __align__(16) uint8_t turn[];  // a page's value codes
-  __shared__ float red[4];
+  __shared__ float red[NT / 64];
   const int seq = blockIdx.z;
   const bool values = blockIdx.y >= static_cast<unsigned>(c.kv_heads);
   const int head = values ? blockIdx.y - c.kv_heads : blockIdx.y;
@@ -82,19 +83,20 @@ __global__ __launch_bounds__(256) void kv_write_kernel(convsel_kv_cache_t c, con
     const int upr = vec ? D / UE : 0;  // units of a token's row, where rows are whole units
     if (vec) {
 #pragma unroll 4
-      for (int u = threadIdx.x; u < (r1 - r0) * upr; u += 256) {
+      for (int u = threadIdx.x; u < (r1 - r0) * upr; u += NT) {
         const vec16 v = load16(src + (r0 + u / upr) * token + u % upr * UE);
 #pragma unroll
         for (int x = 0; x < UE; ++x) see(elem<T>::to_f32(vec16_get<T>(v, x)));
       }
     } else {
-      for (int i = threadIdx.x; i < (r1 - r0) * D; i += 256) see(elem<T>::load(src + (r0 + i / D) * token + i % D));
+      for (int i = threadIdx.x; i < (r1 - r0) * D; i += NT) see(elem<T>::load(src + (r0 + i / D) * token + i % D));
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = amax;
     wild = __syncthreads_or(wild);
-    amax = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) amax = fmaxf(amax, red[w]);
     __syncthreads();  // every thread has `old` and red before either is written again
     float scale = fmaxf(amax / qmax_of(FMT), kMinScale);
     if (r0 > 0) scale = fmaxf(scale, old);
@@ -105,7 +107,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(convsel_kv_cache_t c, con
     const bool whole = vec && D == dp && r0 == 0 && !wild && (!values || (r1 & 15) == 0);
     if (whole && !values) {
 #pragma unroll 2
-      for (int u = threadIdx.x; u < r1 * upr; u += 256) {
+      for (int u = threadIdx.x; u < r1 * upr; u += NT) {
         const vec16 v = load16(src + (u / upr) * token + u % upr * UE);
         uint32_t w[UE / 4];
 #pragma unroll
@@ -118,7 +120,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(convsel_kv_cache_t c, con
         else *reinterpret_cast<uint32_t*>(at) = w[0];
       }
     } else if (whole) {
-      for (int u = threadIdx.x; u < (r1 >> 2) * upr; u += 256) {
+      for (int u = threadIdx.x; u < (r1 >> 2) * upr; u += NT) {
         const int t = u / upr * 4, d = u % upr * UE;
         vec16 v[4];
 #pragma unroll
@@ -131,7 +133,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(convsel_kv_cache_t c, con
                               inv);
       }
       __syncthreads();
-      for (int i = threadIdx.x; i < r1 * dp / 16; i += 256) store16(codes + i * 16, load16(turn + i * 16));
+      for (int i = threadIdx.x; i < r1 * dp / 16; i += NT) store16(codes + i * 16, load16(turn + i * 16));
       __syncthreads();
     } else {
       auto code_at = [&](int t, int d, uint32_t was) -> uint32_t {
@@ -142,7 +144,8 @@ __global__ __launch_bounds__(256) void kv_write_kernel(convsel_kv_cache_t c, con
       // Keys: a word is four columns of a token.  Values: four tokens of a column.
       const int from = grown ? 0 : r0;
       const int i0 = values ? (from >> 2) * dp : from * (dp / 4), i1 = values ? ((r1 + 3) >> 2) * dp : r1 * (dp / 4);
-      for (int i = i0 + threadIdx.x; i < i1; i += 256) {
+#pragma unroll 2
+      for (int i = i0 + threadIdx.x; i < i1; i += NT) {
         const int t = values ? i / dp * 4 : i / (dp / 4), d = values ? i % dp : i % (dp / 4) * 4;
         uint32_t* at = reinterpret_cast<uint32_t*>(codes + (values ? v_byte(t, d, dp) : t * dp + d));
         const uint32_t was = t < r0 || (values && t + 4 > r1) ? *at : 0u;
@@ -228,6 +231,19 @@ __global__ __launch_bounds__(256) void kv_read_kernel(convsel_kv_cache_t c, conv
   }
 }
 
+typedef void (*WriteKernel)(convsel_kv_cache_t, convsel_kv_batch_t, KvTokens, int);
+
+template <typename T, int NT>
+WriteKernel write_kernel(int format) {
+  return format == CONVSEL_KV_INT8 ? kv_write_kernel<T, CONVSEL_KV_INT8, NT> : kv_write_kernel<T, CONVSEL_KV_FP8, NT>;
+}
+
+template <typename T>
+WriteKernel write_kernel(int format, int threads) {
+  return threads == 64 ? write_kernel<T, 64>(format) : threads == 128 ? write_kernel<T, 128>(format)
+                                                                       : write_kernel<T, 256>(format);
+}
+
 }  // namespace
 
 hipError_t launch_kv_write(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const KvTokens& t,
@@ -239,24 +255,22 @@ hipError_t launch_kv_write(const convsel_kv_cache_t& c, const convsel_kv_batch_t
     p.table += s0 * b.table_width;
     p.lengths += s0;
     p.offsets += s0;
-    const int64_t pages = (b.tokens + b.seqs - 1) / b.seqs / c.page_size + 2;
+    // The pages that a sequence of the average number of tokens reaches from anywhere; longer ones walk on.  One
+    // workgroup more for nothing cost a single token of each of 64 sequences 3 of 10 us.
+    const int64_t pages = ((b.tokens + b.seqs - 1) / b.seqs + 2 * c.page_size - 2) / c.page_size;
     const dim3 grid((unsigned)(pages < 65536 ? pages : 65536), 2 * c.kv_heads, (unsigned)p.seqs);
     // Rows of whole 16-byte units that start on one.
     const int64_t ue = t.dtype == CONV_F32 ? 4 : 8;
     const int vec = c.head_dim % ue == 0 && t.k_token % ue == 0 && t.k_head % ue == 0 && t.v_token % ue == 0 &&
                     t.v_head % ue == 0 && (uintptr_t)t.k % 16 == 0 && (uintptr_t)t.v % 16 == 0;
     const size_t lds = (size_t)c.page_size * kv_row_bytes(c.head_dim);  // at most 32 KiB
-    if (t.dtype == CONV_F32) {
-      if (c.format == CONVSEL_KV_INT8)
-        hipLaunchKernelGGL((kv_write_kernel<float, CONVSEL_KV_INT8>), grid, dim3(256), lds, stream, c, p, t, vec);
-      else
-        hipLaunchKernelGGL((kv_write_kernel<float, CONVSEL_KV_FP8>), grid, dim3(256), lds, stream, c, p, t, vec);
-    } else {
-      if (c.format == CONVSEL_KV_INT8)
-        hipLaunchKernelGGL((kv_write_kernel<bf16_t, CONVSEL_KV_INT8>), grid, dim3(256), lds, stream, c, p, t, vec);
-      else
-        hipLaunchKernelGGL((kv_write_kernel<bf16_t, CONVSEL_KV_FP8>), grid, dim3(256), lds, stream, c, p, t, vec);
-    }
+    // Small pages in few threads: a workgroup's start costs as much as a page of 16 tokens.  (16 prompts of 2048 tokens of
+    // 8 heads of 128 in bf16: pages of 16 tokens, 53, 78 and 117 us in 64, 128 and 256 threads; of 32, 47, 54, 81; of
+    // 128, 65, 54, 48; of 16 in fp32, 97, 83, 116; six prompts of unlike lengths in pages of 64, 37 in 128, 34 in 256.)
+    const int64_t size = c.page_size * c.head_dim * (t.dtype == CONV_F32 ? 3 : 1);
+    const int threads = size <= 4096 ? 64 : size <= 6144 ? 128 : 256;
+    const auto f = t.dtype == CONV_F32 ? write_kernel<float>(c.format, threads) : write_kernel<bf16_t>(c.format, threads);
+    hipLaunchKernelGGL(f, grid, dim3(threads), lds, stream, c, p, t, vec);
   }
   return hipGetLastError();
 }
@@ -269,7 +283,7 @@ hipError_t launch_kv_read(const convsel_kv_cache_t& c, const convsel_kv_batch_t&
     p.table += s0 * b.table_width;
     p.lengths += s0;
     p.offsets += s0;
-    const int64_t blocks = (b.tokens + b.seqs - 1) / b.seqs / 16 + 2;
+    const int64_t blocks = ((b.tokens + b.seqs - 1) / b.seqs + 30) / 16;
     const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536), c.kv_heads, (unsigned)p.seqs);
     const int64_t ue = t.dtype == CONV_F32 ? 4 : 8;
     const int vec = c.head_dim % ue == 0 && (uintptr_t)t.k % 16 == 0 && (uintptr_t)t.v % 16 == 0;

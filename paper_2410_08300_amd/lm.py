@@ -15,7 +15,6 @@ import math
 import torch
 
 from . import _lib
-from .conv import _on, _stream_of
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
 
@@ -25,17 +24,30 @@ FORMATS = {"int8": 0, "fp8": 1}
 
 def _dtype_of(what, first, *others):
     dt, dev = first.dtype, first.device
-    if dt not in _DTYPES:
+    code = _DTYPES.get(dt)
+    if code is None:
         raise ValueError("%s: unsupported dtype %s (float32 or bfloat16)" % (what, dt))
-    if dev.type != "cuda":
+    if not first.is_cuda:
         raise ValueError("%s runs on the GPU only: move its tensors to a HIP device" % what)
     for t in others:
         if t is not None and (t.dtype is not dt or t.device != dev):
             raise ValueError("%s: tensors must share one dtype and one HIP device" % what)
-    return _DTYPES[dt]
+    return code
 
 
 def _raise(st, what):
+    if st:
+        raise _lib.Conv2dError(st, what)
+
+
+def _run(what, function, device, *args):
+    """The library call on PyTorch's current stream of ``device``."""
+    index = device.index
+    if index == torch._C._cuda_getDevice():
+        st = function(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        with torch.cuda.device(device):
+            st = function(*args, torch._C._cuda_getCurrentRawStream(index))
     if st:
         raise _lib.Conv2dError(st, what)
 
@@ -86,7 +98,7 @@ def linear(x, w, b=None, act="none", residual=None, out=None):
     if residual is not None and residual.shape != shape:
         raise ValueError("linear: residual must have shape %s" % (tuple(shape),))
     if out is None:
-        out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        out = x.new_empty(shape)
     elif out.shape != shape:
         raise ValueError("linear: out must have shape %s" % (tuple(shape),))
     if i == 0 or o == 0:
@@ -105,13 +117,9 @@ def linear(x, w, b=None, act="none", residual=None, out=None):
         x2, ldx = (x2, ldx) if x2.data_ptr() % 16 == 0 else (x2.clone(memory_format=torch.contiguous_format), i)
         w = w if w.data_ptr() % 16 == 0 else w.clone()
     d, n = _linear_plan(x2.shape[0], i, o, ldx, ldr, ldy, dt, act, b is not None, r2 is not None)
-    dev = x.device
-    with _on(dev):
-        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
-        st = _lib.lib().convsel_linear(x2.data_ptr(), w.data_ptr(), None if b is None else b.data_ptr(),
-                                       None if r2 is None else r2.data_ptr(), y2.data_ptr(), d,
-                                       None if ws is None else ws.data_ptr(), n, _stream_of(dev))
-    _raise(st, "linear")
+    ws = torch.empty(n, dtype=torch.uint8, device=x.device) if n else None
+    _run("linear", _lib.lib().convsel_linear, x.device, x2.data_ptr(), w.data_ptr(), None if b is None else b.data_ptr(),
+         None if r2 is None else r2.data_ptr(), y2.data_ptr(), d, None if ws is None else ws.data_ptr(), n)
     return out
 
 
@@ -158,46 +166,43 @@ def qk_norm_rope(q, k, positions, cos, sin, q_weight=None, k_weight=None, eps=1e
     """
     dt = _dtype_of("qk_norm_rope", q, k, q_weight, k_weight, q_out, k_out)
     q, k = _heads(q, "qk_norm_rope"), _heads(k, "qk_norm_rope")
-    t, hq, dim = q.shape
-    hk = k.shape[1]
-    if k.shape[0] != t or k.shape[2] != dim:
+    (t, hq, dim), (tk, hk, dim_k), dev = q.shape, k.shape, q.device
+    if tk != t or dim_k != dim:
         raise ValueError("qk_norm_rope: q %s and k %s differ in tokens or width" % (tuple(q.shape), tuple(k.shape)))
     if norm not in ("rms", "none"):
         raise ValueError("unknown norm %r (rms or none)" % (norm,))
     for wt in (q_weight, k_weight):
-        if wt is not None and tuple(wt.shape) != (dim,):
+        if wt is not None and wt.shape != (dim,):
             raise ValueError("qk_norm_rope: a weight must hold %d values" % dim)
     if (cos is None) != (sin is None):
         raise ValueError("qk_norm_rope: cos and sin come together")
     rotary = rows = 0
     if cos is not None:
         if (cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32
-                or cos.device != q.device or sin.device != q.device):
-            raise ValueError("qk_norm_rope: cos and sin must be float32 tables of one shape on %s" % q.device)
-        rows, rotary = cos.shape[0], 2 * cos.shape[1]
+                or cos.device != dev or sin.device != dev):
+            raise ValueError("qk_norm_rope: cos and sin must be float32 tables of one shape on %s" % dev)
+        rows, rotary = cos.shape
+        rotary *= 2
         if rotary > dim:
             raise ValueError("qk_norm_rope: tables rotate %d of %d values" % (rotary, dim))
         cos, sin = cos.contiguous(), sin.contiguous()
-        positions = _ints(positions, (t,), "positions", q.device)
+        positions = _ints(positions, (t,), "positions", dev)
     q_weight = None if q_weight is None else q_weight.contiguous()
     k_weight = None if k_weight is None else k_weight.contiguous()
-    q_out = torch.empty((t, hq, dim), dtype=q.dtype, device=q.device) if q_out is None else q_out
-    k_out = torch.empty((t, hk, dim), dtype=q.dtype, device=q.device) if k_out is None else k_out
     for o, ref in ((q_out, q), (k_out, k)):
-        if o.shape != ref.shape or (o.stride(2) != 1 and dim > 1):
+        if o is not None and (o.shape != ref.shape or (o.stride(2) != 1 and dim > 1)):
             raise ValueError("qk_norm_rope: an output must have its input's shape and a dense last dimension")
+    q_out = q.new_empty((t, hq, dim)) if q_out is None else q_out
+    k_out = q.new_empty((t, hk, dim)) if k_out is None else k_out
     if dim == 0:
         raise ValueError("qk_norm_rope: empty heads")
     qs, ks, qo, ko = q.stride(), k.stride(), q_out.stride(), k_out.stride()
     d = _qk_plan(t, hq, hk, dim, rotary, qs[0], qs[1], ks[0], ks[1], qo[0], qo[1], ko[0], ko[1], rows, dt,
                  1 if norm == "rms" else 0, bool(interleaved), eps)
-    with _on(q.device):
-        st = _lib.lib().convsel_qk_norm_rope(
-            q.data_ptr(), k.data_ptr(), None if q_weight is None else q_weight.data_ptr(),
-            None if k_weight is None else k_weight.data_ptr(), positions.data_ptr() if rotary else None,
-            cos.data_ptr() if rotary else None, sin.data_ptr() if rotary else None, q_out.data_ptr(),
-            k_out.data_ptr(), d, _stream_of(q.device))
-    _raise(st, "qk_norm_rope")
+    _run("qk_norm_rope", _lib.lib().convsel_qk_norm_rope, dev, q.data_ptr(), k.data_ptr(),
+         None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+         positions.data_ptr() if rotary else None, cos.data_ptr() if rotary else None,
+         sin.data_ptr() if rotary else None, q_out.data_ptr(), k_out.data_ptr(), d)
     return q_out, k_out
 
 
@@ -261,10 +266,8 @@ class KVCache:
                              % (self.kv_heads, self.head_dim, self.device))
         b, keep = self._batch("KVCache.write", table, starts, offsets, k.shape[0])
         ks, vs = k.stride(), v.stride()
-        with _on(self.device):
-            st = _lib.lib().convsel_kv_write(self._desc, b, k.data_ptr(), v.data_ptr(), ks[0],
-                                             ks[1], vs[0], vs[1], dt, _stream_of(self.device))
-        _raise(st, "KVCache.write")
+        _run("KVCache.write", _lib.lib().convsel_kv_write, self.device, self._desc, b, k.data_ptr(), v.data_ptr(), ks[0],
+             ks[1], vs[0], vs[1], dt)
 
     def read(self, table, starts, offsets, tokens, dtype=torch.bfloat16):
         """(k, v) as values, [tokens][kv_heads][head_dim]: for each sequence the
@@ -273,12 +276,10 @@ class KVCache:
         if dtype not in _DTYPES:
             raise ValueError("KVCache.read: unsupported dtype %s (float32 or bfloat16)" % dtype)
         b, keep = self._batch("KVCache.read", table, starts, offsets, int(tokens))
-        with _on(self.device):
-            k = torch.empty((tokens, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
-            v = torch.empty_like(k)
-            st = _lib.lib().convsel_kv_read(self._desc, b, k.data_ptr(), v.data_ptr(),
-                                            _DTYPES[dtype], _stream_of(self.device))
-        _raise(st, "KVCache.read")
+        k = torch.empty((tokens, self.kv_heads, self.head_dim), dtype=dtype, device=self.device)
+        v = torch.empty_like(k)
+        _run("KVCache.read", _lib.lib().convsel_kv_read, self.device, self._desc, b, k.data_ptr(), v.data_ptr(),
+             _DTYPES[dtype])
         return k, v
 
 
@@ -311,7 +312,7 @@ def cached_attention(q, cache, table, lengths, offsets, causal=True, window=0, s
         raise ValueError("cached_attention: q must be [tokens][multiple of %d heads][%d] on %s"
                          % (cache.kv_heads, cache.head_dim, cache.device))
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = q.new_empty(q.shape)
     elif out.shape != q.shape or (out.stride(2) != 1 and q.shape[2] > 1):
         raise ValueError("cached_attention: out must have q's shape and a dense last dimension")
     b, keep = cache._batch("cached_attention", table, lengths, offsets, q.shape[0])
@@ -320,11 +321,9 @@ def cached_attention(q, cache, table, lengths, offsets, causal=True, window=0, s
                            table.shape[0], q.shape[0], table.shape[1], q.shape[1], dt, bool(causal), int(window),
                            1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), qs[0], qs[1], ys[0],
                            ys[1])
-    with _on(q.device):
-        ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
-        st = _lib.lib().convsel_attention(q.data_ptr(), c, b, out.data_ptr(), d, None if ws is None else ws.data_ptr(),
-                                          n, _stream_of(q.device))
-    _raise(st, "cached_attention")
+    ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
+    _run("cached_attention", _lib.lib().convsel_attention, q.device, q.data_ptr(), c, b, out.data_ptr(), d,
+         None if ws is None else ws.data_ptr(), n)
     return out
 
 
