@@ -490,7 +490,8 @@ __global__ __launch_bounds__(256) void linear_pack_kernel(LinearArgs g, T* dst, 
 
 // A wave's block is 128 x 64, 64 x 64 and 32 x 32 (outputs x rows).
 typedef Tile<2, 2, 2, 2, 2> Tile128;
-typedef Tile<1, 1, 2, 2, 4> Tile64;
+// Three stages: three workgroups fit on a CU (four stages, two: 700 rows, 4096 -> 4096 in bf16, 55 us, not 48).
+typedef Tile<1, 1, 2, 2, 3> Tile64;
 constexpr int kSide[3] = {256, 128, 64};
 
 template <typename T, typename S>
@@ -565,9 +566,9 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
   // `one`, and with k of them k * `each`, or `one` for the last of an odd number of 128s, which two share a CU; tiles of
   // 256, one a CU, add `alone` for their first loads and last stores.  Joining parts adds 2.5 and their way through the
   // caches at 8 TB/s.  At 4096 -> 4096 in bf16: 4096 rows 125 us in 256s, 171 in 128s, 271 in 64s; 2048 rows 81 (2
-  // parts), 80, 138; 700 rows 46 (5), 56 (4), 56; 256 rows 32 (11), 27 (4), 25 (2).
+  // parts), 80, 138; 700 rows 46 (5), 56 (4), 48; 256 rows 32 (11), 27 (4), 25 (2).
   static const double kOne[2][3] = {{8.3, 2.35, 0.7}, {1.72, 0.83, 0.36}};
-  static const double kEach[2][3] = {{8.3, 2.15, 0.625}, {1.72, 0.61, 0.25}};
+  static const double kEach[2][3] = {{8.3, 2.15, 0.61}, {1.72, 0.61, 0.25}};
   static const double kAlone[3] = {6., 0., 0.};
   const int ty = a.dtype == CONV_F32 ? 0 : 1;
   double best = 0.;
