@@ -2,7 +2,6 @@
 #include <math.h>
 #include <stdio.h>
 
-
 #include "attention_common.hpp"
 
 namespace convsel {
@@ -52,6 +51,10 @@ __device__ __forceinline__ f32x4v_t mfma16(const f16x8_t& a, const f16x8_t& b, c
 // the cache those are the weights that the second product wants from it: no
 // value is moved between lanes, and codes go from memory to the matrix cores
 // through registers alone.
+//
+// What bounds it: the codes' way from memory.  64 sequences of one query on 2048
+// .. 8192 tokens, 32 heads of 128 on 8, fp8: 136 us, 4.9 TB/s; one on 32768 in
+// 64 parts, int8: 18 us, 3.7 TB/s, and 3.8 us for the join.
 // ---------------------------------------------------------------------------
 template <typename T, int FMT, int NC>
 __global__ __launch_bounds__(256) void attention_rows_kernel(
@@ -429,7 +432,7 @@ __global__ __launch_bounds__(256) void attention_join_few_kernel(const float* __
     if (4 * col + x < a.dim) elem<T>::store(dst + x, r[x]);
 }
 
-// How a call is cut: rows, in 16s or 128s, and parts of the keys.  The host
+// How a call is cut: rows, in 16s, 128s or 256s, and parts of the keys.  The host
 // knows how many tokens the call has and how many a sequence may hold, not how
 // they are spread; every count only sets the grid, and kernels walk what there
 // is.
@@ -459,7 +462,7 @@ Plan plan(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convse
     const int64_t groups = p.tiles * c.kv_heads * b.seqs;
     // Two workgroups a CU (one of 256 rows), with 256 keys at least in each part.
     const int64_t want = rows == 256 ? 256 : 512;
-    int64_t n = (want + groups - 1) / groups;
+    int64_t n = rows > 16 ? (want + groups - 1) / groups : want / groups;
     if (n > keys / 256) n = keys / 256;
     if (rows > 16) {
       // 64 keys take 2.3 us where nothing else runs on the CU, a part's results 2e-6 us a value to write and join: the
@@ -467,9 +470,14 @@ Plan plan(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convse
       const double walk = keys / 64 * 2.3, join = (double)b.tokens * d.q_heads * c.head_dim * 2e-6;
       const int64_t best = (int64_t)sqrt(walk / join);
       if (n > best) n = best;
-    } else if (n < 4 && groups < 4096) {
+    } else {
+      // The join's launch costs what 400 keys do (8 key heads of 128: 4 sequences of 20 queries on 500, 13.8 us in one
+      // part and 16.1 in two; 16 of one on 1000, 20.7 and 17.7 in three), and a few workgroups more than run at once
+      // as much again (24 of one on 1000: 21.8, and 26.5 in three parts).
+      if (n > 1 && keys * (n - 1) / n < 400) n = 1;
       // Sequences of unlike lengths end together where each is cut (64 of 2048 .. 8192 tokens: 145 -> 134 us).
-      n = keys / 2048 < 4 ? keys / 2048 : 4;
+      const int64_t even = groups >= 4096 ? 1 : keys / 2048 < 4 ? keys / 2048 : 4;
+      if (n < even) n = even;
     }
     if (n > kMaxSplit) n = kMaxSplit;
     p.nsplit = (int)(n < 1 ? 1 : n);
@@ -592,8 +600,8 @@ void attention_describe(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b
   const Plan p = plan(c, b, d);
   snprintf(buf, len, "attention kernels=attention_%s_kernel%s rows=%d tiles=%d split=%d workspace=%zu",
            p.rows > 16 ? "tiles" : "rows",
-           p.nsplit <= 1 ? "" : p.nsplit <= kFewParts ? ";attention_join_few_kernel" : ";attention_join_kernel", p.rows, p.tiles,
-           p.nsplit, attention_workspace(c, b, d));
+           p.nsplit <= 1 ? "" : p.nsplit <= kFewParts ? ";attention_join_few_kernel" : ";attention_join_kernel", p.rows,
+           p.tiles, p.nsplit, attention_workspace(c, b, d));
 }
 
 }  // namespace convsel

@@ -181,8 +181,8 @@ void linear_describe(const LinearArgs& a, char* buf, size_t len) {
     return;
   }
   snprintf(buf, len, "linear kernels=%slinear_tiles%s_kernel%s tile=%s split=%d workspace=%zu",
-           t.pack ? "linear_pack_kernel;" : "", t.config == 0 ? "256" : "", t.splits > 1 ? ";linear_join_kernel" : "", linear_tiles_name(t.config),
-           t.splits, linear_workspace(a));
+           t.pack ? "linear_pack_kernel;" : "", t.config == 0 ? "256" : "", t.splits > 1 ? ";linear_join_kernel" : "",
+           linear_tiles_name(t.config), t.splits, linear_workspace(a));
 }
 
 }  // namespace convsel

@@ -56,9 +56,9 @@ struct TileArgs {
   float* part;         // [split][m][out rounded up to 4]
 };
 
-// The workgroup's part of the reduction and tile.  Workgroup w runs on XCD w % 8: each XCD has a contiguous run of tiles,
-// eight rows of tiles deep before the next outputs, so that the workgroups of one L2 share both operands.  False for a
-// workgroup without work.
+// The workgroup's part of the reduction and tile.  Workgroup w runs on XCD w % 8: each XCD has a contiguous run of
+// tiles, eight rows of tiles deep before the next outputs, so that the workgroups of one L2 share both operands.  False
+// for a workgroup without work.
 __device__ __forceinline__ bool place(const TileArgs& a, int& split, int& tm, int& to) {
   const int units = a.to * a.tm * a.splits;
   const int per_xcd = (units + 7) >> 3;
@@ -362,7 +362,8 @@ __global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
   };
   auto multiply = [&](int t, int q) {
     // Blocks in the order in which their operands come: (0,0) (1,0) (0,1) (1,1) (2,0) ...
-    constexpr int O[16] = {0, 1, 0, 1, 2, 2, 0, 1, 2, 3, 3, 3, 0, 1, 2, 3}, M[16] = {0, 0, 1, 1, 0, 1, 2, 2, 2, 0, 1, 2, 3, 3, 3, 3};
+    constexpr int O[16] = {0, 1, 0, 1, 2, 2, 0, 1, 2, 3, 3, 3, 0, 1, 2, 3};
+    constexpr int M[16] = {0, 0, 1, 1, 0, 1, 2, 2, 2, 0, 1, 2, 3, 3, 3, 3};
     mfma_32x32<T>(acc[O[q]][M[q]], f[t][O[q]], f[t][4 + M[q]]);
   };
   auto fix = [] { __builtin_amdgcn_sched_barrier(0); };

@@ -20,7 +20,8 @@ _spec = importlib.util.spec_from_file_location("decoder_example", os.path.join(R
 decoder = importlib.util.module_from_spec(_spec)
 _spec.loader.exec_module(decoder)
 
-SMALL = dict(layers=2, hidden=96, q_heads=6, kv_heads=2, dim=16, mlp=200, vocab=50, positions=300, pages=64, page_size=16)
+SMALL = dict(layers=2, hidden=96, q_heads=6, kv_heads=2, dim=16, mlp=200, vocab=50, positions=300, pages=64,
+             page_size=16)
 
 
 def plain(model, fmt, tokens, positions, table, starts, lengths, offsets, caches):
