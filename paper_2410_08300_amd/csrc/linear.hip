@@ -9,22 +9,6 @@ namespace {
 
 using namespace lm;
 
-typedef float f32x4v_t __attribute__((ext_vector_type(4)));
-
-// One 16-byte unit of a 16 x 16 product's operands: 8 bf16 or 4 fp32 of a lane.
-__device__ __forceinline__ f32x4v_t mac16(bf16_t, const vec16& a, const vec16& b, f32x4v_t c) {
-  bf16x8_t av, bv;
-  __builtin_memcpy(&av, &a, 16);
-  __builtin_memcpy(&bv, &b, 16);
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bv, c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4v_t mac16(float, const vec16& a, const vec16& b, f32x4v_t c) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.d[i]), __uint_as_float(b.d[i]), c, 0, 0, 0);
-  return c;
-}
-
 // Few rows: a workgroup owns 16 outputs and 16 rows of x, and its waves share
 // out the reduction, whose sums meet in LDS.  A lane holds 32
 // neighbouring bytes of one weight row (four lanes read a whole 128-byte line)
@@ -181,7 +165,7 @@ void linear_describe(const LinearArgs& a, char* buf, size_t len) {
     return;
   }
   snprintf(buf, len, "linear kernels=%slinear_tiles%s_kernel%s tile=%s split=%d workspace=%zu",
-           t.pack ? "linear_pack_kernel;" : "", t.config == 0 ? "256" : "", t.splits > 1 ? ";linear_join_kernel" : "",
+           t.pack ? "linear_pack_kernel;" : "", t.config == 0 && a.dtype != CONV_F32 ? "256" : "", t.splits > 1 ? ";linear_join_kernel" : "",
            linear_tiles_name(t.config), t.splits, linear_workspace(a));
 }
 

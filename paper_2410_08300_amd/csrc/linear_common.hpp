@@ -7,6 +7,22 @@
 namespace convsel {
 namespace lm {
 
+typedef float f32x4v_t __attribute__((ext_vector_type(4)));
+
+// One 16-byte unit of a 16 x 16 product's operands: 8 bf16 or 4 fp32 of a lane.
+__device__ __forceinline__ f32x4v_t mac16(bf16_t, const vec16& a, const vec16& b, f32x4v_t c) {
+  bf16x8_t av, bv;
+  __builtin_memcpy(&av, &a, 16);
+  __builtin_memcpy(&bv, &b, 16);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, bv, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4v_t mac16(float, const vec16& a, const vec16& b, f32x4v_t c) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.d[i]), __uint_as_float(b.d[i]), c, 0, 0, 0);
+  return c;
+}
+
 // The biases of outputs o .. o + 3.
 template <typename T>
 __device__ __forceinline__ void load_bias4(const LinearArgs& g, int64_t o, float (&b)[4]) {

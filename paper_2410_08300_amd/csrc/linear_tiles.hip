@@ -14,13 +14,13 @@
 // filled again as soon as its last unit is read.  A wave multiplies FO x FM
 // blocks of 32 x 32 in four steps a k-tile; the operands of a step are read
 // while the step before it multiplies, those of the next k-tile's first step
-// behind the tile's one barrier.  Two workgroups share a CU and fill each
-// other's waits.  Tiles of 256: linear_tiles256_kernel.
+// behind the tile's one barrier.  Two or three workgroups share a CU and fill
+// each other's waits.  Tiles of 256 in bf16: linear_tiles256_kernel.
 //
 // What bounds them: few tiles, the way of a k-tile from memory, once a k-tile;
 // many, the matrix cores at the clock that the card's power leaves them (bf16
-// 4096 rows, 4096 -> 16384: 455 us, 1210 TFLOP/s, 84 % of the kernel's cycles in
-// products, at 1.6 GHz; fp32 4096 rows, 2048 -> 4096: 138 TFLOP/s of 149).
+// 4096 rows, 4096 -> 16384: 430 us, 1280 TFLOP/s, 78 % of the kernel's cycles in
+// products, at 1.8 GHz; fp32 4096 rows, 2048 -> 4096: 526 us, 131 TFLOP/s).
 #include <stdio.h>
 
 #include <type_traits>
@@ -73,14 +73,19 @@ __device__ __forceinline__ bool place(const TileArgs& a, int& split, int& tm, in
   return true;
 }
 
-// Writes a wave's FO x FM blocks, whose first row and output are m0 and o0: through its own place in LDS, so that every
-// row of y is read (residual) and written along its outputs.
-template <typename T, typename S>
-__device__ __forceinline__ void store_blocks(const TileArgs& a, const f32x16_t (&acc)[S::FO][S::FM], char* lds, int wave,
-                                             int lane, int64_t m0, int64_t o0, int split) {
+// f(0), f(1) ... with constants.
+template <int... I, typename F>
+__device__ __forceinline__ void times(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
+// Writes a wave's results, whose first row and output are m0 and o0: through its own place in LDS, where put(j, place)
+// lays rows 32 j .. of them, so that every row of y is read (residual) and written along its outputs.
+template <typename T, typename S, typename Put>
+__device__ __forceinline__ void store_blocks(const TileArgs& a, const Put& put, char* lds, int wave, int lane, int64_t m0,
+                                             int64_t o0, int split) {
   constexpr int FO = S::FO, FM = S::FM;
   const LinearArgs& g = a.g;
-  const int half = lane >> 5, l32 = lane & 31;
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * S::OUT_ROW;
   const int64_t opad = (g.out + 3) & ~static_cast<int64_t>(3);
   // A lane has the same four outputs of all its rows.  Rows go in fours, so that what they read is on its way together;
@@ -94,16 +99,9 @@ __device__ __forceinline__ void store_blocks(const TileArgs& a, const f32x16_t (
   load_bias4<T>(g, o, bias);
 #pragma unroll 1
   for (int j = 0; j < FM; ++j) {
-#pragma unroll
-    for (int jj = 0; jj < FM; ++jj)
-      if (jj == j) {
-#pragma unroll
-        for (int i = 0; i < FO; ++i)
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-            *reinterpret_cast<float4*>(mine + l32 * S::OUT_ROW + 32 * i + 8 * v + 4 * half) =
-                make_float4(acc[i][jj][4 * v], acc[i][jj][4 * v + 1], acc[i][jj][4 * v + 2], acc[i][jj][4 * v + 3]);
-      }
+    times(std::make_integer_sequence<int, FM>{}, [&](auto j_c) {
+      if (decltype(j_c)::value == j) put(j_c, mine);
+    });
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
@@ -132,7 +130,7 @@ __device__ __forceinline__ void store_blocks(const TileArgs& a, const f32x16_t (
 }
 
 template <typename T, typename S>
-__global__ __launch_bounds__(S::WAVES * 64, 1) void linear_tiles_kernel(TileArgs a) {
+__global__ __launch_bounds__(S::WAVES * 64, S::WAVES == 8 ? 2 : 1) void linear_tiles_kernel(TileArgs a) {
   constexpr int FO = S::FO, FM = S::FM, NDMA = S::NDMA, STAGE = S::STAGE;
   constexpr int NST = S::NST, ES = elem<T>::bytes, UE = elem<T>::per16, BK = 128 / ES;
   __shared__ __align__(16) char lds[S::LDS];
@@ -261,23 +259,36 @@ __global__ __launch_bounds__(S::WAVES * 64, 1) void linear_tiles_kernel(TileArgs
   }
   CONVSEL_WAIT_VMCNT(0);  // the zeros behind the last k-tile too
   lds_sync();             // every wave is done with the stages
-  store_blocks<T, S>(a, acc, lds, wave, lane, m0 + wm * FM * 32, o0 + wo * FO * 32, split);
+  const auto put = [&](auto j_c, float* mine) {
+    times(std::make_integer_sequence<int, 4 * FO>{}, [&](auto n_c) {
+      constexpr int i = decltype(n_c)::value / 4, v = decltype(n_c)::value % 4;
+      const f32x16_t& z = acc[i][decltype(j_c)::value];
+      *reinterpret_cast<float4*>(mine + l32 * S::OUT_ROW + 32 * i + 8 * v + 4 * half) =
+          make_float4(z[4 * v], z[4 * v + 1], z[4 * v + 2], z[4 * v + 3]);
+    });
+  };
+  store_blocks<T, S>(a, put, lds, wave, lane, m0 + wm * FM * 32, o0 + wo * FO * 32, split);
 }
 
-// f(0), f(1) ... with constants.
-template <int... I, typename F>
-__device__ __forceinline__ void times(std::integer_sequence<int, I...>, F f) {
-  (f(std::integral_constant<int, I>{}), ...);
+struct Place {
+  int i, j;
+};
+constexpr Place place_of(int n) {
+  int r = 0;
+  while ((r + 1) * (r + 1) <= n) ++r;
+  const int k = n - r * r;
+  return k <= r ? Place{r, k} : Place{k - r - 1, r};
 }
 
-// Tiles of 256: four waves, one to each SIMD, of 4 x 4 blocks.  (Eight waves of 4 x 2 read half as much again from LDS:
-// 540 us where this kernel takes 455.)  The ring holds five units of one operand's 256 rows and one k-tile, in the
-// order w, x, w, x ...; a wave reads all of a k-tile's operands by the middle of its products, so that a unit is on its
-// way for a whole k-tile at least.
+// Tiles of 256 in bf16: four waves, one to each SIMD, of 128 x 128.  (Eight waves of 128 x 64 read half as much again
+// from LDS: 540 us where this kernel takes 430.)  Products of 16 x 16 x 32: alone, on random operands, they reach 2065
+// TFLOP/s, those of 32 x 32 x 16 1810, because the card's power bounds both (430 us against 453).  The ring holds five
+// units of one operand's 256 rows and one k-tile, in the order w, x, w, x ...; a wave reads all of a k-tile's operands
+// in its first half, so that a unit is on its way for three quarters of a k-tile at least.
 typedef Tile<4, 4, 2, 2, 2> Tile256;
 
-template <typename T>
 __global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
+  typedef bf16_t T;
   typedef Tile256 S;
   constexpr int ES = elem<T>::bytes, UE = elem<T>::per16, BK = 128 / ES, UNIT = 256 * 128, RING = 5;
   static_assert(S::OUT <= RING * UNIT, "epilogue");
@@ -343,33 +354,34 @@ __global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
   auto issue_w = [&](int slot, auto d_c) { issue(wr, slot, wvo[decltype(d_c)::value], d_c); };
   auto issue_x = [&](int slot, auto d_c) { issue(xr, slot, xvo[decltype(d_c)::value], d_c); };
 
-  const int half = lane >> 5, l32 = lane & 31;
-  int off[4];
+  // Unit 4 t + quarter of row r16 of a block of 16 rows.
+  const int quarter = lane >> 4, r16 = lane & 15;
+  int off[2];
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
-    off[t] = (l32 >> 1) * 256 + ((8 * (l32 & 1) + ((2 * t + half) ^ ((l32 >> 1) & 7))) << 4);
-  f32x16_t acc[4][4];
+  for (int t = 0; t < 2; ++t)
+    off[t] = (r16 >> 1) * 256 + ((8 * (r16 & 1) + ((4 * t + quarter) ^ (r16 >> 1))) << 4);
+  f32x4v_t acc[8][8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = zero16();
-  vec16 f[4][8];  // step, w's blocks and x's
-  // Operand n of step t: in the order in which the products want them.
+    for (int j = 0; j < 8; ++j) acc[i][j] = f32x4v_t{0.f, 0.f, 0.f, 0.f};
+  vec16 f[2][16];  // half of the k-tile, w's blocks and x's
+  // Operand n of a half: w's and x's blocks in turn.
   auto read = [&](int sw, int sx, int t, int n) {
     const int i = n >> 1;
-    const char* st = lds + ((n & 1) ? sx * UNIT + wm * 16384 : sw * UNIT + wo * 16384) + off[t] + i * 4096;
-    f[t][(n & 1) * 4 + i] = *reinterpret_cast<const vec16*>(st);
-  };
-  auto multiply = [&](int t, int q) {
-    // Blocks in the order in which their operands come: (0,0) (1,0) (0,1) (1,1) (2,0) ...
-    constexpr int O[16] = {0, 1, 0, 1, 2, 2, 0, 1, 2, 3, 3, 3, 0, 1, 2, 3};
-    constexpr int M[16] = {0, 0, 1, 1, 0, 1, 2, 2, 2, 0, 1, 2, 3, 3, 3, 3};
-    mfma_32x32<T>(acc[O[q]][M[q]], f[t][O[q]], f[t][4 + M[q]]);
+    const char* st = lds + ((n & 1) ? sx * UNIT + wm * 16384 : sw * UNIT + wo * 16384) + off[t] + i * 2048;
+    f[t][(n & 1) * 8 + i] = *reinterpret_cast<const vec16*>(st);
   };
   auto fix = [] { __builtin_amdgcn_sched_barrier(0); };
+  // Product q of a half, in the order in which their operands come: those of the first r blocks of either are the first
+  // r^2.
+  auto multiply = [&](int t, auto q_c) {
+    constexpr Place p = place_of(decltype(q_c)::value);
+    acc[p.i][p.j] = mac16(T{}, f[t][p.i], f[t][8 + p.j], acc[p.i][p.j]);
+  };
 
   const std::make_integer_sequence<int, 8> eight{};
-  const std::make_integer_sequence<int, 16> sixteen{};
+  const std::make_integer_sequence<int, 32> pairs{};
 
   for (int kt = 0; kt < 2; ++kt) {
     next(kt);
@@ -380,7 +392,7 @@ __global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 #pragma unroll
-  for (int n = 0; n < 8; ++n) read(0, 1, 0, n);
+  for (int n = 0; n < 16; ++n) read(0, 1, 0, n);
   fix();
   // A CU takes 64 bytes of a DMA a cycle, and a wave that finds it busy stops, its products too: behind every product
   // just one of the four waves issues, so each has code of its own.
@@ -398,43 +410,32 @@ __global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
         }
         fix();
       };
-      times(sixteen, [&](auto q_c) {
+      times(pairs, [&](auto q_c) {
         constexpr int q = decltype(q_c)::value;
-        multiply(0, q);
+        multiply(0, std::integral_constant<int, 2 * q>{});
+        if constexpr (q < 16) read(sw, sx, 1, q);
+        multiply(0, std::integral_constant<int, 2 * q + 1>{});
         fix();
-        read(sw, sx, 1 + (q >> 3), q & 7);
-        refill(std::integral_constant<int, q>{});
-      });
-      times(sixteen, [&](auto q_c) {
-        constexpr int q = decltype(q_c)::value;
-        multiply(1, q);
-        fix();
-        if constexpr (q < 8) read(sw, sx, 3, q);
-        refill(std::integral_constant<int, 16 + q>{});
+        refill(q_c);
       });
       // All of the k-tile's operands are in registers: behind the barrier its two units may be filled again.
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      times(sixteen, [&](auto q_c) {
+      times(pairs, [&](auto q_c) {
         constexpr int q = decltype(q_c)::value;
-        multiply(2, q);
+        multiply(1, std::integral_constant<int, 2 * q>{});
+        if constexpr (q >= 16) read(nw, nx, 0, q - 16);
+        multiply(1, std::integral_constant<int, 2 * q + 1>{});
         fix();
         refill(std::integral_constant<int, 32 + q>{});
-      });
-      times(sixteen, [&](auto q_c) {
-        constexpr int q = decltype(q_c)::value;
-        multiply(3, q);
-        fix();
-        refill(std::integral_constant<int, 48 + q>{});
-        if constexpr (q == 7) {
+        if constexpr (q == 15) {
           // The next k-tile's units are in once no DMAs but those issued after them are on their way: all of w's in
-          // this k-tile, and x's but two.
-          CONVSEL_WAIT_VMCNT(14);
+          // this k-tile, and half of x's.
+          CONVSEL_WAIT_VMCNT(12);
           __builtin_amdgcn_s_barrier();
           asm volatile("" ::: "memory");
         }
-        if constexpr (q >= 8) read(nw, nx, 0, q - 8);
         fix();
       });
       sw = nw;
@@ -448,7 +449,15 @@ __global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
   }
   CONVSEL_WAIT_VMCNT(0);  // the zeros behind the last k-tile too
   lds_sync();             // every wave is done with the ring
-  store_blocks<T, S>(a, acc, lds, wave, lane, m0 + wm * 128, o0 + wo * 128, split);
+  const auto put = [&](auto j_c, float* mine) {
+    times(std::make_integer_sequence<int, 16>{}, [&](auto n_c) {
+      constexpr int i = decltype(n_c)::value / 2, h = decltype(n_c)::value % 2;
+      const f32x4v_t& z = acc[i][2 * decltype(j_c)::value + h];
+      *reinterpret_cast<float4*>(mine + (16 * h + r16) * S::OUT_ROW + 16 * i + 4 * quarter) =
+          make_float4(z[0], z[1], z[2], z[3]);
+    });
+  };
+  store_blocks<T, S>(a, put, lds, wave, lane, m0 + wm * 128, o0 + wo * 128, split);
 }
 // Sums the parts of a split reduction, in their order, four outputs a thread.
 template <typename T>
@@ -531,9 +540,13 @@ hipError_t launch_all(const LinearArgs& a0, const LinearTiles& p, void* workspac
               (!a0.r || (a0.ldr % 4 == 0 && (uintptr_t)a0.r % unit == 0));
   hipError_t e = hipSuccess;
   if (p.config == 0) {
-    const int units = a.to * a.tm * a.splits;
-    hipLaunchKernelGGL(linear_tiles256_kernel<T>, dim3((unsigned)(8 * ((units + 7) / 8))), dim3(256), 0, st, a);
-    e = hipGetLastError();
+    if constexpr (sizeof(T) == 4) {
+      e = launch<T, Tile256>(a, st);
+    } else {
+      const int units = a.to * a.tm * a.splits;
+      hipLaunchKernelGGL(linear_tiles256_kernel, dim3((unsigned)(8 * ((units + 7) / 8))), dim3(256), 0, st, a);
+      e = hipGetLastError();
+    }
   } else {
     e = p.config == 1 ? launch<T, Tile128>(a, st) : launch<T, Tile64>(a, st);
   }
@@ -568,8 +581,8 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
   // 256, one a CU, add `alone` for their first loads and last stores.  Joining parts adds 2.5 and their way through the
   // caches at 8 TB/s.  At 4096 -> 4096 in bf16: 4096 rows 125 us in 256s, 171 in 128s, 271 in 64s; 2048 rows 81 (2
   // parts), 80, 138; 700 rows 46 (5), 56 (4), 48; 256 rows 32 (11), 27 (4), 25 (2).
-  static const double kOne[2][3] = {{8.3, 2.35, 0.7}, {1.72, 0.83, 0.36}};
-  static const double kEach[2][3] = {{8.3, 2.15, 0.61}, {1.72, 0.61, 0.25}};
+  static const double kOne[2][3] = {{8.3, 2.35, 0.7}, {1.67, 0.83, 0.36}};
+  static const double kEach[2][3] = {{8.3, 2.15, 0.61}, {1.67, 0.61, 0.25}};
   static const double kAlone[3] = {6., 0., 0.};
   const int ty = a.dtype == CONV_F32 ? 0 : 1;
   double best = 0.;

@@ -105,9 +105,9 @@ def test_linear_in_every_tile(size, dtype):
 
 # The kernel for tiles of 256: a cut last k-tile and none, rows and outputs that end inside a tile, copied operands, parts.
 BIG_TILES = [("bf16", 3999, 720, 4000, "linear_tiles256_kernel tile=256x256 split=1"),
-             ("f32", 3999, 720, 4000, "linear_tiles256_kernel tile=256x256 split=1"),
+             ("f32", 3999, 720, 4000, "linear_tiles_kernel tile=256x256 split=1"),
              ("bf16", 3850, 1030, 4001, "linear_pack_kernel;linear_tiles256_kernel tile=256x256 split=1"),
-             ("f32", 3850, 1023, 4001, "linear_pack_kernel;linear_tiles256_kernel tile=256x256 split=1"),
+             ("f32", 3850, 1023, 4001, "linear_pack_kernel;linear_tiles_kernel tile=256x256 split=1"),
              ("bf16", 700, 4096, 4096, "tile=256x256 split=5"), ("bf16", 1500, 4104, 4096, "tile=256x256 split=2")]
 
 
