@@ -19,7 +19,7 @@
 //
 // What bounds them: few tiles, the way of a k-tile from memory, once a k-tile;
 // many, the matrix cores at the clock that the card's power leaves them (bf16
-// 4096 rows, 4096 -> 16384: 430 us, 1280 TFLOP/s, 78 % of the kernel's cycles in
+// 4096 rows, 4096 -> 16384: 416 us, 1320 TFLOP/s, 78 % of the kernel's cycles in
 // products, at 1.8 GHz; fp32 4096 rows, 2048 -> 4096: 526 us, 131 TFLOP/s).
 #include <stdio.h>
 
@@ -37,6 +37,7 @@ using namespace lm;
 
 template <int FO_, int FM_, int WO_, int WM_, int NST_>
 struct Tile {
+  static constexpr int PER_CU = FO_ * WO_ == 8 ? 1 : FO_ * WO_ == 4 ? 2 : 3;  // workgroups that a CU holds
   static constexpr int FO = FO_, FM = FM_, WO = WO_, WM = WM_, NST = NST_;
   static constexpr int TO = FO * 32 * WO, TM = FM * 32 * WM, WAVES = WO * WM;
   static constexpr int STAGE = (TO + TM) * 128;
@@ -79,6 +80,74 @@ __device__ __forceinline__ void times(std::integer_sequence<int, I...>, F f) {
   (f(std::integral_constant<int, I>{}), ...);
 }
 
+// Four neighbouring values of y's type.
+template <typename T> struct Quad;
+template <> struct Quad<float> {
+  float4 v;
+  __device__ __forceinline__ void to(float (&z)[4]) const { z[0] += v.x; z[1] += v.y; z[2] += v.z; z[3] += v.w; }
+  __device__ __forceinline__ static Quad from(const float (&z)[4]) { return {make_float4(z[0], z[1], z[2], z[3])}; }
+};
+template <> struct Quad<bf16_t> {
+  uint2 v;
+  __device__ __forceinline__ void to(float (&z)[4]) const {
+    z[0] += bf16_to_f32(v.x & 0xffffu); z[1] += bf16_to_f32(v.x >> 16);
+    z[2] += bf16_to_f32(v.y & 0xffffu); z[3] += bf16_to_f32(v.y >> 16);
+  }
+  __device__ __forceinline__ static Quad from(const float (&z)[4]) {
+    return {make_uint2(f32x2_to_bf16x2(z[0], z[1]), f32x2_to_bf16x2(z[2], z[3]))};
+  }
+};
+
+// What store_blocks does, of a wave whose rows and outputs all exist, in whole units: eight rows of a lane at most at a
+// time, without a test, and the residual's next ones on their way while these are written.  (4096 rows, 512 -> 16384 in
+// bf16: 110 us by the general way, 91 by this; with a residual 217 and 120.)
+template <typename T, typename S, typename Put>
+__device__ __forceinline__ void store_whole(const TileArgs& a, const Put& put, float* mine, int lane, int64_t m0,
+                                            int64_t o0) {
+  constexpr int FM = S::FM, PER = S::FO * 8, STEP = 64 / PER, PARTS = S::FO == 4 ? 2 : 1, G = 32 / STEP / PARTS;
+  const LinearArgs& g = a.g;
+  const int row = lane / PER, col = 4 * (lane % PER);
+  T* y = reinterpret_cast<T*>(g.y) + (m0 + row) * g.ldy + o0 + col;
+  const T* r = reinterpret_cast<const T*>(g.r) + (m0 + row) * g.ldr + o0 + col;
+  const std::make_integer_sequence<int, G> all{};
+  Quad<T> rest[G];
+  auto fetch = [&] {
+    times(all, [&](auto n_c) {
+      rest[decltype(n_c)::value] = *reinterpret_cast<const Quad<T>*>(r + decltype(n_c)::value * STEP * g.ldr);
+    });
+    r += G * STEP * g.ldr;
+  };
+  if (g.r) fetch();
+  float bias[4];
+  load_bias4<T>(g, o0 + col, bias);
+#pragma unroll 1
+  for (int k = 0; k < FM * PARTS; ++k) {
+    times(std::make_integer_sequence<int, FM>{}, [&](auto j_c) {
+      if (decltype(j_c)::value * PARTS == k) put(j_c, mine);
+    });
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    const float* from = mine + ((k % PARTS) * G * STEP + row) * S::OUT_ROW + col;
+    float z[G][4];
+    times(all, [&](auto n_c) {
+      constexpr int n = decltype(n_c)::value;
+      const float4 v = *reinterpret_cast<const float4*>(from + n * STEP * S::OUT_ROW);
+      z[n][0] = v.x + bias[0]; z[n][1] = v.y + bias[1]; z[n][2] = v.z + bias[2]; z[n][3] = v.w + bias[3];
+    });
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    activate_all<T, G>(z, g.act);
+    if (g.r) {
+      times(all, [&](auto n_c) { rest[decltype(n_c)::value].to(z[decltype(n_c)::value]); });
+      if (k + 1 < FM * PARTS) fetch();
+    }
+    times(all, [&](auto n_c) {
+      *reinterpret_cast<Quad<T>*>(y + decltype(n_c)::value * STEP * g.ldy) = Quad<T>::from(z[decltype(n_c)::value]);
+    });
+    y += G * STEP * g.ldy;
+  }
+}
+
 // Writes a wave's results, whose first row and output are m0 and o0: through its own place in LDS, where put(j, place)
 // lays rows 32 j .. of them, so that every row of y is read (residual) and written along its outputs.
 template <typename T, typename S, typename Put>
@@ -87,10 +156,12 @@ __device__ __forceinline__ void store_blocks(const TileArgs& a, const Put& put, 
   constexpr int FO = S::FO, FM = S::FM;
   const LinearArgs& g = a.g;
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * S::OUT_ROW;
+  if (a.splits == 1 && a.vec_out && m0 + 32 * FM <= g.m && o0 + 32 * FO <= g.out)  // uniform in a wave
+    return store_whole<T, S>(a, put, mine, lane, m0, o0);
   const int64_t opad = (g.out + 3) & ~static_cast<int64_t>(3);
   // A lane has the same four outputs of all its rows.  Rows go in fours, so that what they read is on its way together;
   // one copy of the code for all, as five activations unrolled over a tile do not stay in the instruction cache (37 us
-  // a tile of 256, with the products 143).
+  // of a tile of 256, where this takes 13).
   constexpr int PER = FO * 8, STEP = 64 / PER, N = 4;
   const int row = lane / PER, col = 4 * (lane % PER);
   const int64_t o = o0 + col;
@@ -130,7 +201,7 @@ __device__ __forceinline__ void store_blocks(const TileArgs& a, const Put& put, 
 }
 
 template <typename T, typename S>
-__global__ __launch_bounds__(S::WAVES * 64, S::WAVES == 8 ? 2 : 1) void linear_tiles_kernel(TileArgs a) {
+__global__ __launch_bounds__(S::WAVES * 64, S::PER_CU) void linear_tiles_kernel(TileArgs a) {
   constexpr int FO = S::FO, FM = S::FM, NDMA = S::NDMA, STAGE = S::STAGE;
   constexpr int NST = S::NST, ES = elem<T>::bytes, UE = elem<T>::per16, BK = 128 / ES;
   __shared__ __align__(16) char lds[S::LDS];
@@ -281,8 +352,8 @@ constexpr Place place_of(int n) {
 }
 
 // Tiles of 256 in bf16: four waves, one to each SIMD, of 128 x 128.  (Eight waves of 128 x 64 read half as much again
-// from LDS: 540 us where this kernel takes 430.)  Products of 16 x 16 x 32: alone, on random operands, they reach 2065
-// TFLOP/s, those of 32 x 32 x 16 1810, because the card's power bounds both (430 us against 453).  The ring holds five
+// from LDS: 540 us where this kernel takes 416.)  Products of 16 x 16 x 32: alone, on random operands, they reach 2065
+// TFLOP/s, those of 32 x 32 x 16 1810, because the card's power bounds both (453 -> 430 us).  The ring holds five
 // units of one operand's 256 rows and one k-tile, in the order w, x, w, x ...; a wave reads all of a k-tile's operands
 // in its first half, so that a unit is on its way for three quarters of a k-tile at least.
 typedef Tile<4, 4, 2, 2, 2> Tile256;
