@@ -1,6 +1,9 @@
 // Linear layers: y = act(x W^T + b) + r.  Few rows stream the weights through
 // registers (here); more rows go in tiles (linear_tiles.hip).
+#include <math.h>
 #include <stdio.h>
+
+#include <type_traits>
 
 #include "linear_common.hpp"
 
@@ -58,20 +61,38 @@ __global__ __launch_bounds__(1024) void linear_rows_kernel(LinearArgs g, int wav
   const int64_t steps = (g.in + SK - 1) / SK;
   f32x4v_t acc = {0.f, 0.f, 0.f, 0.f};
   vec16 wv[kDepth][2], xv[kDepth][2];
-  auto fetch = [&](int d, int64_t s) {
-    const int64_t k = s * SK + q * 2 * UE;
+  auto walk = [&](int64_t s0, auto depth_c, const auto& get) {
+    constexpr int DEPTH = decltype(depth_c)::value;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) wv[d][u] = unit(W, k + u * UE);
+    for (int d = 0; d < DEPTH; ++d) {
+      const int64_t k = (s0 + static_cast<int64_t>(d) * waves) * SK + q * 2 * UE;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) xv[d][u] = unit(X, k + u * UE);
-  };
-  for (int64_t s0 = wave; s0 < steps; s0 += static_cast<int64_t>(waves) * kDepth) {
+      for (int u = 0; u < 2; ++u) wv[d][u] = get(W, k + u * UE);
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d) fetch(d, s0 + static_cast<int64_t>(d) * waves);
+      for (int u = 0; u < 2; ++u) xv[d][u] = get(X, k + u * UE);
+    }
 #pragma unroll
-    for (int d = 0; d < kDepth; ++d)
+    for (int d = 0; d < DEPTH; ++d)
 #pragma unroll
       for (int u = 0; u < 2; ++u) acc = mac16(T{}, wv[d][u], xv[d][u], acc);
+  };
+  const std::integral_constant<int, kDepth> deep{};
+  int64_t s0 = wave;
+  const int64_t stride = static_cast<int64_t>(waves) * kDepth;
+  if constexpr (!VEC) {
+    // Away from the rows' ends 16 bytes are read at once from where they lie, on no 16 bytes (15 rows, 2041 -> 2752 in
+    // fp32: 10.6 us; 24.3 value by value).
+    const auto near = [](const T* row, int64_t k) -> vec16 {
+      vec16 v;
+      __builtin_memcpy(&v, row + k, 16);
+      return v;
+    };
+    const std::integral_constant<int, 1> one{};
+    for (; (s0 + (kDepth - 1) * static_cast<int64_t>(waves) + 1) * SK <= g.in; s0 += stride) walk(s0, deep, near);
+    for (; (s0 + 1) * SK <= g.in; s0 += waves) walk(s0, one, near);
+    for (; s0 < steps; s0 += waves) walk(s0, one, unit);
+  } else {
+    for (; s0 < steps; s0 += stride) walk(s0, deep, unit);
   }
   part[wave][lane] = acc;
   __syncthreads();
@@ -88,7 +109,7 @@ __global__ __launch_bounds__(1024) void linear_rows_kernel(LinearArgs g, int wav
   finish4<T, 1>(g, m, 0, o, sum, bias, vec_out);
 }
 
-// Which kernel: up to kFewRows rows, or operands the tiles cannot address.
+// Up to so many rows are few.
 constexpr int64_t kFewRows = 16;
 
 struct RowsPlan {
@@ -136,9 +157,20 @@ int outputs_vec(const LinearArgs& a) {
   return a.ldy % 4 == 0 && (uintptr_t)a.y % unit == 0 && (!a.r || (a.ldr % 4 == 0 && (uintptr_t)a.r % unit == 0));
 }
 
+// A workgroup of rows brings its weights in at some 22 GB/s, for 16 rows.  With few outputs there are few workgroups, and
+// the tiles, which cut the reduction into parts, are through sooner (7 rows, 14088 -> 541 in fp32: 44 us by rows, 26 in
+// tiles; 5 rows, 11648 -> 68 in bf16: 17 and 10; but 1 row, 4096 -> 1024: 7.5 and 8.5, 2 rows, 16384 -> 4096: 31 and
+// 35).  Rows that would be copied for the tiles are read as they lie where they are few, 1.8 times as slowly in fp32 and
+// 3.5 times in bf16 (24 rows, 2611 -> 7680 in fp32: 61 us in tiles, 51 by rows; 29, 2282 -> 1496: 24 and 12; but 50,
+// 3897 -> 7064 in bf16: 47 and 131).
 bool in_rows(const LinearArgs& a, LinearTiles* t) {
   *t = linear_tiles_plan(a);
-  return a.m <= kFewRows || t->config < 0;
+  if (t->config < 0) return true;
+  const double bytes = 16. * a.in * (a.dtype == CONV_F32 ? 4 : 2);
+  const double groups = (double)((a.out + 15) / 16) * ((a.m + 15) / 16);
+  const double us = bytes / 22e3 * ceil(groups / 256);
+  if (a.m <= kFewRows) return us <= 2.5 + 1.15 * t->us;
+  return a.m <= 4 * kFewRows && t->pack && us * (a.dtype == CONV_F32 ? 1.8 : 3.5) <= t->us;
 }
 
 }  // namespace

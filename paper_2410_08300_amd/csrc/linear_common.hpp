@@ -96,6 +96,7 @@ struct LinearTiles {
   int splits;
   bool pack;   // operands are copied to rows of whole 16-byte units first
   size_t part_bytes, pack_bytes;
+  double us;   // what it should take
 };
 LinearTiles linear_tiles_plan(const LinearArgs& a);
 hipError_t launch_linear_tiles(const LinearArgs& a, const LinearTiles& p, void* workspace, hipStream_t stream);

@@ -643,6 +643,7 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
   const int64_t ld = p.pack || a.in > a.ldx ? padded : a.ldx;
   if (ld * es >= ((int64_t)1 << 31) / 256 || (!p.pack && ((uintptr_t)a.x % 16 != 0 || (uintptr_t)a.w % 16 != 0))) {
     p.config = -1;
+    p.us = 0.;
     return p;
   }
   auto tiles = [&](int c) { return ((a.out + kSide[c] - 1) / kSide[c]) * ((a.m + kSide[c] - 1) / kSide[c]); };
@@ -675,6 +676,8 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
       }
     }
   }
+  // Copying both operands first: a launch, and their way there and back.
+  p.us = best + (p.pack ? 2.5 + (double)(a.m + a.out) * a.in * es * 2 / 4e6 : 0.);
   if (p.splits > 1) p.part_bytes = (size_t)p.splits * a.m * ((a.out + 3) / 4 * 4) * 4;
   return p;
 }

@@ -103,6 +103,31 @@ def test_linear_in_every_tile(size, dtype):
     assert torch.equal(cs.linear(x, w, b, act="silu", residual=r), y)
 
 
+# Few rows: by rows, read on 16 bytes and on none, and in tiles where outputs are few; rows that would be copied first.
+FEW_ROWS = [("f32", 15, 2041, 300, "linear_rows_kernel"), ("bf16", 5, 1363, 1867, "linear_rows_kernel"),
+            ("bf16", 3, 67, 33, "linear_rows_kernel"), ("f32", 7, 14088, 41, "linear_tiles_kernel;linear_join_kernel"),
+            ("bf16", 5, 11648, 68, "linear_tiles_kernel;linear_join_kernel"),
+            ("f32", 29, 2282, 1496, "linear_rows_kernel"), ("bf16", 28, 717, 119, "linear_rows_kernel")]
+
+
+@pytest.mark.parametrize("size", FEW_ROWS, ids=lambda s: "%s-%dx%dx%d" % s[:4])
+def test_linear_of_few_rows(size):
+    dtype, m, i, o, runs = size
+    dt = DT[dtype]
+    say("case linear few", size, cs.describe_linear(m, i, o, dt))
+    assert runs in cs.describe_linear(m, i, o, dt)
+    g = gen(m * o)
+    # Behind the operands lies NaN: nothing past a row's end may count.
+    x = torch.full((m * i + 64,), float("nan"), device=DEV, dtype=dt)[:m * i].view(m, i)
+    w = torch.full((o * i + 64,), float("nan"), device=DEV, dtype=dt)[:o * i].view(o, i)
+    x.copy_(torch.randn(m, i, generator=g, device=DEV))
+    w.copy_(torch.randn(o, i, generator=g, device=DEV))
+    b, r = torch.randn(o, generator=g, device=DEV).to(dt), torch.randn(m, o, generator=g, device=DEV).to(dt)
+    want, bound = ref.linear(x, w, b, "gelu_tanh", r)
+    within(cs.linear(x, w, b, act="gelu_tanh", residual=r), want, bound + ref.half_ulp(dt) * want.abs() * 1.01,
+           "few %s" % (size,))
+
+
 # The kernel for tiles of 256: a cut last k-tile and none, rows and outputs that end inside a tile, copied operands, parts.
 BIG_TILES = [("bf16", 3999, 720, 4000, "linear_tiles256_kernel tile=256x256 split=1"),
              ("f32", 3999, 720, 4000, "linear_tiles_kernel tile=256x256 split=1"),
