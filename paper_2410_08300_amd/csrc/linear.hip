@@ -1,6 +1,5 @@
 // Linear layers: y = act(x W^T + b) + r.  Few rows stream the weights through
 // registers (here); more rows go in tiles (linear_tiles.hip).
-#include <math.h>
 #include <stdio.h>
 
 #include <type_traits>
@@ -157,20 +156,20 @@ int outputs_vec(const LinearArgs& a) {
   return a.ldy % 4 == 0 && (uintptr_t)a.y % unit == 0 && (!a.r || (a.ldr % 4 == 0 && (uintptr_t)a.r % unit == 0));
 }
 
-// A workgroup of rows brings its weights in at some 22 GB/s, for 16 rows.  With few outputs there are few workgroups, and
-// the tiles, which cut the reduction into parts, are through sooner (7 rows, 14088 -> 541 in fp32: 44 us by rows, 26 in
-// tiles; 5 rows, 11648 -> 68 in bf16: 17 and 10; but 1 row, 4096 -> 1024: 7.5 and 8.5, 2 rows, 16384 -> 4096: 31 and
-// 35).  Rows that would be copied for the tiles are read as they lie where they are few, 1.8 times as slowly in fp32 and
-// 3.5 times in bf16 (24 rows, 2611 -> 7680 in fp32: 61 us in tiles, 51 by rows; 29, 2282 -> 1496: 24 and 12; but 50,
-// 3897 -> 7064 in bf16: 47 and 131).
+// A workgroup of rows brings its weights in at some 22 GB/s; 16 rows of x take 0.4 as long again.  With few outputs
+// there are few workgroups, and the tiles, which cut the reduction into parts, are through sooner (7 rows, 14088 -> 541 in
+// fp32: 44 us by rows, 26 in tiles; 5 rows, 11648 -> 68 in bf16: 17 and 10; 16 rows, 11008 -> 4100: 38 and 27; but 1 row,
+// 4096 -> 1024: 7.5 and 8.5, 5000 -> 5120: 17 and 20).  Rows that would be copied for the tiles are read as they lie
+// where they are few, 1.3 times as slowly in fp32 and 2.5 times in bf16 (24 rows, 2611 -> 7680 in fp32: 61 us in tiles,
+// 51 by rows; 29, 2282 -> 1496: 24 and 12; but 50, 3897 -> 7064 in bf16: 47 and 131).
 bool in_rows(const LinearArgs& a, LinearTiles* t) {
   *t = linear_tiles_plan(a);
   if (t->config < 0) return true;
   const double bytes = 16. * a.in * (a.dtype == CONV_F32 ? 4 : 2);
   const double groups = (double)((a.out + 15) / 16) * ((a.m + 15) / 16);
-  const double us = bytes / 22e3 * ceil(groups / 256);
-  if (a.m <= kFewRows) return us <= 2.5 + 1.15 * t->us;
-  return a.m <= 4 * kFewRows && t->pack && us * (a.dtype == CONV_F32 ? 1.8 : 3.5) <= t->us;
+  const double us = bytes / 22e3 * (groups > 256 ? groups / 256 : 1.) * (1 + 0.4 * (a.m < 16 ? a.m : 16) / 16);
+  if (a.m <= kFewRows) return us <= 3 + 1.15 * t->us;
+  return a.m <= 4 * kFewRows && t->pack && us * (a.dtype == CONV_F32 ? 1.3 : 2.5) <= t->us;
 }
 
 }  // namespace
