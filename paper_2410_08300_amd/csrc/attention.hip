@@ -226,9 +226,9 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(
           float w = u * vd;
           // One rounded w: the compiler would fuse the product into one of the two conversions below only, and
           // the second would then miss by a step where the first fell the other way.
-          if constexpr (TWO) asm volatile("" : "+v"(w));
+          asm volatile("" : "+v"(w));
           wh[4 * i + x] = static_cast<_Float16>(w);
-          if constexpr (TWO) wl[4 * i + x] = static_cast<_Float16>(w - static_cast<float>(wh[4 * i + x]));
+          wl[4 * i + x] = static_cast<_Float16>(w - static_cast<float>(wh[4 * i + x]));
         }
         if (__any(tmax < kFar && tmax > -__builtin_inff())) {
           sum = 0.f;
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(
       for (int d = 0; d < DT; ++d) {
         const f16x8_t vf8 = widen8<FMT>(r[0].v[d], r[1].v[d]);
         o[d] = mfma16(vf8, wh, o[d]);
-        if constexpr (TWO) o[d] = mfma16(vf8, wl, o[d]);
+        o[d] = mfma16(vf8, wl, o[d]);
       }
     };
 

@@ -11,11 +11,13 @@
 // values may hold the weight, and no scale overflows.  Scales reach from 2^-100
 // to 2^121, so a change of M is an exponent added, and where u would leave fp32
 // (scales 2^100 apart within a row) the sum's terms are formed without it.
-// Weights go to the matrix cores in 11 bits, 2^15 times as large (their steps
-// are then 2^-39 of the largest); codes are exact in them.  fp32 calls hold
-// queries and weights as two such numbers, 22 bits.  Queries are brought to
-// [2^14, 2^15) by a power of two, which bf16 survives exactly.  Sums and
-// statistics are fp32.
+// Weights go to the matrix cores as two 16-bit floats, 22 bits, 2^15 times as
+// large (their steps are then 2^-39 of the largest); codes are exact in one.
+// One number, 11 bits, turns 7 % of bf16 results into a neighbour of the rounded
+// one, though it saves a fifth of a long prompt (4096 tokens of 32 heads of 128
+// on 8: 217 us, 269 with two).  fp32 calls hold queries as two such numbers;
+// bf16 queries are exact in one, brought to [2^14, 2^15) by a power of two.  Sums
+// and statistics are fp32.
 #pragma once
 
 #include "lm_common.hpp"

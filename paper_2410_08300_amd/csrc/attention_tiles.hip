@@ -13,12 +13,11 @@
 // to the second product, V^T P^T, without moving them.  A row's statistics need
 // one exchange, with the lane that holds the other tokens.
 //
-// What bounds it: the vector unit, with the waits between its phases.  A weight
-// costs a fused product, a transcendental (four slots), an addition to the sum,
-// half a conversion and half a maximum; 16 of them a lane and 32 keys stand
-// beside 16 products of 32 cycles each.  4096 new tokens of 32 heads of 128 on 8,
-// causal, int8: 195 us, 705 TFLOP/s; the products alone would take 90 at the
-// rate of a large product.
+// What bounds it: the vector unit and the matrix cores in turn, with the waits
+// between.  A weight costs a fused product, a transcendental (four slots), an
+// addition to the sum, a conversion to each of two halves with a subtraction
+// between, and half a maximum; 16 of them a lane and 32 keys stand beside 24
+// products of 32 cycles each.
 #include "attention_common.hpp"
 #include "lm_common.hpp"
 
@@ -318,7 +317,7 @@ __global__ __launch_bounds__(64 * W, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void a
 #pragma unroll
         for (int i = 0; i < NC; ++i) o[i] *= s;
       }
-      f16x8_t wh[2], wl[TWO ? 2 : 1];
+      f16x8_t wh[2], wl[2];
       float add = 0.f;
       bool far = false;
       const float from = m == -kInf ? 0.f : m;  // a row with nothing yet: its weights are 2^-inf
@@ -333,7 +332,7 @@ __global__ __launch_bounds__(64 * W, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void a
           if constexpr (TWO) w *= bm[b].scale;
           if constexpr (TWO) asm volatile("" : "+v"(w));  // one rounded weight for both halves
           wh[b][x] = static_cast<_Float16>(w);
-          if constexpr (TWO) wl[b][x] = static_cast<_Float16>(w - static_cast<float>(wh[b][x]));
+          wl[b][x] = static_cast<_Float16>(w - static_cast<float>(wh[b][x]));
         }
         far |= top[b] + up < kFar && top[b] > -kInf;
         add += ldexpf(TWO ? sum : sum * bm[b].scale, -static_cast<int>(bm[b].ve));
@@ -350,7 +349,7 @@ __global__ __launch_bounds__(64 * W, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void a
       l += add;
       use_groups<2 * NC>(frag, value, [&](int i, const f16x8_t& vf) {
         o[i % NC] = mfma32(vf, wh[i / NC], o[i % NC]);
-        if constexpr (TWO) o[i % NC] = mfma32(vf, wl[i / NC], o[i % NC]);
+        o[i % NC] = mfma32(vf, wl[i / NC], o[i % NC]);
       });
     };
 
