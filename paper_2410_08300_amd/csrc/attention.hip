@@ -180,7 +180,7 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(
           acc = mfma16(kf, qh[c], acc);
           if constexpr (TWO) acc = mfma16(kf, ql[c], acc);
         }
-        vf[i] = frexpf(there ? r[i].vs : 1.f, &ve[i]);
+        vf[i] = split_scale(there ? r[i].vs : 1.f, ve[i]);
         const float f = (there ? r[i].ks : 0.f) * cs;
         const bool whole = there && j0 >= lo && j0 + 16 <= hi && (!a.causal || j0 + 15 <= first + tile * 16 / a.group) &&
                            a.window == 0;

@@ -83,6 +83,14 @@ constexpr float kWeight = 0x1p15f;  // weights as the matrix cores take them, an
 constexpr float kResult = 0x1p-15f;
 constexpr float kFar = -100.f;      // exponents of u below this are near the end of fp32
 
+// A value scale as mantissa and exponent.  Zero, which a page has that nothing was written to yet, takes the exponent of
+// the least scale that a write gives: its values are zeros, and must not raise the maximum above what others need.
+__device__ __forceinline__ float split_scale(float s, int& e) {
+  const float f = frexpf(s, &e);
+  if (s == 0.f) e = -99;
+  return f;
+}
+
 // Exponent to add to what was kept at maximum `from`, now at `to` >= from.
 __device__ __forceinline__ int shift_of(float from, float to) {
   return from == to ? 0 : static_cast<int>(fmaxf(from - to, -300.f));

@@ -15,8 +15,8 @@
 //
 // What bounds it: the vector unit and the matrix cores in turn, with the waits
 // between.  A weight costs a fused product, a transcendental (four slots), an
-// addition to the sum, a conversion to each of two halves with a subtraction
-// between, and half a maximum; 16 of them a lane and 32 keys stand beside 24
+// addition to the sum, a product with its scale, a conversion to each of two
+// halves with a subtraction between, and half a maximum; 16 of them a lane and 32 keys stand beside 24
 // products of 32 cycles each.
 #include "attention_common.hpp"
 #include "lm_common.hpp"
@@ -32,15 +32,14 @@ __device__ __forceinline__ f32x16_t mfma32(const f16x8_t& a, const f16x8_t& b, c
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
 }
 
-// What a tile's block of 16 tokens comes with.  bf16 calls take the mantissa of
-// the value scale and the weights' 2^15 into the exponent (one operation a
-// weight less; it costs the weights of different blocks up to 2^-20 of each
-// other), fp32 calls multiply by them.
+// What a tile's block of 16 tokens comes with.  (With the value scale's mantissa
+// as a summand of the weights' exponent they would take an operation less, 4096
+// tokens 4 % less time, but be off by up to 2^-20 between blocks, and a scale of
+// zero has no such summand.)
 struct BlockMeta {
   float ks;     // key scale, -1 where there is no page
   float ve;     // exponent of the value scale
-  float up;     // bf16: 15 + log2 of its mantissa
-  float scale;  // bf16: 2^-15 / mantissa; fp32: 2^15 mantissa
+  float scale;  // 2^15 times its mantissa
 };
 
 __device__ __forceinline__ float uniform(float v) {
@@ -193,12 +192,11 @@ __global__ __launch_bounds__(64 * W, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void a
       }
       if (lane == 0) {
         int e;
-        const float f = frexpf(pg < 0 ? 1.f : vsr, &e);
+        const float f = split_scale(pg < 0 ? 1.f : vsr, e);
         BlockMeta m;
         m.ks = pg < 0 ? -1.f : ksr;
         m.ve = e;
-        m.up = TWO ? 0.f : 15.f + __builtin_amdgcn_logf(f);
-        m.scale = TWO ? kWeight * f : kResult * __builtin_amdgcn_rcpf(f);
+        m.scale = kWeight * f;
         meta[buf][wave] = m;
       }
     };
@@ -272,7 +270,7 @@ __global__ __launch_bounds__(64 * W, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void a
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
         const BlockMeta& mb = meta[buf][2 * tt + b];
-        bm[b].ks = uniform(mb.ks); bm[b].ve = uniform(mb.ve); bm[b].up = uniform(mb.up); bm[b].scale = uniform(mb.scale);
+        bm[b].ks = uniform(mb.ks); bm[b].ve = uniform(mb.ve); bm[b].scale = uniform(mb.scale);
       }
       f32x16_t sc = zero16();
       f16x8_t frag[kAhead];
@@ -323,19 +321,19 @@ __global__ __launch_bounds__(64 * W, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void a
       const float from = m == -kInf ? 0.f : m;  // a row with nothing yet: its weights are 2^-inf
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const float up = (bm[b].ve - from) + bm[b].up;
+        const float up = bm[b].ve - from;
         float sum = 0.f;
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
           float w = __builtin_amdgcn_exp2f(fmaf(sc[b * 8 + x], f[b], up));
           sum += w;
-          if constexpr (TWO) w *= bm[b].scale;
-          if constexpr (TWO) asm volatile("" : "+v"(w));  // one rounded weight for both halves
+          w *= bm[b].scale;
+          asm volatile("" : "+v"(w));  // one rounded weight for both halves
           wh[b][x] = static_cast<_Float16>(w);
           wl[b][x] = static_cast<_Float16>(w - static_cast<float>(wh[b][x]));
         }
         far |= top[b] + up < kFar && top[b] > -kInf;
-        add += ldexpf(TWO ? sum : sum * bm[b].scale, -static_cast<int>(bm[b].ve));
+        add += ldexpf(sum, -static_cast<int>(bm[b].ve));
       }
       if (__any(far)) {
         add = 0.f;

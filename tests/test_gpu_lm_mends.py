@@ -61,3 +61,68 @@ def test_attention_differs_from_its_definition_by_the_last_rounding(dtype, fmt, 
     assert smag.max() <= 12
     before = 2.0 ** -16 * mag
     within(y, exact, before + half_step(np.abs(exact) + before, dt), "bits %s %s %s" % (dtype, fmt, kernel))
+
+
+# ---- attention: scales of zero ----------------------------------------------------
+
+def planned(kernel, case, table, dtype):
+    """(times that the sequences are repeated, table) that bring a call to the kernel named, "rows", "128" or "256"."""
+    hq, hk, dim, page, lengths, new = case[:6]
+    if kernel == "rows":
+        rep, t = 1, ints(table)
+    elif kernel == "128" and dtype == "bf16":
+        rep = int(2e9 / (sum(new) * hq * len(table[0]) * page * ((dim + 31) // 32 * 32))) + 1
+        t = ints(table)
+    else:
+        rep, t = 1, wide(table, case)
+    t = t.repeat(rep, 1)
+    text = cs.describe_attention(_Shape(hk, dim, page), len(new) * rep, sum(new) * rep, t.shape[1], hq, DT[dtype])
+    assert " rows=%s " % (16 if kernel == "rows" else kernel) in text, text
+    return rep, t
+
+
+class _Shape:
+    """What describe_attention reads of a cache: its sizes."""
+
+    def __init__(self, kv_heads, head_dim, page):
+        self._cache = cs.KVCache(1, kv_heads, head_dim, page_size=page)
+        self._desc, self.head_dim = self._cache._desc, head_dim
+
+
+ZERO_CASE = (4, 1, 64, 16, [400, 63, 200, 17], [130, 40, 200, 20], True, 0)
+
+
+@pytest.mark.parametrize("kernel,dtype", [("rows", "bf16"), ("rows", "f32"), ("128", "bf16"), ("128", "f32"), ("256", "bf16")])
+def test_attention_over_pages_that_nothing_was_written_to(kernel, dtype):
+    """A new cache holds zeros in pages of scale zero, and a warm-up call reads them: the result is zero.  Among written
+    pages, of values so small that a scale of one beside them would leave their weights no bits, such pages count with
+    their scores (zero keys) and add zeros."""
+    say("case attention zero scales", kernel, dtype)
+    hq, hk, dim, page, lengths, new = ZERO_CASE[:6]
+    small = [2, 2, 2, 2] if kernel == "rows" else new
+    case = ZERO_CASE[:5] + (small, True, 0)
+    for what in ("all", "one", "tiny"):
+        cache, want, table, q = build(case, "int8", dtype, seed=8)
+        if what == "all":
+            cache = cs.KVCache(cache.pages, hk, dim, page_size=page)
+            for s in want.scales.values():
+                s[:] = 0
+        else:
+            gain = np.float32(1.0 if what == "one" else 1e-9)
+            cache.v_scales.mul_(float(gain))
+            want.scales["v"] *= gain
+            for b, i in ((0, 3), (1, 0), (2, 1), (2, 12), (3, 0)):  # one that a causal mask hides from whole waves
+                cache.v_scales[table[b][i], 0] = 0
+                want.scales["v"][table[b][i], 0] = 0
+                cache.k_scales[table[b][i], 0] = 0
+                want.scales["k"][table[b][i], 0] = 0
+        rep, t = planned(kernel, case, table, dtype)
+        offs = [0]
+        for _ in range(rep):
+            offs += [offs[-1] + o for o in offsets_of(small)[1:]]
+        y = cs.cached_attention(q.repeat(rep, 1, 1), cache, t, ints(lengths * rep), ints(offs)).view(rep, -1, hq, dim)
+        exact, mag, smag, top = ref.attention(q, want, table, lengths, offsets_of(small), True, 0, 0.125)
+        within(y[0], exact, ref.attention_bound(exact, mag, smag, top, dim, q.dtype), "zero scales %s" % what)
+        assert bool((y == y[0]).all())
+        if what == "all":
+            assert bool((y == 0).all())
