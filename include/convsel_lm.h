@@ -188,7 +188,7 @@ conv_status_t convsel_kv_read(const convsel_kv_cache_t* cache, const convsel_kv_
  * nothing is zero.  What lies in masked places (rows never written, pages
  * handed back) has no influence, whatever bits it holds. */
 typedef struct convsel_attention_desc {
-  int32_t q_heads; /* tokens * q_heads < 2^31 */
+  int32_t q_heads; /* tokens * q_heads <= 2^31 - 2^20 */
   int32_t dtype;   /* of q and y */
   int32_t causal;
   int32_t window;  /* 0: none */
