@@ -237,8 +237,9 @@ class KVCache:
         # Pages need no first value (their scale is set by the first write), but a read of one is then defined.
         self.k_codes = torch.zeros(n.value, dtype=torch.uint8, device=device)
         self.v_codes = torch.zeros(n.value, dtype=torch.uint8, device=device)
-        self.k_scales = torch.zeros(self.pages, self.kv_heads, device=device)
-        self.v_scales = torch.zeros(self.pages, self.kv_heads, device=device)
+        # fp32 whatever torch's default type is: the library takes their addresses alone.
+        self.k_scales = torch.zeros(self.pages, self.kv_heads, dtype=torch.float32, device=device)
+        self.v_scales = torch.zeros(self.pages, self.kv_heads, dtype=torch.float32, device=device)
         self.device = self.k_codes.device
         # The cache as the library takes it; its buffers stay for the object's life.
         self._desc = ctypes.byref(_lib.KvCacheDesc(

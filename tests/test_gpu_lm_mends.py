@@ -126,3 +126,24 @@ def test_attention_over_pages_that_nothing_was_written_to(kernel, dtype):
         assert bool((y == y[0]).all())
         if what == "all":
             assert bool((y == 0).all())
+
+
+# ---- cache: its buffers -------------------------------------------------------------
+
+@pytest.mark.parametrize("default", [torch.bfloat16, torch.float64])
+def test_cache_scales_are_fp32_under_any_default_type(default):
+    say("case cache default type", default)
+    before = torch.get_default_dtype()
+    torch.set_default_dtype(default)
+    try:
+        cache = cs.KVCache(8, 2, 32, page_size=16)
+    finally:
+        torch.set_default_dtype(before)
+    for s in (cache.k_scales, cache.v_scales):
+        assert s.dtype == torch.float32 and s.shape == (8, 2)
+    want = ref.Cache(8, 2, 32, 16, "int8")
+    x = torch.randn(100, 2, 32, generator=gen(1), device=DEV)
+    table, off = [[7, 6, 5, 4, 3, 2, 1]], [0, 100]
+    cache.write(x, x, ints(table), ints([0]), ints(off))
+    want.write(x, x, table, [0], off)
+    assert np.array_equal(cache.k_scales.cpu().numpy()[1:], want.scales["k"][1:])
