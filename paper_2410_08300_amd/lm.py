@@ -208,6 +208,20 @@ def qk_norm_rope(q, k, positions, cos, sin, q_weight=None, k_weight=None, eps=1e
 
 # ---- cache ----------------------------------------------------------------------
 
+class _Buffer:
+    """A tensor whose address the library was given: it takes new values in place, and no other tensor in its place."""
+
+    def __set_name__(self, owner, name):
+        self.name = name
+
+    def __get__(self, obj, owner=None):
+        return self if obj is None else obj.__dict__[self.name]
+
+    def __set__(self, obj, value):
+        if obj.__dict__.setdefault(self.name, value) is not value:
+            raise AttributeError("KVCache.%s cannot be replaced: copy new values into it" % self.name)
+
+
 class KVCache:
     """A paged key/value cache held in 8 bits: ``pages`` pages of ``page_size``
     (16, 32, 64 or 128) tokens of ``kv_heads`` heads of ``head_dim`` (up to
@@ -219,8 +233,10 @@ class KVCache:
     page.  ``offsets`` (int32, [sequences + 1]) divides a call's packed tokens
     among the sequences.  include/convsel_lm.h has the layout of ``k_codes``,
     ``v_codes``, ``k_scales`` and ``v_scales``, and what a write does to the
-    scale of a page that fills up.
+    scale of a page that fills up; they take new values in place.
     """
+
+    k_codes, v_codes, k_scales, v_scales = _Buffer(), _Buffer(), _Buffer(), _Buffer()
 
     def __init__(self, pages, kv_heads, head_dim, page_size=16, fmt="int8", device="cuda"):
         if fmt not in FORMATS:

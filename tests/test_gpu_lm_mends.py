@@ -147,3 +147,17 @@ def test_cache_scales_are_fp32_under_any_default_type(default):
     cache.write(x, x, ints(table), ints([0]), ints(off))
     want.write(x, x, table, [0], off)
     assert np.array_equal(cache.k_scales.cpu().numpy()[1:], want.scales["k"][1:])
+
+
+@pytest.mark.parametrize("name", ["k_codes", "v_codes", "k_scales", "v_scales"])
+def test_cache_buffers_take_values_and_no_other_tensor(name):
+    """The library holds their addresses: another tensor in their place would leave it with freed memory."""
+    cache = cs.KVCache(4, 2, 32)
+    held = getattr(cache, name)
+    with pytest.raises(AttributeError, match="cannot be replaced"):
+        setattr(cache, name, held.clone())
+    assert getattr(cache, name) is held
+    held.copy_(torch.ones_like(held))
+    cache.k_scales *= 2
+    cache.v_scales += 1
+    assert bool((held != 0).all()) and getattr(cache, name) is held
