@@ -52,13 +52,24 @@ EXPORTED_LM = ("convsel_linear_workspace_bytes", "convsel_linear", "convsel_line
                "convsel_attention", "convsel_attention_describe")
 
 
-class LinearDesc(ctypes.Structure):
+class _Sizes(ctypes.Structure):
+    """A structure whose whole numbers fit its fields: ctypes would cut them off without a word."""
+
+    def __init__(self, *args, **kw):
+        super().__init__(*args, **kw)
+        given = dict(zip((n for n, _ in self._fields_), args), **kw)
+        for name, kind in self._fields_:
+            if kind in (ctypes.c_int32, ctypes.c_int64) and name in given and getattr(self, name) != given[name]:
+                raise ValueError("%s=%s does not fit %d bits" % (name, given[name], 8 * ctypes.sizeof(kind)))
+
+
+class LinearDesc(_Sizes):
     """convsel_linear_desc_t."""
     _fields_ = ([(n, ctypes.c_int64) for n in ("m", "in_features", "out_features", "ldx", "ldr", "ldy")]
                 + [(n, ctypes.c_int32) for n in ("dtype", "act", "has_bias", "has_residual")])
 
 
-class QkDesc(ctypes.Structure):
+class QkDesc(_Sizes):
     """convsel_qk_desc_t."""
     _fields_ = ([("tokens", ctypes.c_int64)]
                 + [(n, ctypes.c_int32) for n in ("q_heads", "k_heads", "head_dim", "rotary_dim")]
@@ -68,7 +79,7 @@ class QkDesc(ctypes.Structure):
                 + [(n, ctypes.c_int32) for n in ("dtype", "norm", "interleaved")] + [("eps", ctypes.c_float)])
 
 
-class KvCacheDesc(ctypes.Structure):
+class KvCacheDesc(_Sizes):
     """convsel_kv_cache_t."""
     _fields_ = ([("pages", ctypes.c_int64)]
                 + [(n, ctypes.c_int32) for n in ("kv_heads", "head_dim", "page_size", "format")]
@@ -81,7 +92,7 @@ class KvBatchDesc(ctypes.Structure):
                 + [(n, ctypes.c_void_p) for n in ("table", "lengths", "offsets")])
 
 
-class AttentionDesc(ctypes.Structure):
+class AttentionDesc(_Sizes):
     """convsel_attention_desc_t."""
     _fields_ = ([(n, ctypes.c_int32) for n in ("q_heads", "dtype", "causal", "window")] + [("scale", ctypes.c_float)]
                 + [(n, ctypes.c_int64) for n in ("q_token_stride", "q_head_stride", "y_token_stride",

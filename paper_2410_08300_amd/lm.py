@@ -302,6 +302,11 @@ class KVCache:
 
 # ---- attention ------------------------------------------------------------------
 
+def _window(window):
+    """``window`` as the library takes it: one that no sequence can fill hides nothing, whatever its size."""
+    return min(int(window), 2 ** 31 - 1)
+
+
 @functools.lru_cache(maxsize=1024)
 def _attention_plan(pages, kv_heads, head_dim, page_size, fmt, seqs, tokens, width, *sizes):
     """(descriptor by reference, workspace bytes) of a call of these sizes."""
@@ -335,7 +340,7 @@ def cached_attention(q, cache, table, lengths, offsets, causal=True, window=0, s
     b, keep = cache._batch("cached_attention", table, lengths, offsets, q.shape[0])
     qs, ys, c = q.stride(), out.stride(), cache._desc
     d, n = _attention_plan(cache.pages, cache.kv_heads, cache.head_dim, cache.page_size, FORMATS[cache.fmt],
-                           table.shape[0], q.shape[0], table.shape[1], q.shape[1], dt, bool(causal), int(window),
+                           table.shape[0], q.shape[0], table.shape[1], q.shape[1], dt, bool(causal), _window(window),
                            1.0 / math.sqrt(cache.head_dim) if scale is None else float(scale), qs[0], qs[1], ys[0],
                            ys[1])
     ws = torch.empty(n, dtype=torch.uint8, device=q.device) if n else None
@@ -348,8 +353,8 @@ def describe_attention(cache, seqs, tokens, table_width, q_heads, dtype=torch.bf
     """How the library runs cached_attention at these sizes, as one line."""
     b = _lib.KvBatchDesc(seqs, tokens, table_width, None, None, None)
     dim = cache.head_dim
-    d = _lib.AttentionDesc(q_heads, _DTYPES[dtype], bool(causal), int(window), 1.0, q_heads * dim, dim, q_heads * dim,
-                           dim)
+    d = _lib.AttentionDesc(q_heads, _DTYPES[dtype], bool(causal), _window(window), 1.0, q_heads * dim, dim,
+                           q_heads * dim, dim)
     buf = ctypes.create_string_buffer(512)
     _raise(_lib.lib().convsel_attention_describe(cache._desc, ctypes.byref(b), ctypes.byref(d), buf, len(buf)),
            "cached_attention")

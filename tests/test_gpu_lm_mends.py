@@ -161,3 +161,15 @@ def test_cache_buffers_take_values_and_no_other_tensor(name):
     cache.k_scales *= 2
     cache.v_scales += 1
     assert bool((held != 0).all()) and getattr(cache, name) is held
+
+
+def test_attention_windows_of_more_than_32_bits_hide_nothing():
+    case = (4, 2, 64, 16, [60], [3], True, 0)
+    cache, _, table, q = build(case, "int8", "bf16")
+    args = (q, cache, ints(table), ints([60]), ints([0, 3]))
+    y = cs.cached_attention(*args)
+    assert not torch.equal(cs.cached_attention(*args, window=8), y)
+    for window in (2 ** 31 - 1, 2 ** 32 + 8, 2 ** 63 - 1):
+        assert torch.equal(cs.cached_attention(*args, window=window), y)
+    with pytest.raises((ValueError, cs.Conv2dError)):
+        cs.cached_attention(*args, window=-2 ** 32 + 8)

@@ -1,8 +1,10 @@
 """Host-side checks of the decoder operators at the ends of their ranges.  No GPU."""
 import ctypes
+import types
 
 import pytest
 
+import paper_2410_08300_amd as cs
 from paper_2410_08300_amd import _lib
 
 from test_lm_host import INVALID, attention_desc, batch_desc, cache_desc
@@ -25,3 +27,42 @@ def test_attention_rows_stay_within_what_the_kernels_count(heads):
     assert attention_bytes(c, batch_desc(seqs=1, tokens=most), d) == _lib.CONV_OK
     for tokens in (most + 1, (2 ** 31 - 1) // heads):
         assert attention_bytes(c, batch_desc(seqs=1, tokens=tokens), d) == INVALID
+
+
+def test_a_window_of_any_size_is_the_window_asked_for():
+    """2^32 + 8 is no window of eight tokens."""
+    cache = types.SimpleNamespace(_desc=ctypes.byref(cache_desc(pages=4096)), head_dim=64)
+
+    def text(window):
+        return cs.describe_attention(cache, 1, 64, 4096, 4, window=window)
+
+    assert text(8) != text(0)  # the plan shows it
+    for window in (2 ** 31 - 1, 2 ** 31, 2 ** 32 + 8, 2 ** 63 - 1, 2 ** 70):
+        assert text(window) == text(0)
+    for window in (-1, -2 ** 32 + 8):
+        with pytest.raises((ValueError, cs.Conv2dError)):
+            text(window)
+
+
+@pytest.mark.parametrize("kw", [dict(kv_heads=2 ** 32 + 2), dict(head_dim=2 ** 32 + 64), dict(page_size=2 ** 32 + 16)],
+                         ids=lambda k: next(iter(k)))
+def test_cache_sizes_that_leave_their_fields_are_refused(kw):
+    sizes = dict(pages=4, kv_heads=2, head_dim=64, page_size=16, device="cpu")
+    sizes.update(kw)
+    with pytest.raises(ValueError, match=next(iter(kw))):
+        cs.KVCache(**sizes)
+
+
+@pytest.mark.parametrize("cls", [_lib.LinearDesc, _lib.QkDesc, _lib.KvCacheDesc, _lib.AttentionDesc])
+def test_structures_refuse_numbers_that_leave_their_fields(cls):
+    for i, (name, kind) in enumerate(cls._fields_):
+        if kind not in (ctypes.c_int32, ctypes.c_int64):
+            continue
+        bits = 8 * ctypes.sizeof(kind)
+        for value in (2 ** (bits - 1), 2 ** bits + 1, -2 ** (bits - 1) - 1):
+            with pytest.raises(ValueError, match=name):
+                cls(**{name: value})
+            with pytest.raises(ValueError, match=name):
+                cls(*([0] * i + [value]))
+        for value in (2 ** (bits - 1) - 1, -2 ** (bits - 1)):
+            assert getattr(cls(**{name: value}), name) == value
