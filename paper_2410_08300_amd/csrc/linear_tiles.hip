@@ -629,6 +629,9 @@ hipError_t launch_all(const LinearArgs& a0, const LinearTiles& p, void* workspac
 
 }  // namespace
 
+// A launch's limit; the grid is rounded up to 8 workgroups.
+constexpr int64_t kThreadsMax = ((int64_t)1 << 32) - 8 * 256;
+
 LinearTiles linear_tiles_plan(const LinearArgs& a) {
   const int64_t es = a.dtype == CONV_F32 ? 4 : 2, per = 16 / es;
   LinearTiles p;
@@ -662,6 +665,7 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
     const int64_t n = tiles(c);
     for (int64_t s = 1; s <= 16; ++s) {
       if (s > 1 && (s > all / 4 || n * s > 2048)) break;
+      if (n * 256 > kThreadsMax) break;  // 2^30 rows of few outputs: tiles of 256 hold 2^31 of them
       const int64_t per_part = (all + s - 1) / s, parts = (all + per_part - 1) / per_part;
       if (parts != s) continue;
       const int64_t k = (n * s + 255) / 256;

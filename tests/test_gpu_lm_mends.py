@@ -173,3 +173,20 @@ def test_attention_windows_of_more_than_32_bits_hide_nothing():
         assert torch.equal(cs.cached_attention(*args, window=window), y)
     with pytest.raises((ValueError, cs.Conv2dError)):
         cs.cached_attention(*args, window=-2 ** 32 + 8)
+
+
+# ---- linear: the end of its range ---------------------------------------------------
+
+def test_linear_of_more_rows_than_a_launch_has_tiles_of_64():
+    """2^30 rows and one, of eight outputs: 17 GB in and out."""
+    m = 2 ** 30 + 1
+    say("case linear", m, cs.describe_linear(m, 8, 8))
+    x = torch.zeros(m, 8, dtype=torch.bfloat16, device=DEV)
+    w = torch.randn(8, 8, generator=gen(2), device=DEV).bfloat16()
+    rows = torch.tensor([0, 1, 255, 256, 2 ** 29, 2 ** 30 - 1, 2 ** 30], device=DEV)
+    x[rows] = torch.randn(len(rows), 8, generator=gen(3), device=DEV).bfloat16()
+    y = cs.linear(x, w)
+    want, bound = ref.linear(x[rows], w)
+    within(y[rows], want, bound + ref.half_ulp(torch.bfloat16) * want.abs() * 1.01, "many rows")
+    y[rows] = 0
+    assert not any(bool(part.any()) for part in y.split(2 ** 26))

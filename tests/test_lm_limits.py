@@ -1,8 +1,10 @@
 """Host-side checks of the decoder operators at the ends of their ranges.  No GPU."""
 import ctypes
+import re
 import types
 
 import pytest
+import torch
 
 import paper_2410_08300_amd as cs
 from paper_2410_08300_amd import _lib
@@ -66,3 +68,17 @@ def test_structures_refuse_numbers_that_leave_their_fields(cls):
                 cls(*([0] * i + [value]))
         for value in (2 ** (bits - 1) - 1, -2 ** (bits - 1)):
             assert getattr(cls(**{name: value}), name) == value
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("outputs", [1, 8, 16, 17, 64, 65])
+def test_linear_of_very_many_rows_fits_a_launch(outputs, dtype):
+    """A launch holds 2^32 threads: tiles of 256 threads, their grid rounded up to 8 of them, stay below that."""
+    most = min(2 ** 31 - 1, 2 ** 35 // outputs)
+    for m in (2 ** 30 - 64, 2 ** 30, 2 ** 30 + 1, most):
+        if m > most:
+            continue
+        text = cs.describe_linear(m, 8, outputs, dtype)
+        side = int(re.search(r" tile=(\d+)x", text).group(1))
+        tiles = -(-m // side) * -(-outputs // side)
+        assert "tiles" in text and (tiles + 7) // 8 * 8 * 256 < 2 ** 32, text
