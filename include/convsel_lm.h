@@ -82,7 +82,10 @@ conv_status_t convsel_linear_describe(const convsel_linear_desc_t* desc, char* b
  * One pass over q and k.
  *
  * A token whose position lies outside [0, max_position) is written as NaN.
- * q_out may be q (same address and strides), k_out may be k. */
+ * q_out may be q (same address and strides), k_out may be k.  Beyond that no
+ * value of an output may lie where one of q, k, the weights, the tables, the
+ * positions or the other output does; slices of one projection, whose rows only
+ * interleave, are apart. */
 typedef struct convsel_qk_desc {
   int64_t tokens;
   int32_t q_heads, k_heads;  /* either may be 0 (its pointers are then ignored) */

@@ -50,6 +50,65 @@ bool rows_apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t inner) {
   return s1 >= inner && s0 >= (n1 - 1) * s1 + inner;
 }
 
+// n0 x n1 rows of `inner` bytes, strides in bytes.
+struct Rows {
+  const void* base;
+  int64_t n0, s0, n1, s1, inner;
+};
+Rows run_of(const void* p, int64_t bytes) { return {p, 1, 0, 1, 0, bytes}; }
+
+bool same_rows(const Rows& a, const Rows& b) {
+  return a.base == b.base && (a.n0 == 1 || a.s0 == b.s0) && (a.n1 == 1 || a.s1 == b.s1);
+}
+
+// Whether rows of a and b have a byte in common; rows that only interleave (slices of one projection) have none.  The
+// distance of two rows is the bases' plus a whole multiple, within bounds, of each stride; equal strides of a and b make
+// one such term.  All terms but the one of most multiples are gone through, that one is solved for.
+bool share_bytes(const Rows& a, const Rows& b) {
+  if (!a.base || !b.base) return false;
+  if (!overlaps(a.base, span(a.n0, a.s0, a.n1, a.s1, a.inner, 1), b.base, span(b.n0, b.s0, b.n1, b.s1, b.inner, 1)))
+    return false;
+  struct Term {
+    int64_t stride, lo, hi;
+  } t[4];
+  int n = 0;
+  auto add = [&](int64_t count, int64_t stride, int sign) {
+    if (count == 1 || stride == 0) return;
+    int i = 0;
+    while (i < n && t[i].stride != stride) ++i;
+    if (i == n) t[n++] = {stride, 0, 0};
+    (sign > 0 ? t[i].hi : t[i].lo) += sign * (count - 1);
+  };
+  add(a.n0, a.s0, 1);
+  add(a.n1, a.s1, 1);
+  add(b.n0, b.s0, -1);
+  add(b.n1, b.s1, -1);
+  const int64_t d0 = (int64_t)((uintptr_t)a.base - (uintptr_t)b.base);
+  // Rows meet where -a.inner < distance < b.inner.
+  if (n == 0) return d0 > -a.inner && d0 < b.inner;
+  int last = 0;
+  for (int i = 1; i < n; ++i)
+    if (t[i].hi - t[i].lo > t[last].hi - t[last].lo) last = i;
+  const Term most = t[last];
+  t[last] = t[--n];
+  double walks = 1;
+  for (int i = 0; i < n; ++i) walks *= (double)(t[i].hi - t[i].lo + 1);
+  if (walks > 1 << 20) return true;  // three strides of many rows each, within one another's span: taken to meet
+  int64_t k[3] = {};
+  for (int i = 0; i < n; ++i) k[i] = t[i].lo;
+  for (;;) {
+    int64_t d = d0 + most.lo * most.stride;
+    for (int i = 0; i < n; ++i) d += k[i] * t[i].stride;
+    // The first multiple that brings the distance above -a.inner.
+    const int64_t up = -a.inner + 1 - d, m = up <= 0 ? 0 : (up + most.stride - 1) / most.stride;
+    if (m <= most.hi - most.lo && d + m * most.stride < b.inner) return true;
+    int i = 0;
+    for (; i < n && k[i] == t[i].hi; ++i) k[i] = t[i].lo;
+    if (i == n) return false;
+    ++k[i];
+  }
+}
+
 // ---- linear ----
 
 conv_status_t linear_sizes(const convsel_linear_desc_t* d) {
@@ -213,11 +272,25 @@ conv_status_t convsel_qk_norm_rope(const void* q, const void* k, const void* q_w
     if (!a.in[i] || !a.out[i] || !aligned(a.in[i], es) || !aligned(a.out[i], es) || !aligned(a.weight[i], es))
       return CONV_ERR_INVALID_ARG;
     if (!rows_apart(t, a.out_token[i], a.heads[i], a.out_head[i], a.dim)) return CONV_ERR_INVALID_ARG;
-    const bool in_place = a.in[i] == a.out[i] && a.in_token[i] == a.out_token[i] && a.in_head[i] == a.out_head[i];
-    if (!in_place && overlaps(a.out[i], span(t, a.out_token[i], a.heads[i], a.out_head[i], a.dim, es), a.in[i],
-                              span(t, a.in_token[i], a.heads[i], a.in_head[i], a.dim, es)))
+  }
+  // What is written may be a head's own input, and nothing else that the call reads or writes.
+  Rows in[2], out[2];
+  for (int i = 0; i < 2; ++i) {
+    const bool there = a.heads[i] > 0;
+    in[i] = {there ? a.in[i] : nullptr, t, a.in_token[i] * es, a.heads[i], a.in_head[i] * es, a.dim * es};
+    out[i] = {there ? a.out[i] : nullptr, t, a.out_token[i] * es, a.heads[i], a.out_head[i] * es, a.dim * es};
+  }
+  const int64_t table = a.rotary > 0 ? a.max_position * (a.rotary / 2) * 4 : 0;
+  for (int i = 0; i < 2; ++i) {
+    if (!same_rows(out[i], in[i]) && share_bytes(out[i], in[i])) return CONV_ERR_INVALID_ARG;
+    if (share_bytes(out[i], in[1 - i])) return CONV_ERR_INVALID_ARG;
+    for (int j = 0; j < 2; ++j)
+      if (a.heads[j] > 0 && share_bytes(out[i], run_of(a.weight[j], a.dim * es))) return CONV_ERR_INVALID_ARG;
+    if (table > 0 && (share_bytes(out[i], run_of(cos, table)) || share_bytes(out[i], run_of(sin, table)) ||
+                      share_bytes(out[i], run_of(positions, t * 4))))
       return CONV_ERR_INVALID_ARG;
   }
+  if (share_bytes(out[0], out[1])) return CONV_ERR_INVALID_ARG;
   const conv_status_t st = convsel::device_ready();
   if (st != CONV_OK) return st;
   return from_hip(convsel::launch_qk_norm_rope(a, (hipStream_t)stream));

@@ -1,15 +1,17 @@
 """Host-side checks of the decoder operators at the ends of their ranges.  No GPU."""
 import ctypes
+import random
 import re
 import types
 
+import numpy as np
 import pytest
 import torch
 
 import paper_2410_08300_amd as cs
 from paper_2410_08300_amd import _lib
 
-from test_lm_host import INVALID, attention_desc, batch_desc, cache_desc
+from test_lm_host import A, B, C, D, E, F, G, INVALID, attention_desc, batch_desc, cache_desc, qk, qk_desc
 
 
 def attention_bytes(c, b, d):
@@ -82,3 +84,90 @@ def test_linear_of_very_many_rows_fits_a_launch(outputs, dtype):
         side = int(re.search(r" tile=(\d+)x", text).group(1))
         tiles = -(-m // side) * -(-outputs // side)
         assert "tiles" in text and (tiles + 7) // 8 * 8 * 256 < 2 ** 32, text
+
+
+# Slices of a fused projection of two tokens' rows, 8 query heads, 2 key heads and 2 value heads of 64 in bf16.
+ROW, Q, K, V = 12 * 64, A, A + 8 * 128, A + 10 * 128
+FUSED = dict(q_token_stride=ROW, k_token_stride=ROW, q_out_token_stride=ROW, k_out_token_stride=ROW)
+
+
+def test_rotation_refuses_outputs_over_what_else_the_call_reads_or_writes():
+    d = qk_desc(**FUSED)
+    far = dict(qo=F, ko=G)
+    cases = [
+        dict(qo=K), dict(ko=Q), dict(qo=F, ko=F), dict(qo=F, ko=F + 128), dict(qo=F, ko=F + 2 * ROW),  # over each other
+        dict(qo=K - 128, ko=G), dict(qo=V, ko=G), dict(ko=Q + 7 * 128),   # over a part of the other's heads or tokens
+        dict(qo=F, ko=F + 2 * ROW - 64),                                  # a tail over the next token's head
+        dict(qw=F + 64), dict(kw=G), dict(qo=C), dict(ko=D + 64 * 4 * 32), dict(qo=E), dict(pos=F + 8)]
+    for kw in cases:
+        got = dict(q=Q, k=K)
+        got.update(far)
+        got.update(kw)
+        assert qk(d, **got) == INVALID, kw
+    # Heads that interleave, q k v q k v: the other's place one head further on.
+    turns = dict(FUSED, q_heads=4, k_heads=4, q_head_stride=192, k_head_stride=192, q_out_head_stride=192,
+                 k_out_head_stride=192)
+    for kw in (dict(qo=A + 128, ko=G), dict(qo=A, ko=A + 64), dict(qo=A, ko=A + 384)):
+        assert qk(qk_desc(**turns), q=A, k=A + 128, **kw) == INVALID, kw
+    # One token: its strides are nobody's.
+    one = qk_desc(tokens=1, q_token_stride=5, q_out_token_stride=1000000, k_out_token_stride=3)
+    assert qk(one, q=A, k=B, qo=B + 128, ko=G) == INVALID
+
+
+@pytest.mark.skipif(torch.cuda.device_count() > 0, reason="checks the no-device path; a GPU is present")
+def test_rotation_takes_outputs_that_only_interleave_with_what_else_it_reads():
+    d = qk_desc(**FUSED)
+    ok = _lib.CONV_ERR_DEVICE  # every check of arguments passed
+    for kw in (dict(qo=Q, ko=K), dict(qo=F, ko=G), dict(qo=F, ko=F + 8 * 128), dict(qo=F, ko=F + 10 * 128),
+               dict(qo=Q, ko=V), dict(qo=F, ko=K)):
+        assert qk(d, q=Q, k=K, **kw) == ok, kw
+    turns = dict(FUSED, q_heads=4, k_heads=4, q_head_stride=192, k_head_stride=192, q_out_head_stride=192,
+                 k_out_head_stride=192)
+    for kw in (dict(qo=A, ko=A + 128), dict(qo=A + 256, ko=A + 128), dict(qo=F, ko=F + 256)):
+        assert qk(qk_desc(**turns), q=A, k=A + 128, **kw) == ok, kw
+    one = qk_desc(tokens=1, q_token_stride=5, q_out_token_stride=1000000, k_token_stride=0, k_out_token_stride=3)
+    assert qk(one, q=A, k=A + 8 * 128, qo=A, ko=A + 8 * 128) == ok  # in place, whatever the strides of one token
+    # Head-major: heads lie far apart, tokens one behind the other.
+    major = dict(q_token_stride=64, q_head_stride=256, k_token_stride=64, k_head_stride=256, q_out_token_stride=64,
+                 q_out_head_stride=256, k_out_token_stride=64, k_out_head_stride=256)
+    assert qk(qk_desc(**major), q=A, k=A + 8 * 512, qo=A, ko=A + 8 * 512) == ok
+    assert qk(qk_desc(k_heads=0, **FUSED), q=A, k=None, qo=A, ko=A) == ok  # no keys: their pointers are nobody's
+
+
+def rows_of(base, tokens, ts, heads, hs, width):
+    at = base + np.arange(tokens)[:, None, None] * ts + np.arange(heads)[None, :, None] * hs + np.arange(width)
+    return set(at.ravel().tolist())
+
+
+@pytest.mark.skipif(torch.cuda.device_count() > 0, reason="checks the no-device path; a GPU is present")
+def test_rotation_finds_shared_values_as_sets_of_addresses_do():
+    """Random small layouts: the call is refused where the output's elements and the other input's have one in common,
+    or are not apart themselves, and nowhere else."""
+    rng = random.Random(11)
+    seen = {True: 0, False: 0}
+    while min(seen.values()) < 400:
+        t, hq, hk, dim = rng.randint(1, 5), rng.randint(1, 4), rng.randint(1, 4), rng.choice((2, 4, 6))
+        pick = (dim, dim + 2, 2 * dim, 3 * dim, hq * dim, (hq + hk) * dim, (hq + 2 * hk) * dim, t * dim, 48, 7)
+        qo, k = (rng.choice(pick), rng.choice(pick)), (rng.choice(pick), rng.choice(pick))
+        if rng.random() < 0.5:
+            k = qo
+        shift = rng.randint(-60, 60)
+        out, other = rows_of(200, t, qo[0], hq, qo[1], dim), rows_of(200 + shift, t, k[0], hk, k[1], dim)
+        apart = len(out) == t * hq * dim
+        d = qk_desc(tokens=t, q_heads=hq, k_heads=hk, head_dim=dim, rotary_dim=0, q_token_stride=hq * dim,
+                    q_head_stride=dim, q_out_token_stride=qo[0], q_out_head_stride=qo[1], k_token_stride=k[0],
+                    k_head_stride=k[1], k_out_token_stride=hk * dim, k_out_head_stride=dim)
+        st = qk(d, q=B, k=A + 2 * (200 + shift), qo=A + 2 * 200, ko=G)
+        if not apart:
+            assert st == INVALID
+            continue
+        shared = bool(out & other)
+        # Rows that are apart as sets, but not as whole tokens or whole heads, are refused before.
+        if st == INVALID and not shared:
+            n0, s0, n1, s1 = t, qo[0], hq, qo[1]
+            nested = (n0 == 1 or n1 == 1 or (s0 >= (n1 - 1) * s1 + dim and s1 >= dim)
+                      or (s1 >= (n0 - 1) * s0 + dim and s0 >= dim))
+            assert not nested, (t, hq, hk, dim, qo, k, shift)
+            continue
+        assert st == (INVALID if shared else _lib.CONV_ERR_DEVICE), (t, hq, hk, dim, qo, k, shift)
+        seen[shared] += 1
