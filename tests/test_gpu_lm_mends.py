@@ -190,3 +190,31 @@ def test_linear_of_more_rows_than_a_launch_has_tiles_of_64():
     within(y[rows], want, bound + ref.half_ulp(torch.bfloat16) * want.abs() * 1.01, "many rows")
     y[rows] = 0
     assert not any(bool(part.any()) for part in y.split(2 ** 26))
+
+
+# ---- linear: activations far left of zero ---------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("activation", ["gelu", "gelu_tanh", "silu"])
+def test_activations_keep_their_precision_where_they_are_small(activation, dtype):
+    """Relative to the result, in units of 2^-24.  gelu in fp32: the fit 0.3, its sum of nine terms up to three times
+    their total 27, t's two roundings 8, the exponential, its correction and four products 8: 48.  silu: the exponential's
+    argument is exact (bf16 multiplies it by log2 e: its rounding and the constant's), a few operations: 16 + 3 |z|.
+    gelu_tanh: six roundings of the exponential's argument u and a few operations: 16 + 8 |u|.  In bf16 gelu's exponent
+    has the roundings of z^2 and of log2 e times half of it, and one more in the constant: 64 + 2 z^2."""
+    say("case activation tails", activation, dtype)
+    dt, low = DT[dtype], {"gelu": -12.5, "gelu_tanh": -9.0, "silu": -80.0}[activation]
+    z = torch.cat([torch.linspace(low, 0, 20001, device=DEV), torch.linspace(0, 12, 2001, device=DEV)]).to(dt)[:, None]
+    y = cs.linear(z, torch.ones(1, 1, device=DEV, dtype=dt), act=activation)
+    a = ref.f64(z).abs()
+    if activation == "gelu":
+        want = ref.act(ref.f64(z), "gelu")  # by erfc, which does not cancel
+        units = 48.0 if dtype == "f32" else 64 + 2 * a ** 2
+    elif activation == "gelu_tanh":
+        want = ref.f64(z) * torch.sigmoid(2 * (2 / torch.pi) ** 0.5 * (ref.f64(z) + 0.044715 * ref.f64(z) ** 3))
+        units = 16 + 8 * 1.6 * (a + 0.044715 * a ** 3)
+    else:
+        want = ref.f64(z) * torch.sigmoid(ref.f64(z))
+        units = 16 + 3 * a
+    before = units * 2.0 ** -24 * want.abs() + 1e-36
+    within(y, want, before + torch.from_numpy(half_step((want.abs() + before).numpy(), dt)), "%s %s" % (activation, dtype))
