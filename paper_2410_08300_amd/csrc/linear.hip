@@ -156,20 +156,39 @@ int outputs_vec(const LinearArgs& a) {
   return a.ldy % 4 == 0 && (uintptr_t)a.y % unit == 0 && (!a.r || (a.ldr % 4 == 0 && (uintptr_t)a.r % unit == 0));
 }
 
-// A workgroup of rows brings its weights in at some 22 GB/s; 16 rows of x take 0.4 as long again.  With few outputs
-// there are few workgroups, and the tiles, which cut the reduction into parts, are through sooner (7 rows, 14088 -> 541 in
-// fp32: 44 us by rows, 26 in tiles; 5 rows, 11648 -> 68 in bf16: 17 and 10; 16 rows, 11008 -> 4100: 38 and 27; but 1 row,
-// 4096 -> 1024: 7.5 and 8.5, 5000 -> 5120: 17 and 20).  Rows that would be copied for the tiles are read as they lie
-// where they are few, 1.3 times as slowly in fp32 and 2.5 times in bf16 (24 rows, 2611 -> 7680 in fp32: 61 us in tiles,
-// 51 by rows; 29, 2282 -> 1496: 24 and 12; but 50, 3897 -> 7064 in bf16: 47 and 131).
+// Few rows.  By rows: 3 us, and the longer of the weights' way from memory (5.3 TB/s; 4.8 in fp32) and the way of one
+// CU's share of them, whole workgroups (25 GB/s; 24 in fp32); 16 rows of x add 0.4 of that, and rows of an odd number of
+// bf16 take 2.2 times as long.  In tiles: by their plan, which counts no bytes, but at least 7.5 us, all bytes at a
+// copy's rate and the copies of rows of no whole 16 bytes.  So wide layers of a row go by rows, and few outputs, which
+// give few workgroups, in tiles, which cut the reduction into parts.  Of 368 sizes, random ones among them, the choice
+// was more than a tenth behind the other in 8.  us by rows and in tiles, weights from memory:
+//   bf16, from 4096   -> 1024      5120      11008     16384     32000   |  8192 -> 8192  11008 -> 4100  14088 -> 541
+//     1 row           7.4  8.9  13.5 17.6  20.9 24.1  27.8 38.1  50.7 59.1 |  28.0 37.2      27.6 25.2      18.6 12.4
+//     4 rows          8.1  9.1  14.9 17.6  22.5 23.5  29.6 37.9  55.0 61.7 |  28.3 36.2      29.9 25.5      20.9 12.8
+//     16 rows        10.1  9.4  18.7 14.8  27.8 24.2  39.0 37.7  71.8 59.4 |  37.4 36.7      38.1 26.3      32.2 13.3
+//   fp32, 1 row      14.3 12.6  27.3 32.6  42.7 61.4  58.3 83.0   107  152 |  63.1 83.4      65.6 62.0      44.2 24.9
+//     16 rows        19.2 13.4  37.5 34.3  57.3 63.8  79.5 85.2   150  157 |  76.7 85.9      85.4 65.1      67.2 25.5
+// More rows.  Those that would be copied for the tiles are read as they lie where they are few, 1.3 times as slowly in
+// fp32 and 2.5 times in bf16 (24 rows, 2611 -> 7680 in fp32: 61 us in tiles, 51 by rows; 29, 2282 -> 1496: 24 and 12; but
+// 50, 3897 -> 7064 in bf16: 47 and 131).
 bool in_rows(const LinearArgs& a, LinearTiles* t) {
   *t = linear_tiles_plan(a);
   if (t->config < 0) return true;
-  const double bytes = 16. * a.in * (a.dtype == CONV_F32 ? 4 : 2);
-  const double groups = (double)((a.out + 15) / 16) * ((a.m + 15) / 16);
-  const double us = bytes / 22e3 * (groups > 256 ? groups / 256 : 1.) * (1 + 0.4 * (a.m < 16 ? a.m : 16) / 16);
-  if (a.m <= kFewRows) return us <= 3 + 1.15 * t->us;
-  return a.m <= 4 * kFewRows && t->pack && us * (a.dtype == CONV_F32 ? 1.3 : 2.5) <= t->us;
+  const bool f32 = a.dtype == CONV_F32;
+  const double es = f32 ? 4 : 2, strip = 16. * a.in * es;  // bytes of a workgroup's weights
+  const int64_t groups = ((a.out + 15) / 16) * ((a.m + 15) / 16);
+  if (a.m <= kFewRows) {
+    const bool odd = !f32 && (a.in % 2 != 0 || a.ldx % 2 != 0);
+    const double memory = (double)a.out * a.in * es / (f32 ? 4.8e6 : 5.3e6);
+    const double cu = (double)((groups + 255) / 256) * strip / (f32 ? 24e3 : 25e3);
+    const double rows = 3 + (memory > cu ? memory : cu) * (1 + 0.4 * a.m / 16) * (odd ? 2.2 : 1.);
+    const double copy = t->pack ? 2.5 + (double)(a.m + a.out) * a.in * es * 2 / 4e6 : 0.;
+    const double least = 7.5 + ((double)a.out * a.in + (double)a.m * (a.in + a.out)) * es / 5.05e6 + copy;
+    const double tiles = 1.05 * t->us;
+    return rows <= (tiles > least ? tiles : least);
+  }
+  const double us = strip / 22e3 * (groups > 256 ? groups / 256. : 1.) * 1.4;
+  return a.m <= 4 * kFewRows && t->pack && us * (f32 ? 1.3 : 2.5) <= t->us;
 }
 
 }  // namespace

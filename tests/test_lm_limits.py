@@ -171,3 +171,19 @@ def test_rotation_finds_shared_values_as_sets_of_addresses_do():
             continue
         assert st == (INVALID if shared else _lib.CONV_ERR_DEVICE), (t, hq, hk, dim, qo, k, shift)
         seen[shared] += 1
+
+
+# us by rows and in tiles, as measured with weights from memory.
+FEW_ROWS = [("bf16", 1, 4096, 16384, 27.8, 38.1), ("bf16", 1, 4096, 32000, 50.7, 59.1), ("bf16", 1, 8192, 8192, 28.0, 37.2),
+            ("bf16", 1, 16384, 4096, 32.3, 36.7), ("bf16", 4, 4096, 14336, 28.0, 31.6), ("bf16", 4, 4096, 16384, 29.6, 37.9),
+            ("bf16", 4, 8192, 8192, 28.3, 36.2), ("bf16", 4, 11008, 4100, 29.9, 25.5), ("bf16", 16, 4096, 5120, 18.7, 14.8),
+            ("bf16", 16, 5000, 5120, 24.5, 19.7), ("f32", 16, 5000, 5120, 52.7, 42.4), ("f32", 16, 11008, 4100, 85.4, 65.1),
+            ("bf16", 1, 4096, 4096, 9.0, 12.8), ("bf16", 1, 14088, 541, 18.6, 12.4), ("bf16", 16, 4096, 32000, 71.8, 59.4),
+            ("f32", 1, 4096, 32000, 107.5, 152.1), ("f32", 4, 14088, 541, 47.9, 25.3)]
+
+
+@pytest.mark.parametrize("case", FEW_ROWS, ids=lambda c: "%s-%dx%dx%d" % c[:4])
+def test_linear_of_few_rows_goes_the_faster_way(case):
+    dtype, m, i, o, rows, tiles = case
+    text = cs.describe_linear(m, i, o, {"bf16": torch.bfloat16, "f32": torch.float32}[dtype])
+    assert ("linear_rows_kernel" in text) == (rows < tiles), text
