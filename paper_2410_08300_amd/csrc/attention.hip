@@ -69,15 +69,17 @@ __global__ __launch_bounds__(256) void attention_rows_kernel(
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, g = lane >> 4;
-  const int seq = blockIdx.z, head = blockIdx.y;
-  const Span sp = span_of(offsets, seq, a.tokens);
+  const int head = blockIdx.y, split = blockIdx.x;
+  const Unit un = find_unit<true>(a.units, offsets, lengths);
+  const Span sp = un.span;
   const int rows = sp.count * a.group;
-  const int split = blockIdx.x % a.nsplit;
-  const int64_t len = lengths[seq];
+  const int64_t len = un.length;
   const int limit = static_cast<int>(max((int64_t)0, min(len, a.table_width << a.ps_shift)));
-  const int32_t* my_table = table + seq * a.table_width;
+  const int32_t* my_table = table + un.seq * a.table_width;
 
-  for (int tile = blockIdx.x / a.nsplit; tile * 16 < rows; tile += a.tiles) {
+  const int ntile = (rows + 15) >> 4;
+
+  for (int tile = un.index; tile < ntile; tile += un.count) {
     // This lane's query row, and what the tile's rows see between them.
     const int row = min(tile * 16 + col, rows - 1);
     const int tok = row / a.group;
@@ -434,11 +436,12 @@ __global__ __launch_bounds__(256) void attention_join_few_kernel(const float* __
 
 // How a call is cut: rows, in 16s, 128s or 256s, and parts of the keys.  The host
 // knows how many tokens the call has and how many a sequence may hold, not how
-// they are spread; every count only sets the grid, and kernels walk what there
-// is.
+// they are spread: kernel and parts go by the average, tiles of rows by what each
+// sequence has.
 struct Plan {
   int rows;  // of a workgroup: 16, 128 or 256
-  int tiles, nsplit;
+  int tiles;  // of a sequence of the average length
+  int nsplit;
 };
 
 Plan plan(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convsel_attention_desc_t& d) {
@@ -494,6 +497,10 @@ Plan plan(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convse
   return p;
 }
 
+UnitRow tiles_of(const convsel_kv_batch_t& b, int64_t group, int rows) {
+  return unit_row(b, group, __builtin_ctz(rows));
+}
+
 size_t part_floats(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convsel_attention_desc_t& d,
                    const Plan& p) {
   const size_t n = (size_t)b.tokens * d.q_heads * p.nsplit * ((c.head_dim + 3) / 4 * 4);
@@ -539,7 +546,7 @@ hipError_t launch_attention(const void* q, const convsel_kv_cache_t& c, const co
   a.y_token = d.y_token_stride; a.y_head = d.y_head_stride;
   a.tokens = (int)b.tokens; a.kv_heads = c.kv_heads; a.group = d.q_heads / c.kv_heads; a.dim = c.head_dim;
   a.ps_shift = c.page_size == 16 ? 4 : c.page_size == 32 ? 5 : c.page_size == 64 ? 6 : 7;
-  a.causal = d.causal; a.window = d.window; a.nsplit = p.nsplit; a.tiles = p.tiles;
+  a.causal = d.causal; a.window = d.window; a.nsplit = p.nsplit;
   a.scale = d.scale * 1.4426950408889634f;
   // Queries are read and results written in 16-byte (results: four-value) units where every row starts on one and
   // has no padding.
@@ -553,24 +560,23 @@ hipError_t launch_attention(const void* q, const convsel_kv_cache_t& c, const co
   ptr.y = y;
   ptr.part = (float*)workspace;
   ptr.stat = p.nsplit > 1 ? ptr.part + part_floats(c, b, d, p) : nullptr;
-  for (int64_t s0 = 0; s0 < b.seqs; s0 += 65535) {
-    const int64_t seqs = b.seqs - s0 < 65535 ? b.seqs - s0 : 65535;
-    ptr.table = b.table + s0 * b.table_width;
-    ptr.lengths = b.lengths + s0;
-    ptr.offsets = b.offsets + s0;
-    if (p.rows > 16) {
-      const hipError_t e = launch_attention_tiles(ptr, a, d.dtype, c.format, p.rows, seqs, stream);
-      if (e != hipSuccess) return e;
-      continue;
-    }
-    const dim3 grid((unsigned)p.tiles * p.nsplit, c.kv_heads, (unsigned)seqs);
-    if (d.dtype == CONV_F32) {
-      if (c.format == CONVSEL_KV_INT8) launch_rows_nc<float, CONVSEL_KV_INT8>(grid, ptr, a, stream);
-      else launch_rows_nc<float, CONVSEL_KV_FP8>(grid, ptr, a, stream);
-    } else {
-      if (c.format == CONVSEL_KV_INT8) launch_rows_nc<bf16_t, CONVSEL_KV_INT8>(grid, ptr, a, stream);
-      else launch_rows_nc<bf16_t, CONVSEL_KV_FP8>(grid, ptr, a, stream);
-    }
+  ptr.table = b.table; ptr.lengths = b.lengths; ptr.offsets = b.offsets;
+  a.units = tiles_of(b, a.group, p.rows);
+  if (p.rows > 16) {
+    const hipError_t e = launch_attention_tiles(ptr, a, d.dtype, c.format, p.rows, stream);
+    if (e != hipSuccess) return e;
+  } else {
+    each_grid(a.units, [&](const UnitRow& r, unsigned n) {
+      a.units = r;
+      const dim3 grid(p.nsplit, c.kv_heads, n);
+      if (d.dtype == CONV_F32) {
+        if (c.format == CONVSEL_KV_INT8) launch_rows_nc<float, CONVSEL_KV_INT8>(grid, ptr, a, stream);
+        else launch_rows_nc<float, CONVSEL_KV_FP8>(grid, ptr, a, stream);
+      } else {
+        if (c.format == CONVSEL_KV_INT8) launch_rows_nc<bf16_t, CONVSEL_KV_INT8>(grid, ptr, a, stream);
+        else launch_rows_nc<bf16_t, CONVSEL_KV_FP8>(grid, ptr, a, stream);
+      }
+    });
   }
   if (p.nsplit > 1) {
     const int64_t rows = b.tokens * d.q_heads, in_wg = p.nsplit <= kFewParts ? 256 / ((c.head_dim + 3) / 4) : 1;
@@ -598,10 +604,10 @@ hipError_t launch_attention(const void* q, const convsel_kv_cache_t& c, const co
 void attention_describe(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convsel_attention_desc_t& d,
                         char* buf, size_t len) {
   const Plan p = plan(c, b, d);
-  snprintf(buf, len, "attention kernels=attention_%s_kernel%s rows=%d tiles=%d split=%d workspace=%zu",
+  snprintf(buf, len, "attention kernels=attention_%s_kernel%s rows=%d tiles=%u split=%d workspace=%zu",
            p.rows > 16 ? "tiles" : "rows",
            p.nsplit <= 1 ? "" : p.nsplit <= kFewParts ? ";attention_join_few_kernel" : ";attention_join_kernel", p.rows,
-           p.tiles, p.nsplit, attention_workspace(c, b, d));
+           units_of(tiles_of(b, d.q_heads / c.kv_heads, p.rows)), p.nsplit, attention_workspace(c, b, d));
 }
 
 }  // namespace convsel

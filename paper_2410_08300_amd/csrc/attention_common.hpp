@@ -32,8 +32,9 @@ namespace lm {
 struct AttnArgs {
   int64_t pages, table_width;
   int64_t q_token, q_head, y_token, y_head;
-  int tokens, kv_heads, group, dim, ps_shift, causal, window, nsplit, tiles, q_vec, y_vec;
+  int tokens, kv_heads, group, dim, ps_shift, causal, window, nsplit, q_vec, y_vec;
   float scale;  // times log2 e
+  UnitRow units;  // tiles of rows, of all sequences in one row
 };
 
 struct AttnPointers {
@@ -109,6 +110,6 @@ __device__ __forceinline__ int query_exponent(float amax) {
 // attention_tiles_wide() has them.
 bool attention_tiles_wide(int dtype, int head_dim);
 hipError_t launch_attention_tiles(const lm::AttnPointers& p, const lm::AttnArgs& a, int dtype, int format, int rows,
-                                  int64_t seqs, hipStream_t stream);
+                                  hipStream_t stream);
 
 }  // namespace convsel

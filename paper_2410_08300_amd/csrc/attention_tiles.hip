@@ -93,16 +93,16 @@ __global__ __launch_bounds__(64 * W, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void a
   const int col = lane & 31, half = lane >> 5;
   // Heads vary fastest: with eight of them, one head's keys stay in one XCD's L2.
   const int head = blockIdx.x % a.kv_heads, split = blockIdx.x / a.kv_heads;
-  const int seq = blockIdx.z;
-  const Span sp = span_of(offsets, seq, a.tokens);
+  const Unit un = find_unit<true>(a.units, offsets, lengths);
+  const Span sp = un.span;
   const int rows = sp.count * a.group;
-  const int64_t len = lengths[seq];
+  const int64_t len = un.length;
   const int limit = static_cast<int>(max((int64_t)0, min(len, a.table_width << a.ps_shift)));
   const int64_t first = len - sp.count;  // position of the sequence's first query
-  const int32_t* my_table = table + seq * a.table_width;
+  const int32_t* my_table = table + un.seq * a.table_width;
   const int ntile = (rows + ROWS - 1) / ROWS;
 
-  for (int nt = blockIdx.y; nt < ntile; nt += a.tiles) {
+  for (int nt = un.index; nt < ntile; nt += un.count) {
     const int tile = ntile - 1 - nt;  // under a causal mask the last rows have the most keys: they start first
     const int r0 = tile * ROWS;
     // Keys that tokens t0..t1 see between them, and that every one of them sees.
@@ -428,32 +428,35 @@ template <typename T, int NC>
 constexpr bool kWide = sizeof(T) == 2 && NC <= 4;
 
 template <typename T, int FMT, int NC, int W>
-hipError_t launch_waves(const AttnPointers& p, const AttnArgs& a, int64_t seqs, hipStream_t st) {
-  const dim3 grid((unsigned)(a.kv_heads * a.nsplit), (unsigned)a.tiles, (unsigned)seqs);
-  hipLaunchKernelGGL((attention_tiles_kernel<T, FMT, NC, W>), grid, dim3(64 * W), 0, st, (const T*)p.q, p.k_codes,
-                     p.v_codes, p.k_scales, p.v_scales, p.table, p.lengths, p.offsets, (T*)p.y, p.part, p.stat, a);
+hipError_t launch_waves(const AttnPointers& p, AttnArgs a, hipStream_t st) {
+  each_grid(a.units, [&](const UnitRow& r, unsigned n) {
+    a.units = r;
+    const dim3 grid((unsigned)(a.kv_heads * a.nsplit), 1, n);
+    hipLaunchKernelGGL((attention_tiles_kernel<T, FMT, NC, W>), grid, dim3(64 * W), 0, st, (const T*)p.q, p.k_codes,
+                       p.v_codes, p.k_scales, p.v_scales, p.table, p.lengths, p.offsets, (T*)p.y, p.part, p.stat, a);
+  });
   return hipGetLastError();
 }
 
 template <typename T, int FMT, int NC>
-hipError_t launch(const AttnPointers& p, const AttnArgs& a, int rows, int64_t seqs, hipStream_t st) {
+hipError_t launch(const AttnPointers& p, const AttnArgs& a, int rows, hipStream_t st) {
   if constexpr (kWide<T, NC>) {
-    if (rows == 256) return launch_waves<T, FMT, NC, 8>(p, a, seqs, st);
+    if (rows == 256) return launch_waves<T, FMT, NC, 8>(p, a, st);
   }
-  return launch_waves<T, FMT, NC, 4>(p, a, seqs, st);
+  return launch_waves<T, FMT, NC, 4>(p, a, st);
 }
 
 template <typename T, int FMT>
-hipError_t launch_nc(const AttnPointers& p, const AttnArgs& a, int rows, int64_t seqs, hipStream_t st) {
+hipError_t launch_nc(const AttnPointers& p, const AttnArgs& a, int rows, hipStream_t st) {
   switch ((a.dim + 31) / 32) {
-    case 1: return launch<T, FMT, 1>(p, a, rows, seqs, st);
-    case 2: return launch<T, FMT, 2>(p, a, rows, seqs, st);
-    case 3: return launch<T, FMT, 3>(p, a, rows, seqs, st);
-    case 4: return launch<T, FMT, 4>(p, a, rows, seqs, st);
-    case 5: return launch<T, FMT, 5>(p, a, rows, seqs, st);
-    case 6: return launch<T, FMT, 6>(p, a, rows, seqs, st);
-    case 7: return launch<T, FMT, 7>(p, a, rows, seqs, st);
-    default: return launch<T, FMT, 8>(p, a, rows, seqs, st);
+    case 1: return launch<T, FMT, 1>(p, a, rows, st);
+    case 2: return launch<T, FMT, 2>(p, a, rows, st);
+    case 3: return launch<T, FMT, 3>(p, a, rows, st);
+    case 4: return launch<T, FMT, 4>(p, a, rows, st);
+    case 5: return launch<T, FMT, 5>(p, a, rows, st);
+    case 6: return launch<T, FMT, 6>(p, a, rows, st);
+    case 7: return launch<T, FMT, 7>(p, a, rows, st);
+    default: return launch<T, FMT, 8>(p, a, rows, st);
   }
 }
 
@@ -462,12 +465,12 @@ hipError_t launch_nc(const AttnPointers& p, const AttnArgs& a, int rows, int64_t
 bool attention_tiles_wide(int dtype, int head_dim) { return dtype == CONV_BF16 && head_dim <= 128; }
 
 hipError_t launch_attention_tiles(const AttnPointers& p, const AttnArgs& a, int dtype, int format, int rows,
-                                  int64_t seqs, hipStream_t st) {
+                                  hipStream_t st) {
   if (dtype == CONV_F32)
-    return format == CONVSEL_KV_INT8 ? launch_nc<float, CONVSEL_KV_INT8>(p, a, rows, seqs, st)
-                                     : launch_nc<float, CONVSEL_KV_FP8>(p, a, rows, seqs, st);
-  return format == CONVSEL_KV_INT8 ? launch_nc<bf16_t, CONVSEL_KV_INT8>(p, a, rows, seqs, st)
-                                   : launch_nc<bf16_t, CONVSEL_KV_FP8>(p, a, rows, seqs, st);
+    return format == CONVSEL_KV_INT8 ? launch_nc<float, CONVSEL_KV_INT8>(p, a, rows, st)
+                                     : launch_nc<float, CONVSEL_KV_FP8>(p, a, rows, st);
+  return format == CONVSEL_KV_INT8 ? launch_nc<bf16_t, CONVSEL_KV_INT8>(p, a, rows, st)
+                                   : launch_nc<bf16_t, CONVSEL_KV_FP8>(p, a, rows, st);
 }
 
 }  // namespace convsel

@@ -46,28 +46,29 @@ __device__ __forceinline__ uint32_t four_codes(float x0, float x1, float x2, flo
   }
 }
 
-template <typename T, int FMT, int NT>
+template <typename T, int FMT, int NT, bool ROW>
 __global__ __launch_bounds__(NT) void kv_write_kernel(convsel_kv_cache_t c, convsel_kv_batch_t b, KvTokens in,
-                                                       int vec) {
+                                                       UnitRow row, int vec) {
   constexpr int UE = elem<T>::per16;
   extern __shared__ __align__(16) uint8_t turn[];  // a page's value codes
   __shared__ float red[NT / 64];
-  const int seq = blockIdx.z;
   const bool values = blockIdx.y >= static_cast<unsigned>(c.kv_heads);
   const int head = values ? blockIdx.y - c.kv_heads : blockIdx.y;
-  const Span sp = span_of(b.offsets, seq, static_cast<int>(b.tokens));
   const int ps = c.page_size, D = c.head_dim, dp = kv_row_bytes(D);
-  const int64_t start = b.lengths[seq] < 0 ? 0 : b.lengths[seq];
-  const int64_t end = min(start + sp.count, b.table_width * ps);
-  if (start >= end) return;
   const int64_t token = values ? in.v_token : in.k_token;
+  const Unit un = find_unit<ROW>(row, b.offsets, b.lengths);
+  const int64_t from = un.length < 0 ? 0 : un.length, to = min(from + un.span.count, b.table_width * ps);
+  if (from >= to || from / ps + un.index >= (to + ps - 1) / ps) return;
+  const int start = static_cast<int>(from), end = static_cast<int>(to);  // within a table: below 2^30
+  const int32_t* table = b.table + un.seq * b.table_width;
   const T* src0 = reinterpret_cast<const T*>(values ? in.v : in.k) +
-                  head * (values ? in.v_head : in.k_head) + sp.first * token;
-  for (int64_t pg = start / ps + blockIdx.x; pg * ps < end; pg += gridDim.x) {
-    const int64_t page = b.table[seq * b.table_width + pg];
+                  head * (values ? in.v_head : in.k_head) + un.span.first * token;
+  // Tokens that start within a page may reach one more than their sequence has units: somebody walks two.
+  const int pages = (end + ps - 1) / ps;
+  for (int pg = start / ps + un.index; pg < pages; pg += un.count) {
+    const int64_t page = table[pg];
     if (page < 0 || page >= c.pages) continue;
-    const int r0 = static_cast<int>(max(start - pg * ps, (int64_t)0));
-    const int r1 = static_cast<int>(min(end - pg * ps, (int64_t)ps));
+    const int r0 = max(start - pg * ps, 0), r1 = min(end - pg * ps, ps);
     const T* src = src0 + (pg * ps - start) * token;  // row r of the page is src + r * token
     const int64_t ph = page * c.kv_heads + head;
     float* scale_at = (values ? c.v_scales : c.k_scales) + ph;
@@ -164,22 +165,25 @@ __global__ __launch_bounds__(NT) void kv_write_kernel(convsel_kv_cache_t c, conv
 // neighbours in the cache: four columns of a key, four tokens of a value, whose
 // codes reach their rows through LDS.  What bounds it: traffic, 4.8 to 5.6 TB/s
 // for prompts in bf16.
-template <typename T>
-__global__ __launch_bounds__(256) void kv_read_kernel(convsel_kv_cache_t c, convsel_kv_batch_t b, T* k, T* v,
-                                                      int vec) {
+template <typename T, bool ROW>
+__global__ __launch_bounds__(256) void kv_read_kernel(convsel_kv_cache_t c, convsel_kv_batch_t b, KvTokens to,
+                                                      UnitRow units, int vec) {
+  T* k = reinterpret_cast<T*>(const_cast<void*>(to.k));
+  T* v = reinterpret_cast<T*>(const_cast<void*>(to.v));
   constexpr int UE = elem<T>::per16;
-  const int seq = blockIdx.z, head = blockIdx.y;
-  const Span sp = span_of(b.offsets, seq, static_cast<int>(b.tokens));
+  const int head = blockIdx.y;
   const int ps = c.page_size, D = c.head_dim, dp = kv_row_bytes(D);
-  const int64_t start = b.lengths[seq], end = start + sp.count;  // 64-bit: bounded below
   const int64_t row = static_cast<int64_t>(c.kv_heads) * D;
   __shared__ __align__(16) uint8_t turn[16 * 256];
+  const Unit un = find_unit<ROW>(units, b.offsets, b.lengths);
+  const Span sp = un.span;
+  const int64_t start = un.length, end = start + sp.count;  // 64-bit: bounded below
   // Floor division: a negative start names positions before the sequence.
   const int64_t first = start >= 0 ? start / 16 : -((-start + 15) / 16);
-  for (int64_t blk = first + blockIdx.x; blk * 16 < end; blk += gridDim.x) {
+  for (int64_t blk = first + un.index; blk * 16 < end; blk += un.count) {
     const int64_t p0 = blk * 16;
     int64_t page = -1;
-    if (p0 >= 0 && p0 / ps < b.table_width) page = b.table[seq * b.table_width + p0 / ps];
+    if (p0 >= 0 && p0 / ps < b.table_width) page = b.table[un.seq * b.table_width + p0 / ps];
     const bool there = page >= 0 && page < c.pages;
     const int t0 = static_cast<int>(there ? p0 % ps : 0);
     const int64_t ph = there ? page * c.kv_heads + head : 0;
@@ -232,68 +236,82 @@ __global__ __launch_bounds__(256) void kv_read_kernel(convsel_kv_cache_t c, conv
   }
 }
 
-typedef void (*WriteKernel)(convsel_kv_cache_t, convsel_kv_batch_t, KvTokens, int);
+// Units of 2^shift tokens.  By sequence, with the units that one of the average number of tokens reaches from anywhere,
+// for single tokens, and where the longest sequence that there can be walks eight of them at most or fills the card by
+// itself (64 sequences of one token: 6.4 and 5.1 us to write and read, 7.5 and 6.4 in a row; 16 prompts of 2048 in pages
+// of 16: 53 and 41, 58 and 44 in a row).  In a row otherwise: a prompt of 4096 beside 127 single tokens takes 24 and 20 us,
+// by sequence 97 and 155.  A workgroup more for nothing costs: one for each of 64 sequences, keys and values of 8 heads,
+// 3 us.
+struct Deal {
+  UnitRow row;
+  unsigned across;
+};
+Deal deal(const convsel_kv_batch_t& b, int shift, int heads) {
+  const int64_t unit = (int64_t)1 << shift, avg = (b.tokens + b.seqs - 1) / b.seqs;
+  int64_t across = (avg + 2 * unit - 2) >> shift;
+  if (across > 65536) across = 65536;
+  if (b.tokens <= b.seqs || (b.tokens >> shift) + 1 <= 8 * across || across * heads >= 1024)
+    return {unit_row(b, 0, shift), (unsigned)across};
+  return {unit_row(b, 1, shift), 1};
+}
 
-template <typename T, int NT>
+typedef void (*WriteKernel)(convsel_kv_cache_t, convsel_kv_batch_t, KvTokens, UnitRow, int);
+
+template <typename T, int NT, bool ROW>
 WriteKernel write_kernel(int format) {
-  return format == CONVSEL_KV_INT8 ? kv_write_kernel<T, CONVSEL_KV_INT8, NT> : kv_write_kernel<T, CONVSEL_KV_FP8, NT>;
+  return format == CONVSEL_KV_INT8 ? kv_write_kernel<T, CONVSEL_KV_INT8, NT, ROW>
+                                   : kv_write_kernel<T, CONVSEL_KV_FP8, NT, ROW>;
+}
+
+template <typename T, bool ROW>
+WriteKernel write_kernel(int format, int threads) {
+  return threads == 64    ? write_kernel<T, 64, ROW>(format)
+         : threads == 128 ? write_kernel<T, 128, ROW>(format)
+                          : write_kernel<T, 256, ROW>(format);
 }
 
 template <typename T>
-WriteKernel write_kernel(int format, int threads) {
-  return threads == 64 ? write_kernel<T, 64>(format) : threads == 128 ? write_kernel<T, 128>(format)
-                                                                       : write_kernel<T, 256>(format);
+WriteKernel write_kernel(int format, int threads, bool row) {
+  return row ? write_kernel<T, true>(format, threads) : write_kernel<T, false>(format, threads);
 }
+
+typedef void (*ReadKernel)(convsel_kv_cache_t, convsel_kv_batch_t, KvTokens, UnitRow, int);
 
 }  // namespace
 
 hipError_t launch_kv_write(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const KvTokens& t,
                            hipStream_t stream) {
-  // Sequences past the grid's 65535 go in further launches.
-  for (int64_t s0 = 0; s0 < b.seqs; s0 += 65535) {
-    convsel_kv_batch_t p = b;
-    p.seqs = b.seqs - s0 < 65535 ? b.seqs - s0 : 65535;
-    p.table += s0 * b.table_width;
-    p.lengths += s0;
-    p.offsets += s0;
-    // The pages that a sequence of the average number of tokens reaches from anywhere; longer ones walk on.  One
-    // workgroup more for nothing cost a single token of each of 64 sequences 3 of 10 us.
-    const int64_t pages = ((b.tokens + b.seqs - 1) / b.seqs + 2 * c.page_size - 2) / c.page_size;
-    const dim3 grid((unsigned)(pages < 65536 ? pages : 65536), 2 * c.kv_heads, (unsigned)p.seqs);
-    // Rows of whole 16-byte units that start on one.
-    const int64_t ue = t.dtype == CONV_F32 ? 4 : 8;
-    const int vec = c.head_dim % ue == 0 && t.k_token % ue == 0 && t.k_head % ue == 0 && t.v_token % ue == 0 &&
-                    t.v_head % ue == 0 && (uintptr_t)t.k % 16 == 0 && (uintptr_t)t.v % 16 == 0;
-    const size_t lds = (size_t)c.page_size * kv_row_bytes(c.head_dim);  // at most 32 KiB
-    // Small pages in few threads: a workgroup's start costs as much as a page of 16 tokens.  (16 prompts of 2048 tokens
-    // of 8 heads of 128 in bf16: pages of 16 tokens, 53, 78 and 117 us in 64, 128 and 256 threads; of 32, 47, 54, 81; of
-    // 128, 65, 54, 48; of 16 in fp32, 97, 83, 116; six prompts of unlike lengths in pages of 64, 37 in 128, 34 in 256.)
-    const int64_t size = c.page_size * c.head_dim * (t.dtype == CONV_F32 ? 3 : 1);
-    const int threads = size <= 4096 ? 64 : size <= 6144 ? 128 : 256;
-    const auto f =
-        t.dtype == CONV_F32 ? write_kernel<float>(c.format, threads) : write_kernel<bf16_t>(c.format, threads);
-    hipLaunchKernelGGL(f, grid, dim3(threads), lds, stream, c, p, t, vec);
-  }
+  // Rows of whole 16-byte units that start on one.
+  const int64_t ue = t.dtype == CONV_F32 ? 4 : 8;
+  const int vec = c.head_dim % ue == 0 && t.k_token % ue == 0 && t.k_head % ue == 0 && t.v_token % ue == 0 &&
+                  t.v_head % ue == 0 && (uintptr_t)t.k % 16 == 0 && (uintptr_t)t.v % 16 == 0;
+  const size_t lds = (size_t)c.page_size * kv_row_bytes(c.head_dim);  // at most 32 KiB
+  // Small pages in few threads: a workgroup's start costs as much as a page of 16 tokens.  (16 prompts of 2048 tokens
+  // of 8 heads of 128 in bf16: pages of 16 tokens, 53, 78 and 117 us in 64, 128 and 256 threads; of 32, 47, 54, 81; of
+  // 128, 65, 54, 48; of 16 in fp32, 97, 83, 116; six prompts of unlike lengths in pages of 64, 37 in 128, 34 in 256.)
+  const int64_t size = c.page_size * c.head_dim * (t.dtype == CONV_F32 ? 3 : 1);
+  const int threads = size <= 4096 ? 64 : size <= 6144 ? 128 : 256;
+  const Deal g = deal(b, __builtin_ctz(c.page_size), 2 * c.kv_heads);
+  const bool row = g.row.num > 0;
+  const WriteKernel f =
+      t.dtype == CONV_F32 ? write_kernel<float>(c.format, threads, row) : write_kernel<bf16_t>(c.format, threads, row);
+  each_grid(g.row, [&](const UnitRow& r, unsigned n) {
+    hipLaunchKernelGGL(f, dim3(g.across, 2 * c.kv_heads, n), dim3(threads), lds, stream, c, b, t, r, vec);
+  });
   return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const KvTokens& t,
                           hipStream_t stream) {
-  for (int64_t s0 = 0; s0 < b.seqs; s0 += 65535) {
-    convsel_kv_batch_t p = b;
-    p.seqs = b.seqs - s0 < 65535 ? b.seqs - s0 : 65535;
-    p.table += s0 * b.table_width;
-    p.lengths += s0;
-    p.offsets += s0;
-    const int64_t blocks = ((b.tokens + b.seqs - 1) / b.seqs + 30) / 16;
-    const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536), c.kv_heads, (unsigned)p.seqs);
-    const int64_t ue = t.dtype == CONV_F32 ? 4 : 8;
-    const int vec = c.head_dim % ue == 0 && (uintptr_t)t.k % 16 == 0 && (uintptr_t)t.v % 16 == 0;
-    if (t.dtype == CONV_F32)
-      hipLaunchKernelGGL(kv_read_kernel<float>, grid, dim3(256), 0, stream, c, p, (float*)t.k, (float*)t.v, vec);
-    else
-      hipLaunchKernelGGL(kv_read_kernel<bf16_t>, grid, dim3(256), 0, stream, c, p, (bf16_t*)t.k, (bf16_t*)t.v, vec);
-  }
+  const int64_t ue = t.dtype == CONV_F32 ? 4 : 8;
+  const int vec = c.head_dim % ue == 0 && (uintptr_t)t.k % 16 == 0 && (uintptr_t)t.v % 16 == 0;
+  const Deal g = deal(b, 4, c.kv_heads);
+  const bool row = g.row.num > 0;
+  const ReadKernel f = t.dtype == CONV_F32 ? (row ? kv_read_kernel<float, true> : kv_read_kernel<float, false>)
+                                           : (row ? kv_read_kernel<bf16_t, true> : kv_read_kernel<bf16_t, false>);
+  each_grid(g.row, [&](const UnitRow& r, unsigned n) {
+    hipLaunchKernelGGL(f, dim3(g.across, c.kv_heads, n), dim3(256), 0, stream, c, b, t, r, vec);
+  });
   return hipGetLastError();
 }
 

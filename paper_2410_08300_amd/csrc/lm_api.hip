@@ -179,7 +179,7 @@ conv_status_t attention_sizes(const convsel_kv_cache_t* c, const convsel_kv_batc
   if (st == CONV_OK) st = batch_sizes(c, b);
   if (st != CONV_OK) return st;
   if (!d || d->q_heads < 1 || d->q_heads > 65535 || d->q_heads % c->kv_heads != 0) return CONV_ERR_INVALID_ARG;
-  // Rows are counted in 32 bits, and a workgroup of 16 rows steps up to 2^19 of them past the last one.
+  // Rows are counted in 32 bits, and rounded up to tiles of them.
   if (b->tokens > kAttentionRowsMax / d->q_heads) return CONV_ERR_INVALID_ARG;
   if (!dtype_ok(d->dtype) || !flag_ok(d->causal) || d->window < 0 || !isfinite(d->scale)) return CONV_ERR_INVALID_ARG;
   if (!stride_ok(d->q_token_stride) || !stride_ok(d->q_head_stride) || !stride_ok(d->y_token_stride) ||

@@ -25,6 +25,73 @@ __device__ __forceinline__ Span span_of(const int32_t* offsets, int64_t b, int t
   return {lo, hi - lo};
 }
 
+// How a call's sequences are dealt to workgroups, whose third axis it is.
+//
+// In one row: the work of sequence b, in units, starts at base(b) = offsets[b] *
+// num / 2^shift + b, and it has one unit at least; num over 2^shift are the units
+// of a token, and what they round off is less than the one more.  (Units behind
+// offsets[seqs] are the last sequence's too, beyond what it needs.)  So a long
+// sequence among short ones has its share of workgroups, which a plan by the
+// average denies it (a prompt of 4096 tokens beside 127 single ones: attention
+// 7.0 ms, where apart they take 0.3 and 0.1).  Each unit searches its sequence,
+// first where it stands if all are alike, then ever further from there, at last
+// by halves.
+//
+// By sequence (num 0): the first axis is for a sequence's units, which it strides
+// by.  Nothing is searched, which a workgroup of a microsecond would feel.
+struct UnitRow {
+  uint32_t first, seqs, num;  // first: the unit or sequence at which the launch starts
+  int32_t tokens, shift;
+  float per;                  // sequences a unit
+};
+struct Unit {
+  int64_t seq;
+  int index, count;  // its place among its sequence's units, and their number
+  Span span;         // the sequence's tokens
+  int length;        // and lengths[seq]
+};
+inline uint32_t units_of(const UnitRow& r) {  // below 2^32: no call has 2^31 tokens times num, nor sequences
+  return r.num ? (static_cast<uint32_t>(r.tokens) * r.num >> r.shift) + r.seqs : r.seqs;
+}
+inline UnitRow unit_row(const convsel_kv_batch_t& b, int64_t num, int shift) {
+  UnitRow r = {0, static_cast<uint32_t>(b.seqs), static_cast<uint32_t>(num), static_cast<int32_t>(b.tokens), shift, 0.f};
+  r.per = static_cast<float>(b.seqs) / static_cast<float>(units_of(r));
+  return r;
+}
+// launch(row, units) for all of them, as many at once as a grid's third axis holds.
+template <typename F>
+void each_grid(UnitRow r, const F& launch) {
+  for (uint32_t left = units_of(r); left > 0;) {
+    const uint32_t n = left < 65535 ? left : 65535;
+    launch(r, n);
+    left -= n;
+    r.first += n;
+  }
+}
+template <bool ROW>
+__device__ __forceinline__ Unit find_unit(const UnitRow& r, const int32_t* offsets, const int32_t* lengths) {
+  const uint32_t unit = r.first + blockIdx.z;
+  if constexpr (!ROW)
+    return {unit, static_cast<int>(blockIdx.x), static_cast<int>(gridDim.x), span_of(offsets, unit, r.tokens),
+            lengths[unit]};
+  uint32_t lo = 0, hi = r.seqs;  // base(lo) <= unit < base(hi)
+  uint32_t b = min(static_cast<uint32_t>((static_cast<float>(unit) + 0.5f) * r.per), hi - 1), step = 1;
+  for (;;) {
+    const Span span = span_of(offsets, b, r.tokens);
+    const int length = lengths[b];
+    const uint32_t base = (span.first * r.num >> r.shift) + b;
+    const uint32_t next = ((span.first + span.count) * r.num >> r.shift) + b + 1;
+    // Offsets that do not rise are nobody's; the search still ends, and what it gives stays within bounds.
+    const bool low = base > unit && b > lo, high = next <= unit && b + 1 < hi;
+    if (!low && !high)
+      return {b, static_cast<int>(unit > base ? min(unit - base, 0x7fffffffu) : 0u), static_cast<int>(next - base), span,
+              length};
+    (low ? hi : lo) = low ? b : b + 1;
+    b = hi - lo <= 2 * step ? lo + ((hi - lo) >> 1) : low ? hi - step : lo + step - 1;
+    step = min(2 * step, 1u << 30);
+  }
+}
+
 // Value that a code stands for, before its scale.
 __device__ __forceinline__ float decode(uint32_t byte, int format) {
   if (format == CONVSEL_KV_INT8) return static_cast<float>(static_cast<int8_t>(byte));

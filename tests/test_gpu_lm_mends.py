@@ -218,3 +218,74 @@ def test_activations_keep_their_precision_where_they_are_small(activation, dtype
         units = 16 + 3 * a
     before = units * 2.0 ** -24 * want.abs() + 1e-36
     within(y, want, before + torch.from_numpy(half_step((want.abs() + before).numpy(), dt)), "%s %s" % (activation, dtype))
+
+
+# ---- sequences of very unlike lengths --------------------------------------------------
+
+@pytest.mark.parametrize("rows,dtype,dim", [(16, "bf16", 32), (16, "f32", 32), (256, "bf16", 32), (128, "f32", 32),
+                                            (128, "bf16", 160)])
+def test_long_sequences_among_many_short_ones(rows, dtype, dim):
+    """150 sequences, most of one new token, some of none (the first and the last too), two of many: written, read back
+    and attended in one call each.  Every workgroup has to find the sequence that its tile is of."""
+    say("case unlike", rows, dtype, dim)
+    g, dt, hq, hk, page, seqs = gen(dim), DT[dtype], 16, 1, 16, 150
+    new, held = [1] * seqs, [(7 * b) % 41 for b in range(seqs)]
+    for b in (0, 1, 50, 51, 52, 120, 149):
+        new[b] = 0
+    new[40], new[121], held[40] = 300, 70, 23
+    total = [h + n for h, n in zip(held, new)]
+    need = [(t + page - 1) // page for t in total]
+    order, at, table = torch.randperm(sum(need) + 2, generator=g, device=DEV).tolist(), 0, []
+    for n in need:
+        table.append(order[at:at + n] + [-1] * (max(need) - n))
+        at += n
+    cache, want = fresh(sum(need) + 2, hk, dim, page, "int8")
+    zeros = [0] * seqs
+    for starts, counts in ((zeros, held), (held, new)):
+        off = offsets_of(counts)
+        k, v = (torch.randn(off[-1], hk, dim, generator=g, device=DEV).to(dt) for _ in range(2))
+        cache.write(k, v, ints(table), ints(starts), ints(off))
+        want.write(k, v, table, starts, off)
+    off = offsets_of(total)
+    for got, name in zip(cache.read(ints(table), ints(zeros), ints(off), off[-1], dtype=torch.float32), "kv"):
+        exact = np.concatenate([np.stack([want.value(name, table, b, p) for p in range(n)])
+                                for b, n in enumerate(total) if n]).astype(np.float32)
+        assert np.array_equal(got.cpu().numpy(), exact), name
+    q = torch.randn(sum(new), hq, dim, generator=g, device=DEV).to(dt)
+    t = ints(table) if rows == 16 else wide(table, (hq, hk, dim, page, total, new))
+    text = cs.describe_attention(cache, seqs, sum(new), t.shape[1], hq, dt)
+    assert " rows=%d " % rows in text, text
+    # Tokens behind the last offset are nobody's, and stay as they are.
+    whole = torch.full((sum(new) + 5, hq, dim), 7.0, device=DEV, dtype=dt)
+    more = torch.cat([q, q[:5]])
+    cs.cached_attention(more, cache, t, ints(total), ints(offsets_of(new)), out=whole)
+    exact, mag, smag, top = ref.attention(q, want, table, total, offsets_of(new), True, 0, dim ** -0.5)
+    within(whole[:-5], exact, ref.attention_bound(exact, mag, smag, top, dim, dt), "unlike")
+    assert bool((whole[-5:] == 7).all())
+
+
+def test_more_sequences_than_a_grids_third_axis_holds():
+    """70001 sequences of one or two tokens and one of 3000, in one call each.  Keys and values are whole numbers up to
+    127, exact in their pages; a sequence's first query sees its first token alone."""
+    seqs, long = 70001, 68000
+    say("case many sequences", seqs)
+    new = torch.ones(seqs, dtype=torch.int64, device=DEV)
+    new[::2] = 2
+    new[long] = 3000
+    off = torch.cat([torch.zeros(1, dtype=torch.int64, device=DEV), new.cumsum(0)])
+    tokens = int(off[-1])
+    table = torch.full((seqs, 188), -1, dtype=torch.int32, device=DEV)
+    table[:, 0] = torch.arange(seqs, device=DEV)
+    table[long, 1:] = torch.arange(seqs, seqs + 187, device=DEV)
+    cache = cs.KVCache(seqs + 187, 1, 16)
+    k, v = (torch.randint(-127, 128, (tokens, 1, 16), generator=gen(s), device=DEV).bfloat16() for s in (1, 2))
+    k[:, :, 0] = v[:, :, 0] = 127
+    off, zeros, lengths = off.int(), torch.zeros(seqs, dtype=torch.int32, device=DEV), new.int()
+    cache.write(k, v, table, zeros, off)
+    k2, v2 = cache.read(table, zeros, off, tokens)
+    assert torch.equal(k2, k) and torch.equal(v2, v)
+    q = torch.randn(tokens, 2, 16, generator=gen(3), device=DEV).bfloat16()
+    y = cs.cached_attention(q, cache, table, lengths, off)
+    first = off[:-1].long()
+    assert torch.equal(y[first], v[first].expand(-1, 2, -1))
+    assert bool(y.isfinite().all())

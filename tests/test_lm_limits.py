@@ -22,8 +22,7 @@ def attention_bytes(c, b, d):
 
 @pytest.mark.parametrize("heads", [1, 2, 8, 65535])
 def test_attention_rows_stay_within_what_the_kernels_count(heads):
-    """A workgroup of 16 rows goes on by up to 32768 tiles of them in 32 bits: past the last row that has to stay below
-    2^31."""
+    """Rows are counted in 32 bits, and a workgroup may look 32768 tiles of 16 past the last one."""
     d = attention_desc(q_heads=heads, q_token_stride=heads, q_head_stride=1, y_token_stride=heads, y_head_stride=1)
     c = cache_desc(kv_heads=1, head_dim=1)
     most = (2 ** 31 - 2 ** 20) // heads
@@ -187,3 +186,15 @@ def test_linear_of_few_rows_goes_the_faster_way(case):
     dtype, m, i, o, rows, tiles = case
     text = cs.describe_linear(m, i, o, {"bf16": torch.bfloat16, "f32": torch.float32}[dtype])
     assert ("linear_rows_kernel" in text) == (rows < tiles), text
+
+
+@pytest.mark.parametrize("prompt,singles,heads", [(4096, 127, 32), (4096, 7, 32), (512, 31, 8), (300, 600, 16), (1, 63, 8)])
+def test_a_prompt_among_single_tokens_has_its_own_tiles_of_rows(prompt, singles, heads):
+    """As many workgroups a key head as the prompt has tiles and the other sequences need, and less than one a sequence
+    more: a plan by the average length left a prompt of 4096 tokens one of them."""
+    cache = types.SimpleNamespace(_desc=ctypes.byref(cache_desc(pages=4096, kv_heads=8)), head_dim=64)
+    text = cs.describe_attention(cache, 1 + singles, prompt + singles, 512, heads)
+    rows, tiles = (int(re.search(r" %s=(\d+)" % n, text).group(1)) for n in ("rows", "tiles"))
+    group = heads // 8
+    need = -(-prompt * group // rows) + singles * -(-group // rows)
+    assert need <= tiles <= need + singles + 1, text
