@@ -143,7 +143,7 @@ typedef struct convsel_kv_cache {
 
 /* The sequences of a call.  Sequence b owns the packed tokens
  * offsets[b] .. offsets[b+1]-1 of the call's q, k, v or output (rising from 0;
- * the kernels clamp them to [0, tokens]). */
+ * the kernels clamp them to [0, tokens]).  No output may lie over these three. */
 typedef struct convsel_kv_batch {
   int64_t seqs;
   int64_t tokens;          /* packed tokens of the call */

@@ -173,6 +173,11 @@ bool hits_cache(const void* p, int64_t bytes, const convsel_kv_cache_t* c) {
          overlaps(p, bytes, c->k_scales, scales) || overlaps(p, bytes, c->v_scales, scales);
 }
 
+bool hits_batch(const void* p, int64_t bytes, const convsel_kv_batch_t* b) {
+  return overlaps(p, bytes, b->table, b->seqs * b->table_width * 4) || overlaps(p, bytes, b->lengths, b->seqs * 4) ||
+         overlaps(p, bytes, b->offsets, (b->seqs + 1) * 4);
+}
+
 conv_status_t attention_sizes(const convsel_kv_cache_t* c, const convsel_kv_batch_t* b,
                               const convsel_attention_desc_t* d) {
   conv_status_t st = cache_sizes(c);
@@ -340,7 +345,9 @@ conv_status_t convsel_kv_read(const convsel_kv_cache_t* cache, const convsel_kv_
   if (st != CONV_OK) return st;
   const int64_t es = esize(dtype), bytes = batch->tokens * cache->kv_heads * cache->head_dim * es;
   if (!k || !v || !aligned(k, es) || !aligned(v, es) || overlaps(k, bytes, v, bytes)) return CONV_ERR_INVALID_ARG;
-  if (hits_cache(k, bytes, cache) || hits_cache(v, bytes, cache)) return CONV_ERR_INVALID_ARG;
+  if (hits_cache(k, bytes, cache) || hits_cache(v, bytes, cache) || hits_batch(k, bytes, batch) ||
+      hits_batch(v, bytes, batch))
+    return CONV_ERR_INVALID_ARG;
   st = convsel::device_ready();
   if (st != CONV_OK) return st;
   const convsel::KvTokens t = {k, v, 0, 0, 0, 0, dtype};
@@ -373,7 +380,8 @@ conv_status_t convsel_attention(const void* q, const convsel_kv_cache_t* cache, 
   if (need > 0 && !aligned(workspace, 256)) return CONV_ERR_INVALID_ARG;
   const int64_t ybytes = span(t, desc->y_token_stride, h, desc->y_head_stride, d, es);
   const int64_t qbytes = span(t, desc->q_token_stride, h, desc->q_head_stride, d, es);
-  if (overlaps(y, ybytes, q, qbytes) || hits_cache(y, ybytes, cache) || overlaps(y, ybytes, workspace, (int64_t)need))
+  if (overlaps(y, ybytes, q, qbytes) || hits_cache(y, ybytes, cache) || hits_batch(y, ybytes, batch) ||
+      overlaps(y, ybytes, workspace, (int64_t)need))
     return CONV_ERR_INVALID_ARG;
   st = convsel::device_ready();
   if (st != CONV_OK) return st;

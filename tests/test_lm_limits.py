@@ -11,7 +11,8 @@ import torch
 import paper_2410_08300_amd as cs
 from paper_2410_08300_amd import _lib
 
-from test_lm_host import A, B, C, D, E, F, G, INVALID, attention_desc, batch_desc, cache_desc, qk, qk_desc
+from test_lm_host import (A, B, C, D, E, F, G, INVALID, attend, attention_desc, batch_desc, cache_desc, qk, qk_desc,
+                          read)
 
 
 def attention_bytes(c, b, d):
@@ -198,3 +199,14 @@ def test_a_prompt_among_single_tokens_has_its_own_tiles_of_rows(prompt, singles,
     group = heads // 8
     need = -(-prompt * group // rows) + singles * -(-group // rows)
     assert need <= tiles <= need + singles + 1, text
+
+
+def test_cache_reads_and_attention_refuse_outputs_over_their_batch():
+    """Every workgroup reads the table, the lengths and the offsets while others write."""
+    c, b, d = cache_desc(pages=4096), batch_desc(), attention_desc()
+    far = F + (1 << 20)
+    for at in (E, E + 28, E + 4096, E + 4100, E + 8192, E + 8196):
+        assert read(c, b, k=at, v=far) == INVALID and read(c, b, k=far, v=at) == INVALID, hex(at)
+        assert attend(c, b, d, y=at) == INVALID, hex(at)
+        # ... and where they only end over it: 10 tokens of 2 heads (4 of queries) of 64 in bf16
+        assert read(c, b, k=at - 2558, v=far) == INVALID and attend(c, b, d, y=at - 5118) == INVALID, hex(at)
