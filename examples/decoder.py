@@ -67,6 +67,8 @@ class Decoder:
     def generate(self, prompts, new, graph=True):
         """``new`` greedy tokens for each of ``prompts`` (lists of tokens), as a tensor [prompts][new], and the seconds
         that a step took."""
+        if new < 1 or not prompts or not all(prompts):
+            raise ValueError("generate: prompts of a token at least, and a token at least to add to them")
         device = self.embed.device
         size = self.caches[0].page_size
         each = max((len(p) + new + size - 1) // size for p in prompts)

@@ -289,3 +289,15 @@ def test_more_sequences_than_a_grids_third_axis_holds():
     first = off[:-1].long()
     assert torch.equal(y[first], v[first].expand(-1, 2, -1))
     assert bool(y.isfinite().all())
+
+
+# ---- the example ------------------------------------------------------------------------
+
+def test_decoder_example_refuses_prompts_that_it_has_no_next_token_for():
+    """An empty prompt has no last token whose logits could be its own."""
+    from test_gpu_decoder import SMALL, decoder
+    model = decoder.Decoder(**SMALL)
+    for prompts, new in (([[], [1, 2]], 3), ([[1, 2], []], 3), ([], 3), ([[1]], 0)):
+        with pytest.raises(ValueError, match="at least"):
+            model.generate(prompts, new)
+    assert model.generate([[1], [2, 3]], 1)[0].shape == (2, 1)
