@@ -72,7 +72,7 @@ conv_status_t convsel_linear_describe(const convsel_linear_desc_t* desc, char* b
 /* ---- norm and rotation of query and key heads ------------------------------
  * For every token t and every head of q and of k, x = its head_dim values:
  *   norm 1 (RMS):  z_d = x_d / sqrt(mean_d x_d^2 + eps) * weight_d
- *   norm 0:        z_d = x_d
+ *   norm 0:        z_d = x_d * weight_d
  * (weight NULL: ones), then the first rotary_dim = R values are rotated by
  * the angle whose cosine and sine are cos[p][i], sin[p][i], p = positions[t],
  * i < R/2, fp32 tables of max_position rows of R/2:

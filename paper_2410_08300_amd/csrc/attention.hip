@@ -53,8 +53,8 @@ __device__ __forceinline__ f32x4v_t mfma16(const f16x8_t& a, const f16x8_t& b, c
 // through registers alone.
 //
 // What bounds it: the codes' way from memory.  64 sequences of one query on 2048
-// .. 8192 tokens, 32 heads of 128 on 8, fp8: 136 us, 4.9 TB/s; one on 32768 in
-// 64 parts, int8: 18 us, 3.7 TB/s, and 3.8 us for the join.
+// .. 8192 tokens, 32 heads of 128 on 8, fp8: 142 us, 4.7 TB/s; one on 32768 in
+// 64 parts, int8: 20 us, 3.4 TB/s, and 4 us for the join.
 // ---------------------------------------------------------------------------
 template <typename T, int FMT, int NC>
 __global__ __launch_bounds__(256) void attention_rows_kernel(
@@ -454,8 +454,8 @@ Plan plan(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convse
   // its first keys; the 16-row kernel is through them in 8.  Measured with
   // heads of 128 and 64, they cross where rows x keys x width reach 1.6e9 in
   // bf16 and 4e9 in fp32 (one sequence, 32 query heads of 128 on 8, bf16: 128
-  // new tokens on 4000, 40 against 53 us; 64 on 1000, 26 against 18; 2048 on
-  // none 92 against 186), provided that its tiles are at least half full.
+  // new tokens on 4000, 46 against 48 us; 64 on 1000, 27 against 18; 2048 on
+  // none 99 against 177), provided that its tiles are at least half full.
   const double work = (double)avg * d.q_heads * b.seqs * keys * kv_row_bytes(c.head_dim);
   const bool many = avg * group >= 64 && work >= (d.dtype == CONV_F32 ? 4e9 : 1.6e9);
   auto cut = [&](int rows) {
@@ -474,11 +474,11 @@ Plan plan(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convse
       const int64_t best = (int64_t)sqrt(walk / join);
       if (n > best) n = best;
     } else {
-      // The join's launch costs what 400 keys do (8 key heads of 128: 4 sequences of 20 queries on 500, 13.8 us in one
-      // part and 16.1 in two; 16 of one on 1000, 20.7 and 17.7 in three), and a few workgroups more than run at once
-      // as much again (24 of one on 1000: 21.8, and 26.5 in three parts).
+      // The join's launch costs what 400 keys do (8 key heads of 128: 4 sequences of 20 queries on 500, 14.6 us in one
+      // part and 17.2 in two; 16 of one on 1000, 23.2 and 20.8 in three), and a few workgroups more than run at once
+      // as much again (24 of one on 1000: 24.4, and 28.9 in three parts).
       if (n > 1 && keys * (n - 1) / n < 400) n = 1;
-      // Sequences of unlike lengths end together where each is cut (64 of 2048 .. 8192 tokens: 145 -> 134 us).
+      // Sequences of unlike lengths end together where each is cut (64 of 2048 .. 8192 tokens: 163 -> 146 us).
       const int64_t even = groups >= 4096 ? 1 : keys / 2048 < 4 ? keys / 2048 : 4;
       if (n < even) n = even;
     }
@@ -488,7 +488,7 @@ Plan plan(const convsel_kv_cache_t& c, const convsel_kv_batch_t& b, const convse
   };
   // 256 rows share codes and barriers among twice as many, and pay where every CU has work for long: long sequences,
   // and either a second workgroup a CU to even out what a causal mask leaves, or a prefix that makes all alike (32 query
-  // heads of 128 on 8: 4096 new tokens 244 -> 223 us, 512 on 8000 136 -> 126; but 2048 new ones 93 -> 100).
+  // heads of 128 on 8: 4096 new tokens 280 -> 250 us, 512 on 8000 152 -> 138; but 2048 new ones 99 -> 116).
   if (many && attention_tiles_wide(d.dtype, c.head_dim) && keys >= 2048) {
     const int64_t wgs = cut(256);
     if (wgs >= 512 || (wgs >= 256 && keys >= 4 * avg)) return p;

@@ -15,9 +15,9 @@
 // large (their steps are then 2^-39 of the largest); codes are exact in one.
 // One number, 11 bits, turns 7 % of bf16 results into a neighbour of the rounded
 // one, though it saves a fifth of a long prompt (4096 tokens of 32 heads of 128
-// on 8: 217 us, 269 with two).  fp32 calls hold queries as two such numbers;
-// bf16 queries are exact in one, brought to [2^14, 2^15) by a power of two.  Sums
-// and statistics are fp32.
+// on 8: 194 us, 241 with two).  fp32 calls hold queries as two such numbers;
+// bf16 queries are exact in one, brought to [2^14, 2^15) by a power of two, but
+// for elements below 2^-32 of a head's largest.  Sums and statistics are fp32.
 #pragma once
 
 #include "lm_common.hpp"

@@ -16,8 +16,10 @@ using namespace lm;
 // belongs to one thread, which keeps the bytes that the call does not write.
 //
 // What bounds it: traffic, two or four bytes in and one out for each value, at
-// 3.8 to 4.3 TB/s for prompts in bf16, and for a few tokens (64 sequences of one:
-// 6.4 us) the way from the lengths to the table to the page.
+// 3.6 to 4.3 TB/s for prompts in bf16, and for a few tokens (64 sequences of one:
+// 6.3 us) the way from the lengths to the table to the page; heads that are no
+// multiple of 32 go word by word (16 prompts of 2048 tokens of 8 heads of 80: 101
+// us, of 96 41).
 
 // The fp32 quotient x / s of finite numbers, correctly rounded, from r = 1 / s
 // (correctly rounded): x r is within two units of it, one step with the exact
@@ -163,7 +165,7 @@ __global__ __launch_bounds__(NT) void kv_write_kernel(convsel_kv_cache_t c, conv
 // Reading: one workgroup per (16 positions of a sequence, head), positions
 // aligned to the cache's 16-token blocks.  A thread takes four codes at a time,
 // neighbours in the cache: four columns of a key, four tokens of a value, whose
-// codes reach their rows through LDS.  What bounds it: traffic, 4.8 to 5.6 TB/s
+// codes reach their rows through LDS.  What bounds it: traffic, 4.1 to 5.1 TB/s
 // for prompts in bf16.
 template <typename T, bool ROW>
 __global__ __launch_bounds__(256) void kv_read_kernel(convsel_kv_cache_t c, convsel_kv_batch_t b, KvTokens to,

@@ -20,7 +20,7 @@ using namespace lm;
 // What bounds it: the weights' way from memory.  A step of a wave is 2 KiB of
 // them; steps are fetched kDepth ahead, and as many waves as leave each of them
 // a few steps keep a CU's share of the weights on their way at once.  One row of
-// 4096 on 4096 x 4096 in bf16: 9.1 us, 3.7 TB/s where a large copy reaches 5.05
+// 4096 on 4096 x 4096 in bf16: 9.0 us, 3.7 TB/s where a large copy reaches 5.05
 // (weights larger than the caches come nearer; here launch and the first loads'
 // latency are a third).
 constexpr int kDepth = 4;

@@ -19,8 +19,8 @@
 //
 // What bounds them: few tiles, the way of a k-tile from memory, once a k-tile;
 // many, the matrix cores at the clock that the card's power leaves them (bf16
-// 4096 rows, 4096 -> 16384: 416 us, 1320 TFLOP/s, 78 % of the kernel's cycles in
-// products, at 1.8 GHz; fp32 4096 rows, 2048 -> 4096: 526 us, 131 TFLOP/s).
+// 4096 rows, 4096 -> 16384: 416 us, 1320 TFLOP/s; fp32 4096 rows, 2048 -> 4096:
+// 494 us, 139 TFLOP/s).
 #include <stdio.h>
 
 #include <type_traits>
@@ -352,8 +352,8 @@ constexpr Place place_of(int n) {
 }
 
 // Tiles of 256 in bf16: four waves, one to each SIMD, of 128 x 128.  (Eight waves of 128 x 64 read half as much again
-// from LDS: 540 us where this kernel takes 416.)  Products of 16 x 16 x 32: alone, on random operands, they reach 2065
-// TFLOP/s, those of 32 x 32 x 16 1810, because the card's power bounds both (453 -> 430 us).  The ring holds five
+// from LDS, which took a quarter longer.)  Products of 16 x 16 x 32: alone, on random operands, they reach 2065
+// TFLOP/s, those of 32 x 32 x 16 1810, because the card's power bounds both (5 % less time here).  The ring holds five
 // units of one operand's 256 rows and one k-tile, in the order w, x, w, x ...; a wave reads all of a k-tile's operands
 // in its first half, so that a unit is on its way for three quarters of a k-tile at least.
 typedef Tile<4, 4, 2, 2, 2> Tile256;

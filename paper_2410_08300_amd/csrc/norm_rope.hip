@@ -140,9 +140,13 @@ __global__ __launch_bounds__(256) void qk_units_kernel(QkArgs a, int lanes, int 
   }
 }
 
-// Any widths, strides and alignment: one wave per (token, head).  The head is
+// Any widths, strides and alignment, among them ordinary heads whose rotated part
+// is no whole units: one wave per (token, head).  The head is
 // read once, its sum of squares joined across the wave, and the scaled values
-// pass through LDS so that every lane finds its rotation partner.
+// pass through LDS so that every lane finds its rotation partner.  What bounds it:
+// instructions, one element a lane at a time (16384 tokens of 40 heads in bf16:
+// of 80, 40 turned, 273 us, of 96, 24 turned, 284, where their bytes take 42 and
+// 50).
 template <typename T>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkArgs a, int64_t items) {
   __shared__ float buf[4][kMaxDim];

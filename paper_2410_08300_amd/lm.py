@@ -158,7 +158,7 @@ def qk_norm_rope(q, k, positions, cos, sin, q_weight=None, k_weight=None, eps=1e
     of one fused projection), then the position rotation, in one pass:
     (q_out, k_out).
 
-    ``norm`` is "rms" (x / sqrt(mean x^2 + eps) * weight) or "none".  ``cos``
+    ``norm`` is "rms" (x / sqrt(mean x^2 + eps) * weight) or "none" (x * weight).  ``cos``
     and ``sin`` are fp32 tables [positions][R/2], ``positions`` an int32 row of
     them per token; the first R values of a head turn, as pairs (i, i + R/2) or
     with ``interleaved`` (2i, 2i + 1).  ``cos=None`` turns nothing.  Outputs may

@@ -301,3 +301,27 @@ def test_decoder_example_refuses_prompts_that_it_has_no_next_token_for():
         with pytest.raises(ValueError, match="at least"):
             model.generate(prompts, new)
     assert model.generate([[1], [2, 3]], 1)[0].shape == (2, 1)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [1, 12, 100, 400])
+def test_linear_carries_infinities_of_both_signs_in_their_own_rows(m, dtype):
+    """An infinity of x meets weights of either sign (and no zeros): its row is infinite, each output with its weight's
+    sign, and both infinities in one row leave NaN where their products differ in sign."""
+    g, dt = gen(m), DT[dtype]
+    x = torch.randn(m, 320, generator=g, device=DEV).to(dt)
+    w = torch.randn(200, 320, generator=g, device=DEV).to(dt)
+    w[w == 0] = 1
+    clean = cs.linear(x, w)
+    row, inf = m // 2, float("inf")
+    keep = torch.arange(m, device=DEV) != row
+    for places in ({5: inf}, {319: -inf}, {0: inf, 200: inf}, {7: inf, 311: -inf}):
+        bad = x.clone()
+        for k, v in places.items():
+            bad[row, k] = v
+        y = cs.linear(bad, w)
+        assert torch.equal(y[keep], clean[keep])
+        signs = torch.stack([w[:, k].sign() * (1 if v > 0 else -1) for k, v in places.items()])
+        same = (signs == signs[0]).all(0)
+        want = torch.where(same, signs[0] * inf, torch.full_like(signs[0], float("nan")))
+        assert torch.equal(torch.nan_to_num(y[row], nan=7.0), torch.nan_to_num(want, nan=7.0)), places
