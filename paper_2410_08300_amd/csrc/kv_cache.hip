@@ -239,11 +239,12 @@ __global__ __launch_bounds__(256) void kv_read_kernel(convsel_kv_cache_t c, conv
 }
 
 // Units of 2^shift tokens.  By sequence, with the units that one of the average number of tokens reaches from anywhere,
-// for single tokens, and where the longest sequence that there can be walks eight of them at most or fills the card by
-// itself (64 sequences of one token: 6.4 and 5.1 us to write and read, 7.5 and 6.4 in a row; 16 prompts of 2048 in pages
-// of 16: 53 and 41, 58 and 44 in a row).  In a row otherwise: a prompt of 4096 beside 127 single tokens takes 24 and 20 us,
-// by sequence 97 and 155.  A workgroup more for nothing costs: one for each of 64 sequences, keys and values of 8 heads,
-// 3 us.
+// where the longest sequence that there can be walks eight of them at most, or sixteen where all may be single tokens, or
+// fills the card by itself (64 sequences of one token: 6.4 and 5.1 us to write and read, 7.5 and 6.4 in a row; 16 prompts
+// of 2048 in pages of 16: 53 and 41, 58 and 44 in a row).  In a row otherwise: a prompt of 4096 beside 127 single tokens
+// takes 24 and 20 us, by sequence 97 and 155; one of 1000 beside 1023 sequences of nothing 18 and 31, 161 and 106; 1024
+// single tokens 27 and 21, 25 and 18.  A workgroup more for nothing costs: one for each of 64 sequences, keys and values
+// of 8 heads, 3 us.
 struct Deal {
   UnitRow row;
   unsigned across;
@@ -252,7 +253,8 @@ Deal deal(const convsel_kv_batch_t& b, int shift, int heads) {
   const int64_t unit = (int64_t)1 << shift, avg = (b.tokens + b.seqs - 1) / b.seqs;
   int64_t across = (avg + 2 * unit - 2) >> shift;
   if (across > 65536) across = 65536;
-  if (b.tokens <= b.seqs || (b.tokens >> shift) + 1 <= 8 * across || across * heads >= 1024)
+  const int64_t longest = (b.tokens >> shift) + 1;
+  if (longest <= 8 * across || (b.tokens <= b.seqs && longest <= 17) || across * heads >= 1024)
     return {unit_row(b, 0, shift), (unsigned)across};
   return {unit_row(b, 1, shift), 1};
 }

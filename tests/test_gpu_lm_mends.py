@@ -325,3 +325,31 @@ def test_linear_carries_infinities_of_both_signs_in_their_own_rows(m, dtype):
         same = (signs == signs[0]).all(0)
         want = torch.where(same, signs[0] * inf, torch.full_like(signs[0], float("nan")))
         assert torch.equal(torch.nan_to_num(y[row], nan=7.0), torch.nan_to_num(want, nan=7.0)), places
+
+
+@pytest.mark.parametrize("seqs,at", [(600, 0), (600, 300), (600, 599), (40, 17)])
+def test_one_sequence_with_tokens_among_idle_ones(seqs, at):
+    """A batch of fixed places of which one has a prompt, of no more tokens than there are places.  Whole numbers up to
+    127 are exact in their pages; the first query sees the first token alone."""
+    n = seqs - 3
+    say("case idle", seqs, at)
+    counts = [0] * seqs
+    counts[at] = n
+    off = ints(offsets_of(counts))
+    pages = (n + 5 + 15) // 16
+    table = torch.full((seqs, pages), -1, dtype=torch.int32, device=DEV)
+    table[at] = torch.arange(pages, device=DEV).flip(0)
+    starts, lengths = torch.zeros_like(off[:-1]), ints(counts)
+    cache = cs.KVCache(pages, 2, 32)
+    k, v = (torch.randint(-127, 128, (n, 2, 32), generator=gen(s), device=DEV).bfloat16() for s in (1, 2))
+    k[:, :, 0] = v[:, :, 0] = 127
+    for start in (0, 5):  # from a page's first row, and from within one: as many tokens reach a page more
+        starts[at], lengths[at] = start, start + n
+        cache.write(k, v, table, starts, off)
+        k2, v2 = cache.read(table, starts, off, n)
+        assert torch.equal(k2, k) and torch.equal(v2, v), start
+        q = torch.randn(n, 4, 32, generator=gen(3), device=DEV).bfloat16()
+        y = cs.cached_attention(q, cache, table, lengths, off)
+        assert bool(y.isfinite().all())
+        if start == 0:
+            assert torch.equal(y[0], v[0].repeat_interleave(2, 0))
