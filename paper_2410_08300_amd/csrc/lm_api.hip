@@ -13,7 +13,8 @@ conv_status_t device_ready();  // api.hip
 namespace {
 
 constexpr int64_t kInt31 = ((int64_t)1 << 31) - 1;
-constexpr int64_t kStrideMax = (int64_t)1 << 40;  // strides times counts stay far below 2^63
+constexpr int64_t kStrideMax = (int64_t)1 << 40;
+constexpr int64_t kReachMax = (int64_t)1 << 45;  // of n rows, in elements: no memory holds it, and bytes stay below 2^63
 constexpr int64_t kOutputsMax = (int64_t)1 << 35;
 constexpr int64_t kAttentionRowsMax = ((int64_t)1 << 31) - ((int64_t)1 << 20);
 
@@ -40,7 +41,8 @@ int64_t span(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t inner, int6
   return ((n0 - 1) * s0 + (n1 - 1) * s1 + inner) * es;
 }
 
-bool stride_ok(int64_t s) { return s >= 0 && s <= kStrideMax; }
+// A stride of n rows.
+bool stride_ok(int64_t s, int64_t n) { return s >= 0 && s <= kStrideMax && (n < 2 || s <= kReachMax / (n - 1)); }
 
 // No two of the n0 x n1 rows of `inner` elements share an element.
 bool rows_apart(int64_t n0, int64_t s0, int64_t n1, int64_t s1, int64_t inner) {
@@ -117,9 +119,9 @@ conv_status_t linear_sizes(const convsel_linear_desc_t* d) {
   if (d->m > 0 && d->out_features > kOutputsMax / d->m) return CONV_ERR_INVALID_ARG;
   if (!dtype_ok(d->dtype) || d->act < CONVSEL_ACT_NONE || d->act > CONVSEL_ACT_SILU) return CONV_ERR_INVALID_ARG;
   if (!flag_ok(d->has_bias) || !flag_ok(d->has_residual)) return CONV_ERR_INVALID_ARG;
-  if (d->ldx < d->in_features || d->ldx > kStrideMax || d->ldy < d->out_features || d->ldy > kStrideMax)
+  if (d->ldx < d->in_features || !stride_ok(d->ldx, d->m) || d->ldy < d->out_features || !stride_ok(d->ldy, d->m))
     return CONV_ERR_INVALID_ARG;
-  if (d->has_residual && (d->ldr < d->out_features || d->ldr > kStrideMax)) return CONV_ERR_INVALID_ARG;
+  if (d->has_residual && (d->ldr < d->out_features || !stride_ok(d->ldr, d->m))) return CONV_ERR_INVALID_ARG;
   return CONV_OK;
 }
 
@@ -187,8 +189,8 @@ conv_status_t attention_sizes(const convsel_kv_cache_t* c, const convsel_kv_batc
   // Rows are counted in 32 bits, and rounded up to tiles of them.
   if (b->tokens > kAttentionRowsMax / d->q_heads) return CONV_ERR_INVALID_ARG;
   if (!dtype_ok(d->dtype) || !flag_ok(d->causal) || d->window < 0 || !isfinite(d->scale)) return CONV_ERR_INVALID_ARG;
-  if (!stride_ok(d->q_token_stride) || !stride_ok(d->q_head_stride) || !stride_ok(d->y_token_stride) ||
-      !stride_ok(d->y_head_stride))
+  if (!stride_ok(d->q_token_stride, b->tokens) || !stride_ok(d->q_head_stride, d->q_heads) ||
+      !stride_ok(d->y_token_stride, b->tokens) || !stride_ok(d->y_head_stride, d->q_heads))
     return CONV_ERR_INVALID_ARG;
   return CONV_OK;
 }
@@ -265,8 +267,8 @@ conv_status_t convsel_qk_norm_rope(const void* q, const void* k, const void* q_w
   a.interleaved = d->interleaved; a.eps = d->eps;
   const int64_t es = esize(d->dtype), t = d->tokens;
   for (int i = 0; i < 2; ++i) {
-    if (!stride_ok(a.in_token[i]) || !stride_ok(a.in_head[i]) || !stride_ok(a.out_token[i]) ||
-        !stride_ok(a.out_head[i]))
+    if (!stride_ok(a.in_token[i], t) || !stride_ok(a.in_head[i], a.heads[i]) || !stride_ok(a.out_token[i], t) ||
+        !stride_ok(a.out_head[i], a.heads[i]))
       return CONV_ERR_INVALID_ARG;
   }
   if (t == 0 || a.heads[0] + a.heads[1] == 0) return CONV_OK;
@@ -315,8 +317,8 @@ conv_status_t convsel_kv_write(const convsel_kv_cache_t* cache, const convsel_kv
   conv_status_t st = cache_sizes(cache);
   if (st == CONV_OK) st = batch_sizes(cache, batch);
   if (st != CONV_OK) return st;
-  if (!dtype_ok(dtype) || !stride_ok(k_token_stride) || !stride_ok(k_head_stride) || !stride_ok(v_token_stride) ||
-      !stride_ok(v_head_stride))
+  if (!dtype_ok(dtype) || !stride_ok(k_token_stride, batch->tokens) || !stride_ok(k_head_stride, cache->kv_heads) ||
+      !stride_ok(v_token_stride, batch->tokens) || !stride_ok(v_head_stride, cache->kv_heads))
     return CONV_ERR_INVALID_ARG;
   if (batch->seqs == 0 || batch->tokens == 0 || batch->table_width == 0) return CONV_OK;
   st = cache_pointers(cache);

@@ -11,8 +11,8 @@ import torch
 import paper_2410_08300_amd as cs
 from paper_2410_08300_amd import _lib
 
-from test_lm_host import (A, B, C, D, E, F, G, INVALID, attend, attention_desc, batch_desc, cache_desc, qk, qk_desc,
-                          read)
+from test_lm_host import (A, B, C, D, E, F, G, INVALID, attend, attention_desc, batch_desc, cache_desc, linear, linear_desc,
+                          qk, qk_desc, read, write)
 
 
 def attention_bytes(c, b, d):
@@ -210,3 +210,25 @@ def test_cache_reads_and_attention_refuse_outputs_over_their_batch():
         assert attend(c, b, d, y=at) == INVALID, hex(at)
         # ... and where they only end over it: 10 tokens of 2 heads (4 of queries) of 64 in bf16
         assert read(c, b, k=at - 2558, v=far) == INVALID and attend(c, b, d, y=at - 5118) == INVALID, hex(at)
+
+
+@pytest.mark.parametrize("n", [2 ** 31 - 1, 2 ** 25])
+def test_rows_that_reach_further_than_64_bits_count_are_refused(n):
+    """Their last byte lies 2^64 and more behind the first: no check of overlaps could count it."""
+    far = 2 ** 40
+    for kw in (dict(ldx=far), dict(ldy=far), dict(ldr=far, has_residual=1)):
+        d = linear_desc(m=n, out_features=8, in_features=8, **dict(dict(ldx=8, ldy=8, ldr=8), **kw))
+        assert linear(d, r=E if d.has_residual else None, ws=G, nws=1 << 60) == INVALID, kw
+    for name in ("q_token_stride", "k_token_stride", "q_out_token_stride", "k_out_token_stride"):
+        assert qk(qk_desc(tokens=n, **{name: far})) == INVALID, name
+    c, b = cache_desc(pages=4096), batch_desc(seqs=1, tokens=n)
+    for i in (0, 2):
+        strides = [128, 64, 128, 64]
+        strides[i] = far
+        assert write(c, b, strides=strides) == INVALID
+    one = cache_desc(pages=4096, kv_heads=1, head_dim=1)
+    for name in ("q_token_stride", "y_token_stride"):
+        strides = dict(dict(q_token_stride=1, q_head_stride=1, y_token_stride=1, y_head_stride=1), **{name: far})
+        assert attention_bytes(one, batch_desc(seqs=1, tokens=2 ** 25), attention_desc(q_heads=1, **strides)) == INVALID
+    # A stride that only one row has is nobody's.
+    assert attention_bytes(one, batch_desc(seqs=1, tokens=1), attention_desc(q_heads=1, **strides)) == _lib.CONV_OK
