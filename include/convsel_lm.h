@@ -2,7 +2,9 @@
  * convsel decoder operators -- the pieces of a decoder (language-model) layer
  * that run beside the convolutions of convsel.h: the linear layer with a fused
  * epilogue, the norm and position rotation of query and key heads, a paged
- * key/value cache held in 8 bits, and attention over that cache.
+ * key/value cache held in 8 bits, and attention over that cache; linear layers
+ * whose weights are held in 8 bits, attention of prompts over their own keys and
+ * values, and the adjustments of logits before a token is chosen.
  *
  * Conventions are those of convsel.h: device pointers, status codes, every
  * check of arguments on the host before the first HIP call, work enqueued on
@@ -208,6 +210,117 @@ conv_status_t convsel_attention(const void* q, const convsel_kv_cache_t* cache, 
 /* One line: kernel, rows and keys of a tile, grid, split and workspace. */
 conv_status_t convsel_attention_describe(const convsel_kv_cache_t* cache, const convsel_kv_batch_t* batch,
                                          const convsel_attention_desc_t* desc, char* buf, size_t len);
+
+/* ---- attention of prompts ----------------------------------------------------
+ * The packed tokens of a call are whole sequences: sequence b owns the tokens
+ * offsets[b] .. offsets[b+1]-1 of q, k, v and y (rising from 0; the kernels clamp
+ * them to [0, tokens]), and no cache is read.  Head h of q reads key/value head
+ * h / (q_heads / kv_heads), and for token i of a sequence of n
+ *   y[i][h] = sum_j softmax_j(scale * q[i][h] . k[j]) v[j]
+ * over its tokens 0 <= j < n, with causal only j <= i, and with window > 0 only
+ * j > i - window.  What lies in masked places has no influence, infinities and
+ * NaN included.  Rows of y behind the last sequence are left as they were. */
+typedef struct convsel_prompt_desc {
+  int64_t seqs, tokens;
+  int32_t q_heads, kv_heads; /* tokens * q_heads <= 2^31 - 2^20 */
+  int32_t head_dim;          /* 1 .. 256 */
+  int32_t dtype;             /* of q, k, v and y */
+  int32_t causal;
+  int32_t window; /* 0: none */
+  float scale;    /* finite */
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+  int64_t v_token_stride, v_head_stride, y_token_stride, y_head_stride;
+} convsel_prompt_desc_t;
+
+/* Device bytes the call needs as workspace (0: none; else 256-byte aligned).
+ * Of q, k and v the addresses' alignment is looked at, nothing else: rows that do
+ * not lie in whole 16-byte units are copied there first. */
+conv_status_t convsel_prompt_attention_workspace_bytes(const void* q, const void* k, const void* v,
+                                                       const convsel_prompt_desc_t* desc, size_t* bytes);
+/* No value of y may lie where the call reads: q, k, v (slices whose rows only
+ * interleave are apart), offsets or the workspace. */
+conv_status_t convsel_prompt_attention(const void* q, const void* k, const void* v, const int32_t* offsets, void* y,
+                                       const convsel_prompt_desc_t* desc, void* workspace, size_t workspace_bytes,
+                                       void* stream);
+/* One line: kernels, rows and keys of a tile, and workspace of the call. */
+conv_status_t convsel_prompt_attention_describe(const void* q, const void* k, const void* v,
+                                                const convsel_prompt_desc_t* desc, char* buf, size_t len);
+
+/* ---- linear layer on 8-bit codes ----------------------------------------------
+ * Rows of numbers are coded with a scale each: with A a row's largest finite
+ * magnitude
+ *   scale = max(A / 127, 2^-100)             (fp32 quotient)
+ *   code  = round(x / scale)                 (fp32 quotient, ties to even)
+ * Infinities become the largest code of their sign and NaN becomes 0.
+ *
+ * x: m rows of in_features numbers of `dtype`, ldx apart; codes: rows of ldc >=
+ * in_features bytes, of which those behind the row are written as zeros; scales:
+ * m values.  No output may lie over x or the other output. */
+typedef struct convsel_quantize_desc {
+  int64_t m, in_features;
+  int64_t ldx, ldc;
+  int32_t dtype;
+} convsel_quantize_desc_t;
+
+conv_status_t convsel_quantize_rows(const void* x, int8_t* codes, float* scales, const convsel_quantize_desc_t* desc,
+                                    void* stream);
+
+/*   y[m][o] = act((sum_i X[m][i] * W[o][i]) * sx[m] * sw[o] + b[o]) + r[m][o]
+ * W: codes, O rows of ldw >= in_features bytes each (all of which can be read;
+ * what those behind in_features hold does not matter), sw their O scales.  x is
+ * codes with m scales sx (x_dtype CONVSEL_CODES) or numbers (CONV_F32, CONV_BF16;
+ * sx NULL), which are coded by rows as above within the call.  The sum is exact;
+ * scales, bias, activation and residual are fp32, and y is rounded once. */
+#define CONVSEL_CODES (-1)
+typedef struct convsel_linear_int8_desc {
+  int64_t m, in_features, out_features; /* in < 2^17, out < 2^26, m * out <= 2^35 */
+  int64_t ldx, ldw, ldr, ldy;           /* ldr is read only with a residual */
+  int32_t x_dtype;                      /* CONVSEL_CODES, or conv_dtype_t of x */
+  int32_t dtype;                        /* of b, r and y */
+  int32_t act;                          /* convsel_act_t */
+  int32_t has_bias, has_residual;
+} convsel_linear_int8_desc_t;
+
+/* Device bytes the call needs as workspace (0: none; else 256-byte aligned).
+ * Codes run fastest where their rows start on 16 bytes, every one of them:
+ * others are copied first.  Of x and w the addresses' alignment is looked at. */
+conv_status_t convsel_linear_int8_workspace_bytes(const void* x, const void* w, const convsel_linear_int8_desc_t* desc,
+                                                  size_t* bytes);
+/* y may be r itself (same address and stride); otherwise its span must not
+ * overlap what the call reads, nor the workspace. */
+conv_status_t convsel_linear_int8(const void* x, const float* x_scale, const int8_t* w, const float* w_scale,
+                                  const void* b, const void* r, void* y, const convsel_linear_int8_desc_t* desc,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+/* One line: kernels, tile, split and workspace of the call. */
+conv_status_t convsel_linear_int8_describe(const void* x, const void* w, const convsel_linear_int8_desc_t* desc,
+                                           char* buf, size_t len);
+
+/* ---- logits before a token is chosen --------------------------------------------
+ * Row b is a sequence's logits over `vocab` tokens.  Its history are the tokens
+ * history[offsets[b]] .. history[offsets[b+1]-1] (rising from 0; clamped to
+ * [0, tokens]), the first prompt_lengths[b] of them its prompt (NULL: none) and
+ * the others generated; tokens outside [0, vocab) are ignored.  With c(t) the
+ * number of times t was generated, for z = x[b][t] in this order:
+ *   t in the history:  z = z > 0 ? z / repetition[b] : z * repetition[b]
+ *   c(t) > 0:          z = z - (frequency[b] * c(t) + presence[b])
+ *   bias:              z = z + bias[b][t]          (ldbias 0: one row for all)
+ *   mask:              z = -inf where bit t % 32 of mask[b][t / 32] is clear
+ * in fp32; y is rounded once.  Each of them is left out where its pointer is NULL
+ * (history NULL leaves out the first two).  A row whose mask allows nothing is
+ * -inf throughout.  y may be x itself (same address and stride). */
+typedef struct convsel_logits_desc {
+  int64_t rows, vocab; /* each < 2^31 */
+  int64_t tokens;      /* of the history */
+  int64_t ldx, ldy;
+  int64_t ldbias; /* 0, or at least vocab */
+  int64_t ldmask; /* words: 0 (one row for all), or at least vocab / 32, rounded up */
+  int32_t dtype;  /* of x and y */
+} convsel_logits_desc_t;
+
+conv_status_t convsel_adjust_logits(const void* x, const int32_t* history, const int32_t* offsets,
+                                    const int32_t* prompt_lengths, const float* repetition, const float* presence,
+                                    const float* frequency, const float* bias, const uint32_t* mask, void* y,
+                                    const convsel_logits_desc_t* desc, void* stream);
 
 #ifdef __cplusplus
 }

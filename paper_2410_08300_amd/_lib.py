@@ -49,7 +49,10 @@ class Desc(ctypes.Structure):
 
 EXPORTED_LM = ("convsel_linear_workspace_bytes", "convsel_linear", "convsel_linear_describe", "convsel_qk_norm_rope",
                "convsel_kv_cache_bytes", "convsel_kv_write", "convsel_kv_read", "convsel_attention_workspace_bytes",
-               "convsel_attention", "convsel_attention_describe")
+               "convsel_attention", "convsel_attention_describe", "convsel_prompt_attention_workspace_bytes",
+               "convsel_prompt_attention", "convsel_prompt_attention_describe", "convsel_quantize_rows",
+               "convsel_linear_int8_workspace_bytes", "convsel_linear_int8", "convsel_linear_int8_describe",
+               "convsel_adjust_logits")
 
 
 class _Sizes(ctypes.Structure):
@@ -97,6 +100,31 @@ class AttentionDesc(_Sizes):
     _fields_ = ([(n, ctypes.c_int32) for n in ("q_heads", "dtype", "causal", "window")] + [("scale", ctypes.c_float)]
                 + [(n, ctypes.c_int64) for n in ("q_token_stride", "q_head_stride", "y_token_stride",
                                                  "y_head_stride")])
+
+
+class PromptDesc(_Sizes):
+    """convsel_prompt_desc_t."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("seqs", "tokens")]
+                + [(n, ctypes.c_int32) for n in ("q_heads", "kv_heads", "head_dim", "dtype", "causal", "window")]
+                + [("scale", ctypes.c_float)]
+                + [(t + s, ctypes.c_int64) for t in "qkvy" for s in ("_token_stride", "_head_stride")])
+
+
+class QuantizeDesc(_Sizes):
+    """convsel_quantize_desc_t."""
+    _fields_ = [(n, ctypes.c_int64) for n in ("m", "in_features", "ldx", "ldc")] + [("dtype", ctypes.c_int32)]
+
+
+class LinearInt8Desc(_Sizes):
+    """convsel_linear_int8_desc_t."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("m", "in_features", "out_features", "ldx", "ldw", "ldr", "ldy")]
+                + [(n, ctypes.c_int32) for n in ("x_dtype", "dtype", "act", "has_bias", "has_residual")])
+
+
+class LogitsDesc(_Sizes):
+    """convsel_logits_desc_t."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("rows", "vocab", "tokens", "ldx", "ldy", "ldbias", "ldmask")]
+                + [("dtype", ctypes.c_int32)])
 
 
 class Conv2dError(RuntimeError):
@@ -201,6 +229,15 @@ def lib():
         L.convsel_attention_workspace_bytes.argtypes = [cp, bp, ap, sp]
         L.convsel_attention.argtypes = [vp, cp, bp, vp, ap, vp, ctypes.c_size_t, vp]
         L.convsel_attention_describe.argtypes = [cp, bp, ap, ctypes.c_char_p, ctypes.c_size_t]
+        pp, zp, ip, gp = (ctypes.POINTER(t) for t in (PromptDesc, QuantizeDesc, LinearInt8Desc, LogitsDesc))
+        L.convsel_prompt_attention_workspace_bytes.argtypes = [vp, vp, vp, pp, sp]
+        L.convsel_prompt_attention.argtypes = [vp] * 5 + [pp, vp, ctypes.c_size_t, vp]
+        L.convsel_prompt_attention_describe.argtypes = [vp, vp, vp, pp, ctypes.c_char_p, ctypes.c_size_t]
+        L.convsel_quantize_rows.argtypes = [vp, vp, vp, zp, vp]
+        L.convsel_linear_int8_workspace_bytes.argtypes = [vp, vp, ip, sp]
+        L.convsel_linear_int8.argtypes = [vp] * 7 + [ip, vp, ctypes.c_size_t, vp]
+        L.convsel_linear_int8_describe.argtypes = [vp, vp, ip, ctypes.c_char_p, ctypes.c_size_t]
+        L.convsel_adjust_logits.argtypes = [vp] * 10 + [gp, vp]
         for n in EXPORTED_LM:
             getattr(L, n).restype = i32
         _lib = L

@@ -21,33 +21,6 @@ using namespace lm;
 // multiple of 32 go word by word (16 prompts of 2048 tokens of 8 heads of 80: 101
 // us, of 96 41).
 
-// The fp32 quotient x / s of finite numbers, correctly rounded, from r = 1 / s
-// (correctly rounded): x r is within two units of it, one step with the exact
-// remainder brings that within one, and from there a second step rounds right
-// (Markstein 1990).  Five operations; the general quotient takes some twelve.
-__device__ __forceinline__ float quotient(float x, float s, float r) {
-  float q = x * r;
-  q = fmaf(fmaf(-q, s, x), r, q);
-  return fmaf(fmaf(-q, s, x), r, q);
-}
-
-// Codes of four finite numbers of magnitudes up to the block's largest: no
-// quotient is more than a rounding beyond the largest code.
-template <int FMT>
-__device__ __forceinline__ uint32_t four_codes(float x0, float x1, float x2, float x3, float s, float r) {
-  const float q0 = quotient(x0, s, r), q1 = quotient(x1, s, r), q2 = quotient(x2, s, r), q3 = quotient(x3, s, r);
-  if constexpr (FMT == CONVSEL_KV_INT8) {
-    // 1.5 * 2^23 + q holds q, rounded to nearest even, in its lowest byte.
-    const uint32_t a = __float_as_uint(q0 + 12582912.f), b = __float_as_uint(q1 + 12582912.f);
-    const uint32_t c = __float_as_uint(q2 + 12582912.f), d = __float_as_uint(q3 + 12582912.f);
-    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u),
-                                 0x05040100u);
-  } else {
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(q0, q1, 0, false);
-    return static_cast<uint32_t>(__builtin_amdgcn_cvt_pk_fp8_f32(q2, q3, lo, true));
-  }
-}
-
 template <typename T, int FMT, int NT, bool ROW>
 __global__ __launch_bounds__(NT) void kv_write_kernel(convsel_kv_cache_t c, convsel_kv_batch_t b, KvTokens in,
                                                        UnitRow row, int vec) {

@@ -8,6 +8,27 @@ namespace convsel {
 namespace lm {
 
 typedef float f32x4v_t __attribute__((ext_vector_type(4)));
+typedef int i32x4v_t __attribute__((ext_vector_type(4)));
+typedef int i32x16v_t __attribute__((ext_vector_type(16)));
+
+// An 8-bit code: an operand, whose products are summed in 32-bit whole numbers.
+struct code_t {
+  int8_t bits;
+};
+
+// Operands' sizes and sums.
+template <typename T> struct operand {
+  static constexpr int bytes = elem<T>::bytes, per16 = elem<T>::per16;
+  static constexpr bool codes = false;
+  typedef f32x4v_t sum4;
+  typedef f32x16_t sum16;
+};
+template <> struct operand<code_t> {
+  static constexpr int bytes = 1, per16 = 16;
+  static constexpr bool codes = true;
+  typedef i32x4v_t sum4;
+  typedef i32x16v_t sum16;
+};
 
 // One 16-byte unit of a 16 x 16 product's operands: 8 bf16 or 4 fp32 of a lane.
 __device__ __forceinline__ f32x4v_t mac16(bf16_t, const vec16& a, const vec16& b, f32x4v_t c) {
@@ -21,6 +42,42 @@ __device__ __forceinline__ f32x4v_t mac16(float, const vec16& a, const vec16& b,
   for (int i = 0; i < 4; ++i)
     c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.d[i]), __uint_as_float(b.d[i]), c, 0, 0, 0);
   return c;
+}
+
+__device__ __forceinline__ i32x4v_t mac16(code_t, const vec16& a, const vec16& b, i32x4v_t c) {
+  i32x4v_t av, bv;
+  __builtin_memcpy(&av, &a, 16);
+  __builtin_memcpy(&bv, &b, 16);
+  return __builtin_amdgcn_mfma_i32_16x16x64_i8(av, bv, c, 0, 0, 0);
+}
+template <typename T>
+__device__ __forceinline__ void mac32(f32x16_t& acc, const vec16& a, const vec16& b) {
+  mfma_32x32<T>(acc, a, b);
+}
+template <typename T>
+__device__ __forceinline__ void mac32(i32x16v_t& acc, const vec16& a, const vec16& b) {
+  i32x4v_t av, bv;
+  __builtin_memcpy(&av, &a, 16);
+  __builtin_memcpy(&bv, &b, 16);
+  acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(av, bv, acc, 0, 0, 0);
+}
+
+// Scales of outputs o .. o + 3 of a product of codes.
+__device__ __forceinline__ void load_scale4(const LinearArgs& g, int64_t o, float (&s)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s[i] = o + i < g.out ? g.w_scale[o + i] : 0.f;
+}
+
+// Four sums that lie as they were stored: of codes 32-bit whole numbers, which become fp32 and take their row's and
+// outputs' scales.  The scales' product may leave fp32, and so may a sum's with one of them, where the result does not;
+// sums 2^-25 times as large stay within it beside any scale from 2^-100 on.
+template <bool CODES>
+__device__ __forceinline__ void sums4(const float4& v, float row, const float (&s)[4], float (&z)[4]) {
+  z[0] = v.x; z[1] = v.y; z[2] = v.z; z[3] = v.w;
+  if constexpr (CODES) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = static_cast<float>(__float_as_int(z[i])) * (row * 0x1p-25f) * s[i] * 0x1p25f;
+  }
 }
 
 // The biases of outputs o .. o + 3.

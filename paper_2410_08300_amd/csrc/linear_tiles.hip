@@ -101,7 +101,7 @@ template <> struct Quad<bf16_t> {
 // What store_blocks does, of a wave whose rows and outputs all exist, in whole units: eight rows of a lane at most at a
 // time, without a test, and the residual's next ones on their way while these are written.  (4096 rows, 512 -> 16384 in
 // bf16: 110 us by the general way, 91 by this; with a residual 217 and 120.)
-template <typename T, typename S, typename Put>
+template <typename T, typename S, bool CODES, typename Put>
 __device__ __forceinline__ void store_whole(const TileArgs& a, const Put& put, float* mine, int lane, int64_t m0,
                                             int64_t o0) {
   constexpr int FM = S::FM, PER = S::FO * 8, STEP = 64 / PER, PARTS = S::FO == 4 ? 2 : 1, G = 32 / STEP / PARTS;
@@ -118,10 +118,16 @@ __device__ __forceinline__ void store_whole(const TileArgs& a, const Put& put, f
     r += G * STEP * g.ldr;
   };
   if (g.r) fetch();
-  float bias[4];
+  float bias[4], scale[4], rows[G];
   load_bias4<T>(g, o0 + col, bias);
+  if constexpr (CODES) load_scale4(g, o0 + col, scale);
+  const float* row_scale = CODES ? g.x_scale + m0 + row : nullptr;
 #pragma unroll 1
   for (int k = 0; k < FM * PARTS; ++k) {
+    if constexpr (CODES) {
+      times(all, [&](auto n_c) { rows[decltype(n_c)::value] = row_scale[decltype(n_c)::value * STEP]; });
+      row_scale += G * STEP;
+    }
     times(std::make_integer_sequence<int, FM>{}, [&](auto j_c) {
       if (decltype(j_c)::value * PARTS == k) put(j_c, mine);
     });
@@ -131,8 +137,8 @@ __device__ __forceinline__ void store_whole(const TileArgs& a, const Put& put, f
     float z[G][4];
     times(all, [&](auto n_c) {
       constexpr int n = decltype(n_c)::value;
-      const float4 v = *reinterpret_cast<const float4*>(from + n * STEP * S::OUT_ROW);
-      z[n][0] = v.x + bias[0]; z[n][1] = v.y + bias[1]; z[n][2] = v.z + bias[2]; z[n][3] = v.w + bias[3];
+      sums4<CODES>(*reinterpret_cast<const float4*>(from + n * STEP * S::OUT_ROW), rows[n], scale, z[n]);
+      z[n][0] += bias[0]; z[n][1] += bias[1]; z[n][2] += bias[2]; z[n][3] += bias[3];
     });
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
@@ -150,14 +156,14 @@ __device__ __forceinline__ void store_whole(const TileArgs& a, const Put& put, f
 
 // Writes a wave's results, whose first row and output are m0 and o0: through its own place in LDS, where put(j, place)
 // lays rows 32 j .. of them, so that every row of y is read (residual) and written along its outputs.
-template <typename T, typename S, typename Put>
+template <typename T, typename S, bool CODES, typename Put>
 __device__ __forceinline__ void store_blocks(const TileArgs& a, const Put& put, char* lds, int wave, int lane, int64_t m0,
                                              int64_t o0, int split) {
   constexpr int FO = S::FO, FM = S::FM;
   const LinearArgs& g = a.g;
   float* mine = reinterpret_cast<float*>(lds) + wave * 32 * S::OUT_ROW;
   if (a.splits == 1 && a.vec_out && m0 + 32 * FM <= g.m && o0 + 32 * FO <= g.out)  // uniform in a wave
-    return store_whole<T, S>(a, put, mine, lane, m0, o0);
+    return store_whole<T, S, CODES>(a, put, mine, lane, m0, o0);
   const int64_t opad = (g.out + 3) & ~static_cast<int64_t>(3);
   // A lane has the same four outputs of all its rows.  Rows go in fours, so that what they read is on its way together;
   // one copy of the code for all, as five activations unrolled over a tile do not stay in the instruction cache (37 us
@@ -166,8 +172,9 @@ __device__ __forceinline__ void store_blocks(const TileArgs& a, const Put& put, 
   const int row = lane / PER, col = 4 * (lane % PER);
   const int64_t o = o0 + col;
   const bool there = o < g.out;
-  float bias[4];
+  float bias[4], scale[4];
   load_bias4<T>(g, o, bias);
+  if constexpr (CODES) load_scale4(g, o, scale);
 #pragma unroll 1
   for (int j = 0; j < FM; ++j) {
     times(std::make_integer_sequence<int, FM>{}, [&](auto j_c) {
@@ -177,21 +184,22 @@ __device__ __forceinline__ void store_blocks(const TileArgs& a, const Put& put, 
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
     for (int r0 = 0; r0 < 32; r0 += N * STEP) {
-      float z[N][4];
+      float4 raw[N];
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        const float4 v = *reinterpret_cast<const float4*>(mine + (r0 + n * STEP + row) * S::OUT_ROW + col);
-        z[n][0] = v.x; z[n][1] = v.y; z[n][2] = v.z; z[n][3] = v.w;
-      }
+      for (int n = 0; n < N; ++n)
+        raw[n] = *reinterpret_cast<const float4*>(mine + (r0 + n * STEP + row) * S::OUT_ROW + col);
       const int64_t m = m0 + j * 32 + r0 + row;
       if (!there || m >= g.m) continue;
       if (a.splits > 1) {
         float* dst = a.part + (split * g.m + m) * opad + o;
 #pragma unroll
         for (int n = 0; n < N; ++n)
-          if (m + n * STEP < g.m)
-            *reinterpret_cast<float4*>(dst + n * STEP * opad) = make_float4(z[n][0], z[n][1], z[n][2], z[n][3]);
+          if (m + n * STEP < g.m) *reinterpret_cast<float4*>(dst + n * STEP * opad) = raw[n];
       } else {
+        float z[N][4];
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+          sums4<CODES>(raw[n], CODES ? g.x_scale[min(m + n * STEP, g.m - 1)] : 1.f, scale, z[n]);
         finish4<T, N>(g, m, STEP, o, z, bias, a.vec_out);
       }
     }
@@ -200,10 +208,12 @@ __device__ __forceinline__ void store_blocks(const TileArgs& a, const Put& put, 
   }
 }
 
-template <typename T, typename S>
+// T: operands; Y: outputs.
+template <typename T, typename Y, typename S>
 __global__ __launch_bounds__(S::WAVES * 64, S::PER_CU) void linear_tiles_kernel(TileArgs a) {
   constexpr int FO = S::FO, FM = S::FM, NDMA = S::NDMA, STAGE = S::STAGE;
-  constexpr int NST = S::NST, ES = elem<T>::bytes, UE = elem<T>::per16, BK = 128 / ES;
+  constexpr int NST = S::NST, ES = operand<T>::bytes, UE = operand<T>::per16, BK = 128 / ES;
+  typedef typename operand<T>::sum16 sum_t;
   __shared__ __align__(16) char lds[S::LDS];
   const LinearArgs& g = a.g;
   const int lane = threadIdx.x & 63;
@@ -214,9 +224,10 @@ __global__ __launch_bounds__(S::WAVES * 64, S::PER_CU) void linear_tiles_kernel(
   const int64_t m0 = static_cast<int64_t>(tm) * S::TM, o0 = static_cast<int64_t>(to) * S::TO;
 
   const int64_t wrows = min(g.out - o0, static_cast<int64_t>(S::TO)), xrows = min(g.m - m0, static_cast<int64_t>(S::TM));
-  const uint32_t wbytes = static_cast<uint32_t>(((wrows - 1) * g.in + g.in) * ES);
+  const int64_t ldw = operand<T>::codes ? g.ldw : g.in;
+  const uint32_t wbytes = static_cast<uint32_t>(((wrows - 1) * ldw + g.in) * ES);
   const uint32_t xbytes = static_cast<uint32_t>(((xrows - 1) * g.ldx + g.in) * ES);
-  const u32x4_t wr = dma_rsrc(reinterpret_cast<const T*>(g.w) + o0 * g.in, wbytes);
+  const u32x4_t wr = dma_rsrc(reinterpret_cast<const T*>(g.w) + o0 * ldw, wbytes);
   const u32x4_t xr = dma_rsrc(reinterpret_cast<const T*>(g.x) + m0 * g.ldx, xbytes);
   const uint32_t lds0 = lds_address(lds);
 
@@ -232,7 +243,7 @@ __global__ __launch_bounds__(S::WAVES * 64, S::PER_CU) void linear_tiles_kernel(
     const bool isw = row < S::TO;
     const int64_t r = isw ? row : row - S::TO;
     const bool ok = r < (isw ? wrows : xrows);
-    dvo[d] = ok ? static_cast<uint32_t>((r * (isw ? g.in : g.ldx) + dku[d]) * ES) : (isw ? wbytes : xbytes);
+    dvo[d] = ok ? static_cast<uint32_t>((r * (isw ? ldw : g.ldx) + dku[d]) * ES) : (isw ? wbytes : xbytes);
   }
   const int k0 = split * a.per, all = static_cast<int>((g.in + BK - 1) / BK);
   const int nk = min(all, k0 + a.per) - k0;
@@ -255,11 +266,11 @@ __global__ __launch_bounds__(S::WAVES * 64, S::PER_CU) void linear_tiles_kernel(
   for (int t = 0; t < 4; ++t)
     off[t] = (l32 >> 1) * 256 + ((8 * (l32 & 1) + ((2 * t + half) ^ ((l32 >> 1) & 7))) << 4);
 
-  f32x16_t acc[FO][FM];
+  sum_t acc[FO][FM];
 #pragma unroll
   for (int i = 0; i < FO; ++i)
 #pragma unroll
-    for (int j = 0; j < FM; ++j) acc[i][j] = zero16();
+    for (int j = 0; j < FM; ++j) acc[i][j] = sum_t{};
   vec16 fw[2][FO], fx[2][FM];
   auto read = [&](int kt, auto t_c) {
     constexpr int t = decltype(t_c)::value;
@@ -274,7 +285,7 @@ __global__ __launch_bounds__(S::WAVES * 64, S::PER_CU) void linear_tiles_kernel(
 #pragma unroll
     for (int i = 0; i < FO; ++i)
 #pragma unroll
-      for (int j = 0; j < FM; ++j) mfma_32x32<T>(acc[i][j], fw[t & 1][i], fx[t & 1][j]);
+      for (int j = 0; j < FM; ++j) mac32<T>(acc[i][j], fw[t & 1][i], fx[t & 1][j]);
   };
   // One step: the reads of the next one between the products of this.
   auto interleave = [&]() {
@@ -322,7 +333,7 @@ __global__ __launch_bounds__(S::WAVES * 64, S::PER_CU) void linear_tiles_kernel(
     // cores idle.
 #pragma unroll
     for (int q = 0; q < FO * FM || q < NDMA; ++q) {
-      if (q < FO * FM) mfma_32x32<T>(acc[q / FM][q % FM], fw[1][q / FM], fx[1][q % FM]);
+      if (q < FO * FM) mac32<T>(acc[q / FM][q % FM], fw[1][q / FM], fx[1][q % FM]);
       __builtin_amdgcn_sched_barrier(0);
       if (q < NDMA) issue(kt + NST, q);
       __builtin_amdgcn_sched_barrier(0);
@@ -333,12 +344,12 @@ __global__ __launch_bounds__(S::WAVES * 64, S::PER_CU) void linear_tiles_kernel(
   const auto put = [&](auto j_c, float* mine) {
     times(std::make_integer_sequence<int, 4 * FO>{}, [&](auto n_c) {
       constexpr int i = decltype(n_c)::value / 4, v = decltype(n_c)::value % 4;
-      const f32x16_t& z = acc[i][decltype(j_c)::value];
+      const f32x16_t z = __builtin_bit_cast(f32x16_t, acc[i][decltype(j_c)::value]);
       *reinterpret_cast<float4*>(mine + l32 * S::OUT_ROW + 32 * i + 8 * v + 4 * half) =
           make_float4(z[4 * v], z[4 * v + 1], z[4 * v + 2], z[4 * v + 3]);
     });
   };
-  store_blocks<T, S>(a, put, lds, wave, lane, m0 + wm * FM * 32, o0 + wo * FO * 32, split);
+  store_blocks<Y, S, operand<T>::codes>(a, put, lds, wave, lane, m0 + wm * FM * 32, o0 + wo * FO * 32, split);
 }
 
 struct Place {
@@ -351,17 +362,18 @@ constexpr Place place_of(int n) {
   return k <= r ? Place{r, k} : Place{k - r - 1, r};
 }
 
-// Tiles of 256 in bf16: four waves, one to each SIMD, of 128 x 128.  (Eight waves of 128 x 64 read half as much again
+// Tiles of 256 in bf16 and of codes: four waves, one to each SIMD, of 128 x 128.  (Eight waves of 128 x 64 read half as much again
 // from LDS, which took a quarter longer.)  Products of 16 x 16 x 32: alone, on random operands, they reach 2065
 // TFLOP/s, those of 32 x 32 x 16 1810, because the card's power bounds both (5 % less time here).  The ring holds five
 // units of one operand's 256 rows and one k-tile, in the order w, x, w, x ...; a wave reads all of a k-tile's operands
 // in its first half, so that a unit is on its way for three quarters of a k-tile at least.
 typedef Tile<4, 4, 2, 2, 2> Tile256;
 
+template <typename T, typename Y>
 __global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
-  typedef bf16_t T;
   typedef Tile256 S;
-  constexpr int ES = elem<T>::bytes, UE = elem<T>::per16, BK = 128 / ES, UNIT = 256 * 128, RING = 5;
+  typedef typename operand<T>::sum4 sum_t;
+  constexpr int ES = operand<T>::bytes, UE = operand<T>::per16, BK = 128 / ES, UNIT = 256 * 128, RING = 5;
   static_assert(S::OUT <= RING * UNIT, "epilogue");
   __shared__ __align__(16) char lds[RING * UNIT];
   const LinearArgs& g = a.g;
@@ -373,9 +385,10 @@ __global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
   const int64_t m0 = static_cast<int64_t>(tm) * 256, o0 = static_cast<int64_t>(to) * 256;
   const int wrows = static_cast<int>(min(g.out - o0, static_cast<int64_t>(256)));
   const int xrows = static_cast<int>(min(g.m - m0, static_cast<int64_t>(256)));
-  const uint32_t wbytes = static_cast<uint32_t>(wrows * g.in * ES);
+  const int64_t ldw = operand<T>::codes ? g.ldw : g.in;
+  const uint32_t wbytes = static_cast<uint32_t>(((wrows - 1) * ldw + g.in) * ES);
   const uint32_t xbytes = static_cast<uint32_t>(((xrows - 1) * g.ldx + g.in) * ES);
-  u32x4_t wr = dma_rsrc(reinterpret_cast<const T*>(g.w) + o0 * g.in, wbytes);
+  u32x4_t wr = dma_rsrc(reinterpret_cast<const T*>(g.w) + o0 * ldw, wbytes);
   u32x4_t xr = dma_rsrc(reinterpret_cast<const T*>(g.x) + m0 * g.ldx, xbytes);
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(lds) + wave * 8192);
   const int all = static_cast<int>((g.in + BK - 1) / BK);
@@ -394,7 +407,7 @@ __global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
     const int line = U >> 4, pos = U & 15;
     const int row = 2 * line + (pos >> 3), c = ((pos & 7) ^ (line & 7)) * UE;
     if (d < 2) col[d] = c;
-    wvo[d] = row < wrows ? static_cast<uint32_t>((row * g.in + c) * ES) : wbytes;
+    wvo[d] = row < wrows ? static_cast<uint32_t>((row * ldw + c) * ES) : wbytes;
     xvo[d] = row < xrows ? static_cast<uint32_t>((row * g.ldx + c) * ES) : xbytes;
   }
   // Before k-tile kt is fetched: columns past the reduction, in its last k-tile, and k-tiles past the last lie beyond
@@ -431,11 +444,11 @@ __global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
 #pragma unroll
   for (int t = 0; t < 2; ++t)
     off[t] = (r16 >> 1) * 256 + ((8 * (r16 & 1) + ((4 * t + quarter) ^ (r16 >> 1))) << 4);
-  f32x4v_t acc[8][8];
+  sum_t acc[8][8];
 #pragma unroll
   for (int i = 0; i < 8; ++i)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) acc[i][j] = f32x4v_t{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < 8; ++j) acc[i][j] = sum_t{};
   vec16 f[2][16];  // half of the k-tile, w's blocks and x's
   // Operand n of a half: w's and x's blocks in turn.
   auto read = [&](int sw, int sx, int t, int n) {
@@ -523,15 +536,15 @@ __global__ __launch_bounds__(256, 1) void linear_tiles256_kernel(TileArgs a) {
   const auto put = [&](auto j_c, float* mine) {
     times(std::make_integer_sequence<int, 16>{}, [&](auto n_c) {
       constexpr int i = decltype(n_c)::value / 2, h = decltype(n_c)::value % 2;
-      const f32x4v_t& z = acc[i][2 * decltype(j_c)::value + h];
+      const f32x4v_t z = __builtin_bit_cast(f32x4v_t, acc[i][2 * decltype(j_c)::value + h]);
       *reinterpret_cast<float4*>(mine + (16 * h + r16) * S::OUT_ROW + 16 * i + 4 * quarter) =
           make_float4(z[0], z[1], z[2], z[3]);
     });
   };
-  store_blocks<T, S>(a, put, lds, wave, lane, m0 + wm * 128, o0 + wo * 128, split);
+  store_blocks<Y, S, operand<T>::codes>(a, put, lds, wave, lane, m0 + wm * 128, o0 + wo * 128, split);
 }
 // Sums the parts of a split reduction, in their order, four outputs a thread.
-template <typename T>
+template <typename T, bool CODES>
 __global__ __launch_bounds__(256) void linear_join_kernel(TileArgs a) {
   const int64_t quads = (a.g.out + 3) / 4;
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
@@ -539,10 +552,19 @@ __global__ __launch_bounds__(256) void linear_join_kernel(TileArgs a) {
   const int64_t m = i / quads, o = (i - m * quads) * 4;
   float s[1][4] = {}, bias[4];
   load_bias4<T>(a.g, o, bias);
+  if constexpr (CODES) {
+    float scale[4];
+    load_scale4(a.g, o, scale);
+    i32x4v_t n = {};
 #pragma unroll 4
-  for (int p = 0; p < a.splits; ++p) {
-    const float4 z = reinterpret_cast<const float4*>(a.part)[p * quads * a.g.m + i];
-    s[0][0] += z.x; s[0][1] += z.y; s[0][2] += z.z; s[0][3] += z.w;
+    for (int p = 0; p < a.splits; ++p) n += reinterpret_cast<const i32x4v_t*>(a.part)[p * quads * a.g.m + i];
+    sums4<true>(__builtin_bit_cast(float4, n), a.g.x_scale[m], scale, s[0]);
+  } else {
+#pragma unroll 4
+    for (int p = 0; p < a.splits; ++p) {
+      const float4 z = reinterpret_cast<const float4*>(a.part)[p * quads * a.g.m + i];
+      s[0][0] += z.x; s[0][1] += z.y; s[0][2] += z.z; s[0][3] += z.w;
+    }
   }
   finish4<T, 1>(a.g, m, 0, o, s, bias, a.vec_out);
 }
@@ -575,20 +597,21 @@ typedef Tile<2, 2, 2, 2, 2> Tile128;
 typedef Tile<1, 1, 2, 2, 3> Tile64;
 constexpr int kSide[3] = {256, 128, 64};
 
-template <typename T, typename S>
+template <typename T, typename Y, typename S>
 hipError_t launch(const TileArgs& a, hipStream_t st) {
   const int units = a.to * a.tm * a.splits;
-  hipLaunchKernelGGL((linear_tiles_kernel<T, S>), dim3((unsigned)(8 * ((units + 7) / 8))), dim3(S::WAVES * 64), 0, st,
+  hipLaunchKernelGGL((linear_tiles_kernel<T, Y, S>), dim3((unsigned)(8 * ((units + 7) / 8))), dim3(S::WAVES * 64), 0, st,
                      a);
   return hipGetLastError();
 }
 
-template <typename T>
+template <typename T, typename Y>
 hipError_t launch_all(const LinearArgs& a0, const LinearTiles& p, void* workspace, hipStream_t st) {
   TileArgs a;
   a.g = a0;
   char* ws = (char*)workspace;
-  if (p.pack) {
+  if constexpr (!operand<T>::codes) {
+    if (p.pack) {
     const int64_t per = elem<T>::per16, padded = (a0.in + per - 1) / per * per;
     const int64_t units = (a0.m + a0.out) * (padded / per);
     const int64_t blocks = (units + 255) / 256;
@@ -598,6 +621,7 @@ hipError_t launch_all(const LinearArgs& a0, const LinearTiles& p, void* workspac
     a.g.w = ws + a0.m * padded * sizeof(T);
     a.g.in = a.g.ldx = padded;
     ws += p.pack_bytes;
+    }
   }
   const int side = kSide[p.config];
   a.to = (int)((a0.out + side - 1) / side);
@@ -606,24 +630,24 @@ hipError_t launch_all(const LinearArgs& a0, const LinearTiles& p, void* workspac
   a.splits = p.splits;
   a.per = (int)((all + p.splits - 1) / p.splits);
   a.part = (float*)ws;
-  const uintptr_t unit = 4 * sizeof(T);
+  const uintptr_t unit = 4 * sizeof(Y);
   a.vec_out = a0.ldy % 4 == 0 && (uintptr_t)a0.y % unit == 0 &&
               (!a0.r || (a0.ldr % 4 == 0 && (uintptr_t)a0.r % unit == 0));
   hipError_t e = hipSuccess;
   if (p.config == 0) {
     if constexpr (sizeof(T) == 4) {
-      e = launch<T, Tile256>(a, st);
+      e = launch<T, Y, Tile256>(a, st);
     } else {
       const int units = a.to * a.tm * a.splits;
-      hipLaunchKernelGGL(linear_tiles256_kernel, dim3((unsigned)(8 * ((units + 7) / 8))), dim3(256), 0, st, a);
+      hipLaunchKernelGGL((linear_tiles256_kernel<T, Y>), dim3((unsigned)(8 * ((units + 7) / 8))), dim3(256), 0, st, a);
       e = hipGetLastError();
     }
   } else {
-    e = p.config == 1 ? launch<T, Tile128>(a, st) : launch<T, Tile64>(a, st);
+    e = p.config == 1 ? launch<T, Y, Tile128>(a, st) : launch<T, Y, Tile64>(a, st);
   }
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t quads = (a0.out + 3) / 4 * a0.m;
-  hipLaunchKernelGGL(linear_join_kernel<T>, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((linear_join_kernel<Y, operand<T>::codes>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 
@@ -633,17 +657,18 @@ hipError_t launch_all(const LinearArgs& a0, const LinearTiles& p, void* workspac
 constexpr int64_t kThreadsMax = ((int64_t)1 << 32) - 8 * 256;
 
 LinearTiles linear_tiles_plan(const LinearArgs& a) {
-  const int64_t es = a.dtype == CONV_F32 ? 4 : 2, per = 16 / es;
+  const int64_t es = a.codes ? 1 : a.dtype == CONV_F32 ? 4 : 2, per = 16 / es;
   LinearTiles p;
-  // By sizes alone: the workspace is asked for before the addresses are known.
-  p.pack = a.in % per != 0 || a.ldx % per != 0;
+  // By sizes alone: the workspace is asked for before the addresses are known.  Rows of codes come in whole units.
+  p.pack = !a.codes && (a.in % per != 0 || a.ldx % per != 0);
   const int64_t padded = (a.in + per - 1) / per * per;
   p.pack_bytes = p.pack ? align256((size_t)(a.m + a.out) * padded * es) : 0;
   p.part_bytes = 0;
   p.config = 0;
   p.splits = 1;
   // A tile's rows are addressed in 32 bits from its first one.
-  const int64_t ld = p.pack || a.in > a.ldx ? padded : a.ldx;
+  int64_t ld = p.pack || a.in > a.ldx ? padded : a.ldx;
+  if (a.codes && a.ldw > ld) ld = a.ldw;
   if (ld * es >= ((int64_t)1 << 31) / 256 || (!p.pack && ((uintptr_t)a.x % 16 != 0 || (uintptr_t)a.w % 16 != 0))) {
     p.config = -1;
     p.us = 0.;
@@ -659,7 +684,7 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
   static const double kOne[2][3] = {{8.3, 2.35, 0.7}, {1.67, 0.83, 0.36}};
   static const double kEach[2][3] = {{8.3, 2.15, 0.61}, {1.67, 0.61, 0.25}};
   static const double kAlone[3] = {6., 0., 0.};
-  const int ty = a.dtype == CONV_F32 ? 0 : 1;
+  const int ty = a.dtype == CONV_F32 && !a.codes ? 0 : 1;
   double best = 0.;
   for (int c = 0; c < 3; ++c) {
     const int64_t n = tiles(c);
@@ -687,8 +712,11 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
 }
 
 hipError_t launch_linear_tiles(const LinearArgs& a, const LinearTiles& p, void* workspace, hipStream_t stream) {
-  return a.dtype == CONV_F32 ? launch_all<float>(a, p, workspace, stream)
-                             : launch_all<bf16_t>(a, p, workspace, stream);
+  if (a.codes)
+    return a.dtype == CONV_F32 ? launch_all<code_t, float>(a, p, workspace, stream)
+                               : launch_all<code_t, bf16_t>(a, p, workspace, stream);
+  return a.dtype == CONV_F32 ? launch_all<float, float>(a, p, workspace, stream)
+                             : launch_all<bf16_t, bf16_t>(a, p, workspace, stream);
 }
 
 const char* linear_tiles_name(int config) {

@@ -195,6 +195,65 @@ conv_status_t attention_sizes(const convsel_kv_cache_t* c, const convsel_kv_batc
   return CONV_OK;
 }
 
+// ---- prompts ----
+
+conv_status_t prompt_sizes(const convsel_prompt_desc_t* d) {
+  if (!d || d->seqs < 0 || d->seqs > kInt31 || d->tokens < 0 || d->tokens > kInt31) return CONV_ERR_INVALID_ARG;
+  if (d->kv_heads < 1 || d->kv_heads > 32767 || d->q_heads < 1 || d->q_heads > 65535 || d->q_heads % d->kv_heads != 0)
+    return CONV_ERR_INVALID_ARG;
+  if (d->head_dim < 1 || d->head_dim > 256 || d->tokens > kAttentionRowsMax / d->q_heads) return CONV_ERR_INVALID_ARG;
+  if (!dtype_ok(d->dtype) || !flag_ok(d->causal) || d->window < 0 || !isfinite(d->scale)) return CONV_ERR_INVALID_ARG;
+  const int64_t t = d->tokens;
+  if (!stride_ok(d->q_token_stride, t) || !stride_ok(d->q_head_stride, d->q_heads) ||
+      !stride_ok(d->k_token_stride, t) || !stride_ok(d->k_head_stride, d->kv_heads) ||
+      !stride_ok(d->v_token_stride, t) || !stride_ok(d->v_head_stride, d->kv_heads) ||
+      !stride_ok(d->y_token_stride, t) || !stride_ok(d->y_head_stride, d->q_heads))
+    return CONV_ERR_INVALID_ARG;
+  return CONV_OK;
+}
+
+convsel::PromptArgs prompt_args(const convsel_prompt_desc_t* d, const void* q, const void* k, const void* v,
+                                const int32_t* offsets, void* y) {
+  convsel::PromptArgs a;
+  a.q = q; a.k = k; a.v = v; a.offsets = offsets; a.y = y;
+  a.seqs = d->seqs; a.tokens = d->tokens;
+  a.q_token = d->q_token_stride; a.q_head = d->q_head_stride;
+  a.k_token = d->k_token_stride; a.k_head = d->k_head_stride;
+  a.v_token = d->v_token_stride; a.v_head = d->v_head_stride;
+  a.y_token = d->y_token_stride; a.y_head = d->y_head_stride;
+  a.q_heads = d->q_heads; a.kv_heads = d->kv_heads; a.dim = d->head_dim; a.dtype = d->dtype;
+  a.causal = d->causal; a.window = d->window; a.scale = d->scale;
+  return a;
+}
+
+// ---- linear on codes ----
+
+conv_status_t linear_int8_sizes(const convsel_linear_int8_desc_t* d) {
+  if (!d || d->m < 0 || d->in_features < 1 || d->out_features < 1) return CONV_ERR_INVALID_ARG;
+  // Sums of 2^17 - 1 products of codes, -128 among them, stay within 32 bits.
+  if (d->m > kInt31 || d->in_features >= (1 << 17) || d->out_features >= ((int64_t)1 << 26)) return CONV_ERR_INVALID_ARG;
+  if (d->m > 0 && d->out_features > kOutputsMax / d->m) return CONV_ERR_INVALID_ARG;
+  if ((d->x_dtype != CONVSEL_CODES && !dtype_ok(d->x_dtype)) || !dtype_ok(d->dtype) || d->act < CONVSEL_ACT_NONE ||
+      d->act > CONVSEL_ACT_SILU || !flag_ok(d->has_bias) || !flag_ok(d->has_residual))
+    return CONV_ERR_INVALID_ARG;
+  if (d->ldx < d->in_features || !stride_ok(d->ldx, d->m) || d->ldw < d->in_features ||
+      !stride_ok(d->ldw, d->out_features) || d->ldy < d->out_features || !stride_ok(d->ldy, d->m))
+    return CONV_ERR_INVALID_ARG;
+  if (d->has_residual && (d->ldr < d->out_features || !stride_ok(d->ldr, d->m))) return CONV_ERR_INVALID_ARG;
+  return CONV_OK;
+}
+
+convsel::LinearArgs linear_int8_args(const convsel_linear_int8_desc_t* d, const void* x, const float* x_scale,
+                                     const void* w, const float* w_scale, const void* b, const void* r, void* y) {
+  convsel::LinearArgs a;
+  a.x = x; a.w = w; a.b = b; a.r = r; a.y = y;
+  a.m = d->m; a.in = d->in_features; a.out = d->out_features;
+  a.ldx = d->ldx; a.ldr = d->ldr; a.ldy = d->ldy;
+  a.dtype = d->dtype; a.act = d->act;
+  a.codes = 1; a.ldw = d->ldw; a.x_scale = x_scale; a.w_scale = w_scale;
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -397,6 +456,169 @@ conv_status_t convsel_attention_describe(const convsel_kv_cache_t* cache, const 
   if (!buf || len == 0) return CONV_ERR_INVALID_ARG;
   convsel::attention_describe(*cache, *batch, *desc, buf, len);
   return CONV_OK;
+}
+
+conv_status_t convsel_prompt_attention_workspace_bytes(const void* q, const void* k, const void* v,
+                                                       const convsel_prompt_desc_t* desc, size_t* bytes) {
+  const conv_status_t st = prompt_sizes(desc);
+  if (st != CONV_OK) return st;
+  if (!bytes) return CONV_ERR_INVALID_ARG;
+  *bytes = desc->seqs == 0 || desc->tokens == 0
+               ? 0
+               : convsel::prompt_attention_workspace(prompt_args(desc, q, k, v, nullptr, nullptr));
+  return CONV_OK;
+}
+
+conv_status_t convsel_prompt_attention(const void* q, const void* k, const void* v, const int32_t* offsets, void* y,
+                                       const convsel_prompt_desc_t* desc, void* workspace, size_t workspace_bytes,
+                                       void* stream) {
+  conv_status_t st = prompt_sizes(desc);
+  if (st != CONV_OK) return st;
+  const convsel_prompt_desc_t* d = desc;
+  if (d->seqs == 0 || d->tokens == 0) return CONV_OK;
+  const int64_t es = esize(d->dtype), t = d->tokens, dim = d->head_dim;
+  if (!q || !k || !v || !offsets || !y || !aligned(q, es) || !aligned(k, es) || !aligned(v, es) || !aligned(y, es) ||
+      !aligned(offsets, 4))
+    return CONV_ERR_INVALID_ARG;
+  if (!rows_apart(t, d->y_token_stride, d->q_heads, d->y_head_stride, dim)) return CONV_ERR_INVALID_ARG;
+  const convsel::PromptArgs a = prompt_args(d, q, k, v, offsets, y);
+  const size_t need = convsel::prompt_attention_workspace(a);
+  if (workspace_bytes < need || (need > 0 && !workspace)) return CONV_ERR_WORKSPACE;
+  if (need > 0 && !aligned(workspace, 256)) return CONV_ERR_INVALID_ARG;
+  const Rows yr = {y, t, a.y_token * es, d->q_heads, a.y_head * es, dim * es};
+  const Rows in[3] = {{q, t, a.q_token * es, d->q_heads, a.q_head * es, dim * es},
+                      {k, t, a.k_token * es, d->kv_heads, a.k_head * es, dim * es},
+                      {v, t, a.v_token * es, d->kv_heads, a.v_head * es, dim * es}};
+  const Rows ws = run_of(need > 0 ? workspace : nullptr, (int64_t)need);
+  for (const Rows& r : in)
+    if (share_bytes(yr, r) || share_bytes(ws, r)) return CONV_ERR_INVALID_ARG;
+  const Rows off = run_of(offsets, (d->seqs + 1) * 4);
+  if (share_bytes(yr, off) || share_bytes(yr, ws) || share_bytes(ws, off)) return CONV_ERR_INVALID_ARG;
+  st = convsel::device_ready();
+  if (st != CONV_OK) return st;
+  return from_hip(convsel::launch_prompt_attention(a, workspace, (hipStream_t)stream));
+}
+
+conv_status_t convsel_prompt_attention_describe(const void* q, const void* k, const void* v,
+                                                const convsel_prompt_desc_t* desc, char* buf, size_t len) {
+  const conv_status_t st = prompt_sizes(desc);
+  if (st != CONV_OK) return st;
+  if (!buf || len == 0) return CONV_ERR_INVALID_ARG;
+  convsel::prompt_attention_describe(prompt_args(desc, q, k, v, nullptr, nullptr), buf, len);
+  return CONV_OK;
+}
+
+conv_status_t convsel_quantize_rows(const void* x, int8_t* codes, float* scales, const convsel_quantize_desc_t* desc,
+                                    void* stream) {
+  const convsel_quantize_desc_t* d = desc;
+  if (!d || d->m < 0 || d->m > kInt31 || d->in_features < 1 || d->in_features > kInt31 || !dtype_ok(d->dtype) ||
+      d->ldx < d->in_features || !stride_ok(d->ldx, d->m) || d->ldc < d->in_features || !stride_ok(d->ldc, d->m))
+    return CONV_ERR_INVALID_ARG;
+  if (d->m == 0) return CONV_OK;
+  const int64_t es = esize(d->dtype);
+  if (!x || !codes || !scales || !aligned(x, es) || !aligned(scales, 4)) return CONV_ERR_INVALID_ARG;
+  const int64_t xbytes = span(d->m, d->ldx, 1, 0, d->in_features, es), cbytes = d->m * d->ldc;
+  if (overlaps(codes, cbytes, x, xbytes) || overlaps(scales, d->m * 4, x, xbytes) ||
+      overlaps(codes, cbytes, scales, d->m * 4))
+    return CONV_ERR_INVALID_ARG;
+  const conv_status_t st = convsel::device_ready();
+  if (st != CONV_OK) return st;
+  const convsel::CodeArgs a = {x, codes, scales, d->m, d->in_features, d->ldx, d->ldc, d->dtype};
+  return from_hip(convsel::launch_quantize_rows(a, (hipStream_t)stream));
+}
+
+conv_status_t convsel_linear_int8_workspace_bytes(const void* x, const void* w, const convsel_linear_int8_desc_t* desc,
+                                                  size_t* bytes) {
+  const conv_status_t st = linear_int8_sizes(desc);
+  if (st != CONV_OK) return st;
+  if (!bytes) return CONV_ERR_INVALID_ARG;
+  *bytes = desc->m == 0 ? 0
+                        : convsel::linear_int8_workspace(
+                              linear_int8_args(desc, x, nullptr, w, nullptr, nullptr, nullptr, nullptr), desc->x_dtype);
+  return CONV_OK;
+}
+
+conv_status_t convsel_linear_int8(const void* x, const float* x_scale, const int8_t* w, const float* w_scale,
+                                  const void* b, const void* r, void* y, const convsel_linear_int8_desc_t* desc,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+  conv_status_t st = linear_int8_sizes(desc);
+  if (st != CONV_OK || desc->m == 0) return st;
+  const convsel_linear_int8_desc_t* d = desc;
+  const bool codes = d->x_dtype == CONVSEL_CODES;
+  if (!x || !w || !w_scale || !y || codes != (x_scale != nullptr) || (d->has_bias != 0) != (b != nullptr) ||
+      (d->has_residual != 0) != (r != nullptr))
+    return CONV_ERR_INVALID_ARG;
+  const int64_t es = esize(d->dtype), xs = codes ? 1 : esize(d->x_dtype), m = d->m, in = d->in_features,
+                out = d->out_features;
+  if (!aligned(x, xs) || !aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(b, es) || !aligned(r, es) ||
+      !aligned(y, es))
+    return CONV_ERR_INVALID_ARG;
+  const convsel::LinearArgs a = linear_int8_args(d, x, x_scale, w, w_scale, b, r, y);
+  const size_t need = convsel::linear_int8_workspace(a, d->x_dtype);
+  if (workspace_bytes < need || (need > 0 && !workspace)) return CONV_ERR_WORKSPACE;
+  if (need > 0 && !aligned(workspace, 256)) return CONV_ERR_INVALID_ARG;
+  // y and the workspace lie over nothing that is read, nor over each other; y may be r.
+  const struct {
+    const void* p;
+    int64_t bytes;
+  } reads[6] = {{x, span(m, a.ldx, 1, 0, in, xs)}, {x_scale, codes ? m * 4 : 0}, {w, out * a.ldw}, {w_scale, out * 4},
+                {b, b ? out * es : 0}, {r, r ? span(m, a.ldr, 1, 0, out, es) : 0}};
+  const int64_t ybytes = span(m, a.ldy, 1, 0, out, es);
+  for (const auto& e : reads) {
+    const bool same = &e == &reads[5] && r == y && a.ldr == a.ldy;
+    if ((!same && overlaps(y, ybytes, e.p, e.bytes)) || overlaps(workspace, (int64_t)need, e.p, e.bytes))
+      return CONV_ERR_INVALID_ARG;
+  }
+  if (overlaps(y, ybytes, workspace, (int64_t)need)) return CONV_ERR_INVALID_ARG;
+  st = convsel::device_ready();
+  if (st != CONV_OK) return st;
+  return from_hip(convsel::launch_linear_int8(a, d->x_dtype, workspace, (hipStream_t)stream));
+}
+
+conv_status_t convsel_linear_int8_describe(const void* x, const void* w, const convsel_linear_int8_desc_t* desc,
+                                           char* buf, size_t len) {
+  const conv_status_t st = linear_int8_sizes(desc);
+  if (st != CONV_OK) return st;
+  if (!buf || len == 0) return CONV_ERR_INVALID_ARG;
+  convsel::linear_int8_describe(linear_int8_args(desc, x, nullptr, w, nullptr, nullptr, nullptr, nullptr),
+                                desc->x_dtype, buf, len);
+  return CONV_OK;
+}
+
+conv_status_t convsel_adjust_logits(const void* x, const int32_t* history, const int32_t* offsets,
+                                    const int32_t* prompt_lengths, const float* repetition, const float* presence,
+                                    const float* frequency, const float* bias, const uint32_t* mask, void* y,
+                                    const convsel_logits_desc_t* desc, void* stream) {
+  const convsel_logits_desc_t* d = desc;
+  if (!d || d->rows < 0 || d->rows > kInt31 || d->vocab < 1 || d->vocab > kInt31 || d->tokens < 0 ||
+      d->tokens > kInt31 || !dtype_ok(d->dtype))
+    return CONV_ERR_INVALID_ARG;
+  const int64_t words = (d->vocab + 31) / 32;
+  if (d->ldx < d->vocab || !stride_ok(d->ldx, d->rows) || d->ldy < d->vocab || !stride_ok(d->ldy, d->rows) ||
+      (bias && d->ldbias != 0 && (d->ldbias < d->vocab || !stride_ok(d->ldbias, d->rows))) ||
+      (mask && d->ldmask != 0 && (d->ldmask < words || !stride_ok(d->ldmask, d->rows))))
+    return CONV_ERR_INVALID_ARG;
+  if (d->rows == 0) return CONV_OK;
+  const int64_t es = esize(d->dtype), n = d->rows;
+  if (!x || !y || !aligned(x, es) || !aligned(y, es) || (history != nullptr) != (offsets != nullptr) ||
+      (!history && (prompt_lengths || repetition || presence || frequency)))
+    return CONV_ERR_INVALID_ARG;
+  const struct {
+    const void* p;
+    int64_t bytes;
+  } reads[8] = {{history, d->tokens * 4}, {offsets, (n + 1) * 4}, {prompt_lengths, n * 4}, {repetition, n * 4},
+                {presence, n * 4}, {frequency, n * 4}, {bias, bias ? span(n, d->ldbias, 1, 0, d->vocab, 4) : 0},
+                {mask, mask ? span(n, d->ldmask, 1, 0, words, 4) : 0}};
+  const int64_t ybytes = span(n, d->ldy, 1, 0, d->vocab, es);
+  for (const auto& e : reads)
+    if (!aligned(e.p, 4) || overlaps(y, ybytes, e.p, e.bytes)) return CONV_ERR_INVALID_ARG;
+  if (!(x == y && (n == 1 || d->ldx == d->ldy)) && overlaps(y, ybytes, x, span(n, d->ldx, 1, 0, d->vocab, es)))
+    return CONV_ERR_INVALID_ARG;
+  const conv_status_t st = convsel::device_ready();
+  if (st != CONV_OK) return st;
+  const convsel::LogitsArgs a = {x, history, offsets, prompt_lengths, repetition, presence, frequency, bias, mask, y,
+                                 n, d->vocab, d->tokens, d->ldx, d->ldy, d->ldbias, d->ldmask, d->dtype};
+  return from_hip(convsel::launch_adjust_logits(a, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,461 @@
+// Attention of packed prompts over their own keys and values, in fp32 and bf16.
+//
+// A workgroup of four waves has 128 rows of a key head (a row is a query and one
+// of the heads that share the key head), 32 a wave, and walks the keys that they
+// see in tiles of 64 (bf16) or 32 (fp32), whose keys and values go to LDS by DMA
+// as they lie in memory, a tile ahead: one barrier a tile.  Scores are K q^T in
+// blocks of 32 x 32, so that a lane ends with 16 keys of one row, in runs of
+// four, and feeds its weights to the second product, V^T P^T, without moving
+// them: in which order a product takes the keys does not matter while both
+// operands agree.  V's operand needs four keys of one column a lane, which the
+// transposing LDS read gives for bf16 and single words for fp32.
+//
+// In LDS a row's 16-byte units are permuted so that the rows that are read
+// together fall on different banks: unit u of row r lies at u ^ turn(r), where
+// turn() takes as many values as rows of U units meet on the same banks.
+//
+// Softmax in one pass, in powers of two (the scale carries log2 e): running
+// maximum m and sum l of a row, weights 2^(s - m).  bf16 calls multiply each
+// weight as two bf16 numbers, 16 bits: one number, 8 bits, is off by as much as
+// the result's own rounding.  fp32 calls use the fp32 matrix instructions.
+#include <stdio.h>
+
+#include <type_traits>
+
+#include "igemm_common.hpp"
+#include "lm_common.hpp"
+#include "lm_kernels.hpp"
+
+namespace convsel {
+namespace {
+
+using namespace igemm;
+using namespace lm;
+
+constexpr float kInf = __builtin_inff();
+constexpr int kWaves = 4, kRows = 32 * kWaves;
+
+struct PromptLaunch {
+  PromptArgs g;
+  int group, y_vec;
+  float scale;  // times log2 e
+  UnitRow units;
+};
+
+__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// Sizes of a tile: T elements, rows of 32 NC columns.
+template <typename T, int NC>
+struct Shape {
+  static constexpr int ES = elem<T>::bytes, UE = elem<T>::per16;
+  static constexpr int KT = ES == 2 ? 64 : 32, SB = KT / 32;  // keys, and blocks of 32 of them
+  static constexpr int RB = 32 * NC * ES, U = RB / 16;        // bytes and units of a row
+  static constexpr int QU = U / 2;                            // units of a lane's half of a row
+  static constexpr int TILE = KT * RB, NDMA = TILE / 1024 / kWaves;
+  __device__ static __forceinline__ int turn_k(int r) {
+    return U % 16 == 0 ? r & 15 : U % 8 == 0 ? (r >> 1) & 7 : (r >> 2) & 3;
+  }
+  // bf16: four rows, of which 64 bytes are read, meet; fp32: a row and the fourth from it.
+  __device__ static __forceinline__ int turn_v(int r) {
+    if constexpr (ES == 2) return U % 16 == 0 ? (r & 3) << 2 : U % 8 == 0 ? ((r >> 1) & 1) << 2 : 0;
+    return U % 16 == 0 ? ((r >> 2) & 1) << 3 : 0;
+  }
+};
+
+template <typename T, int NC>
+__global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void prompt_attention_kernel(
+    PromptLaunch a) {
+  typedef Shape<T, NC> S;
+  constexpr int ES = S::ES, UE = S::UE, KT = S::KT, SB = S::SB, RB = S::RB, U = S::U, QU = S::QU, TILE = S::TILE;
+  constexpr int NDMA = S::NDMA;
+  constexpr uint32_t kNowhere = 0xfffffff0u;  // beyond every buffer: zeros
+  __shared__ __align__(1024) char lds[4 * TILE];  // keys of two tiles, then values
+  __shared__ int spoilt[kWaves];
+  const PromptArgs& g = a.g;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, half = lane >> 5;
+  const int head = blockIdx.x;  // heads vary fastest: eight of them have an XCD's L2 each
+  const Unit un = find_unit<true>(a.units, g.offsets, g.offsets);
+  const Span sp = un.span;
+  const int rows = sp.count * a.group;
+  const int ntile = (rows + kRows - 1) / kRows;
+  const uint32_t lds0 = lds_address(lds);
+
+  // DMA instruction d of this wave fills units 64 (wave NDMA + d) .. of a tile, keys and values alike.
+  int drow[NDMA];
+  uint32_t kvo[NDMA], vvo[NDMA];
+  const uint32_t kstep = static_cast<uint32_t>(g.k_token * ES), vstep = static_cast<uint32_t>(g.v_token * ES);
+  const int dim_units = (g.dim + UE - 1) / UE;
+#pragma unroll
+  for (int d = 0; d < NDMA; ++d) {
+    const int s = (wave * NDMA + d) * 64 + lane, r = s / U, p = s % U;
+    drow[d] = r;
+    const int ku = p ^ S::turn_k(r), vu = p ^ S::turn_v(r);
+    kvo[d] = ku < dim_units ? r * kstep + ku * 16 : kNowhere;
+    vvo[d] = vu < dim_units ? r * vstep + vu * 16 : kNowhere;
+  }
+  // Tile of keys j0 .. of the sequence; rows behind its last key are zeros, whatever lies there.
+  auto issue = [&](int buf, int j0) {
+    const int n = min(KT, sp.count - j0);
+    const int64_t tok = sp.first + j0;
+    const u32x4_t kr = dma_rsrc(reinterpret_cast<const T*>(g.k) + tok * g.k_token + head * g.k_head,
+                                (n - 1) * kstep + dim_units * 16);
+    const u32x4_t vr = dma_rsrc(reinterpret_cast<const T*>(g.v) + tok * g.v_token + head * g.v_head,
+                                (n - 1) * vstep + dim_units * 16);
+#pragma unroll
+    for (int d = 0; d < NDMA; ++d) {
+      const uint32_t at = lds0 + buf * TILE + (wave * NDMA + d) * 1024;
+      dma16(kr, at, drow[d] < n ? kvo[d] : kNowhere, 0);
+      dma16(vr, at + 2 * TILE, drow[d] < n ? vvo[d] : kNowhere, 0);
+    }
+  };
+
+  for (int nt = un.index; nt < ntile; nt += un.count) {
+    const int tile = ntile - 1 - nt;  // under a causal mask the last rows have the most keys: they start first
+    const int r0 = tile * kRows;
+    // Keys that tokens t0..t1 see between them, and that every one of them sees.
+    auto seen_by = [&](int t0, int t1, int& lo, int& hi, int& in_lo, int& in_hi) {
+      hi = g.causal ? t1 + 1 : sp.count;
+      in_hi = g.causal ? t0 + 1 : sp.count;
+      lo = g.window > 0 ? max(0, t0 - g.window + 1) : 0;
+      in_lo = g.window > 0 ? max(0, t1 - g.window + 1) : 0;
+    };
+    int lo, hi, in_lo, in_hi;
+    seen_by(r0 / a.group, min(r0 + kRows - 1, rows - 1) / a.group, lo, hi, in_lo, in_hi);
+    const int kt0 = lo / KT, kt1 = (hi + KT - 1) / KT;
+    issue(0, kt0 * KT);
+    // This wave's rows and this lane's; rows past the last one work on the last one's values.
+    const int w0 = min(r0 + wave * 32, rows - 1), w1 = min(r0 + wave * 32 + 31, rows - 1);
+    int wlo, whi;
+    seen_by(w0 / a.group, w1 / a.group, wlo, whi, in_lo, in_hi);
+    const bool idle = r0 + wave * 32 >= rows;
+    const int row = min(r0 + wave * 32 + col, rows - 1);
+    const int tok = row / a.group, hq = head * a.group + row % a.group;
+    const int row_hi = g.causal ? tok + 1 : sp.count;
+    const int row_lo = g.window > 0 ? max(0, tok - g.window + 1) : 0;
+
+    // The queries: lane (row, half) holds units half, half + 2 ... of its row.
+    vec16 qf[QU];
+    {
+      const T* src = reinterpret_cast<const T*>(g.q) + (sp.first + tok) * g.q_token + hq * g.q_head;
+#pragma unroll
+      for (int u = 0; u < QU; ++u) {
+        const int d = (2 * u + half) * UE;
+        qf[u] = d < g.dim ? load16(src + d) : vec16_zero();
+      }
+      // The sign of the scale goes with the query: scores then grow with the products.
+      if (a.scale < 0.f) {
+#pragma unroll
+        for (int u = 0; u < QU; ++u)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) qf[u].d[x] ^= ES == 2 ? 0x80008000u : 0x80000000u;
+      }
+    }
+    // Never zero: a masked score of -inf times it stays -inf.
+    const float cs = fmaxf(fabsf(a.scale), 0x1p-126f);
+    f32x16_t o[NC];
+#pragma unroll
+    for (int i = 0; i < NC; ++i) o[i] = zero16();
+    float m = -kInf, l = 0.f;
+
+    auto compute = [&](int buf, int j0, bool masked, auto exact_c) {
+      const char* kl = lds + buf * TILE;
+      const char* vl = lds + (2 + buf) * TILE;
+      f32x16_t sc[SB];
+#pragma unroll
+      for (int b = 0; b < SB; ++b) sc[b] = zero16();
+#pragma unroll
+      for (int u = 0; u < QU; ++u)
+#pragma unroll
+        for (int b = 0; b < SB; ++b) {
+          const vec16 kf = *reinterpret_cast<const vec16*>(kl + (32 * b + col) * RB + (((2 * u + half) ^ S::turn_k(col)) << 4));
+          mfma_32x32<T>(sc[b], kf, qf[u]);
+        }
+      if (masked) {
+#pragma unroll
+        for (int b = 0; b < SB; ++b)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int j = j0 + 32 * b + 8 * (v >> 2) + 4 * half + (v & 3);
+            if (!(j >= row_lo && j < row_hi)) sc[b][v] = -kInf;
+          }
+      }
+      float most = -kInf;
+#pragma unroll
+      for (int b = 0; b < SB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) most = fmaxf(most, sc[b][v]);
+      most = fmaxf(most, __shfl_xor(most, 32)) * cs;
+      if (__any(most > m)) {
+        const float mn = fmaxf(m, most);
+        const float s = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= s;
+#pragma unroll
+        for (int i = 0; i < NC; ++i) o[i] *= s;
+      }
+      const float from = m == -kInf ? 0.f : m;  // a row with nothing yet: its weights are 2^-inf
+#pragma unroll
+      for (int b = 0; b < SB; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          sc[b][v] = __builtin_amdgcn_exp2f(fmaf(sc[b][v], cs, -from));
+          l += sc[b][v];
+        }
+      if constexpr (decltype(exact_c)::value) {
+#pragma unroll 1
+        for (int k = 0; k < KT; ++k) {
+          const int v = 4 * ((k & 31) >> 3) + (k & 3);
+          float mine = sc[0][v];
+          if constexpr (SB == 2) mine = k < 32 ? mine : sc[1][v];
+          const float w = __shfl(mine, col + 8 * (k & 4));
+          if (j0 + k < row_lo || j0 + k >= row_hi) continue;
+#pragma unroll
+          for (int i = 0; i < NC; ++i)
+#pragma unroll
+            for (int v4 = 0; v4 < 4; ++v4) {
+              const int d = 32 * i + 8 * v4 + 4 * half;
+              const char* at = vl + k * RB + (((d / UE) ^ S::turn_v(k)) << 4) + d % UE * ES;
+              float z[4];
+              if constexpr (ES == 2) {
+                const uint2 t = *reinterpret_cast<const uint2*>(at);
+                z[0] = low_half(t.x); z[1] = high_half(t.x); z[2] = low_half(t.y); z[3] = high_half(t.y);
+              } else {
+                const float4 t = *reinterpret_cast<const float4*>(at);
+                z[0] = t.x; z[1] = t.y; z[2] = t.z; z[3] = t.w;
+              }
+#pragma unroll
+              for (int x = 0; x < 4; ++x) o[i][4 * v4 + x] = fmaf(w, z[x], o[i][4 * v4 + x]);
+            }
+        }
+        return;
+      }
+      if constexpr (ES == 2) {
+        // Lane i16 of sixteen reads 8 bytes; their 4 keys x 16 columns come back transposed.
+        const int i16 = lane & 15, key = 4 * half + (i16 >> 2);
+        const int unit = 2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1);
+        typedef __attribute__((address_space(3))) v4s_t* lds_t;
+        auto value = [&](int kb, int i) {  // 16 keys from 16 kb on, columns 32 i ..
+          vec16 r;
+#pragma unroll
+          for (int p = 0; p < 2; ++p) {
+            const char* at = vl + (16 * kb + 8 * p + key) * RB + (((4 * i + unit) ^ S::turn_v(key)) << 4) + (i16 & 1) * 8;
+            const v4s_t t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(uintptr_t)lds_address(at));
+            uint2 w;
+            __builtin_memcpy(&w, &t, 8);
+            r.d[2 * p] = w.x;
+            r.d[2 * p + 1] = w.y;
+          }
+          return r;
+        };
+#pragma unroll
+        for (int kb = 0; kb < 2 * SB; ++kb) {
+          vec16 wh, wl;
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int b = kb >> 1, v = 8 * (kb & 1) + 2 * x;
+            const float w0 = sc[b][v], w1 = sc[b][v + 1];
+            wh.d[x] = f32x2_to_bf16x2(w0, w1);
+            wl.d[x] = f32x2_to_bf16x2(w0 - low_half(wh.d[x]), w1 - high_half(wh.d[x]));
+          }
+#pragma unroll
+          for (int i = 0; i < NC; ++i) {
+            const vec16 vf = value(kb, i);
+            mfma_32x32<T>(o[i], vf, wh);
+            mfma_32x32<T>(o[i], vf, wl);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int key = 8 * (v >> 2) + 4 * half + (v & 3);
+#pragma unroll
+          for (int i = 0; i < NC; ++i) {
+            const float z = *reinterpret_cast<const float*>(
+                vl + key * RB + (((8 * i + (col >> 2)) ^ S::turn_v(key)) << 4) + (col & 3) * 4);
+            o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(z, sc[0][v], o[i], 0, 0, 0);
+          }
+        }
+      }
+    };
+
+    // Values that are not finite spoil products that they have no part in: a weight of zero, where they are hidden, or
+    // the second half of one, which may be zero or negative.  Rows that end so go once more, adding up key by key what
+    // they see.
+    auto walk = [&](auto exact_c) {
+      for (int kt = kt0; kt < kt1; ++kt) {
+        // This tile's DMAs are in; behind the barrier everyone's are, and all are done with the other buffer.
+        CONVSEL_WAIT_VMCNT(0);
+        lds_sync();
+        const int buf = (kt - kt0) & 1, j0 = kt * KT;
+        if (kt + 1 < kt1) issue(buf ^ 1, j0 + KT);
+        if (idle || j0 >= whi || j0 + KT <= wlo) continue;
+        compute(buf, j0, !(j0 >= in_lo && j0 + KT <= in_hi), exact_c);
+      }
+    };
+    walk(std::false_type{});
+    float odd = 0.f;  // NaN if a result is not finite
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) odd = fmaf(o[i][v], 0.f, odd);
+    const int again = __any(odd != 0.f);
+    if (lane == 0) spoilt[wave] = again;
+    lds_sync();  // also before another tile is fetched
+    if (spoilt[0] | spoilt[1] | spoilt[2] | spoilt[3]) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) o[i] = zero16();
+      m = -kInf;
+      l = 0.f;
+      issue(0, kt0 * KT);
+      walk(std::true_type{});
+      lds_sync();
+    }
+
+    // Lane (row, half) holds columns 32 i + 8 (v / 4) + 4 half + v % 4.
+    l += __shfl_xor(l, 32);
+    if (r0 + wave * 32 + col < rows) {
+      const float inv = 1.f / l;
+      T* dst = reinterpret_cast<T*>(g.y) + (sp.first + tok) * g.y_token + hq * g.y_head;
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4) {
+          const int d = 32 * i + 8 * v4 + 4 * half;
+          float v[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) v[x] = o[i][4 * v4 + x] * inv;
+          if (a.y_vec) {
+            if (d < g.dim) {
+              if constexpr (ES == 4)
+                *reinterpret_cast<float4*>(dst + d) = make_float4(v[0], v[1], v[2], v[3]);
+              else
+                *reinterpret_cast<uint2*>(dst + d) = make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]));
+            }
+          } else {
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+              if (d + x < g.dim) elem<T>::store(dst + d + x, v[x]);
+          }
+        }
+    }
+  }
+}
+
+// Rows that cannot be read in 16-byte units where they lie, copied to [token][head] rows of whole ones.
+template <typename T>
+__global__ __launch_bounds__(256) void prompt_pack_kernel(const T* src, int64_t token, int64_t head, int64_t tokens,
+                                                          int heads, int dim, int units, T* dst) {
+  constexpr int UE = elem<T>::per16;
+  const int64_t all = tokens * heads * units;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all;
+       i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t r = i / units, t = r / heads, h = r - t * heads;
+    const int d = static_cast<int>(i - r * units) * UE;
+    const T* row = src + t * token + h * head;
+    uint32_t e[UE];
+#pragma unroll
+    for (int x = 0; x < UE; ++x) {
+      const uint32_t bits = load_bits(row + min(d + x, dim - 1));
+      e[x] = d + x < dim ? bits : 0u;
+    }
+    vec16 v;
+    pack16<T>(v, e);
+    store16(dst + i * UE, v);
+  }
+}
+
+int64_t elem_bytes(const PromptArgs& a) { return a.dtype == CONV_F32 ? 4 : 2; }
+int64_t row_units(const PromptArgs& a) { return (a.dim * elem_bytes(a) + 15) / 16; }
+
+// Whether rows are no whole 16-byte units, or so far apart that a tile of 64 of them does not fit a buffer.
+bool needs_pack(const PromptArgs& a, const void* p, int64_t token, int64_t head) {
+  const int64_t es = elem_bytes(a), per = 16 / es, far = ((int64_t)1 << 31) / 64 / es - 256;
+  return a.dim % per != 0 || token % per != 0 || head % per != 0 || (uintptr_t)p % 16 != 0 || token > far;
+}
+
+// Bytes of the copies of q, k and v.
+struct Packs {
+  size_t q, k, v;
+};
+Packs packs_of(const PromptArgs& a) {
+  auto bytes = [&](int heads) { return ((size_t)(a.tokens * heads * row_units(a) * 16) + 255) / 256 * 256; };
+  Packs p;
+  p.q = needs_pack(a, a.q, a.q_token, a.q_head) ? bytes(a.q_heads) : 0;
+  p.k = needs_pack(a, a.k, a.k_token, a.k_head) ? bytes(a.kv_heads) : 0;
+  p.v = needs_pack(a, a.v, a.v_token, a.v_head) ? bytes(a.kv_heads) : 0;
+  return p;
+}
+
+template <typename T>
+void pack(const PromptArgs& g, const void*& src, int64_t& token, int64_t& head, int heads, size_t bytes, char*& ws,
+          hipStream_t st) {
+  if (bytes == 0) return;
+  const int64_t units = row_units(g), blocks = (g.tokens * heads * units + 255) / 256;
+  hipLaunchKernelGGL(prompt_pack_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, st,
+                     (const T*)src, token, head, g.tokens, heads, g.dim, (int)units, (T*)ws);
+  src = ws;
+  head = units * elem<T>::per16;
+  token = heads * head;
+  ws += bytes;
+}
+
+template <typename T, int NC>
+hipError_t launch_nc(PromptLaunch a, hipStream_t st) {
+  each_grid(a.units, [&](const UnitRow& r, unsigned n) {
+    a.units = r;
+    hipLaunchKernelGGL((prompt_attention_kernel<T, NC>), dim3((unsigned)a.g.kv_heads, 1, n), dim3(64 * kWaves), 0, st, a);
+  });
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch(const PromptArgs& g, void* workspace, hipStream_t st) {
+  PromptLaunch a;
+  a.g = g;
+  const Packs p = packs_of(g);
+  char* ws = (char*)workspace;
+  pack<T>(g, a.g.q, a.g.q_token, a.g.q_head, g.q_heads, p.q, ws, st);
+  pack<T>(g, a.g.k, a.g.k_token, a.g.k_head, g.kv_heads, p.k, ws, st);
+  pack<T>(g, a.g.v, a.g.v_token, a.g.v_head, g.kv_heads, p.v, ws, st);
+  a.group = g.q_heads / g.kv_heads;
+  a.scale = g.scale * 1.4426950408889634f;
+  a.y_vec = g.dim % 4 == 0 && g.y_token % 4 == 0 && g.y_head % 4 == 0 && (uintptr_t)g.y % (4 * sizeof(T)) == 0;
+  convsel_kv_batch_t b = {};
+  b.seqs = g.seqs;
+  b.tokens = g.tokens;
+  int shift = 0;
+  while ((1 << shift) < kRows) ++shift;
+  a.units = unit_row(b, a.group, shift);
+  switch ((g.dim + 31) / 32) {
+    case 1: return launch_nc<T, 1>(a, st);
+    case 2: return launch_nc<T, 2>(a, st);
+    case 3: return launch_nc<T, 3>(a, st);
+    case 4: return launch_nc<T, 4>(a, st);
+    case 5: return launch_nc<T, 5>(a, st);
+    case 6: return launch_nc<T, 6>(a, st);
+    case 7: return launch_nc<T, 7>(a, st);
+    default: return launch_nc<T, 8>(a, st);
+  }
+}
+
+}  // namespace
+
+size_t prompt_attention_workspace(const PromptArgs& a) {
+  const Packs p = packs_of(a);
+  return p.q + p.k + p.v;
+}
+
+hipError_t launch_prompt_attention(const PromptArgs& a, void* workspace, hipStream_t stream) {
+  return a.dtype == CONV_F32 ? launch<float>(a, workspace, stream) : launch<bf16_t>(a, workspace, stream);
+}
+
+void prompt_attention_describe(const PromptArgs& a, char* buf, size_t len) {
+  snprintf(buf, len, "prompt_attention kernels=%sprompt_attention_kernel rows=%d keys=%d workspace=%zu",
+           prompt_attention_workspace(a) ? "prompt_pack_kernel;" : "", kRows, a.dtype == CONV_F32 ? 32 : 64,
+           prompt_attention_workspace(a));
+}
+
+}  // namespace convsel
