@@ -1,9 +1,9 @@
 // Penalties of repeated tokens, biases and masks on the logits of a batch.
 //
-// A workgroup owns kChunk neighbouring tokens of a row.  It counts in LDS how
-// often its row's history holds each of them (whole numbers, in any order), then
-// passes once over its logits.  What bounds it: traffic, and the history, which
-// every workgroup of a row reads from the caches.
+// A workgroup owns 2048 STEPS neighbouring tokens of a row, eight at a time a
+// thread, whose logits are on their way while it counts in LDS how often its row's
+// history holds each of them (whole numbers, in any order).  What bounds it:
+// traffic, and the history, which every workgroup of a row reads from the caches.
 #include "lm_common.hpp"
 #include "lm_kernels.hpp"
 
@@ -12,16 +12,49 @@ namespace {
 
 using namespace lm;
 
-constexpr int kThreads = 256, kChunk = 8192;
+constexpr int kThreads = 256, kEach = 8;
 constexpr uint32_t kSeen = 0x80000000u;  // the prompt holds it; the bits below count generated ones
 
+// Eight values; rows lie on any alignment of elements, which wide loads and stores of global memory may too.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void adjust_logits_kernel(LogitsArgs a, int64_t chunks, int vec) {
-  constexpr int N = 8;  // tokens of a step of a thread
-  __shared__ uint32_t count[kChunk];
+__device__ __forceinline__ void get8(const T* p, float (&z)[8]) {
+  constexpr int UE = elem<T>::per16;
+#pragma unroll
+  for (int u = 0; u < 8 / UE; ++u) {
+    vec16 v;
+    __builtin_memcpy(&v, p + u * UE, 16);
+#pragma unroll
+    for (int e = 0; e < UE; ++e) z[u * UE + e] = elem<T>::to_f32(vec16_get<T>(v, e));
+  }
+}
+__device__ __forceinline__ void put8(float* p, const float (&z)[8]) { __builtin_memcpy(p, z, 32); }
+__device__ __forceinline__ void put8(bf16_t* p, const float (&z)[8]) {
+  vec16 v;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) v.d[w] = f32x2_to_bf16x2(z[2 * w], z[2 * w + 1]);
+  __builtin_memcpy(p, &v, 16);
+}
+
+template <typename T, int STEPS>
+__global__ __launch_bounds__(kThreads) void adjust_logits_kernel(LogitsArgs a, int64_t chunks) {
+  constexpr int CHUNK = kThreads * kEach * STEPS;
+  extern __shared__ __align__(16) uint32_t count[];  // CHUNK of them, with a history
   for (int64_t unit = blockIdx.x; unit < chunks * a.rows; unit += gridDim.x) {
-    const int64_t row = unit / chunks, c0 = (unit - row * chunks) * kChunk;
-    const int width = static_cast<int>(min(a.vocab - c0, static_cast<int64_t>(kChunk)));
+    const int64_t row = unit / chunks, c0 = (unit - row * chunks) * CHUNK;
+    const int width = static_cast<int>(min(a.vocab - c0, static_cast<int64_t>(CHUNK)));
+    const T* x = reinterpret_cast<const T*>(a.x) + row * a.ldx + c0;
+    T* y = reinterpret_cast<T*>(a.y) + row * a.ldy + c0;
+    float z[STEPS][kEach];
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int i = (s * kThreads + threadIdx.x) * kEach;
+      if (i + kEach <= width) {
+        get8(x + i, z[s]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) z[s][e] = i + e < width ? elem<T>::load(x + i + e) : 0.f;
+      }
+    }
     int first = 0, end = 0;
     if (a.history) {
       const int limit = static_cast<int>(a.tokens);
@@ -30,94 +63,99 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(LogitsArgs a, i
     }
     const bool counted = end > first;  // uniform
     if (counted) {
-      const int prompt = a.prompt_lengths ? clampi(a.prompt_lengths[row], 0, end - first) : 0;
-      for (int i = threadIdx.x; i < width; i += kThreads) count[i] = 0;
-      __syncthreads();
-      for (int i = first + static_cast<int>(threadIdx.x); i < end; i += kThreads) {
-        const int64_t at = a.history[i] - c0;
-        if (at >= 0 && at < width) {
-          if (i - first < prompt)
-            atomicOr(&count[at], kSeen);
-          else
-            atomicAdd(&count[at], 1u);
-        }
-      }
-      __syncthreads();
-    }
-    const float r = a.repetition ? a.repetition[row] : 1.f;
-    const float p = a.presence ? a.presence[row] : 0.f, f = a.frequency ? a.frequency[row] : 0.f;
-    const T* x = reinterpret_cast<const T*>(a.x) + row * a.ldx + c0;
-    T* y = reinterpret_cast<T*>(a.y) + row * a.ldy + c0;
-    const float* bias = a.bias ? a.bias + row * a.ldbias + c0 : nullptr;
-    const uint32_t* mask = a.mask ? a.mask + row * a.ldmask + c0 / 32 : nullptr;
-    for (int i = threadIdx.x * N; i < width; i += kThreads * N) {
-      const int n = min(N, width - i);
-      const bool whole = vec && n == N;
-      float z[N];
-      if (whole) {
-        constexpr int UE = elem<T>::per16;
+      const int generated = first + (a.prompt_lengths ? clampi(a.prompt_lengths[row], 0, end - first) : 0);
 #pragma unroll
-        for (int u = 0; u < N / UE; ++u) {
-          const vec16 v = load16(x + i + u * UE);
+      for (int s = 0; s < 2 * STEPS; ++s)
+        *reinterpret_cast<uint4*>(count + (s * kThreads + threadIdx.x) * 4) = make_uint4(0, 0, 0, 0);
+      lds_sync();
+      for (int64_t i0 = first + static_cast<int>(threadIdx.x); i0 < end; i0 += 4 * kThreads) {
+        int64_t at[4];
 #pragma unroll
-          for (int e = 0; e < UE; ++e) z[u * UE + e] = elem<T>::to_f32(vec16_get<T>(v, e));
-        }
-      } else {
+        for (int n = 0; n < 4; ++n) at[n] = a.history[min(i0 + n * kThreads, static_cast<int64_t>(end) - 1)] - c0;
 #pragma unroll
-        for (int e = 0; e < N; ++e) z[e] = elem<T>::load(x + i + min(e, n - 1));
-      }
-      if (counted) {
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const uint32_t c = count[i + min(e, n - 1)];
-          if (c != 0) {
-            if (a.repetition) z[e] = z[e] > 0.f ? z[e] / r : z[e] * r;
-            const uint32_t made = c & ~kSeen;
-            if (made != 0) z[e] -= fmaf(f, static_cast<float>(made), p);
+        for (int n = 0; n < 4; ++n) {
+          const int64_t i = i0 + n * kThreads;
+          if (i < end && at[n] >= 0 && at[n] < width) {
+            if (i < generated)
+              atomicOr(&count[at[n]], kSeen);
+            else
+              atomicAdd(&count[at[n]], 1u);
           }
         }
       }
-      if (bias) {
+      lds_sync();
+    }
+    const float r = a.repetition ? a.repetition[row] : 1.f;
+    const float p = a.presence ? a.presence[row] : 0.f, f = a.frequency ? a.frequency[row] : 0.f;
+    const float* bias = a.bias ? a.bias + row * a.ldbias + c0 : nullptr;
+    const uint32_t* mask = a.mask ? a.mask + row * a.ldmask + c0 / 32 : nullptr;
 #pragma unroll
-        for (int e = 0; e < N; ++e) z[e] += bias[i + min(e, n - 1)];
+    for (int s = 0; s < STEPS; ++s) {
+      const int i = (s * kThreads + threadIdx.x) * kEach;
+      if (i >= width) break;
+      float(&v)[kEach] = z[s];
+      if (counted) {
+        uint32_t c[kEach];
+        *reinterpret_cast<uint4*>(c) = *reinterpret_cast<const uint4*>(count + i);
+        *reinterpret_cast<uint4*>(c + 4) = *reinterpret_cast<const uint4*>(count + i + 4);
+        if ((c[0] | c[1] | c[2] | c[3] | c[4] | c[5] | c[6] | c[7]) != 0) {
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) {
+            if (c[e] == 0) continue;
+            if (a.repetition) v[e] = v[e] > 0.f ? v[e] / r : v[e] * r;
+            const uint32_t made = c[e] & ~kSeen;
+            if (made != 0) v[e] -= fmaf(f, static_cast<float>(made), p);
+          }
+        }
+      }
+      const bool whole = i + kEach <= width;
+      if (bias) {
+        float b[kEach];
+        if (whole) {
+          get8(bias + i, b);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) b[e] = i + e < width ? bias[i + e] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) v[e] += b[e];
       }
       if (mask) {
         const uint32_t bits = mask[i >> 5] >> (i & 31);
 #pragma unroll
-        for (int e = 0; e < N; ++e) z[e] = (bits >> e) & 1u ? z[e] : -__builtin_inff();
+        for (int e = 0; e < kEach; ++e) v[e] = (bits >> e) & 1u ? v[e] : -__builtin_inff();
       }
       if (whole) {
-        if constexpr (sizeof(T) == 4) {
-          *reinterpret_cast<float4*>(y + i) = make_float4(z[0], z[1], z[2], z[3]);
-          *reinterpret_cast<float4*>(y + i + 4) = make_float4(z[4], z[5], z[6], z[7]);
-        } else {
-          vec16 v;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) v.d[w] = f32x2_to_bf16x2(z[2 * w], z[2 * w + 1]);
-          store16(y + i, v);
-        }
+        put8(y + i, v);
       } else {
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (e < n) elem<T>::store(y + i + e, z[e]);
+        for (int e = 0; e < kEach; ++e)
+          if (i + e < width) elem<T>::store(y + i + e, v[e]);
       }
     }
-    __syncthreads();  // before the next row's counts
+    if (counted) lds_sync();  // before the next row's counts
   }
+}
+
+template <typename T, int STEPS>
+hipError_t launch(const LogitsArgs& a, hipStream_t st) {
+  constexpr int chunk = kThreads * kEach * STEPS;
+  const int64_t chunks = (a.vocab + chunk - 1) / chunk, units = chunks * a.rows;
+  hipLaunchKernelGGL((adjust_logits_kernel<T, STEPS>), dim3((unsigned)(units < (1 << 20) ? units : 1 << 20)),
+                     dim3(kThreads), a.history ? chunk * 4 : 0, st, a, chunks);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_steps(const LogitsArgs& a, hipStream_t st) {
+  // Few tokens in all: more workgroups, of fewer tokens each.
+  return a.rows * ((a.vocab + 8191) / 8192) < 512 ? launch<T, 1>(a, st) : launch<T, 4>(a, st);
 }
 
 }  // namespace
 
 hipError_t launch_adjust_logits(const LogitsArgs& a, hipStream_t stream) {
-  const int64_t chunks = (a.vocab + kChunk - 1) / kChunk, units = chunks * a.rows;
-  const dim3 grid((unsigned)(units < (1 << 20) ? units : 1 << 20));
-  const int64_t per = a.dtype == CONV_F32 ? 4 : 8;
-  const int vec = a.ldx % per == 0 && a.ldy % per == 0 && (uintptr_t)a.x % 16 == 0 && (uintptr_t)a.y % 16 == 0;
-  if (a.dtype == CONV_F32)
-    hipLaunchKernelGGL(adjust_logits_kernel<float>, grid, dim3(kThreads), 0, stream, a, chunks, vec);
-  else
-    hipLaunchKernelGGL(adjust_logits_kernel<bf16_t>, grid, dim3(kThreads), 0, stream, a, chunks, vec);
-  return hipGetLastError();
+  return a.dtype == CONV_F32 ? launch_steps<float>(a, stream) : launch_steps<bf16_t>(a, stream);
 }
 
 }  // namespace convsel
