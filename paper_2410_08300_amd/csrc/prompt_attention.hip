@@ -40,10 +40,31 @@ struct PromptLaunch {
   int group, y_vec;
   float scale;  // times log2 e
   UnitRow units;
+  uint32_t magic, shift;  // row / group = row * magic >> shift
+
+  // magic = ceil(2^shift / group), shift = 31 + ceil(log2 group): exact for rows below 2^31.
+  __device__ __forceinline__ int token_of(int row) const {
+    return static_cast<int>((static_cast<uint64_t>(static_cast<uint32_t>(row)) * magic) >> shift);
+  }
 };
+
+typedef __attribute__((address_space(3))) char lds_char_t;
+typedef const __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
 
 __device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// The largest of three, of which the compiler would first quiet signalling NaN, an operation each.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm volatile("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+// w less a number of a pair of bf16, in one operation: the pair's product with (-1, 0) or (0, -1) added to w.
+typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ float less(float w, uint32_t pair, uint32_t which) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2v_t, pair), __builtin_bit_cast(bf16x2v_t, which), w,
+                                         false);
+}
 
 // Sizes of a tile: T elements, rows of 32 NC columns.
 template <typename T, int NC>
@@ -69,6 +90,7 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
   typedef Shape<T, NC> S;
   constexpr int ES = S::ES, UE = S::UE, KT = S::KT, SB = S::SB, RB = S::RB, U = S::U, QU = S::QU, TILE = S::TILE;
   constexpr int NDMA = S::NDMA;
+  constexpr bool PIPED = ES == 2;
   constexpr uint32_t kNowhere = 0xfffffff0u;  // beyond every buffer: zeros
   __shared__ __align__(1024) char lds[4 * TILE];  // keys of two tiles, then values
   __shared__ int spoilt[kWaves];
@@ -83,264 +105,408 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
   const int ntile = (rows + kRows - 1) / kRows;
   const uint32_t lds0 = lds_address(lds);
 
-  // DMA instruction d of this wave fills units 64 (wave NDMA + d) .. of a tile, keys and values alike.
-  int drow[NDMA];
-  uint32_t kvo[NDMA], vvo[NDMA];
+  // DMA instruction d of this wave fills units 64 (4 d + wave) .. of a tile, keys and values alike.  Where a row's
+  // units divide 256 and rows 16 apart are turned alike, instructions differ by whole rows only.
+  constexpr bool EVEN = 256 % U == 0 && 256 / U % 16 == 0;
+  constexpr int ND = EVEN ? 1 : NDMA, STEP = EVEN ? 256 / U : 0;
+  int drow[ND];
+  uint32_t kvo[ND], vvo[ND];
   const uint32_t kstep = static_cast<uint32_t>(g.k_token * ES), vstep = static_cast<uint32_t>(g.v_token * ES);
   const int dim_units = (g.dim + UE - 1) / UE;
 #pragma unroll
-  for (int d = 0; d < NDMA; ++d) {
-    const int s = (wave * NDMA + d) * 64 + lane, r = s / U, p = s % U;
+  for (int d = 0; d < ND; ++d) {
+    const int s = (4 * d + wave) * 64 + lane, r = s / U, p = s % U;
     drow[d] = r;
     const int ku = p ^ S::turn_k(r), vu = p ^ S::turn_v(r);
     kvo[d] = ku < dim_units ? r * kstep + ku * 16 : kNowhere;
     vvo[d] = vu < dim_units ? r * vstep + vu * 16 : kNowhere;
   }
   // Tile of keys j0 .. of the sequence; rows behind its last key are zeros, whatever lies there.
-  auto issue = [&](int buf, int j0) {
+  auto issue = [&](int buf, int j0, bool values) {
     const int n = min(KT, sp.count - j0);
     const int64_t tok = sp.first + j0;
-    const u32x4_t kr = dma_rsrc(reinterpret_cast<const T*>(g.k) + tok * g.k_token + head * g.k_head,
-                                (n - 1) * kstep + dim_units * 16);
-    const u32x4_t vr = dma_rsrc(reinterpret_cast<const T*>(g.v) + tok * g.v_token + head * g.v_head,
-                                (n - 1) * vstep + dim_units * 16);
+    const T* src = values ? reinterpret_cast<const T*>(g.v) + tok * g.v_token + head * g.v_head
+                          : reinterpret_cast<const T*>(g.k) + tok * g.k_token + head * g.k_head;
+    const uint32_t step = values ? vstep : kstep;
+    const u32x4_t r = dma_rsrc(src, (n - 1) * step + dim_units * 16);
 #pragma unroll
     for (int d = 0; d < NDMA; ++d) {
-      const uint32_t at = lds0 + buf * TILE + (wave * NDMA + d) * 1024;
-      dma16(kr, at, drow[d] < n ? kvo[d] : kNowhere, 0);
-      dma16(vr, at + 2 * TILE, drow[d] < n ? vvo[d] : kNowhere, 0);
+      const uint32_t at = lds0 + (buf + (values ? 2 : 0)) * TILE + (4 * d + wave) * 1024;
+      const uint32_t vo = values ? vvo[EVEN ? 0 : d] : kvo[EVEN ? 0 : d];
+      if constexpr (EVEN)
+        dma16(r, at, drow[0] + d * STEP < n ? vo : kNowhere, d * STEP < n ? d * STEP * step : 0);
+      else
+        dma16(r, at, drow[d] < n ? vo : kNowhere, 0);
     }
   };
 
-  for (int nt = un.index; nt < ntile; nt += un.count) {
-    const int tile = ntile - 1 - nt;  // under a causal mask the last rows have the most keys: they start first
-    const int r0 = tile * kRows;
-    // Keys that tokens t0..t1 see between them, and that every one of them sees.
-    auto seen_by = [&](int t0, int t1, int& lo, int& hi, int& in_lo, int& in_hi) {
-      hi = g.causal ? t1 + 1 : sp.count;
-      in_hi = g.causal ? t0 + 1 : sp.count;
-      lo = g.window > 0 ? max(0, t0 - g.window + 1) : 0;
-      in_lo = g.window > 0 ? max(0, t1 - g.window + 1) : 0;
-    };
-    int lo, hi, in_lo, in_hi;
-    seen_by(r0 / a.group, min(r0 + kRows - 1, rows - 1) / a.group, lo, hi, in_lo, in_hi);
-    const int kt0 = lo / KT, kt1 = (hi + KT - 1) / KT;
-    issue(0, kt0 * KT);
-    // This wave's rows and this lane's; rows past the last one work on the last one's values.
-    const int w0 = min(r0 + wave * 32, rows - 1), w1 = min(r0 + wave * 32 + 31, rows - 1);
-    int wlo, whi;
-    seen_by(w0 / a.group, w1 / a.group, wlo, whi, in_lo, in_hi);
-    const bool idle = r0 + wave * 32 >= rows;
-    const int row = min(r0 + wave * 32 + col, rows - 1);
-    const int tok = row / a.group, hq = head * a.group + row % a.group;
-    const int row_hi = g.causal ? tok + 1 : sp.count;
-    const int row_lo = g.window > 0 ? max(0, tok - g.window + 1) : 0;
+  if (un.index >= ntile) return;  // uniform
+  // Every tile of rows has a unit.  Under a causal mask the last rows have the most keys: they start first.
+  const int tile = ntile - 1 - un.index;
+  const int r0 = tile * kRows;
+  // Keys that tokens t0..t1 see between them, and that every one of them sees.
+  auto seen_by = [&](int t0, int t1, int& lo, int& hi, int& in_lo, int& in_hi) {
+    hi = g.causal ? t1 + 1 : sp.count;
+    in_hi = g.causal ? t0 + 1 : sp.count;
+    lo = g.window > 0 ? max(0, t0 - g.window + 1) : 0;
+    in_lo = g.window > 0 ? max(0, t1 - g.window + 1) : 0;
+  };
+  int lo, hi, in_lo, in_hi;
+  seen_by(a.token_of(r0), a.token_of(min(r0 + kRows - 1, rows - 1)), lo, hi, in_lo, in_hi);
+  const int kt0 = lo / KT, kt1 = (hi + KT - 1) / KT;
+  const int b0 = PIPED ? ((kt1 - kt0) & 1) ^ 1 : 0;  // the first tile's buffer
+  issue(b0, kt0 * KT, false);
+  issue(b0, kt0 * KT, true);
+  if (PIPED && kt0 + 1 < kt1) issue(b0 ^ 1, kt0 * KT + KT, false);
+  // This wave's rows and this lane's; rows past the last one work on the last one's values.
+  const int w0 = min(r0 + wave * 32, rows - 1), w1 = min(r0 + wave * 32 + 31, rows - 1);
+  int wlo, whi;
+  seen_by(a.token_of(w0), a.token_of(w1), wlo, whi, in_lo, in_hi);
+  const bool idle = r0 + wave * 32 >= rows;
+  const int row = min(r0 + wave * 32 + col, rows - 1);
+  const int tok = a.token_of(row), hq = head * a.group + row - tok * a.group;
+  const int row_hi = g.causal ? tok + 1 : sp.count;
+  const int row_lo = g.window > 0 ? max(0, tok - g.window + 1) : 0;
 
-    // The queries: lane (row, half) holds units half, half + 2 ... of its row.
-    vec16 qf[QU];
-    {
-      const T* src = reinterpret_cast<const T*>(g.q) + (sp.first + tok) * g.q_token + hq * g.q_head;
+  // The queries: lane (row, half) holds units half, half + 2 ... of its row.
+  vec16 qf[QU];
+  {
+    const T* src = reinterpret_cast<const T*>(g.q) + (sp.first + tok) * g.q_token + hq * g.q_head;
 #pragma unroll
-      for (int u = 0; u < QU; ++u) {
-        const int d = (2 * u + half) * UE;
-        qf[u] = d < g.dim ? load16(src + d) : vec16_zero();
-      }
-      // The sign of the scale goes with the query: scores then grow with the products.
-      if (a.scale < 0.f) {
-#pragma unroll
-        for (int u = 0; u < QU; ++u)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) qf[u].d[x] ^= ES == 2 ? 0x80008000u : 0x80000000u;
-      }
+    for (int u = 0; u < QU; ++u) {
+      const int d = (2 * u + half) * UE;
+      qf[u] = d < g.dim ? load16(src + d) : vec16_zero();
     }
-    // Never zero: a masked score of -inf times it stays -inf.
-    const float cs = fmaxf(fabsf(a.scale), 0x1p-126f);
-    f32x16_t o[NC];
-#pragma unroll
-    for (int i = 0; i < NC; ++i) o[i] = zero16();
-    float m = -kInf, l = 0.f;
-
-    auto compute = [&](int buf, int j0, bool masked, auto exact_c) {
-      const char* kl = lds + buf * TILE;
-      const char* vl = lds + (2 + buf) * TILE;
-      f32x16_t sc[SB];
-#pragma unroll
-      for (int b = 0; b < SB; ++b) sc[b] = zero16();
+    // The sign of the scale goes with the query: scores then grow with the products.
+    if (a.scale < 0.f) {
 #pragma unroll
       for (int u = 0; u < QU; ++u)
 #pragma unroll
-        for (int b = 0; b < SB; ++b) {
-          const vec16 kf = *reinterpret_cast<const vec16*>(kl + (32 * b + col) * RB + (((2 * u + half) ^ S::turn_k(col)) << 4));
-          mfma_32x32<T>(sc[b], kf, qf[u]);
-        }
-      if (masked) {
+        for (int x = 0; x < 4; ++x) qf[u].d[x] ^= ES == 2 ? 0x80008000u : 0x80000000u;
+    }
+  }
+  // Never zero: a masked score of -inf times it stays -inf.
+  const float cs = fmaxf(fabsf(a.scale), 0x1p-126f);
+  f32x16_t o[NC];
 #pragma unroll
-        for (int b = 0; b < SB; ++b)
+  for (int i = 0; i < NC; ++i) o[i] = zero16();
+  float m = -kInf, l = 0.f;
+
+  // Scores of keys j0 .. that the lane's row does not see.
+  auto hide = [&](f32x16_t (&sc)[SB], int j0) {
+    const int lo_at = row_lo - j0 - 4 * half, hi_at = row_hi - j0 - 4 * half;
 #pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int j = j0 + 32 * b + 8 * (v >> 2) + 4 * half + (v & 3);
-            if (!(j >= row_lo && j < row_hi)) sc[b][v] = -kInf;
-          }
+    for (int b = 0; b < SB; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int j = 32 * b + 8 * (v >> 2) + (v & 3);
+        sc[b][v] = j >= lo_at && j < hi_at ? sc[b][v] : -kInf;
       }
-      float most = -kInf;
+  };
+  // Brings the row's results to a new maximum.
+  auto rescale = [&](float most) {
+    const float mn = fmaxf(m, most);
+    const float s = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+    m = mn;
+    l *= s;
 #pragma unroll
-      for (int b = 0; b < SB; ++b)
+    for (int i = 0; i < NC; ++i) o[i] *= s;
+  };
+  auto compute = [&](int buf, int j0, bool masked, auto exact_c) {
+    const char* kl = lds + buf * TILE;
+    const char* vl = lds + (2 + buf) * TILE;
+    f32x16_t sc[SB];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) most = fmaxf(most, sc[b][v]);
-      most = fmaxf(most, __shfl_xor(most, 32)) * cs;
-      if (__any(most > m)) {
-        const float mn = fmaxf(m, most);
-        const float s = m == mn ? 1.f : __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
-        l *= s;
+    for (int b = 0; b < SB; ++b) sc[b] = zero16();
 #pragma unroll
-        for (int i = 0; i < NC; ++i) o[i] *= s;
+    for (int u = 0; u < QU; ++u)
+#pragma unroll
+      for (int b = 0; b < SB; ++b) {
+        const vec16 kf = *reinterpret_cast<const vec16*>(kl + (32 * b + col) * RB + (((2 * u + half) ^ S::turn_k(col)) << 4));
+        mfma_32x32<T>(sc[b], kf, qf[u]);
       }
-      const float from = m == -kInf ? 0.f : m;  // a row with nothing yet: its weights are 2^-inf
+    if (masked) hide(sc, j0);
+    float most = -kInf;
 #pragma unroll
-      for (int b = 0; b < SB; ++b)
+    for (int b = 0; b < SB; ++b)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          sc[b][v] = __builtin_amdgcn_exp2f(fmaf(sc[b][v], cs, -from));
-          l += sc[b][v];
-        }
-      if constexpr (decltype(exact_c)::value) {
+      for (int v = 0; v < 16; ++v) most = fmaxf(most, sc[b][v]);
+    most = fmaxf(most, __shfl_xor(most, 32)) * cs;
+    if (__any(most > m)) rescale(most);
+    const float from = m == -kInf ? 0.f : m;  // a row with nothing yet: its weights are 2^-inf
+#pragma unroll
+    for (int b = 0; b < SB; ++b)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        sc[b][v] = __builtin_amdgcn_exp2f(fmaf(sc[b][v], cs, -from));
+        l += sc[b][v];
+      }
+    if constexpr (decltype(exact_c)::value) {
 #pragma unroll 1
-        for (int k = 0; k < KT; ++k) {
-          const int v = 4 * ((k & 31) >> 3) + (k & 3);
-          float mine = sc[0][v];
-          if constexpr (SB == 2) mine = k < 32 ? mine : sc[1][v];
-          const float w = __shfl(mine, col + 8 * (k & 4));
-          if (j0 + k < row_lo || j0 + k >= row_hi) continue;
+      for (int k = 0; k < KT; ++k) {
+        const int v = 4 * ((k & 31) >> 3) + (k & 3);
+        float mine = sc[0][v];
+        if constexpr (SB == 2) mine = k < 32 ? mine : sc[1][v];
+        const float w = __shfl(mine, col + 8 * (k & 4));
+        if (j0 + k < row_lo || j0 + k >= row_hi) continue;
 #pragma unroll
-          for (int i = 0; i < NC; ++i)
+        for (int i = 0; i < NC; ++i)
 #pragma unroll
-            for (int v4 = 0; v4 < 4; ++v4) {
-              const int d = 32 * i + 8 * v4 + 4 * half;
-              const char* at = vl + k * RB + (((d / UE) ^ S::turn_v(k)) << 4) + d % UE * ES;
-              float z[4];
-              if constexpr (ES == 2) {
-                const uint2 t = *reinterpret_cast<const uint2*>(at);
-                z[0] = low_half(t.x); z[1] = high_half(t.x); z[2] = low_half(t.y); z[3] = high_half(t.y);
-              } else {
-                const float4 t = *reinterpret_cast<const float4*>(at);
-                z[0] = t.x; z[1] = t.y; z[2] = t.z; z[3] = t.w;
-              }
-#pragma unroll
-              for (int x = 0; x < 4; ++x) o[i][4 * v4 + x] = fmaf(w, z[x], o[i][4 * v4 + x]);
+          for (int v4 = 0; v4 < 4; ++v4) {
+            const int d = 32 * i + 8 * v4 + 4 * half;
+            const char* at = vl + k * RB + (((d / UE) ^ S::turn_v(k)) << 4) + d % UE * ES;
+            float z[4];
+            if constexpr (ES == 2) {
+              const uint2 t = *reinterpret_cast<const uint2*>(at);
+              z[0] = low_half(t.x); z[1] = high_half(t.x); z[2] = low_half(t.y); z[3] = high_half(t.y);
+            } else {
+              const float4 t = *reinterpret_cast<const float4*>(at);
+              z[0] = t.x; z[1] = t.y; z[2] = t.z; z[3] = t.w;
             }
-        }
-        return;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[i][4 * v4 + x] = fmaf(w, z[x], o[i][4 * v4 + x]);
+          }
       }
-      if constexpr (ES == 2) {
-        // Lane i16 of sixteen reads 8 bytes; their 4 keys x 16 columns come back transposed.
-        const int i16 = lane & 15, key = 4 * half + (i16 >> 2);
-        const int unit = 2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1);
-        typedef __attribute__((address_space(3))) v4s_t* lds_t;
-        auto value = [&](int kb, int i) {  // 16 keys from 16 kb on, columns 32 i ..
-          vec16 r;
+      return;
+    }
+    if constexpr (!PIPED) {
 #pragma unroll
-          for (int p = 0; p < 2; ++p) {
-            const char* at = vl + (16 * kb + 8 * p + key) * RB + (((4 * i + unit) ^ S::turn_v(key)) << 4) + (i16 & 1) * 8;
-            const v4s_t t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t)(uintptr_t)lds_address(at));
-            uint2 w;
-            __builtin_memcpy(&w, &t, 8);
-            r.d[2 * p] = w.x;
-            r.d[2 * p + 1] = w.y;
-          }
-          return r;
-        };
+      for (int v = 0; v < 16; ++v) {
+        const int key = 8 * (v >> 2) + 4 * half + (v & 3);
 #pragma unroll
-        for (int kb = 0; kb < 2 * SB; ++kb) {
-          vec16 wh, wl;
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int b = kb >> 1, v = 8 * (kb & 1) + 2 * x;
-            const float w0 = sc[b][v], w1 = sc[b][v + 1];
-            wh.d[x] = f32x2_to_bf16x2(w0, w1);
-            wl.d[x] = f32x2_to_bf16x2(w0 - low_half(wh.d[x]), w1 - high_half(wh.d[x]));
-          }
-#pragma unroll
-          for (int i = 0; i < NC; ++i) {
-            const vec16 vf = value(kb, i);
-            mfma_32x32<T>(o[i], vf, wh);
-            mfma_32x32<T>(o[i], vf, wl);
-          }
+        for (int i = 0; i < NC; ++i) {
+          const float z = *reinterpret_cast<const float*>(
+              vl + key * RB + (((8 * i + (col >> 2)) ^ S::turn_v(key)) << 4) + (col & 3) * 4);
+          o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(z, sc[0][v], o[i], 0, 0, 0);
         }
+      }
+    }
+  };
+
+  // Values that are not finite spoil products that they have no part in: a weight of zero, where they are hidden, or
+  // the second half of one, which may be zero or negative.  Rows that end so go once more, adding up key by key what
+  // they see.
+  auto walk = [&](auto exact_c) {
+    for (int kt = kt0; kt < kt1; ++kt) {
+      // This tile's DMAs are in; behind the barrier everyone's are, and all are done with the other buffer.
+      CONVSEL_WAIT_VMCNT(0);
+      lds_sync();
+      const int buf = (kt - kt0) & 1, j0 = kt * KT;
+      if (kt + 1 < kt1) {
+        issue(buf ^ 1, j0 + KT, false);
+        issue(buf ^ 1, j0 + KT, true);
+      }
+      if (idle || j0 >= whi || j0 + KT <= wlo) continue;
+      compute(buf, j0, !(j0 >= in_lo && j0 + KT <= in_hi), exact_c);
+    }
+  };
+  // bf16: the scores of the next tile are formed among the softmax of this one, and its weights, 16 keys ahead, among
+  // the products with its values: a wave's vector operations run beside its own matrix ones.
+  auto piped = [&] {
+    if constexpr (PIPED) {
+    const auto fix = [] { __builtin_amdgcn_sched_barrier(0); };
+    // Places of the lane's operands that differ by more than a constant.
+    constexpr int PK = U % 16 == 0 ? 8 : U % 8 == 0 ? 4 : 2, PV = U % 16 == 0 ? 4 : U % 8 == 0 ? 2 : 1;
+    lds_char_t *ka[PK], *va[PV];
+#pragma unroll
+    for (int j = 0; j < PK; ++j) ka[j] = (lds_char_t*)lds + col * RB + (((2 * j + half) ^ S::turn_k(col)) << 4);
+    // Lane i16 of sixteen reads 8 bytes of values; their 4 keys x 16 columns come back transposed.
+    const int i16 = lane & 15, vkey = 4 * half + (i16 >> 2);
+    const int unit = 2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1);
+#pragma unroll
+    for (int j = 0; j < PV; ++j)
+      va[j] = (lds_char_t*)lds + 2 * TILE + vkey * RB + (((4 * j + unit) ^ S::turn_v(vkey)) << 4) + (i16 & 1) * 8;
+    auto key = [&](int buf, int u, int b) {
+      const u32x4_t w = *(lds_u32x4_t*)(ka[u % PK] + (buf * TILE + 32 * b * RB + u / PK * PK * 32));
+      return __builtin_bit_cast(vec16, w);
+    };
+    auto value = [&](int buf, int kb, int i) {  // 16 keys from 16 kb on, columns 32 i ..
+      vec16 r;
+#pragma unroll
+      for (int p = 0; p < 2; ++p) {
+        lds_char_t* at = va[i % PV] + (buf * TILE + (16 * kb + 8 * p) * RB + i / PV * PV * 64);
+        const v4s_t t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)at);
+        uint2 w;
+        __builtin_memcpy(&w, &t, 8);
+        r.d[2 * p] = w.x;
+        r.d[2 * p + 1] = w.y;
+      }
+      return r;
+    };
+    constexpr int AHEAD = 4, NQ = 2 * QU;  // operands of keys on their way; products of a tile's scores
+    auto scores = [&](auto buf_c, f32x16_t (&sc)[SB], auto between) {
+      constexpr int buf = decltype(buf_c)::value;
+      vec16 f[AHEAD];
+      static_for<AHEAD>([&](auto n) { f[n] = key(buf, n / 2, n % 2); });
+      sc[0] = zero16();
+      sc[1] = zero16();
+      static_for<NQ>([&](auto n) {
+        mfma_32x32<T>(sc[n % 2], f[n % AHEAD], qf[n / 2]);
+        if constexpr (n + AHEAD < NQ) f[n % AHEAD] = key(buf, (n + AHEAD) / 2, n % 2);
+        between(n);
+        fix();
+      });
+    };
+    vec16 wh[2], wl[2];
+    float from = 0.f, held = 0.f;
+    // Kept from the compiler, which would write (-1, 0) as the fp32 constant -1, which is (0, -1).
+    uint32_t low = 0x0000bf80u, high = 0xbf800000u;
+    asm volatile("" : "+s"(low), "+s"(high));
+    // Weight e of 16 keys kb of a lane's eight; with every second one, the pair as two bf16 numbers each.
+    auto weigh = [&](f32x16_t (&sc)[SB], auto kb_c, auto e_c) {
+      constexpr int kb = decltype(kb_c)::value, e = decltype(e_c)::value, b = kb >> 1, v = 8 * (kb & 1) + e;
+      const float w = __builtin_amdgcn_exp2f(fmaf(sc[b][v], cs, -from));
+      l += w;
+      if constexpr (e % 2 == 0) {
+        held = w;
       } else {
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int key = 8 * (v >> 2) + 4 * half + (v & 3);
-#pragma unroll
-          for (int i = 0; i < NC; ++i) {
-            const float z = *reinterpret_cast<const float*>(
-                vl + key * RB + (((8 * i + (col >> 2)) ^ S::turn_v(key)) << 4) + (col & 3) * 4);
-            o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(z, sc[0][v], o[i], 0, 0, 0);
-          }
-        }
+        const uint32_t hi = f32x2_to_bf16x2(held, w);
+        wh[kb & 1].d[e / 2] = hi;
+        wl[kb & 1].d[e / 2] = f32x2_to_bf16x2(less(held, hi, low), less(w, hi, high));
       }
     };
-
-    // Values that are not finite spoil products that they have no part in: a weight of zero, where they are hidden, or
-    // the second half of one, which may be zero or negative.  Rows that end so go once more, adding up key by key what
-    // they see.
-    auto walk = [&](auto exact_c) {
-      for (int kt = kt0; kt < kt1; ++kt) {
-        // This tile's DMAs are in; behind the barrier everyone's are, and all are done with the other buffer.
+    const std::integral_constant<int, 0> zero{};
+    // Tile it of the walk, whose scores are sc; the next one's go to nx.
+    auto step = [&](int it, auto p_c, f32x16_t (&sc)[SB], f32x16_t (&nx)[SB], auto last_c) {
+      constexpr int P = decltype(p_c)::value;
+      constexpr bool LAST = decltype(last_c)::value;
+      const int j0 = (kt0 + it) * KT;
+      CONVSEL_WAIT_VMCNT(0);
+      lds_sync();
+      if (kt0 + it + 2 < kt1) issue(P, j0 + 2 * KT, false);
+      if constexpr (!LAST) issue(P ^ 1, j0 + KT, true);
+      if (!(j0 >= in_lo && j0 + KT <= in_hi)) hide(sc, j0);
+      float most = -kInf;
+      vec16 fv[NC];
+      auto top = [&](auto n) {  // an eighth of the scores
+        most = max3(max3(most, sc[0][2 * n], sc[0][2 * n + 1]), sc[1][2 * n], sc[1][2 * n + 1]);
+      };
+      auto settle = [&] {
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
+        most = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * cs;
+        // Weights may grow to 2^8 before the results are brought to a new maximum.
+        if (__any(most > m + 8.f)) rescale(most);
+        from = m == -kInf ? 0.f : m;  // a row with nothing yet: its weights are 2^-inf
+      };
+      auto first_values = [&] { static_for<NC>([&](auto i) { fv[i] = value(P, 0, i); }); };
+      if constexpr (LAST) {
+        first_values();
+        static_for<8>(top);
+        settle();
+        static_for<8>([&](auto e) { weigh(sc, zero, e); });
+      } else {
+        constexpr int M = NQ >= 16 ? 4 : 2;  // products beside the maximum; 8 weights beside the others
+        scores(std::integral_constant<int, P ^ 1>{}, nx, [&](auto n) {
+          if constexpr (n < M)
+            static_for<8 / M>([&](auto x) { top(std::integral_constant<int, decltype(n)::value * (8 / M) + decltype(x)::value>{}); });
+          if constexpr (n == M - 1) {
+            fix();
+            settle();
+          }
+          constexpr int R = NQ - M, i0 = n < M ? 0 : (n - M) * 8 / R, i1 = n < M ? 0 : (n - M + 1) * 8 / R;
+          static_for<i1 - i0>([&](auto e) { weigh(sc, zero, std::integral_constant<int, i0 + decltype(e)::value>{}); });
+          if constexpr (n == NQ - 4 || (NQ < 4 && n == 0)) first_values();
+        });
+      }
+      static_for<4>([&](auto kb) {
+        static_for<2 * NC>([&](auto n) {
+          constexpr int i = n % NC;
+          mfma_32x32<T>(o[i], fv[i], n < NC ? wh[kb & 1] : wl[kb & 1]);
+          if constexpr (kb + 1 < 4) {
+            if constexpr (n >= NC) fv[i] = value(P, kb + 1, i);
+            constexpr int i0 = n * 8 / (2 * NC), i1 = (n + 1) * 8 / (2 * NC);
+            static_for<i1 - i0>([&](auto e) {
+              weigh(sc, std::integral_constant<int, decltype(kb)::value + 1>{}, std::integral_constant<int, i0 + decltype(e)::value>{});
+            });
+          }
+          fix();
+        });
+      });
+    };
+    const int count = kt1 - kt0;
+    const std::integral_constant<int, 1> one{};
+    f32x16_t sa[SB];
+    // The first keys are in; behind the barrier everyone's are.
+    if (count > 1) CONVSEL_WAIT_VMCNT(2 * NDMA);
+    else CONVSEL_WAIT_VMCNT(NDMA);
+    lds_sync();
+    int it = 0;
+    if (idle) {
+      for (; it < count; ++it) {
         CONVSEL_WAIT_VMCNT(0);
         lds_sync();
-        const int buf = (kt - kt0) & 1, j0 = kt * KT;
-        if (kt + 1 < kt1) issue(buf ^ 1, j0 + KT);
-        if (idle || j0 >= whi || j0 + KT <= wlo) continue;
-        compute(buf, j0, !(j0 >= in_lo && j0 + KT <= in_hi), exact_c);
+        if (it + 2 < count) issue((it + b0) & 1, (kt0 + it + 2) * KT, false);
+        if (it + 1 < count) issue(((it + b0) & 1) ^ 1, (kt0 + it + 1) * KT, true);
       }
-    };
+      return;
+    }
+    // The last tile's scores are sa, so the first one's are sb if there is an even number: one copy of the last step.
+    if (b0 != 0) {
+      f32x16_t sb[SB];
+      scores(one, sb, [](auto) {});
+      asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+      step(it++, one, sb, sa, std::false_type{});
+    } else {
+      scores(zero, sa, [](auto) {});
+    }
+    asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");  // max3() reads products' results unseen by the compiler
+    for (; it + 1 < count; it += 2) {
+      f32x16_t sb[SB];
+      step(it, zero, sa, sb, std::false_type{});
+      step(it + 1, one, sb, sa, std::false_type{});
+    }
+    step(it, zero, sa, sa, std::true_type{});
+    }
+  };
+  if constexpr (PIPED)
+    piped();
+  else
     walk(std::false_type{});
-    float odd = 0.f;  // NaN if a result is not finite
+  float odd = 0.f;  // NaN if a result is not finite
+#pragma unroll
+  for (int i = 0; i < NC; ++i)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) odd = fmaf(o[i][v], 0.f, odd);
+  const int again = __any(odd != 0.f);
+  if (lane == 0) spoilt[wave] = again;
+  lds_sync();  // also before another tile is fetched
+  if (spoilt[0] | spoilt[1] | spoilt[2] | spoilt[3]) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) o[i] = zero16();
+    m = -kInf;
+    l = 0.f;
+    issue(0, kt0 * KT, false);
+    issue(0, kt0 * KT, true);
+    walk(std::true_type{});
+    lds_sync();
+  }
+
+  // Lane (row, half) holds columns 32 i + 8 (v / 4) + 4 half + v % 4.
+  l += __shfl_xor(l, 32);
+  if (r0 + wave * 32 + col < rows) {
+    const float inv = 1.f / l;
+    T* dst = reinterpret_cast<T*>(g.y) + (sp.first + tok) * g.y_token + hq * g.y_head;
 #pragma unroll
     for (int i = 0; i < NC; ++i)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) odd = fmaf(o[i][v], 0.f, odd);
-    const int again = __any(odd != 0.f);
-    if (lane == 0) spoilt[wave] = again;
-    lds_sync();  // also before another tile is fetched
-    if (spoilt[0] | spoilt[1] | spoilt[2] | spoilt[3]) {
+      for (int v4 = 0; v4 < 4; ++v4) {
+        const int d = 32 * i + 8 * v4 + 4 * half;
+        float v[4];
 #pragma unroll
-      for (int i = 0; i < NC; ++i) o[i] = zero16();
-      m = -kInf;
-      l = 0.f;
-      issue(0, kt0 * KT);
-      walk(std::true_type{});
-      lds_sync();
-    }
-
-    // Lane (row, half) holds columns 32 i + 8 (v / 4) + 4 half + v % 4.
-    l += __shfl_xor(l, 32);
-    if (r0 + wave * 32 + col < rows) {
-      const float inv = 1.f / l;
-      T* dst = reinterpret_cast<T*>(g.y) + (sp.first + tok) * g.y_token + hq * g.y_head;
-#pragma unroll
-      for (int i = 0; i < NC; ++i)
-#pragma unroll
-        for (int v4 = 0; v4 < 4; ++v4) {
-          const int d = 32 * i + 8 * v4 + 4 * half;
-          float v[4];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) v[x] = o[i][4 * v4 + x] * inv;
-          if (a.y_vec) {
-            if (d < g.dim) {
-              if constexpr (ES == 4)
-                *reinterpret_cast<float4*>(dst + d) = make_float4(v[0], v[1], v[2], v[3]);
-              else
-                *reinterpret_cast<uint2*>(dst + d) = make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]));
-            }
-          } else {
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-              if (d + x < g.dim) elem<T>::store(dst + d + x, v[x]);
+        for (int x = 0; x < 4; ++x) v[x] = o[i][4 * v4 + x] * inv;
+        if (a.y_vec) {
+          if (d < g.dim) {
+            if constexpr (ES == 4)
+              *reinterpret_cast<float4*>(dst + d) = make_float4(v[0], v[1], v[2], v[3]);
+            else
+              *reinterpret_cast<uint2*>(dst + d) = make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]));
           }
+        } else {
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (d + x < g.dim) elem<T>::store(dst + d + x, v[x]);
         }
-    }
+      }
   }
 }
 
@@ -422,6 +588,9 @@ hipError_t launch(const PromptArgs& g, void* workspace, hipStream_t st) {
   pack<T>(g, a.g.v, a.g.v_token, a.g.v_head, g.kv_heads, p.v, ws, st);
   a.group = g.q_heads / g.kv_heads;
   a.scale = g.scale * 1.4426950408889634f;
+  a.shift = 31;
+  while (((int64_t)1 << (a.shift - 31)) < a.group) ++a.shift;
+  a.magic = (uint32_t)((((uint64_t)1 << a.shift) + a.group - 1) / a.group);
   a.y_vec = g.dim % 4 == 0 && g.y_token % 4 == 0 && g.y_head % 4 == 0 && (uintptr_t)g.y % (4 * sizeof(T)) == 0;
   convsel_kv_batch_t b = {};
   b.seqs = g.seqs;
