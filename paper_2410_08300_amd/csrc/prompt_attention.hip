@@ -33,7 +33,7 @@ using namespace igemm;
 using namespace lm;
 
 constexpr float kInf = __builtin_inff();
-constexpr int kWaves = 4, kRows = 32 * kWaves;
+constexpr int kWaves = 4;
 
 struct PromptLaunch {
   PromptArgs g;
@@ -50,6 +50,7 @@ struct PromptLaunch {
 
 typedef __attribute__((address_space(3))) char lds_char_t;
 typedef const __attribute__((address_space(3))) u32x4_t lds_u32x4_t;
+typedef uint32_t u32x2v_t __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -66,14 +67,19 @@ __device__ __forceinline__ float less(float w, uint32_t pair, uint32_t which) {
                                          false);
 }
 
-// Sizes of a tile: T elements, rows of 32 NC columns.
-template <typename T, int NC>
+// Sizes of a tile: T elements, rows of 32 NC columns, R blocks of 32 rows.  The four waves are R blocks of rows times G
+// groups of keys.
+template <typename T, int NC, int R>
 struct Shape {
   static constexpr int ES = elem<T>::bytes, UE = elem<T>::per16;
-  static constexpr int KT = ES == 2 ? 64 : 32, SB = KT / 32;  // keys, and blocks of 32 of them
+  static constexpr int G = kWaves / R, ROWS = 32 * R;
+  static constexpr int SB = ES == 2 && G == 1 ? 2 : 1;        // blocks of 32 keys of a wave
+  static constexpr int KT = 32 * SB * G;                      // keys
   static constexpr int RB = 32 * NC * ES, U = RB / 16;        // bytes and units of a row
   static constexpr int QU = U / 2;                            // units of a lane's half of a row
   static constexpr int TILE = KT * RB, NDMA = TILE / 1024 / kWaves;
+  static constexpr int BUFS = 4 * TILE <= 144 * 1024 ? 2 : 1;  // tiles in LDS
+  static constexpr int PER_CU = ES == 2 && NC <= 4 && TILE <= 20 * 1024 - 16 ? 2 : 1;  // workgroups that a CU holds
   __device__ static __forceinline__ int turn_k(int r) {
     return U % 16 == 0 ? r & 15 : U % 8 == 0 ? (r >> 1) & 7 : (r >> 2) & 3;
   }
@@ -84,15 +90,14 @@ struct Shape {
   }
 };
 
-template <typename T, int NC>
-__global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) void prompt_attention_kernel(
-    PromptLaunch a) {
-  typedef Shape<T, NC> S;
+template <typename T, int NC, int R>
+__global__ __launch_bounds__(64 * kWaves, (Shape<T, NC, R>::PER_CU)) void prompt_attention_kernel(PromptLaunch a) {
+  typedef Shape<T, NC, R> S;
   constexpr int ES = S::ES, UE = S::UE, KT = S::KT, SB = S::SB, RB = S::RB, U = S::U, QU = S::QU, TILE = S::TILE;
-  constexpr int NDMA = S::NDMA;
+  constexpr int NDMA = S::NDMA, G = S::G, ROWS = S::ROWS, BUFS = S::BUFS;
   constexpr bool PIPED = ES == 2;
   constexpr uint32_t kNowhere = 0xfffffff0u;  // beyond every buffer: zeros
-  __shared__ __align__(1024) char lds[4 * TILE];  // keys of two tiles, then values
+  __shared__ __align__(1024) char lds[2 * BUFS * TILE];  // keys of the tiles, then values
   __shared__ int spoilt[kWaves];
   const PromptArgs& g = a.g;
   const int lane = threadIdx.x & 63;
@@ -102,7 +107,8 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
   const Unit un = find_unit<true>(a.units, g.offsets, g.offsets);
   const Span sp = un.span;
   const int rows = sp.count * a.group;
-  const int ntile = (rows + kRows - 1) / kRows;
+  const int ntile = (rows + ROWS - 1) / ROWS;
+  const int wrow = 32 * (wave % R), wkey = 32 * SB * (wave / R);  // the wave's first row, and key of a tile
   const uint32_t lds0 = lds_address(lds);
 
   // DMA instruction d of this wave fills units 64 (4 d + wave) .. of a tile, keys and values alike.  Where a row's
@@ -131,7 +137,7 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
     const u32x4_t r = dma_rsrc(src, (n - 1) * step + dim_units * 16);
 #pragma unroll
     for (int d = 0; d < NDMA; ++d) {
-      const uint32_t at = lds0 + (buf + (values ? 2 : 0)) * TILE + (4 * d + wave) * 1024;
+      const uint32_t at = lds0 + (buf + (values ? BUFS : 0)) * TILE + (4 * d + wave) * 1024;
       const uint32_t vo = values ? vvo[EVEN ? 0 : d] : kvo[EVEN ? 0 : d];
       if constexpr (EVEN)
         dma16(r, at, drow[0] + d * STEP < n ? vo : kNowhere, d * STEP < n ? d * STEP * step : 0);
@@ -143,7 +149,7 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
   if (un.index >= ntile) return;  // uniform
   // Every tile of rows has a unit.  Under a causal mask the last rows have the most keys: they start first.
   const int tile = ntile - 1 - un.index;
-  const int r0 = tile * kRows;
+  const int r0 = tile * ROWS;
   // Keys that tokens t0..t1 see between them, and that every one of them sees.
   auto seen_by = [&](int t0, int t1, int& lo, int& hi, int& in_lo, int& in_hi) {
     hi = g.causal ? t1 + 1 : sp.count;
@@ -152,18 +158,18 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
     in_lo = g.window > 0 ? max(0, t1 - g.window + 1) : 0;
   };
   int lo, hi, in_lo, in_hi;
-  seen_by(a.token_of(r0), a.token_of(min(r0 + kRows - 1, rows - 1)), lo, hi, in_lo, in_hi);
+  seen_by(a.token_of(r0), a.token_of(min(r0 + ROWS - 1, rows - 1)), lo, hi, in_lo, in_hi);
   const int kt0 = lo / KT, kt1 = (hi + KT - 1) / KT;
   const int b0 = PIPED ? ((kt1 - kt0) & 1) ^ 1 : 0;  // the first tile's buffer
   issue(b0, kt0 * KT, false);
   issue(b0, kt0 * KT, true);
   if (PIPED && kt0 + 1 < kt1) issue(b0 ^ 1, kt0 * KT + KT, false);
   // This wave's rows and this lane's; rows past the last one work on the last one's values.
-  const int w0 = min(r0 + wave * 32, rows - 1), w1 = min(r0 + wave * 32 + 31, rows - 1);
+  const int w0 = min(r0 + wrow, rows - 1), w1 = min(r0 + wrow + 31, rows - 1);
   int wlo, whi;
   seen_by(a.token_of(w0), a.token_of(w1), wlo, whi, in_lo, in_hi);
-  const bool idle = r0 + wave * 32 >= rows;
-  const int row = min(r0 + wave * 32 + col, rows - 1);
+  const bool idle = r0 + wrow >= rows;
+  const int row = min(r0 + wrow + col, rows - 1);
   const int tok = a.token_of(row), hq = head * a.group + row - tok * a.group;
   const int row_hi = g.causal ? tok + 1 : sp.count;
   const int row_lo = g.window > 0 ? max(0, tok - g.window + 1) : 0;
@@ -213,18 +219,23 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
     for (int i = 0; i < NC; ++i) o[i] *= s;
   };
   auto compute = [&](int buf, int j0, bool masked, auto exact_c) {
-    const char* kl = lds + buf * TILE;
-    const char* vl = lds + (2 + buf) * TILE;
+    const lds_char_t* kl = (lds_char_t*)lds + buf * TILE + wkey * RB;
+    const lds_char_t* vl = (lds_char_t*)lds + (BUFS + buf) * TILE + wkey * RB;
     f32x16_t sc[SB];
 #pragma unroll
     for (int b = 0; b < SB; ++b) sc[b] = zero16();
-#pragma unroll
-    for (int u = 0; u < QU; ++u)
-#pragma unroll
-      for (int b = 0; b < SB; ++b) {
-        const vec16 kf = *reinterpret_cast<const vec16*>(kl + (32 * b + col) * RB + (((2 * u + half) ^ S::turn_k(col)) << 4));
-        mfma_32x32<T>(sc[b], kf, qf[u]);
-      }
+    constexpr int AHEAD = 2;  // operands on their way
+    vec16 kf[AHEAD];
+    auto key = [&](int n) {
+      return __builtin_bit_cast(
+          vec16, *(lds_u32x4_t*)(kl + (32 * (n % SB) + col) * RB + (((2 * (n / SB) + half) ^ S::turn_k(col)) << 4)));
+    };
+    static_for<AHEAD>([&](auto n) { kf[n] = key(n); });
+    static_for<SB * QU>([&](auto n) {
+      mfma_32x32<T>(sc[n % SB], kf[n % AHEAD], qf[n / SB]);
+      if constexpr (n + AHEAD < SB * QU) kf[n % AHEAD] = key(n + AHEAD);
+      __builtin_amdgcn_sched_barrier(0);
+    });
     if (masked) hide(sc, j0);
     float most = -kInf;
 #pragma unroll
@@ -243,7 +254,7 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
       }
     if constexpr (decltype(exact_c)::value) {
 #pragma unroll 1
-      for (int k = 0; k < KT; ++k) {
+      for (int k = 0; k < 32 * SB; ++k) {
         const int v = 4 * ((k & 31) >> 3) + (k & 3);
         float mine = sc[0][v];
         if constexpr (SB == 2) mine = k < 32 ? mine : sc[1][v];
@@ -254,14 +265,14 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
 #pragma unroll
           for (int v4 = 0; v4 < 4; ++v4) {
             const int d = 32 * i + 8 * v4 + 4 * half;
-            const char* at = vl + k * RB + (((d / UE) ^ S::turn_v(k)) << 4) + d % UE * ES;
+            const lds_char_t* at = vl + k * RB + (((d / UE) ^ S::turn_v(k)) << 4) + d % UE * ES;
             float z[4];
             if constexpr (ES == 2) {
-              const uint2 t = *reinterpret_cast<const uint2*>(at);
-              z[0] = low_half(t.x); z[1] = high_half(t.x); z[2] = low_half(t.y); z[3] = high_half(t.y);
+              const u32x2v_t t = *(const __attribute__((address_space(3))) u32x2v_t*)at;
+              z[0] = low_half(t[0]); z[1] = high_half(t[0]); z[2] = low_half(t[1]); z[3] = high_half(t[1]);
             } else {
-              const float4 t = *reinterpret_cast<const float4*>(at);
-              z[0] = t.x; z[1] = t.y; z[2] = t.z; z[3] = t.w;
+              const f32x4_t t = *(const __attribute__((address_space(3))) f32x4_t*)at;
+              z[0] = t[0]; z[1] = t[1]; z[2] = t[2]; z[3] = t[3];
             }
 #pragma unroll
             for (int x = 0; x < 4; ++x) o[i][4 * v4 + x] = fmaf(w, z[x], o[i][4 * v4 + x]);
@@ -270,16 +281,19 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
       return;
     }
     if constexpr (!PIPED) {
-#pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int key = 8 * (v >> 2) + 4 * half + (v & 3);
-#pragma unroll
-        for (int i = 0; i < NC; ++i) {
-          const float z = *reinterpret_cast<const float*>(
-              vl + key * RB + (((8 * i + (col >> 2)) ^ S::turn_v(key)) << 4) + (col & 3) * 4);
-          o[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(z, sc[0][v], o[i], 0, 0, 0);
-        }
-      }
+      constexpr int FAR = 8;
+      float z[FAR];
+      auto value = [&](int n) {  // of key 8 (v / 4) + 4 half + v % 4, v = n / NC, column 32 (n % NC) + col
+        const int v = n / NC, k = 8 * (v >> 2) + 4 * half + (v & 3);
+        return *(const __attribute__((address_space(3))) float*)(
+            vl + k * RB + (((8 * (n % NC) + (col >> 2)) ^ S::turn_v(k)) << 4) + (col & 3) * 4);
+      };
+      static_for<FAR>([&](auto n) { z[n] = value(n); });
+      static_for<16 * NC>([&](auto n) {
+        o[n % NC] = __builtin_amdgcn_mfma_f32_32x32x2f32(z[n % FAR], sc[0][n / NC], o[n % NC], 0, 0, 0);
+        if constexpr (n + FAR < 16 * NC) z[n % FAR] = value(n + FAR);
+        __builtin_amdgcn_sched_barrier(0);
+      });
     }
   };
 
@@ -288,16 +302,22 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
   // they see.
   auto walk = [&](auto exact_c) {
     for (int kt = kt0; kt < kt1; ++kt) {
+      const int buf = BUFS == 2 ? (kt - kt0) & 1 : 0, j0 = kt * KT;
+      if (BUFS == 1 && kt > kt0) {
+        lds_sync();  // all are done with the tile before
+        issue(0, j0, false);
+        issue(0, j0, true);
+      }
       // This tile's DMAs are in; behind the barrier everyone's are, and all are done with the other buffer.
       CONVSEL_WAIT_VMCNT(0);
       lds_sync();
-      const int buf = (kt - kt0) & 1, j0 = kt * KT;
-      if (kt + 1 < kt1) {
+      if (BUFS == 2 && kt + 1 < kt1) {
         issue(buf ^ 1, j0 + KT, false);
         issue(buf ^ 1, j0 + KT, true);
       }
-      if (idle || j0 >= whi || j0 + KT <= wlo) continue;
-      compute(buf, j0, !(j0 >= in_lo && j0 + KT <= in_hi), exact_c);
+      const int jw = j0 + wkey, je = jw + 32 * SB;
+      if (idle || jw >= whi || je <= wlo) continue;
+      compute(buf, jw, !(jw >= in_lo && je <= in_hi), exact_c);
     }
   };
   // bf16: the scores of the next tile are formed among the softmax of this one, and its weights, 16 keys ahead, among
@@ -309,13 +329,13 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
     constexpr int PK = U % 16 == 0 ? 8 : U % 8 == 0 ? 4 : 2, PV = U % 16 == 0 ? 4 : U % 8 == 0 ? 2 : 1;
     lds_char_t *ka[PK], *va[PV];
 #pragma unroll
-    for (int j = 0; j < PK; ++j) ka[j] = (lds_char_t*)lds + col * RB + (((2 * j + half) ^ S::turn_k(col)) << 4);
+    for (int j = 0; j < PK; ++j) ka[j] = (lds_char_t*)lds + (wkey + col) * RB + (((2 * j + half) ^ S::turn_k(col)) << 4);
     // Lane i16 of sixteen reads 8 bytes of values; their 4 keys x 16 columns come back transposed.
     const int i16 = lane & 15, vkey = 4 * half + (i16 >> 2);
     const int unit = 2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1);
 #pragma unroll
     for (int j = 0; j < PV; ++j)
-      va[j] = (lds_char_t*)lds + 2 * TILE + vkey * RB + (((4 * j + unit) ^ S::turn_v(vkey)) << 4) + (i16 & 1) * 8;
+      va[j] = (lds_char_t*)lds + 2 * TILE + (wkey + vkey) * RB + (((4 * j + unit) ^ S::turn_v(vkey)) << 4) + (i16 & 1) * 8;
     auto key = [&](int buf, int u, int b) {
       const u32x4_t w = *(lds_u32x4_t*)(ka[u % PK] + (buf * TILE + 32 * b * RB + u / PK * PK * 32));
       return __builtin_bit_cast(vec16, w);
@@ -333,16 +353,15 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
       }
       return r;
     };
-    constexpr int AHEAD = 4, NQ = 2 * QU;  // operands of keys on their way; products of a tile's scores
+    constexpr int AHEAD = SB * QU < 4 ? SB * QU : 4, NQ = SB * QU;  // operands of keys on their way; products of a tile's scores
     auto scores = [&](auto buf_c, f32x16_t (&sc)[SB], auto between) {
       constexpr int buf = decltype(buf_c)::value;
       vec16 f[AHEAD];
-      static_for<AHEAD>([&](auto n) { f[n] = key(buf, n / 2, n % 2); });
-      sc[0] = zero16();
-      sc[1] = zero16();
+      static_for<AHEAD>([&](auto n) { f[n] = key(buf, n / SB, n % SB); });
+      static_for<SB>([&](auto b) { sc[b] = zero16(); });
       static_for<NQ>([&](auto n) {
-        mfma_32x32<T>(sc[n % 2], f[n % AHEAD], qf[n / 2]);
-        if constexpr (n + AHEAD < NQ) f[n % AHEAD] = key(buf, (n + AHEAD) / 2, n % 2);
+        mfma_32x32<T>(sc[n % SB], f[n % AHEAD], qf[n / SB]);
+        if constexpr (n + AHEAD < NQ) f[n % AHEAD] = key(buf, (n + AHEAD) / SB, (n + AHEAD) % SB);
         between(n);
         fix();
       });
@@ -370,16 +389,16 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
     auto step = [&](int it, auto p_c, f32x16_t (&sc)[SB], f32x16_t (&nx)[SB], auto last_c) {
       constexpr int P = decltype(p_c)::value;
       constexpr bool LAST = decltype(last_c)::value;
-      const int j0 = (kt0 + it) * KT;
+      const int j0 = (kt0 + it) * KT, jw = j0 + wkey;
       CONVSEL_WAIT_VMCNT(0);
       lds_sync();
       if (kt0 + it + 2 < kt1) issue(P, j0 + 2 * KT, false);
       if constexpr (!LAST) issue(P ^ 1, j0 + KT, true);
-      if (!(j0 >= in_lo && j0 + KT <= in_hi)) hide(sc, j0);
+      if (!(jw >= in_lo && jw + 32 * SB <= in_hi)) hide(sc, jw);
       float most = -kInf;
       vec16 fv[NC];
       auto top = [&](auto n) {  // an eighth of the scores
-        most = max3(max3(most, sc[0][2 * n], sc[0][2 * n + 1]), sc[1][2 * n], sc[1][2 * n + 1]);
+        static_for<SB>([&](auto b) { most = max3(most, sc[b][2 * n], sc[b][2 * n + 1]); });
       };
       auto settle = [&] {
         const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
@@ -395,7 +414,7 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
         settle();
         static_for<8>([&](auto e) { weigh(sc, zero, e); });
       } else {
-        constexpr int M = NQ >= 16 ? 4 : 2;  // products beside the maximum; 8 weights beside the others
+        constexpr int M = NQ >= 16 ? 4 : NQ >= 4 ? 2 : 1;  // products beside the maximum; 8 weights beside the others
         scores(std::integral_constant<int, P ^ 1>{}, nx, [&](auto n) {
           if constexpr (n < M)
             static_for<8 / M>([&](auto x) { top(std::integral_constant<int, decltype(n)::value * (8 / M) + decltype(x)::value>{}); });
@@ -403,16 +422,16 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
             fix();
             settle();
           }
-          constexpr int R = NQ - M, i0 = n < M ? 0 : (n - M) * 8 / R, i1 = n < M ? 0 : (n - M + 1) * 8 / R;
+          constexpr int rest = NQ - M, i0 = n < M ? 0 : (n - M) * 8 / rest, i1 = n < M ? 0 : (n - M + 1) * 8 / rest;
           static_for<i1 - i0>([&](auto e) { weigh(sc, zero, std::integral_constant<int, i0 + decltype(e)::value>{}); });
-          if constexpr (n == NQ - 4 || (NQ < 4 && n == 0)) first_values();
+          if constexpr (n == (NQ > 4 ? NQ - 4 : 0)) first_values();
         });
       }
-      static_for<4>([&](auto kb) {
+      static_for<2 * SB>([&](auto kb) {
         static_for<2 * NC>([&](auto n) {
           constexpr int i = n % NC;
           mfma_32x32<T>(o[i], fv[i], n < NC ? wh[kb & 1] : wl[kb & 1]);
-          if constexpr (kb + 1 < 4) {
+          if constexpr (kb + 1 < 2 * SB) {
             if constexpr (n >= NC) fv[i] = value(P, kb + 1, i);
             constexpr int i0 = n * 8 / (2 * NC), i1 = (n + 1) * 8 / (2 * NC);
             static_for<i1 - i0>([&](auto e) {
@@ -481,9 +500,53 @@ __global__ __launch_bounds__(64 * kWaves, (NC <= 4 && sizeof(T) == 2) ? 2 : 1) v
     lds_sync();
   }
 
-  // Lane (row, half) holds columns 32 i + 8 (v / 4) + 4 half + v % 4.
   l += __shfl_xor(l, 32);
-  if (r0 + wave * 32 + col < rows) {
+  if constexpr (G > 1) {
+    // The groups' results meet in the first one's waves, brought to the largest of their maxima.
+    typedef __attribute__((address_space(3))) float lds_float_t;
+    typedef __attribute__((address_space(3))) f32x4_t lds_f32x4_t;
+    lds_float_t* stat = (lds_float_t*)(lds_char_t*)lds;
+    lds_f32x4_t* part = (lds_f32x4_t*)((lds_char_t*)lds + 1024);
+    if (half == 0) {
+      stat[2 * (wave * 32 + col)] = m;
+      stat[2 * (wave * 32 + col) + 1] = l;
+    }
+    lds_sync();
+    float most = m, sum = 0.f;
+#pragma unroll
+    for (int x = 0; x < G; ++x) most = fmaxf(most, stat[2 * ((x * R + wave % R) * 32 + col)]);
+#pragma unroll
+    for (int x = 0; x < G; ++x) {
+      const lds_float_t* at = stat + 2 * ((x * R + wave % R) * 32 + col);
+      sum += at[1] * __builtin_amdgcn_exp2f(at[0] - most);
+    }
+    const float s = __builtin_amdgcn_exp2f(m - most);
+    l = sum;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) o[i] *= s;
+    if (wave >= R) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4)
+          part[((wave - R) * NC * 4 + i * 4 + v4) * 64 + lane] =
+              f32x4_t{o[i][4 * v4], o[i][4 * v4 + 1], o[i][4 * v4 + 2], o[i][4 * v4 + 3]};
+    }
+    lds_sync();
+    if (wave >= R) return;
+#pragma unroll
+    for (int x = 1; x < G; ++x)
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+#pragma unroll
+        for (int v4 = 0; v4 < 4; ++v4) {
+          const f32x4_t t = part[(((x - 1) * R + wave) * NC * 4 + i * 4 + v4) * 64 + lane];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][4 * v4 + e] += t[e];
+        }
+  }
+  // Lane (row, half) holds columns 32 i + 8 (v / 4) + 4 half + v % 4.
+  if (r0 + wrow + col < rows) {
     const float inv = 1.f / l;
     T* dst = reinterpret_cast<T*>(g.y) + (sp.first + tok) * g.y_token + hq * g.y_head;
 #pragma unroll
@@ -568,13 +631,58 @@ void pack(const PromptArgs& g, const void*& src, int64_t& token, int64_t& head, 
   ws += bytes;
 }
 
-template <typename T, int NC>
-hipError_t launch_nc(PromptLaunch a, hipStream_t st) {
+template <typename T, int NC, int R>
+hipError_t launch_rows(PromptLaunch a, hipStream_t st) {
   each_grid(a.units, [&](const UnitRow& r, unsigned n) {
     a.units = r;
-    hipLaunchKernelGGL((prompt_attention_kernel<T, NC>), dim3((unsigned)a.g.kv_heads, 1, n), dim3(64 * kWaves), 0, st, a);
+    hipLaunchKernelGGL((prompt_attention_kernel<T, NC, R>), dim3((unsigned)a.g.kv_heads, 1, n), dim3(64 * kWaves), 0, st,
+                       a);
   });
   return hipGetLastError();
+}
+
+// Whether tiles of so many blocks of rows fit in LDS: two of them in bf16, one at least in fp32.
+constexpr bool fits(int blocks, int es, int nc) {
+  return blocks == 4 || (es == 2 ? 4 : 2) * (blocks == 2 ? 64 : 128) * 32 * nc * es <= 144 * 1024;
+}
+
+UnitRow units_for(const PromptArgs& g, int blocks) {
+  convsel_kv_batch_t b = {};
+  b.seqs = g.seqs;
+  b.tokens = g.tokens;
+  return unit_row(b, g.q_heads / g.kv_heads, blocks == 4 ? 7 : blocks == 2 ? 6 : 5);
+}
+
+// Blocks of 32 rows a workgroup: four, or, where that gives few workgroups, two or one, whose keys the waves share out.
+// us of a call (and 8 of a graph's launch) with four, two and one:
+//   bf16, 32/8 heads of 128, 700, 1024, 2048 tokens   27 24 36 | 36 30 53 | 72 74 137
+//         8/8 heads of 128, 1024, 2048, 4096          32 25 22 | 55 40 38 | 104 81 106
+//         16/4 heads of 64, 1024, 2048, 4096          25 21 17 | 41 32 32 | 86 75 85
+//   fp32, 8/8 heads of 64, 300, 1024, 2048            34 22 18 | 88 51 33 | 167 92 62
+//         12/4 heads of 80, 300, 1024, 2048           44 28 24 | 122 70 47 | 233 135 143
+//         32/8 heads of 128, 300, 701                 56 36 30 | 114 67 81
+int blocks_for(const PromptArgs& g) {
+  const bool f32 = g.dtype == CONV_F32;
+  const int64_t enough[2] = {560, f32 && g.dim <= 64 ? 512 : 256};  // workgroups, of four blocks and of two
+  int best = 4;
+  for (int blocks = 2; blocks > 0; blocks /= 2) {
+    if ((int64_t)units_of(units_for(g, best)) * g.kv_heads >= enough[best == 2]) break;
+    if (fits(blocks, (int)elem_bytes(g), (g.dim + 31) / 32)) best = blocks;
+  }
+  return best;
+}
+
+template <typename T, int NC>
+hipError_t launch_nc(PromptLaunch a, hipStream_t st) {
+  const int blocks = blocks_for(a.g);
+  a.units = units_for(a.g, blocks);
+  if constexpr (fits(1, sizeof(T), NC)) {
+    if (blocks == 1) return launch_rows<T, NC, 1>(a, st);
+  }
+  if constexpr (fits(2, sizeof(T), NC)) {
+    if (blocks == 2) return launch_rows<T, NC, 2>(a, st);
+  }
+  return launch_rows<T, NC, 4>(a, st);
 }
 
 template <typename T>
@@ -592,12 +700,6 @@ hipError_t launch(const PromptArgs& g, void* workspace, hipStream_t st) {
   while (((int64_t)1 << (a.shift - 31)) < a.group) ++a.shift;
   a.magic = (uint32_t)((((uint64_t)1 << a.shift) + a.group - 1) / a.group);
   a.y_vec = g.dim % 4 == 0 && g.y_token % 4 == 0 && g.y_head % 4 == 0 && (uintptr_t)g.y % (4 * sizeof(T)) == 0;
-  convsel_kv_batch_t b = {};
-  b.seqs = g.seqs;
-  b.tokens = g.tokens;
-  int shift = 0;
-  while ((1 << shift) < kRows) ++shift;
-  a.units = unit_row(b, a.group, shift);
   switch ((g.dim + 31) / 32) {
     case 1: return launch_nc<T, 1>(a, st);
     case 2: return launch_nc<T, 2>(a, st);
@@ -622,9 +724,8 @@ hipError_t launch_prompt_attention(const PromptArgs& a, void* workspace, hipStre
 }
 
 void prompt_attention_describe(const PromptArgs& a, char* buf, size_t len) {
-  snprintf(buf, len, "prompt_attention kernels=%sprompt_attention_kernel rows=%d keys=%d workspace=%zu",
-           prompt_attention_workspace(a) ? "prompt_pack_kernel;" : "", kRows, a.dtype == CONV_F32 ? 32 : 64,
-           prompt_attention_workspace(a));
+  snprintf(buf, len, "prompt_attention kernels=%sprompt_attention_kernel rows=%d workspace=%zu",
+           prompt_attention_workspace(a) ? "prompt_pack_kernel;" : "", 32 * blocks_for(a), prompt_attention_workspace(a));
 }
 
 }  // namespace convsel

@@ -154,6 +154,22 @@ def test_prompt_offsets_are_bounded():
         assert y.shape == q.shape
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [40, 64, 128, 200])
+@pytest.mark.parametrize("rows,counts", [(128, [301] * 14), (64, [370] * 5 + [1, 0, 7]), (32, [100, 31])])
+def test_prompt_rows_of_a_workgroup(dtype, dim, rows, counts):
+    """Waves that share out rows, keys, or both."""
+    say("case prompt rows", dtype, dim, rows)
+    assert "rows=%d " % rows in cs.describe_prompt_attention(len(counts), sum(counts), 16, 8, dim, DT[dtype]) or (
+        dim == 200 and rows == 32)
+    q, k, v = heads_of(gen(rows + dim), sum(counts), 16, 8, dim, DT[dtype])
+    check_prompt(q, k, v, counts)
+    check_prompt(q, k, v, counts, True, 77)
+    v[counts[0] - 40, 2, 5] = float("inf")
+    k[20, 1, 0] = k[20, 1, 0] * 0 + 60
+    check_prompt(q, k, v, counts)
+
+
 def test_prompt_repeats_bit_for_bit_and_long_rows_agree_with_many_heads():
     q, k, v = heads_of(gen(8), 2000, 8, 2, 128, torch.bfloat16)
     off = ints([0, 1300, 2000])
