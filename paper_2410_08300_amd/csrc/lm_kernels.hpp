@@ -27,6 +27,7 @@ struct LinearArgs {
   int64_t ldw = 0;
   const float* x_scale = nullptr;
   const float* w_scale = nullptr;
+  int64_t numbers = 0;  // of a row of x that the product's kernel codes itself; `in` is then that in whole 16-byte units
 };
 
 size_t linear_workspace(const LinearArgs& a);
