@@ -79,7 +79,7 @@ struct Shape {
   static constexpr int QU = U / 2;                            // units of a lane's half of a row
   static constexpr int TILE = KT * RB, NDMA = TILE / 1024 / kWaves;
   static constexpr int BUFS = 4 * TILE <= 144 * 1024 ? 2 : 1;  // tiles in LDS
-  static constexpr int PER_CU = ES == 2 && NC <= 4 && TILE <= 20 * 1024 - 16 ? 2 : 1;  // workgroups that a CU holds
+  static constexpr int PER_CU = ES == 2 && NC <= 4 && TILE <= 20 * 1024 - 16 ? (NC <= 2 && KT == 64 ? 3 : 2) : 1;  // workgroups that a CU holds
   __device__ static __forceinline__ int turn_k(int r) {
     return U % 16 == 0 ? r & 15 : U % 8 == 0 ? (r >> 1) & 7 : (r >> 2) & 3;
   }
@@ -658,12 +658,14 @@ UnitRow units_for(const PromptArgs& g, int blocks) {
 //   bf16, 32/8 heads of 128, 700, 1024, 2048 tokens   27 24 36 | 36 30 53 | 72 74 137
 //         8/8 heads of 128, 1024, 2048, 4096          32 25 22 | 55 40 38 | 104 81 106
 //         16/4 heads of 64, 1024, 2048, 4096          25 21 17 | 41 32 32 | 86 75 85
+//         8/2 heads of 256, 4096, 8192                170 125 | 389 460
 //   fp32, 8/8 heads of 64, 300, 1024, 2048            34 22 18 | 88 51 33 | 167 92 62
 //         12/4 heads of 80, 300, 1024, 2048           44 28 24 | 122 70 47 | 233 135 143
 //         32/8 heads of 128, 300, 701                 56 36 30 | 114 67 81
 int blocks_for(const PromptArgs& g) {
   const bool f32 = g.dtype == CONV_F32;
-  const int64_t enough[2] = {560, f32 && g.dim <= 64 ? 512 : 256};  // workgroups, of four blocks and of two
+  // Workgroups that are enough, of four blocks and of two.
+  const int64_t enough[2] = {!f32 && (g.dim > 128 || !g.causal) ? 400 : 560, f32 && g.dim <= 64 ? 512 : 256};
   int best = 4;
   for (int blocks = 2; blocks > 0; blocks /= 2) {
     if ((int64_t)units_of(units_for(g, best)) * g.kv_heads >= enough[best == 2]) break;
