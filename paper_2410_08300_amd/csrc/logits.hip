@@ -1,7 +1,7 @@
 // Penalties of repeated tokens, biases and masks on the logits of a batch.
 //
-// A workgroup owns 2048 STEPS neighbouring tokens of a row, eight at a time a
-// thread, whose logits are on their way while it counts in LDS how often its row's
+// A workgroup owns 8 THREADS STEPS neighbouring tokens of a row, eight at a time
+// a thread, whose logits are on their way while it counts in LDS how often its row's
 // history holds each of them (whole numbers, in any order).  What bounds it:
 // traffic, and the history, which every workgroup of a row reads from the caches.
 #include "lm_common.hpp"
@@ -12,7 +12,7 @@ namespace {
 
 using namespace lm;
 
-constexpr int kThreads = 256, kEach = 8;
+constexpr int kEach = 8;  // tokens of a step of a thread
 constexpr uint32_t kSeen = 0x80000000u;  // the prompt holds it; the bits below count generated ones
 
 // Eight values; rows lie on any alignment of elements, which wide loads and stores of global memory may too.
@@ -35,9 +35,9 @@ __device__ __forceinline__ void put8(bf16_t* p, const float (&z)[8]) {
   __builtin_memcpy(p, &v, 16);
 }
 
-template <typename T, int STEPS>
-__global__ __launch_bounds__(kThreads) void adjust_logits_kernel(LogitsArgs a, int64_t chunks) {
-  constexpr int CHUNK = kThreads * kEach * STEPS;
+template <typename T, int THREADS, int STEPS>
+__global__ __launch_bounds__(THREADS) void adjust_logits_kernel(LogitsArgs a, int64_t chunks) {
+  constexpr int CHUNK = THREADS * kEach * STEPS;
   extern __shared__ __align__(16) uint32_t count[];  // CHUNK of them, with a history
   for (int64_t unit = blockIdx.x; unit < chunks * a.rows; unit += gridDim.x) {
     const int64_t row = unit / chunks, c0 = (unit - row * chunks) * CHUNK;
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(LogitsArgs a, i
     float z[STEPS][kEach];
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-      const int i = (s * kThreads + threadIdx.x) * kEach;
+      const int i = (s * THREADS + threadIdx.x) * kEach;
       if (i + kEach <= width) {
         get8(x + i, z[s]);
       } else {
@@ -66,15 +66,15 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(LogitsArgs a, i
       const int generated = first + (a.prompt_lengths ? clampi(a.prompt_lengths[row], 0, end - first) : 0);
 #pragma unroll
       for (int s = 0; s < 2 * STEPS; ++s)
-        *reinterpret_cast<uint4*>(count + (s * kThreads + threadIdx.x) * 4) = make_uint4(0, 0, 0, 0);
+        *reinterpret_cast<uint4*>(count + (s * THREADS + threadIdx.x) * 4) = make_uint4(0, 0, 0, 0);
       lds_sync();
-      for (int64_t i0 = first + static_cast<int>(threadIdx.x); i0 < end; i0 += 4 * kThreads) {
+      for (int64_t i0 = first + static_cast<int>(threadIdx.x); i0 < end; i0 += 4 * THREADS) {
         int64_t at[4];
 #pragma unroll
-        for (int n = 0; n < 4; ++n) at[n] = a.history[min(i0 + n * kThreads, static_cast<int64_t>(end) - 1)] - c0;
+        for (int n = 0; n < 4; ++n) at[n] = a.history[min(i0 + n * THREADS, static_cast<int64_t>(end) - 1)] - c0;
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
-          const int64_t i = i0 + n * kThreads;
+          const int64_t i = i0 + n * THREADS;
           if (i < end && at[n] >= 0 && at[n] < width) {
             if (i < generated)
               atomicOr(&count[at[n]], kSeen);
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(LogitsArgs a, i
     const uint32_t* mask = a.mask ? a.mask + row * a.ldmask + c0 / 32 : nullptr;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-      const int i = (s * kThreads + threadIdx.x) * kEach;
+      const int i = (s * THREADS + threadIdx.x) * kEach;
       if (i >= width) break;
       float(&v)[kEach] = z[s];
       if (counted) {
@@ -137,19 +137,29 @@ __global__ __launch_bounds__(kThreads) void adjust_logits_kernel(LogitsArgs a, i
   }
 }
 
-template <typename T, int STEPS>
+template <typename T, int THREADS, int STEPS>
 hipError_t launch(const LogitsArgs& a, hipStream_t st) {
-  constexpr int chunk = kThreads * kEach * STEPS;
+  constexpr int chunk = THREADS * kEach * STEPS;
   const int64_t chunks = (a.vocab + chunk - 1) / chunk, units = chunks * a.rows;
-  hipLaunchKernelGGL((adjust_logits_kernel<T, STEPS>), dim3((unsigned)(units < (1 << 20) ? units : 1 << 20)),
-                     dim3(kThreads), a.history ? chunk * 4 : 0, st, a, chunks);
+  hipLaunchKernelGGL((adjust_logits_kernel<T, THREADS, STEPS>), dim3((unsigned)(units < (1 << 20) ? units : 1 << 20)),
+                     dim3(THREADS), a.history ? chunk * 4 : 0, st, a, chunks);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_steps(const LogitsArgs& a, hipStream_t st) {
-  // Few tokens in all: more workgroups, of fewer tokens each.
-  return a.rows * ((a.vocab + 8191) / 8192) < 512 ? launch<T, 1>(a, st) : launch<T, 4>(a, st);
+  // Threads and steps, in us with 256 x 1, 256 x 4, 512 x 2 and 1024 x 4:
+  //   bf16, 8 rows of 128000, histories of 2000 and 1 of 8000    5.4 8.7 6.0 9.1 | 7.2 12.1 6.8 10.1
+  //         32 and 256 of 128000, 2000                           9.7 10.1 8.1 10.4 | 46.9 47.5 43.6 44.6
+  //         64 of 128000, 8000                                   24.3 18.7 16.6 13.5
+  //   fp32, 256 of 128000, 600, and with a bias and a mask       62.0 63.9 64.9 71.5 | 71.3 68.7 70.9 75.1
+  //         16 of 200000, 8000                                   15.0 15.1 12.2 14.4
+  // Few logits need many workgroups, long histories few readers of them.
+  const int64_t units = a.rows * ((a.vocab + 8191) / 8192);
+  const bool longs = a.tokens / a.rows >= 4000;
+  if (units < 256) return longs ? launch<T, 512, 2>(a, st) : launch<T, 256, 1>(a, st);
+  if (longs && units >= 1024) return launch<T, 1024, 4>(a, st);
+  return sizeof(T) == 4 && !longs ? launch<T, 256, 4>(a, st) : launch<T, 512, 2>(a, st);
 }
 
 }  // namespace

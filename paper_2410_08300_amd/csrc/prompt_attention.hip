@@ -662,6 +662,10 @@ UnitRow units_for(const PromptArgs& g, int blocks) {
 //   fp32, 8/8 heads of 64, 300, 1024, 2048            34 22 18 | 88 51 33 | 167 92 62
 //         12/4 heads of 80, 300, 1024, 2048           44 28 24 | 122 70 47 | 233 135 143
 //         32/8 heads of 128, 300, 701                 56 36 30 | 114 67 81
+// One block has most to join, so sequences are to be long enough for it.  us of the kernel alone:
+//   bf16, 8/8 heads of 128, 64, 200, 400 tokens        6 7 8 | 11 9 9 | 15 12 11
+//         16/4 heads of 64, 64, 200, 400               6 5 6 | 8 7 6 | 11 9 8
+//   fp32, 12/4 heads of 80, 37, 100                    12 9 10 | 19 13 10
 int blocks_for(const PromptArgs& g) {
   const bool f32 = g.dtype == CONV_F32;
   // Workgroups that are enough, of four blocks and of two.
@@ -669,6 +673,7 @@ int blocks_for(const PromptArgs& g) {
   int best = 4;
   for (int blocks = 2; blocks > 0; blocks /= 2) {
     if ((int64_t)units_of(units_for(g, best)) * g.kv_heads >= enough[best == 2]) break;
+    if (blocks == 1 && g.tokens < g.seqs * (f32 ? 64 : 3 * (int64_t)g.dim)) break;
     if (fits(blocks, (int)elem_bytes(g), (g.dim + 31) / 32)) best = blocks;
   }
   return best;

@@ -373,6 +373,24 @@ def test_logits_penalties_alone(prompts, rep, pres, freq):
     check_logits(randn(gen(4), 4, 500), [0, 3000, 1, 77], 5, prompts, rep, pres, freq)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,vocab,seen", [(3, 700, 4100), (40, 60001, 30), (33, 70000, 30), (260, 33000, 4000)])
+def test_logits_of_many_rows_and_long_histories(dtype, n, vocab, seen):
+    """Every width of a workgroup; the last of these only where rows differ from the adjusted logits of one alone."""
+    say("case logits", dtype, n, vocab, seen)
+    x = randn(gen(n), n, vocab, dtype=DT[dtype])
+    if n < 100:
+        check_logits(x, [seen + i % 3 for i in range(n)], n, mask=1)
+        return
+    h = torch.randint(0, vocab, (n * seen,), generator=gen(1), device=DEV, dtype=torch.int32)
+    off = torch.arange(n + 1, device=DEV, dtype=torch.int32) * seen
+    p = [0.5 + torch.rand(n, generator=gen(2 + i), device=DEV) for i in range(3)]
+    whole = cs.adjust_logits(x, h, off, None, *p)
+    for b in (0, 1, 130, 259):
+        one = cs.adjust_logits(x[b:b + 1], h[b * seen:(b + 1) * seen], ints([0, seen]), None, *(t[b:b + 1] for t in p))
+        assert torch.equal(whole[b], one[0])
+
+
 def test_logits_history_of_nothing_and_tokens_outside():
     x = randn(gen(4), 4, 50, dtype=torch.bfloat16)
     check_logits(x, [0, 0, 0, 0], 1)
