@@ -156,7 +156,7 @@ def test_prompt_offsets_are_bounded():
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("dim", [40, 64, 128, 200])
-@pytest.mark.parametrize("rows,counts", [(128, [301] * 14), (64, [370] * 5 + [1, 0, 7]), (32, [100, 31])])
+@pytest.mark.parametrize("rows,counts", [(128, [301] * 14), (64, [370] * 5 + [1, 0, 7]), (32, [450, 400])])
 def test_prompt_rows_of_a_workgroup(dtype, dim, rows, counts):
     """Waves that share out rows, keys, or both."""
     say("case prompt rows", dtype, dim, rows)
