@@ -347,7 +347,7 @@ Plan plan_of(const LinearArgs& a, int x_dtype) {
 hipError_t launch_quantize_rows(const CodeArgs& a, hipStream_t stream) {
   const int64_t per = a.dtype == CONV_F32 ? 4 : 8;
   const int vec = a.ldx % per == 0 && (uintptr_t)a.x % 16 == 0;
-  const int64_t x = a.m < 65535 * (int64_t)256 ? (a.m < 65535 ? a.m : 65535) : 1 << 24;
+  const int64_t x = a.m < 65535 * (int64_t)256 ? (a.m < 65535 ? a.m : 65535) : 1 << 23;
   const dim3 grid((unsigned)x, (unsigned)((a.m + x - 1) / x));
   if (a.dtype == CONV_F32)
     hipLaunchKernelGGL(quantize_rows_kernel<float>, grid, dim3(256), 0, stream, a, vec);

@@ -390,6 +390,9 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<T, NC, R>::PER_CU)) void prompt
       constexpr int P = decltype(p_c)::value;
       constexpr bool LAST = decltype(last_c)::value;
       const int j0 = (kt0 + it) * KT, jw = j0 + wkey;
+      // Formed before the barrier, whatever the compiler moves: max3() reads them without its knowledge.
+#pragma unroll
+      for (int b = 0; b < SB; ++b) asm volatile("" : "+v"(sc[b]));
       CONVSEL_WAIT_VMCNT(0);
       lds_sync();
       if (kt0 + it + 2 < kt1) issue(P, j0 + 2 * KT, false);
@@ -599,9 +602,9 @@ __global__ __launch_bounds__(256) void prompt_pack_kernel(const T* src, int64_t 
 int64_t elem_bytes(const PromptArgs& a) { return a.dtype == CONV_F32 ? 4 : 2; }
 int64_t row_units(const PromptArgs& a) { return (a.dim * elem_bytes(a) + 15) / 16; }
 
-// Whether rows are no whole 16-byte units, or so far apart that a tile of 64 of them does not fit a buffer.
+// Whether rows are no whole 16-byte units, or so far apart that a tile of 128 of them does not fit a buffer.
 bool needs_pack(const PromptArgs& a, const void* p, int64_t token, int64_t head) {
-  const int64_t es = elem_bytes(a), per = 16 / es, far = ((int64_t)1 << 31) / 64 / es - 256;
+  const int64_t es = elem_bytes(a), per = 16 / es, far = ((int64_t)1 << 31) / 128 / es - 256;
   return a.dim % per != 0 || token % per != 0 || head % per != 0 || (uintptr_t)p % 16 != 0 || token > far;
 }
 

@@ -89,6 +89,14 @@ def test_prompt_workspace_follows_alignment():
     assert prompt(d, ws=A, n=n) == INVALID and prompt(d, ws=E, n=n) == INVALID and prompt(d, ws=D - 256, n=n) == INVALID
 
 
+def test_prompt_rows_far_apart_are_copied():
+    """A tile of 128 keys is addressed in 32 bits."""
+    near, far = (1 << 31) // 128 // 2 - 256, (1 << 31) // 128 // 2
+    assert prompt_bytes(prompt_desc(k_token_stride=near, v_token_stride=near)) == (0, 0)
+    assert prompt_bytes(prompt_desc(k_token_stride=far))[1] == (10 * 2 * 128 + 255) // 256 * 256
+    assert prompt_bytes(prompt_desc(dtype=0, v_token_stride=far // 2))[1] == 10 * 2 * 256
+
+
 def test_prompt_over_nothing_is_a_no_op():
     assert prompt(prompt_desc(tokens=0), q=None, y=None) == 0 and prompt(prompt_desc(seqs=0), q=None) == 0
     assert prompt_bytes(prompt_desc(tokens=0, head_dim=3)) == (0, 0)
