@@ -683,7 +683,7 @@ LinearTiles linear_tiles_plan(const LinearArgs& a) {
   // parts), 80, 138; 700 rows 46 (5), 56 (4), 48; 256 rows 32 (11), 27 (4), 25 (2).
   // Codes (4096 -> 4096): 4096 rows 60 us in 256s, 81 in 128s, 113 in 64s; 2048 rows 47, 43, 61; 512 rows 45, 27, 19;
   // joining s parts adds 6 + s / 2 (64 rows, 11008 -> 4096 in 64s: 37 in one part, 18 in 4 or 8).
-  static const double kOne[3][3] = {{8.3, 2.35, 0.7}, {1.67, 0.83, 0.36}, {1.6, 0.8, 0.42}};
+  static const double kOne[3][3] = {{8.3, 2.35, 0.7}, {1.67, 0.83, 0.36}, {1.6, 0.95, 0.42}};
   static const double kEach[3][3] = {{8.3, 2.15, 0.61}, {1.67, 0.61, 0.25}, {1.6, 0.645, 0.28}};
   static const double kAlone[3] = {6., 0., 0.};
   const int ty = a.codes ? 2 : a.dtype == CONV_F32 ? 0 : 1;
