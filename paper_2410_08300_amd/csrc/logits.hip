@@ -27,15 +27,30 @@ __device__ __forceinline__ void get8(const T* p, float (&z)[8]) {
     for (int e = 0; e < UE; ++e) z[u * UE + e] = elem<T>::to_f32(vec16_get<T>(v, e));
   }
 }
-__device__ __forceinline__ void put8(float* p, const float (&z)[8]) { __builtin_memcpy(p, z, 32); }
-__device__ __forceinline__ void put8(bf16_t* p, const float (&z)[8]) {
-  vec16 v;
+// Stored past the caches where there is more than they hold: what a call reads then stays in them (256 rows of 128000 in
+// bf16 with histories of 2000: 44 us, 34 so; in fp32, 64 and 61).
+typedef uint32_t words_t __attribute__((ext_vector_type(4), aligned(2)));
+template <bool PAST>
+__device__ __forceinline__ void put16(void* p, const words_t& w) {
+  if constexpr (PAST)
+    __builtin_nontemporal_store(w, reinterpret_cast<words_t*>(p));
+  else
+    *reinterpret_cast<words_t*>(p) = w;
+}
+template <bool PAST>
+__device__ __forceinline__ void put8(float* p, const float (&z)[8]) {
 #pragma unroll
-  for (int w = 0; w < 4; ++w) v.d[w] = f32x2_to_bf16x2(z[2 * w], z[2 * w + 1]);
-  __builtin_memcpy(p, &v, 16);
+  for (int u = 0; u < 8; u += 4)
+    put16<PAST>(p + u, words_t{__float_as_uint(z[u]), __float_as_uint(z[u + 1]), __float_as_uint(z[u + 2]),
+                               __float_as_uint(z[u + 3])});
+}
+template <bool PAST>
+__device__ __forceinline__ void put8(bf16_t* p, const float (&z)[8]) {
+  put16<PAST>(p, words_t{f32x2_to_bf16x2(z[0], z[1]), f32x2_to_bf16x2(z[2], z[3]), f32x2_to_bf16x2(z[4], z[5]),
+                         f32x2_to_bf16x2(z[6], z[7])});
 }
 
-template <typename T, int THREADS, int STEPS>
+template <typename T, int THREADS, int STEPS, bool PAST>
 __global__ __launch_bounds__(THREADS) void adjust_logits_kernel(LogitsArgs a, int64_t chunks) {
   constexpr int CHUNK = THREADS * kEach * STEPS;
   extern __shared__ __align__(16) uint32_t count[];  // CHUNK of them, with a history
@@ -126,7 +141,7 @@ __global__ __launch_bounds__(THREADS) void adjust_logits_kernel(LogitsArgs a, in
         for (int e = 0; e < kEach; ++e) v[e] = (bits >> e) & 1u ? v[e] : -__builtin_inff();
       }
       if (whole) {
-        put8(y + i, v);
+        put8<PAST>(y + i, v);
       } else {
 #pragma unroll
         for (int e = 0; e < kEach; ++e)
@@ -137,11 +152,11 @@ __global__ __launch_bounds__(THREADS) void adjust_logits_kernel(LogitsArgs a, in
   }
 }
 
-template <typename T, int THREADS, int STEPS>
+template <typename T, int THREADS, int STEPS, bool PAST>
 hipError_t launch(const LogitsArgs& a, hipStream_t st) {
   constexpr int chunk = THREADS * kEach * STEPS;
   const int64_t chunks = (a.vocab + chunk - 1) / chunk, units = chunks * a.rows;
-  hipLaunchKernelGGL((adjust_logits_kernel<T, THREADS, STEPS>), dim3((unsigned)(units < (1 << 20) ? units : 1 << 20)),
+  hipLaunchKernelGGL((adjust_logits_kernel<T, THREADS, STEPS, PAST>), dim3((unsigned)(units < (1 << 20) ? units : 1 << 20)),
                      dim3(THREADS), a.history ? chunk * 4 : 0, st, a, chunks);
   return hipGetLastError();
 }
@@ -157,9 +172,9 @@ hipError_t launch_steps(const LogitsArgs& a, hipStream_t st) {
   // Few logits need many workgroups, long histories few readers of them.
   const int64_t units = a.rows * ((a.vocab + 8191) / 8192);
   const bool longs = a.tokens / a.rows >= 4000;
-  if (units < 256) return longs ? launch<T, 512, 2>(a, st) : launch<T, 256, 1>(a, st);
-  if (longs && units >= 1024) return launch<T, 1024, 4>(a, st);
-  return sizeof(T) == 4 && !longs ? launch<T, 256, 4>(a, st) : launch<T, 512, 2>(a, st);
+  if (units < 256) return longs ? launch<T, 512, 2, false>(a, st) : launch<T, 256, 1, false>(a, st);
+  if (longs && units >= 1024) return launch<T, 1024, 4, true>(a, st);
+  return sizeof(T) == 4 && !longs ? launch<T, 256, 4, true>(a, st) : launch<T, 512, 2, true>(a, st);
 }
 
 }  // namespace
