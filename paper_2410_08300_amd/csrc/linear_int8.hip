@@ -5,7 +5,13 @@
 // Many rows go in the tiles of linear_tiles.hip, whose walk of 16-byte units is
 // the same for codes, sixteen a unit; few stream the weights through registers
 // (here).  Rows of x that come as numbers are coded by a kernel before the
-// product.
+// product (4096 rows of 4096 in bf16: 13 us, 3.8 TB/s), one or two of them by the
+// product's own.
+//
+// What bounds it: few rows, the weights' way from memory (1 row, 4096 -> 4096:
+// 6.5 us in the kernel, 2.6 TB/s, of which launch and first loads are half); many,
+// the matrix cores at the clock that the card's power leaves (4096 rows, 4096 ->
+// 16384: 231 us, 2380 TOP/s; a large library product reaches 2130).
 #include <stdio.h>
 
 #include <type_traits>
@@ -269,8 +275,8 @@ hipError_t launch_rows(const LinearArgs& a, hipStream_t st) {
     b.m = a.m - m0;
     const int64_t n = groups - g0 < 65535 ? groups - g0 : 65535;
     if (n * 16 < b.m) b.m = n * 16;
-    hipLaunchKernelGGL((linear_int8_rows_kernel<Y, X>), dim3((unsigned)((a.out + 15) / 16), (unsigned)n), dim3(64 * waves),
-                       lds, st, b, waves, vec_out, vec_in);
+    const dim3 grid((unsigned)((a.out + 15) / 16), (unsigned)n);
+    hipLaunchKernelGGL((linear_int8_rows_kernel<Y, X>), grid, dim3(64 * waves), lds, st, b, waves, vec_out, vec_in);
   }
   return hipGetLastError();
 }
@@ -291,8 +297,8 @@ struct Plan {
 };
 
 // Few rows, in us.  By rows: 2.3 and the way of a CU's share of the weights, 16.8 GB/s, a quarter longer with 16 rows.
-// In tiles: by their plan, which counts no bytes, but at least 7 and all bytes at a copy's rate.  us by rows and in tiles,
-// rows coded before, weights from memory:
+// In tiles: by their plan, which counts no bytes, but at least 7 and all bytes at a copy's rate.  us by rows and in
+// tiles, rows coded before, weights from memory:
 //   from 4096 -> 4096     4096 -> 12288   11008 -> 4096    2048 -> 1024
 //     1 row    6.3  9.3    14.1 16.1       13.6 15.1        4.1 6.9
 //     16       7.2  9.9    17.7 16.6       15.6 15.2        4.7 7.1
@@ -304,12 +310,13 @@ bool in_rows(const LinearArgs& a, const LinearTiles& t) {
   if (t.config < 0) return true;
   if (a.m > kFewRows) return false;
   const double groups = (double)((a.out + 15) / 16 * ((a.m + 15) / 16));
-  const double rows = 2.3 + (groups > 256 ? groups / 256 : 1.) * 16. * a.in / 16.8e3 * (1 + 0.25 * (a.m < 16 ? a.m : 16) / 16);
+  const double share = (groups > 256 ? groups / 256 : 1.) * 16. * a.in;
+  const double rows = 2.3 + share / 16.8e3 * (1 + 0.25 * (a.m < 16 ? a.m : 16) / 16);
   const double least = 7 + ((double)a.out * a.in + (double)a.m * (a.in + 4 * a.out)) / 5.05e6;
   return rows <= (t.us + 1.7 > least ? t.us + 1.7 : least);
 }
 
-// Whether the kernel for few rows codes them itself: every workgroup does, one row after the other.  us of both ways, from
+// Whether the kernel for few rows codes them itself: every workgroup does, one row after the other.  us of both ways,
 // 4096 -> 4096 in bf16: 1 row 7.8 and 9.9, 2 rows 9.0 and 10.2, 4 rows 11.7 and 10.4; 1 row, 16384 -> 4096: 19 and 24.
 bool coded_inside(const LinearArgs& a) { return a.m <= 2 && a.m * (padded(a.in) + 16) <= 40 * 1024; }
 

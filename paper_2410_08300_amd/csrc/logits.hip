@@ -3,7 +3,9 @@
 // A workgroup owns 8 THREADS STEPS neighbouring tokens of a row, eight at a time
 // a thread, whose logits are on their way while it counts in LDS how often its row's
 // history holds each of them (whole numbers, in any order).  What bounds it:
-// traffic, and the history, which every workgroup of a row reads from the caches.
+// traffic (256 rows of 128000 in fp32 without a history: 52 us, 5.0 TB/s, a copy's
+// rate), and the history, which every workgroup of a row reads from the caches (in
+// bf16 with histories of 2000: 34 us, 3.9 TB/s).
 #include "lm_common.hpp"
 #include "lm_kernels.hpp"
 
@@ -27,8 +29,8 @@ __device__ __forceinline__ void get8(const T* p, float (&z)[8]) {
     for (int e = 0; e < UE; ++e) z[u * UE + e] = elem<T>::to_f32(vec16_get<T>(v, e));
   }
 }
-// Stored past the caches where there is more than they hold: what a call reads then stays in them (256 rows of 128000 in
-// bf16 with histories of 2000: 44 us, 34 so; in fp32, 64 and 61).
+// Stored past the caches where there is more than they hold: what a call reads then stays in them (256 rows of 128000
+// in bf16 with histories of 2000: 44 us, 34 so; in fp32, 64 and 61).
 typedef uint32_t words_t __attribute__((ext_vector_type(4), aligned(2)));
 template <bool PAST>
 __device__ __forceinline__ void put16(void* p, const words_t& w) {
@@ -156,8 +158,9 @@ template <typename T, int THREADS, int STEPS, bool PAST>
 hipError_t launch(const LogitsArgs& a, hipStream_t st) {
   constexpr int chunk = THREADS * kEach * STEPS;
   const int64_t chunks = (a.vocab + chunk - 1) / chunk, units = chunks * a.rows;
-  hipLaunchKernelGGL((adjust_logits_kernel<T, THREADS, STEPS, PAST>), dim3((unsigned)(units < (1 << 20) ? units : 1 << 20)),
-                     dim3(THREADS), a.history ? chunk * 4 : 0, st, a, chunks);
+  const dim3 grid((unsigned)(units < (1 << 20) ? units : 1 << 20));
+  hipLaunchKernelGGL((adjust_logits_kernel<T, THREADS, STEPS, PAST>), grid, dim3(THREADS),
+                     a.history ? chunk * 4 : 0, st, a, chunks);
   return hipGetLastError();
 }
 

@@ -1,14 +1,16 @@
 // Attention of packed prompts over their own keys and values, in fp32 and bf16.
 //
-// A workgroup of four waves has 128 rows of a key head (a row is a query and one
-// of the heads that share the key head), 32 a wave, and walks the keys that they
-// see in tiles of 64 (bf16) or 32 (fp32), whose keys and values go to LDS by DMA
-// as they lie in memory, a tile ahead: one barrier a tile.  Scores are K q^T in
-// blocks of 32 x 32, so that a lane ends with 16 keys of one row, in runs of
-// four, and feeds its weights to the second product, V^T P^T, without moving
-// them: in which order a product takes the keys does not matter while both
-// operands agree.  V's operand needs four keys of one column a lane, which the
-// transposing LDS read gives for bf16 and single words for fp32.
+// A workgroup of four waves has 128, 64 or 32 rows of a key head (a row is a query
+// and one of the heads that share the key head), 32 a wave, and walks the keys
+// that they see in tiles, whose keys and values go to LDS by DMA as they lie in
+// memory, a tile ahead: one barrier a tile.  With fewer than 128 rows the waves
+// of a block of 32 share out each tile's keys, and their results meet at the end.
+//
+// Scores are K q^T in blocks of 32 x 32, so that a lane ends with 16 keys of one
+// row, in runs of four, and feeds its weights to the second product, V^T P^T,
+// without moving them: in which order a product takes the keys does not matter
+// while both operands agree.  V's operand needs four keys of one column a lane,
+// which the transposing LDS read gives for bf16 and single words for fp32.
 //
 // In LDS a row's 16-byte units are permuted so that the rows that are read
 // together fall on different banks: unit u of row r lies at u ^ turn(r), where
@@ -17,7 +19,17 @@
 // Softmax in one pass, in powers of two (the scale carries log2 e): running
 // maximum m and sum l of a row, weights 2^(s - m).  bf16 calls multiply each
 // weight as two bf16 numbers, 16 bits: one number, 8 bits, is off by as much as
-// the result's own rounding.  fp32 calls use the fp32 matrix instructions.
+// the result's own rounding (and would take 26 % less time).  fp32 calls use the
+// fp32 matrix instructions.
+//
+// What bounds it.  Heads of 128 and more, long: the matrix cores, half of whose
+// work with values is the weights' second numbers, at the clock that the card's
+// power leaves (8192 tokens of 32 heads on 8, causal: 710 us, 775 TFLOP/s, 1160
+// with the second numbers, at 1.77 GHz; matrix cores 65 % busy, vector unit 57 %).
+// Heads of 64: the vector unit (8192 tokens of 16 on 4: 227 us, 605 TFLOP/s, 78 %
+// busy); a weight costs a fused product, a transcendental (four slots), an
+// addition, three operations for its two numbers and half a maximum.  fp32: the
+// fp32 products (2048 tokens of 12 heads of 128 on 4: 162 us, 80 TFLOP/s).
 #include <stdio.h>
 
 #include <type_traits>
@@ -79,7 +91,8 @@ struct Shape {
   static constexpr int QU = U / 2;                            // units of a lane's half of a row
   static constexpr int TILE = KT * RB, NDMA = TILE / 1024 / kWaves;
   static constexpr int BUFS = 4 * TILE <= 144 * 1024 ? 2 : 1;  // tiles in LDS
-  static constexpr int PER_CU = ES == 2 && NC <= 4 && TILE <= 20 * 1024 - 16 ? (NC <= 2 && KT == 64 ? 3 : 2) : 1;  // workgroups that a CU holds
+  // Workgroups that a CU holds.
+  static constexpr int PER_CU = ES == 2 && NC <= 4 && TILE <= 20 * 1024 - 16 ? (NC <= 2 && KT == 64 ? 3 : 2) : 1;
   __device__ static __forceinline__ int turn_k(int r) {
     return U % 16 == 0 ? r & 15 : U % 8 == 0 ? (r >> 1) & 7 : (r >> 2) & 3;
   }
@@ -324,160 +337,168 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<T, NC, R>::PER_CU)) void prompt
   // the products with its values: a wave's vector operations run beside its own matrix ones.
   auto piped = [&] {
     if constexpr (PIPED) {
-    const auto fix = [] { __builtin_amdgcn_sched_barrier(0); };
-    // Places of the lane's operands that differ by more than a constant.
-    constexpr int PK = U % 16 == 0 ? 8 : U % 8 == 0 ? 4 : 2, PV = U % 16 == 0 ? 4 : U % 8 == 0 ? 2 : 1;
-    lds_char_t *ka[PK], *va[PV];
+      const auto fix = [] { __builtin_amdgcn_sched_barrier(0); };
+      // Places of the lane's operands that differ by more than a constant.
+      constexpr int PK = U % 16 == 0 ? 8 : U % 8 == 0 ? 4 : 2, PV = U % 16 == 0 ? 4 : U % 8 == 0 ? 2 : 1;
+      lds_char_t *ka[PK], *va[PV];
 #pragma unroll
-    for (int j = 0; j < PK; ++j) ka[j] = (lds_char_t*)lds + (wkey + col) * RB + (((2 * j + half) ^ S::turn_k(col)) << 4);
-    // Lane i16 of sixteen reads 8 bytes of values; their 4 keys x 16 columns come back transposed.
-    const int i16 = lane & 15, vkey = 4 * half + (i16 >> 2);
-    const int unit = 2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1);
+      for (int j = 0; j < PK; ++j)
+        ka[j] = (lds_char_t*)lds + (wkey + col) * RB + (((2 * j + half) ^ S::turn_k(col)) << 4);
+      // Lane i16 of sixteen reads 8 bytes of values; their 4 keys x 16 columns come back transposed.
+      const int i16 = lane & 15, vkey = 4 * half + (i16 >> 2);
+      const int unit = 2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1);
 #pragma unroll
-    for (int j = 0; j < PV; ++j)
-      va[j] = (lds_char_t*)lds + 2 * TILE + (wkey + vkey) * RB + (((4 * j + unit) ^ S::turn_v(vkey)) << 4) + (i16 & 1) * 8;
-    auto key = [&](int buf, int u, int b) {
-      const u32x4_t w = *(lds_u32x4_t*)(ka[u % PK] + (buf * TILE + 32 * b * RB + u / PK * PK * 32));
-      return __builtin_bit_cast(vec16, w);
-    };
-    auto value = [&](int buf, int kb, int i) {  // 16 keys from 16 kb on, columns 32 i ..
-      vec16 r;
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        lds_char_t* at = va[i % PV] + (buf * TILE + (16 * kb + 8 * p) * RB + i / PV * PV * 64);
-        const v4s_t t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)at);
-        uint2 w;
-        __builtin_memcpy(&w, &t, 8);
-        r.d[2 * p] = w.x;
-        r.d[2 * p + 1] = w.y;
-      }
-      return r;
-    };
-    constexpr int AHEAD = SB * QU < 4 ? SB * QU : 4, NQ = SB * QU;  // operands of keys on their way; products of a tile's scores
-    auto scores = [&](auto buf_c, f32x16_t (&sc)[SB], auto between) {
-      constexpr int buf = decltype(buf_c)::value;
-      vec16 f[AHEAD];
-      static_for<AHEAD>([&](auto n) { f[n] = key(buf, n / SB, n % SB); });
-      static_for<SB>([&](auto b) { sc[b] = zero16(); });
-      static_for<NQ>([&](auto n) {
-        mfma_32x32<T>(sc[n % SB], f[n % AHEAD], qf[n / SB]);
-        if constexpr (n + AHEAD < NQ) f[n % AHEAD] = key(buf, (n + AHEAD) / SB, (n + AHEAD) % SB);
-        between(n);
-        fix();
-      });
-    };
-    vec16 wh[2], wl[2];
-    float from = 0.f, held = 0.f;
-    // Kept from the compiler, which would write (-1, 0) as the fp32 constant -1, which is (0, -1).
-    uint32_t low = 0x0000bf80u, high = 0xbf800000u;
-    asm volatile("" : "+s"(low), "+s"(high));
-    // Weight e of 16 keys kb of a lane's eight; with every second one, the pair as two bf16 numbers each.
-    auto weigh = [&](f32x16_t (&sc)[SB], auto kb_c, auto e_c) {
-      constexpr int kb = decltype(kb_c)::value, e = decltype(e_c)::value, b = kb >> 1, v = 8 * (kb & 1) + e;
-      const float w = __builtin_amdgcn_exp2f(fmaf(sc[b][v], cs, -from));
-      l += w;
-      if constexpr (e % 2 == 0) {
-        held = w;
-      } else {
-        const uint32_t hi = f32x2_to_bf16x2(held, w);
-        wh[kb & 1].d[e / 2] = hi;
-        wl[kb & 1].d[e / 2] = f32x2_to_bf16x2(less(held, hi, low), less(w, hi, high));
-      }
-    };
-    const std::integral_constant<int, 0> zero{};
-    // Tile it of the walk, whose scores are sc; the next one's go to nx.
-    auto step = [&](int it, auto p_c, f32x16_t (&sc)[SB], f32x16_t (&nx)[SB], auto last_c) {
-      constexpr int P = decltype(p_c)::value;
-      constexpr bool LAST = decltype(last_c)::value;
-      const int j0 = (kt0 + it) * KT, jw = j0 + wkey;
-      // Formed before the barrier, whatever the compiler moves: max3() reads them without its knowledge.
-#pragma unroll
-      for (int b = 0; b < SB; ++b) asm volatile("" : "+v"(sc[b]));
-      CONVSEL_WAIT_VMCNT(0);
-      lds_sync();
-      if (kt0 + it + 2 < kt1) issue(P, j0 + 2 * KT, false);
-      if constexpr (!LAST) issue(P ^ 1, j0 + KT, true);
-      if (!(jw >= in_lo && jw + 32 * SB <= in_hi)) hide(sc, jw);
-      float most = -kInf;
-      vec16 fv[NC];
-      auto top = [&](auto n) {  // an eighth of the scores
-        static_for<SB>([&](auto b) { most = max3(most, sc[b][2 * n], sc[b][2 * n + 1]); });
+      for (int j = 0; j < PV; ++j)
+        va[j] = (lds_char_t*)lds + 2 * TILE + (wkey + vkey) * RB + (((4 * j + unit) ^ S::turn_v(vkey)) << 4) +
+                (i16 & 1) * 8;
+      auto key = [&](int buf, int u, int b) {
+        const u32x4_t w = *(lds_u32x4_t*)(ka[u % PK] + (buf * TILE + 32 * b * RB + u / PK * PK * 32));
+        return __builtin_bit_cast(vec16, w);
       };
-      auto settle = [&] {
-        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(most), __float_as_uint(most), false, false);
-        most = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * cs;
-        // Weights may grow to 2^8 before the results are brought to a new maximum.
-        if (__any(most > m + 8.f)) rescale(most);
-        from = m == -kInf ? 0.f : m;  // a row with nothing yet: its weights are 2^-inf
+      auto value = [&](int buf, int kb, int i) {  // 16 keys from 16 kb on, columns 32 i ..
+        vec16 r;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          lds_char_t* at = va[i % PV] + (buf * TILE + (16 * kb + 8 * p) * RB + i / PV * PV * 64);
+          const v4s_t t = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t*)at);
+          uint2 w;
+          __builtin_memcpy(&w, &t, 8);
+          r.d[2 * p] = w.x;
+          r.d[2 * p + 1] = w.y;
+        }
+        return r;
       };
-      auto first_values = [&] { static_for<NC>([&](auto i) { fv[i] = value(P, 0, i); }); };
-      if constexpr (LAST) {
-        first_values();
-        static_for<8>(top);
-        settle();
-        static_for<8>([&](auto e) { weigh(sc, zero, e); });
-      } else {
-        constexpr int M = NQ >= 16 ? 4 : NQ >= 4 ? 2 : 1;  // products beside the maximum; 8 weights beside the others
-        scores(std::integral_constant<int, P ^ 1>{}, nx, [&](auto n) {
-          if constexpr (n < M)
-            static_for<8 / M>([&](auto x) { top(std::integral_constant<int, decltype(n)::value * (8 / M) + decltype(x)::value>{}); });
-          if constexpr (n == M - 1) {
-            fix();
-            settle();
-          }
-          constexpr int rest = NQ - M, i0 = n < M ? 0 : (n - M) * 8 / rest, i1 = n < M ? 0 : (n - M + 1) * 8 / rest;
-          static_for<i1 - i0>([&](auto e) { weigh(sc, zero, std::integral_constant<int, i0 + decltype(e)::value>{}); });
-          if constexpr (n == (NQ > 4 ? NQ - 4 : 0)) first_values();
-        });
-      }
-      static_for<2 * SB>([&](auto kb) {
-        static_for<2 * NC>([&](auto n) {
-          constexpr int i = n % NC;
-          mfma_32x32<T>(o[i], fv[i], n < NC ? wh[kb & 1] : wl[kb & 1]);
-          if constexpr (kb + 1 < 2 * SB) {
-            if constexpr (n >= NC) fv[i] = value(P, kb + 1, i);
-            constexpr int i0 = n * 8 / (2 * NC), i1 = (n + 1) * 8 / (2 * NC);
-            static_for<i1 - i0>([&](auto e) {
-              weigh(sc, std::integral_constant<int, decltype(kb)::value + 1>{}, std::integral_constant<int, i0 + decltype(e)::value>{});
-            });
-          }
+      // Products of a tile's scores, and operands of keys on their way.
+      constexpr int NQ = SB * QU, AHEAD = NQ < 4 ? NQ : 4;
+      auto scores = [&](auto buf_c, f32x16_t (&sc)[SB], auto between) {
+        constexpr int buf = decltype(buf_c)::value;
+        vec16 f[AHEAD];
+        static_for<AHEAD>([&](auto n) { f[n] = key(buf, n / SB, n % SB); });
+        static_for<SB>([&](auto b) { sc[b] = zero16(); });
+        static_for<NQ>([&](auto n) {
+          mfma_32x32<T>(sc[n % SB], f[n % AHEAD], qf[n / SB]);
+          if constexpr (n + AHEAD < NQ) f[n % AHEAD] = key(buf, (n + AHEAD) / SB, (n + AHEAD) % SB);
+          between(n);
           fix();
         });
-      });
-    };
-    const int count = kt1 - kt0;
-    const std::integral_constant<int, 1> one{};
-    f32x16_t sa[SB];
-    // The first keys are in; behind the barrier everyone's are.
-    if (count > 1) CONVSEL_WAIT_VMCNT(2 * NDMA);
-    else CONVSEL_WAIT_VMCNT(NDMA);
-    lds_sync();
-    int it = 0;
-    if (idle) {
-      for (; it < count; ++it) {
+      };
+      vec16 wh[2], wl[2];
+      float from = 0.f, held = 0.f;
+      // Kept from the compiler, which would write (-1, 0) as the fp32 constant -1, which is (0, -1).
+      uint32_t low = 0x0000bf80u, high = 0xbf800000u;
+      asm volatile("" : "+s"(low), "+s"(high));
+      // Weight e of 16 keys kb of a lane's eight; with every second one, the pair as two bf16 numbers each.
+      auto weigh = [&](f32x16_t (&sc)[SB], auto kb_c, auto e_c) {
+        constexpr int kb = decltype(kb_c)::value, e = decltype(e_c)::value, b = kb >> 1, v = 8 * (kb & 1) + e;
+        const float w = __builtin_amdgcn_exp2f(fmaf(sc[b][v], cs, -from));
+        l += w;
+        if constexpr (e % 2 == 0) {
+          held = w;
+        } else {
+          const uint32_t hi = f32x2_to_bf16x2(held, w);
+          wh[kb & 1].d[e / 2] = hi;
+          wl[kb & 1].d[e / 2] = f32x2_to_bf16x2(less(held, hi, low), less(w, hi, high));
+        }
+      };
+      const std::integral_constant<int, 0> zero{};
+      // Tile it of the walk, whose scores are sc; the next one's go to nx.
+      auto step = [&](int it, auto p_c, f32x16_t (&sc)[SB], f32x16_t (&nx)[SB], auto last_c) {
+        constexpr int P = decltype(p_c)::value;
+        constexpr bool LAST = decltype(last_c)::value;
+        const int j0 = (kt0 + it) * KT, jw = j0 + wkey;
+        // Formed before the barrier, whatever the compiler moves: max3() reads them without its knowledge.
+#pragma unroll
+        for (int b = 0; b < SB; ++b) asm volatile("" : "+v"(sc[b]));
         CONVSEL_WAIT_VMCNT(0);
         lds_sync();
-        if (it + 2 < count) issue((it + b0) & 1, (kt0 + it + 2) * KT, false);
-        if (it + 1 < count) issue(((it + b0) & 1) ^ 1, (kt0 + it + 1) * KT, true);
+        if (kt0 + it + 2 < kt1) issue(P, j0 + 2 * KT, false);
+        if constexpr (!LAST) issue(P ^ 1, j0 + KT, true);
+        if (!(jw >= in_lo && jw + 32 * SB <= in_hi)) hide(sc, jw);
+        float most = -kInf;
+        vec16 fv[NC];
+        auto top = [&](auto n) {  // an eighth of the scores
+          static_for<SB>([&](auto b) { most = max3(most, sc[b][2 * n], sc[b][2 * n + 1]); });
+        };
+        auto settle = [&] {
+          const uint32_t mine = __float_as_uint(most);
+          const auto both = __builtin_amdgcn_permlane32_swap(mine, mine, false, false);
+          most = fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * cs;
+          // Weights may grow to 2^8 before the results are brought to a new maximum.
+          if (__any(most > m + 8.f)) rescale(most);
+          from = m == -kInf ? 0.f : m;  // a row with nothing yet: its weights are 2^-inf
+        };
+        auto first_values = [&] { static_for<NC>([&](auto i) { fv[i] = value(P, 0, i); }); };
+        if constexpr (LAST) {
+          first_values();
+          static_for<8>(top);
+          settle();
+          static_for<8>([&](auto e) { weigh(sc, zero, e); });
+        } else {
+          constexpr int M = NQ >= 16 ? 4 : NQ >= 4 ? 2 : 1;  // products beside the maximum; 8 weights beside the others
+          scores(std::integral_constant<int, P ^ 1>{}, nx, [&](auto n) {
+            if constexpr (n < M)
+              static_for<8 / M>([&](auto x) {
+                  top(std::integral_constant<int, decltype(n)::value * (8 / M) + decltype(x)::value>{});
+                });
+            if constexpr (n == M - 1) {
+              fix();
+              settle();
+            }
+            constexpr int rest = NQ - M, i0 = n < M ? 0 : (n - M) * 8 / rest, i1 = n < M ? 0 : (n - M + 1) * 8 / rest;
+            static_for<i1 - i0>(
+                [&](auto e) { weigh(sc, zero, std::integral_constant<int, i0 + decltype(e)::value>{}); });
+            if constexpr (n == (NQ > 4 ? NQ - 4 : 0)) first_values();
+          });
+        }
+        static_for<2 * SB>([&](auto kb) {
+          static_for<2 * NC>([&](auto n) {
+            constexpr int i = n % NC;
+            mfma_32x32<T>(o[i], fv[i], n < NC ? wh[kb & 1] : wl[kb & 1]);
+            if constexpr (kb + 1 < 2 * SB) {
+              if constexpr (n >= NC) fv[i] = value(P, kb + 1, i);
+              constexpr int i0 = n * 8 / (2 * NC), i1 = (n + 1) * 8 / (2 * NC);
+              static_for<i1 - i0>([&](auto e) {
+                weigh(sc, std::integral_constant<int, decltype(kb)::value + 1>{},
+                      std::integral_constant<int, i0 + decltype(e)::value>{});
+              });
+            }
+            fix();
+          });
+        });
+      };
+      const int count = kt1 - kt0;
+      const std::integral_constant<int, 1> one{};
+      f32x16_t sa[SB];
+      // The first keys are in; behind the barrier everyone's are.
+      if (count > 1) CONVSEL_WAIT_VMCNT(2 * NDMA);
+      else CONVSEL_WAIT_VMCNT(NDMA);
+      lds_sync();
+      int it = 0;
+      if (idle) {
+        for (; it < count; ++it) {
+          CONVSEL_WAIT_VMCNT(0);
+          lds_sync();
+          if (it + 2 < count) issue((it + b0) & 1, (kt0 + it + 2) * KT, false);
+          if (it + 1 < count) issue(((it + b0) & 1) ^ 1, (kt0 + it + 1) * KT, true);
+        }
+        return;
       }
-      return;
-    }
-    // The last tile's scores are sa, so the first one's are sb if there is an even number: one copy of the last step.
-    if (b0 != 0) {
-      f32x16_t sb[SB];
-      scores(one, sb, [](auto) {});
-      asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
-      step(it++, one, sb, sa, std::false_type{});
-    } else {
-      scores(zero, sa, [](auto) {});
-    }
-    asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");  // max3() reads products' results unseen by the compiler
-    for (; it + 1 < count; it += 2) {
-      f32x16_t sb[SB];
-      step(it, zero, sa, sb, std::false_type{});
-      step(it + 1, one, sb, sa, std::false_type{});
-    }
-    step(it, zero, sa, sa, std::true_type{});
+      // The last tile's scores are sa, so the first one's are sb if there is an even number: one copy of the last step.
+      if (b0 != 0) {
+        f32x16_t sb[SB];
+        scores(one, sb, [](auto) {});
+        asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");
+        step(it++, one, sb, sa, std::false_type{});
+      } else {
+        scores(zero, sa, [](auto) {});
+      }
+      asm volatile("s_nop 15\n\ts_nop 7" ::: "memory");  // max3() reads products' results unseen by the compiler
+      for (; it + 1 < count; it += 2) {
+        f32x16_t sb[SB];
+        step(it, zero, sa, sb, std::false_type{});
+        step(it + 1, one, sb, sa, std::false_type{});
+      }
+      step(it, zero, sa, sa, std::true_type{});
     }
   };
   if constexpr (PIPED)
@@ -638,8 +659,8 @@ template <typename T, int NC, int R>
 hipError_t launch_rows(PromptLaunch a, hipStream_t st) {
   each_grid(a.units, [&](const UnitRow& r, unsigned n) {
     a.units = r;
-    hipLaunchKernelGGL((prompt_attention_kernel<T, NC, R>), dim3((unsigned)a.g.kv_heads, 1, n), dim3(64 * kWaves), 0, st,
-                       a);
+    const dim3 grid((unsigned)a.g.kv_heads, 1, n);
+    hipLaunchKernelGGL((prompt_attention_kernel<T, NC, R>), grid, dim3(64 * kWaves), 0, st, a);
   });
   return hipGetLastError();
 }
@@ -735,7 +756,8 @@ hipError_t launch_prompt_attention(const PromptArgs& a, void* workspace, hipStre
 
 void prompt_attention_describe(const PromptArgs& a, char* buf, size_t len) {
   snprintf(buf, len, "prompt_attention kernels=%sprompt_attention_kernel rows=%d workspace=%zu",
-           prompt_attention_workspace(a) ? "prompt_pack_kernel;" : "", 32 * blocks_for(a), prompt_attention_workspace(a));
+           prompt_attention_workspace(a) ? "prompt_pack_kernel;" : "", 32 * blocks_for(a),
+           prompt_attention_workspace(a));
 }
 
 }  // namespace convsel
