@@ -55,8 +55,8 @@ def plain(model, tokens, positions, offsets):
 def test_fresh_prompts_in_fp32_against_64_bits(weights):
     """The operators are good to some 2^-18 of the hidden values here.  Without codes a chain of ten of them, each
     adding as much and none with a gain above a few, stays within 2^-12 of the largest logit.  With codes, a number so
-    near the middle between two of them that 2^-18 decides gives a code's difference, 2^-7 of its row's largest, to one of
-    16 or more products: 2^-5 lies above a few such, and a wrong row, scale or mask moves logits by their own size."""
+    near the middle between two of them that 2^-18 decides gives a code's difference, 2^-7 of its row's largest, to one
+    of 16 or more products: 2^-5 lies above a few such, and a wrong row, scale or mask moves logits by their own size."""
     say("case fresh prompts", weights)
     model = decoder.Decoder(weights=weights, direct=True, dtype=torch.float32, **SMALL)
     dev = model.embed.device

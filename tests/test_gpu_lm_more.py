@@ -325,6 +325,24 @@ def test_int8_residual_in_place_and_leading_dimensions():
     assert cs.linear_int8(x[:0], wc, ws).shape == (0, 5, 48)
 
 
+@pytest.mark.parametrize("m", [1, 2, 3, 50])
+def test_int8_results_of_another_type_than_the_rows(m):
+    g = gen(m)
+    x, w = randn(g, m, 90), randn(g, 70, 90) * 0.1
+    for a, b in ((torch.bfloat16, torch.float32), (torch.float32, torch.bfloat16)):
+        check_int8(x.to(a), w, randn(g, 70, dtype=b), "relu", randn(g, m, 70, dtype=b), b, False)
+
+
+def test_int8_of_one_row_without_leading_dimensions():
+    g = gen(12)
+    x, w = randn(g, 48, dtype=torch.bfloat16), randn(g, 33, 48, dtype=torch.bfloat16)
+    wc, ws = cs.quantize_rows(w)
+    xc, xs = cs.quantize_rows(x)
+    want = cs.linear_int8(x[None], wc, ws)[0]
+    assert xs.shape == () and torch.equal(cs.linear_int8(x, wc, ws), want)
+    assert torch.equal(cs.linear_int8(xc, wc, ws, x_scale=xs), want)
+
+
 # ---- logits -----------------------------------------------------------------------
 
 def check_logits(x, counts, seed, prompts=True, rep=True, pres=True, freq=True, bias=0, mask=0, history=True, out=None,
@@ -456,3 +474,30 @@ def test_replayed_on_new_inputs_and_another_stream():
         torch.cuda.current_stream().wait_stream(side)
         for a, b in zip(again, eager):
             assert torch.equal(a, b)
+
+
+def test_two_streams_at_once():
+    """Calls share nothing: two streams' results are those of one after the other."""
+    g = gen(21)
+    sets = []
+    for n in (700, 531):
+        q, k, v = heads_of(g, n, 8, 2, 60, torch.bfloat16)
+        w, x = randn(g, 512, 1000, dtype=torch.bfloat16), randn(g, n, 1000, dtype=torch.bfloat16)
+        sets.append((q, k, v, ints([0, n // 3, n]), x, *cs.quantize_rows(w)))
+
+    def calls(q, k, v, off, x, wc, ws):
+        y = cs.linear_int8(x, wc, ws, act="gelu")
+        return cs.prompt_attention(q, k, v, off), y, cs.adjust_logits(y, mask=ints([-2 ** 31 + 5] * 16))
+
+    want = [calls(*a) for a in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(5):
+        got = []
+        for st, a in zip(streams, sets):
+            with torch.cuda.stream(st):
+                got.append(calls(*a))
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            for t, u in zip(a, b):
+                assert torch.equal(t, u)
