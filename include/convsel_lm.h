@@ -266,8 +266,8 @@ conv_status_t convsel_quantize_rows(const void* x, int8_t* codes, float* scales,
                                     void* stream);
 
 /*   y[m][o] = act((sum_i X[m][i] * W[o][i]) * sx[m] * sw[o] + b[o]) + r[m][o]
- * W: codes, O rows of ldw >= in_features bytes each (all of which can be read;
- * what those behind in_features hold does not matter), sw their O scales.  x is
+ * W: codes, O rows of in_features bytes, ldw apart (up to 15 bytes behind a row,
+ * less where ldw is, can be read; what they hold does not matter), sw their O scales.  x is
  * codes with m scales sx (x_dtype CONVSEL_CODES) or numbers (CONV_F32, CONV_BF16;
  * sx NULL), which are coded by rows as above within the call.  The sum is exact;
  * scales, bias, activation and residual are fp32, and y is rounded once. */

@@ -557,11 +557,13 @@ conv_status_t convsel_linear_int8(const void* x, const float* x_scale, const int
   const size_t need = convsel::linear_int8_workspace(a, d->x_dtype);
   if (workspace_bytes < need || (need > 0 && !workspace)) return CONV_ERR_WORKSPACE;
   if (need > 0 && !aligned(workspace, 256)) return CONV_ERR_INVALID_ARG;
-  // y and the workspace lie over nothing that is read, nor over each other; y may be r.
+  // y and the workspace lie over nothing that is read, nor over each other; y may be r.  w's last row is
+  // read in whole units.
+  const int64_t units = (in + 15) / 16 * 16, wbytes = span(out, a.ldw, 1, 0, a.ldw < units ? a.ldw : units, 1);
   const struct {
     const void* p;
     int64_t bytes;
-  } reads[6] = {{x, span(m, a.ldx, 1, 0, in, xs)}, {x_scale, codes ? m * 4 : 0}, {w, out * a.ldw}, {w_scale, out * 4},
+  } reads[6] = {{x, span(m, a.ldx, 1, 0, in, xs)}, {x_scale, codes ? m * 4 : 0}, {w, wbytes}, {w_scale, out * 4},
                 {b, b ? out * es : 0}, {r, r ? span(m, a.ldr, 1, 0, out, es) : 0}};
   const int64_t ybytes = span(m, a.ldy, 1, 0, out, es);
   for (const auto& e : reads) {

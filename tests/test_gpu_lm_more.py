@@ -343,6 +343,22 @@ def test_int8_of_one_row_without_leading_dimensions():
     assert torch.equal(cs.linear_int8(xc, wc, ws, x_scale=xs), want)
 
 
+@pytest.mark.parametrize("m", [1, 70])
+def test_int8_weights_that_are_columns_of_a_table(m):
+    """The result lies right behind the last row's codes."""
+    g = gen(m)
+    o, i = 96, 256
+    wc, ws = cs.quantize_rows(randn(g, o, i))
+    x = randn(g, m, i, dtype=torch.bfloat16)
+    want = cs.linear_int8(x, wc, ws)
+    held = torch.zeros(o * 2 * i + m * o * 2, dtype=torch.int8, device=DEV)
+    w = held[:o * 2 * i].view(o, 2 * i)[:, :i]
+    w.copy_(wc)
+    at = (o - 1) * 2 * i + i
+    out = held[at:at + m * o * 2].view(torch.bfloat16).view(m, o)
+    assert torch.equal(cs.linear_int8(x, w, ws, out=out), want) and torch.equal(w, wc)
+
+
 # ---- logits -----------------------------------------------------------------------
 
 def check_logits(x, counts, seed, prompts=True, rep=True, pres=True, freq=True, bias=0, mask=0, history=True, out=None,

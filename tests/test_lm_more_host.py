@@ -175,6 +175,16 @@ def test_int8_refuses_pointers_and_overlaps():
     assert int8(int8_desc(x_dtype=1), work=H, n=1 << 20) == INVALID
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="a call that is not refused would run on these addresses")
+def test_int8_weights_end_with_their_last_row():
+    """Rows of w may be columns of a wider table: what lies right behind the last one's units is not w's."""
+    d, end = int8_desc(ldw=128), C + 31 * 128 + 64
+    assert int8(d, y=end - 2) == INVALID and int8(d, y=end) == _lib.CONV_ERR_DEVICE
+    d, end = int8_desc(in_features=60, ldx=64, ldw=128), C + 31 * 128 + 64
+    work = dict(work=H, n=1 << 12)
+    assert int8(d, y=end - 2, **work) == INVALID and int8(d, y=end, **work) == _lib.CONV_ERR_DEVICE
+
+
 def test_int8_workspace():
     assert int8_bytes(int8_desc()) == (0, 0)
     st, n = int8_bytes(int8_desc(x_dtype=1))
