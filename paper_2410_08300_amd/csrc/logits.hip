@@ -85,7 +85,7 @@ __global__ __launch_bounds__(THREADS) void adjust_logits_kernel(LogitsArgs a, in
       for (int s = 0; s < 2 * STEPS; ++s)
         *reinterpret_cast<uint4*>(count + (s * THREADS + threadIdx.x) * 4) = make_uint4(0, 0, 0, 0);
       lds_sync();
-      for (int64_t i0 = first + static_cast<int>(threadIdx.x); i0 < end; i0 += 4 * THREADS) {
+      for (int64_t i0 = static_cast<int64_t>(first) + threadIdx.x; i0 < end; i0 += 4 * THREADS) {
         int64_t at[4];
 #pragma unroll
         for (int n = 0; n < 4; ++n) at[n] = a.history[min(i0 + n * THREADS, static_cast<int64_t>(end) - 1)] - c0;

@@ -492,6 +492,24 @@ def test_replayed_on_new_inputs_and_another_stream():
             assert torch.equal(a, b)
 
 
+def test_logits_of_the_longest_history():
+    """A row's tokens may be the last before the largest 32-bit number."""
+    n = 2 ** 31 - 1
+    history = torch.full((n,), 7, dtype=torch.int32, device=DEV)
+    history[-5:] = ints([3, 900, 3, 5, 3])
+    x = torch.ones(3, 1000, device=DEV)
+    y = cs.adjust_logits(x, history=history, offsets=ints([0, 2, 2, 2]),
+                         frequency=torch.full((3,), 0.25, device=DEV))
+    want = x.clone()
+    want[0, 7] = 0.5
+    assert torch.equal(y, want)
+    y = cs.adjust_logits(x[:1], history=history, offsets=ints([n - 5, n]), prompt_lengths=ints([1]),
+                         repetition=torch.full((1,), 2.0, device=DEV), frequency=torch.full((1,), 0.25, device=DEV))
+    want = x[:1].clone()
+    want[0, 3], want[0, 5], want[0, 900] = 0.0, 0.25, 0.25
+    assert torch.equal(y, want)
+
+
 def test_two_streams_at_once():
     """Calls share nothing: two streams' results are those of one after the other."""
     g = gen(21)
