@@ -18,17 +18,18 @@
 //
 // Softmax in one pass, in powers of two (the scale carries log2 e): running
 // maximum m and sum l of a row, weights 2^(s - m).  bf16 calls multiply each
-// weight as two bf16 numbers, 16 bits: one number, 8 bits, is off by as much as
-// the result's own rounding (and would take 26 % less time).  fp32 calls use the
-// fp32 matrix instructions.
+// weight as three bf16 numbers, which hold all of its 24 bits: with two, 16 bits,
+// 20 % less time, 0.20 % of the results of 8192 tokens were a neighbour of the
+// rounded one, where fp32 steps throughout leave 0.08 and three numbers 0.06.
+// fp32 calls use the fp32 matrix instructions.
 //
-// What bounds it.  Heads of 128 and more, long: the matrix cores, half of whose
-// work with values is the weights' second numbers, at the clock that the card's
-// power leaves (8192 tokens of 32 heads on 8, causal: 710 us, 775 TFLOP/s, 1160
-// with the second numbers, at 1.77 GHz; matrix cores 65 % busy, vector unit 57 %).
-// Heads of 64: the vector unit (8192 tokens of 16 on 4: 227 us, 605 TFLOP/s, 78 %
-// busy); a weight costs a fused product, a transcendental (four slots), an
-// addition, three operations for its two numbers and half a maximum.  fp32: the
+// What bounds it.  Heads of 128 and more, long: the matrix cores, two thirds of
+// whose work with values is the weights' second and third numbers, at the clock
+// that the card's power leaves (8192 tokens of 32 heads on 8, causal: 900 us, 611
+// TFLOP/s, 1220 with those numbers).  Heads of 64: the vector unit beside them
+// (8192 tokens of 16 on 4: 295 us, 466 TFLOP/s); a weight costs a fused product, a
+// transcendental (four slots), an addition, seven halves of an operation for its
+// three numbers and half a maximum.  fp32: the
 // fp32 products (2048 tokens of 12 heads of 128 on 4: 162 us, 80 TFLOP/s).
 #include <stdio.h>
 
@@ -311,8 +312,8 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<T, NC, R>::PER_CU)) void prompt
   };
 
   // Values that are not finite spoil products that they have no part in: a weight of zero, where they are hidden, or
-  // the second half of one, which may be zero or negative.  Rows that end so go once more, adding up key by key what
-  // they see.
+  // the second or third part of one, which may be zero or negative.  Rows that end so go once more, adding up key by
+  // key what they see.
   auto walk = [&](auto exact_c) {
     for (int kt = kt0; kt < kt1; ++kt) {
       const int buf = BUFS == 2 ? (kt - kt0) & 1 : 0, j0 = kt * KT;
@@ -382,23 +383,29 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<T, NC, R>::PER_CU)) void prompt
           fix();
         });
       };
-      vec16 wh[2], wl[2];
-      float from = 0.f, held = 0.f;
+      constexpr int PARTS = 3;
+      vec16 part[PARTS];  // of the weights of 16 keys, a lane's eight
+      float from = 0.f;
       // Kept from the compiler, which would write (-1, 0) as the fp32 constant -1, which is (0, -1).
       uint32_t low = 0x0000bf80u, high = 0xbf800000u;
       asm volatile("" : "+s"(low), "+s"(high));
-      // Weight e of 16 keys kb of a lane's eight; with every second one, the pair as two bf16 numbers each.
+      // Weight e of a lane's eight of 16 keys kb, in its score's place.
       auto weigh = [&](f32x16_t (&sc)[SB], auto kb_c, auto e_c) {
-        constexpr int kb = decltype(kb_c)::value, e = decltype(e_c)::value, b = kb >> 1, v = 8 * (kb & 1) + e;
-        const float w = __builtin_amdgcn_exp2f(fmaf(sc[b][v], cs, -from));
+        constexpr int kb = decltype(kb_c)::value, v = 8 * (kb & 1) + decltype(e_c)::value;
+        const float w = __builtin_amdgcn_exp2f(fmaf(sc[kb >> 1][v], cs, -from));
         l += w;
-        if constexpr (e % 2 == 0) {
-          held = w;
-        } else {
-          const uint32_t hi = f32x2_to_bf16x2(held, w);
-          wh[kb & 1].d[e / 2] = hi;
-          wl[kb & 1].d[e / 2] = f32x2_to_bf16x2(less(held, hi, low), less(w, hi, high));
+        sc[kb >> 1][v] = w;
+      };
+      // Part p of weights 2 e and 2 e + 1: what the part before leaves of them, rounded.  Of 24 bits it leaves 16 at
+      // most, and the next one 8: three parts hold all.
+      auto split = [&](f32x16_t (&sc)[SB], auto kb_c, auto p_c, auto e_c) {
+        constexpr int kb = decltype(kb_c)::value, p = decltype(p_c)::value, e = decltype(e_c)::value;
+        constexpr int b = kb >> 1, v = 8 * (kb & 1) + 2 * e;
+        if constexpr (p > 0) {
+          sc[b][v] = less(sc[b][v], part[p - 1].d[e], low);
+          sc[b][v + 1] = less(sc[b][v + 1], part[p - 1].d[e], high);
         }
+        part[p].d[e] = f32x2_to_bf16x2(sc[b][v], sc[b][v + 1]);
       };
       const std::integral_constant<int, 0> zero{};
       // Tile it of the walk, whose scores are sc; the next one's go to nx.
@@ -433,6 +440,7 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<T, NC, R>::PER_CU)) void prompt
           static_for<8>(top);
           settle();
           static_for<8>([&](auto e) { weigh(sc, zero, e); });
+          static_for<4>([&](auto e) { split(sc, zero, zero, e); });
         } else {
           constexpr int M = NQ >= 16 ? 4 : NQ >= 4 ? 2 : 1;  // products beside the maximum; 8 weights beside the others
           scores(std::integral_constant<int, P ^ 1>{}, nx, [&](auto n) {
@@ -448,19 +456,33 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<T, NC, R>::PER_CU)) void prompt
             static_for<i1 - i0>(
                 [&](auto e) { weigh(sc, zero, std::integral_constant<int, i0 + decltype(e)::value>{}); });
             if constexpr (n == (NQ > 4 ? NQ - 4 : 0)) first_values();
+            if constexpr (n == NQ - 1) static_for<4>([&](auto e) { split(sc, zero, zero, e); });
           });
         }
         static_for<2 * SB>([&](auto kb) {
-          static_for<2 * NC>([&](auto n) {
-            constexpr int i = n % NC;
-            mfma_32x32<T>(o[i], fv[i], n < NC ? wh[kb & 1] : wl[kb & 1]);
-            if constexpr (kb + 1 < 2 * SB) {
-              if constexpr (n >= NC) fv[i] = value(P, kb + 1, i);
-              constexpr int i0 = n * 8 / (2 * NC), i1 = (n + 1) * 8 / (2 * NC);
-              static_for<i1 - i0>([&](auto e) {
-                weigh(sc, std::integral_constant<int, decltype(kb)::value + 1>{},
-                      std::integral_constant<int, i0 + decltype(e)::value>{});
+          static_for<PARTS * NC>([&](auto n) {
+            constexpr int i = n % NC, p = n / NC;
+            mfma_32x32<T>(o[i], fv[i], part[p]);
+            // Beside the products with a part the next one, and the next 16 keys' weights and first part.
+            constexpr bool next = kb + 1 < 2 * SB;
+            const std::integral_constant<int, decltype(kb)::value + 1> kb1{};
+            if constexpr (next && p == PARTS - 1) fv[i] = value(P, kb + 1, i);
+            constexpr int s0 = i * 4 / NC, s1 = (i + 1) * 4 / NC;
+            constexpr int i0 = n * 8 / (PARTS * NC), i1 = (n + 1) * 8 / (PARTS * NC);
+            static_assert(p + 1 < PARTS || 2 * s1 <= i1, "split after they are weighed");
+            if constexpr (p + 1 < PARTS)
+              static_for<s1 - s0>([&](auto e) {
+                split(sc, kb, std::integral_constant<int, p + 1>{},
+                      std::integral_constant<int, s0 + decltype(e)::value>{});
               });
+            if constexpr (next) {
+              static_for<i1 - i0>([&](auto e) {
+                weigh(sc, kb1, std::integral_constant<int, i0 + decltype(e)::value>{});
+              });
+              if constexpr (p == PARTS - 1)
+                static_for<s1 - s0>([&](auto e) {
+                  split(sc, kb1, zero, std::integral_constant<int, s0 + decltype(e)::value>{});
+                });
             }
             fix();
           });

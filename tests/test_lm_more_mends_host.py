@@ -1,0 +1,19 @@
+"""Host-side checks of single properties of prompt attention, linear layers on
+codes and logit adjustments, and that the GPU tests' bounds refuse what they are
+there to refuse.  No GPU."""
+import pytest
+import torch
+
+import ref_prompt_bits as bits
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=str)
+def test_bound_of_cancelling_values_tells_16_bits_of_a_weight_from_24(dtype):
+    q, k, v, _, w, places = bits.cancelling(1, 64, 3, 8, 64, dtype)
+    want, mag = bits.result(v, w, places, 3)
+    limit = bits.bound(want, mag, dtype)
+    w = w.float()
+    assert bool(((bits.result(v, w.double(), places, 3)[0] - want).abs() <= limit).all())
+    high = w.bfloat16().float()
+    two = high.double() + (w - high).bfloat16().double()
+    assert bool(((bits.result(v, two, places, 3)[0] - want).abs() > limit).any())
