@@ -246,7 +246,8 @@ __global__ __launch_bounds__(1024) void linear_int8_rows_kernel(LinearArgs g, in
   // Lane (row of x, q) holds outputs 4 q .. 4 q + 3: the first wave finishes them.
   const int64_t m = m0 + r16, o = o0 + 4 * q;
   if (wave != 0 || m >= g.m || o >= g.out) return;
-  float z[1][4], bias[4], scale[4];
+  float z[1][4], bias[4];
+  Scale scale[4];
   load_bias4<Y>(g, o, bias);
   load_scale4(g, o, scale);
   i32x4v_t sum = {0, 0, 0, 0};

@@ -118,7 +118,8 @@ __device__ __forceinline__ void store_whole(const TileArgs& a, const Put& put, f
     r += G * STEP * g.ldr;
   };
   if (g.r) fetch();
-  float bias[4], scale[4], rows[G];
+  float bias[4], rows[G];
+  Scale scale[4];
   load_bias4<T>(g, o0 + col, bias);
   if constexpr (CODES) load_scale4(g, o0 + col, scale);
   const float* row_scale = CODES ? g.x_scale + m0 + row : nullptr;
@@ -172,7 +173,8 @@ __device__ __forceinline__ void store_blocks(const TileArgs& a, const Put& put, 
   const int row = lane / PER, col = 4 * (lane % PER);
   const int64_t o = o0 + col;
   const bool there = o < g.out;
-  float bias[4], scale[4];
+  float bias[4];
+  Scale scale[4];
   load_bias4<T>(g, o, bias);
   if constexpr (CODES) load_scale4(g, o, scale);
 #pragma unroll 1
@@ -553,7 +555,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(TileArgs a) {
   float s[1][4] = {}, bias[4];
   load_bias4<T>(a.g, o, bias);
   if constexpr (CODES) {
-    float scale[4];
+    Scale scale[4];
     load_scale4(a.g, o, scale);
     i32x4v_t n = {};
 #pragma unroll 4

@@ -1,5 +1,6 @@
 """GPU checks of single properties of prompt attention, linear layers on codes and
 logit adjustments, each at the calls where it can be lost."""
+import numpy as np
 import pytest
 import torch
 
@@ -29,3 +30,33 @@ def test_prompt_holds_its_weights_in_24_bits(dtype, dim, seqs, n):
     y = cs.prompt_attention(q.to(DEV), k.to(DEV), v.to(DEV), ints(offsets), causal=False, scale=1.0)
     every = lambda t: t[:, None].expand(-1, n, -1, -1).reshape(seqs * n, 8, dim).repeat_interleave(2, 1)  # noqa: E731
     close(y, every(want), every(bits.bound(want, mag, DT[dtype])), "bits")
+
+
+# ---- codes ------------------------------------------------------------------------
+
+def powers(g, n, low, high):
+    """n scales spread over 2^low .. 2^high."""
+    e = low + (high - low) * torch.rand(n, generator=g, dtype=torch.float64)
+    return torch.exp2(e).float()
+
+
+# One and several rows through registers, and tiles of 64, of 128, of 256, and of parts that are joined.
+@pytest.mark.parametrize("m,i,o", [(1, 64, 40), (3, 200, 35), (70, 64, 260), (2048, 128, 6144), (4090, 1024, 4090),
+                                   (64, 16384, 320)])
+@pytest.mark.parametrize("low,high", [(-149, -20), (-60, 0), (-100, 100), (0, 127)])
+def test_int8_results_of_scales_far_apart(m, i, o, low, high):
+    """What a sum and two scales give in fp32 is right to its last bits wherever fp32 holds it, whatever the scales'
+    product: a sum's conversion, two products of numbers near one and, below 2^-126, the place of the last bit."""
+    say("case int8 scales", m, i, o, low, high, cs.describe_linear_int8(m, i, o, torch.float32, True))
+    g = torch.Generator().manual_seed(m + i + o)
+    x, w = (torch.randint(-128, 128, (n, i), generator=g, dtype=torch.int8) for n in (m, o))
+    xs = powers(g, m, low, high)
+    # Results within fp32 and beside its ends: scales of the outputs are the others' reciprocals, more or less.
+    ws = powers(g, o, max(-149, -90 - high), min(127, -20 - low))
+    y = cs.linear_int8(x.to(DEV), w.to(DEV), ws.to(DEV), x_scale=xs.to(DEV), dtype=torch.float32)
+    want = (x.double() @ w.double().T) * xs.double()[:, None] * ws.double()[None]
+    most = torch.finfo(torch.float32).max
+    near = (want.abs() / most - 1).abs() < 2.0 ** -20  # on either side of infinity
+    want = torch.where(near, 0.0, torch.where(want.abs() > most, want * np.inf, want))
+    y = torch.where(near, 0.0, y.cpu())
+    close(y, want, 3.01 * 2.0 ** -24 * want.abs() + 2.0 ** -149, "scales")
