@@ -207,6 +207,7 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<T, NC, R>::PER_CU)) void prompt
   }
   // Never zero: a masked score of -inf times it stays -inf.
   const float cs = fmaxf(fabsf(a.scale), 0x1p-126f);
+  const float share = __builtin_amdgcn_ldexpf(1.f, __builtin_clz(sp.count) - 32);
   f32x16_t o[NC];
 #pragma unroll
   for (int i = 0; i < NC; ++i) o[i] = zero16();
@@ -264,6 +265,7 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<T, NC, R>::PER_CU)) void prompt
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         sc[b][v] = __builtin_amdgcn_exp2f(fmaf(sc[b][v], cs, -from));
+        if constexpr (decltype(exact_c)::value) sc[b][v] *= share;
         l += sc[b][v];
       }
     if constexpr (decltype(exact_c)::value) {
@@ -313,7 +315,8 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<T, NC, R>::PER_CU)) void prompt
 
   // Values that are not finite spoil products that they have no part in: a weight of zero, where they are hidden, or
   // the second or third part of one, which may be zero or negative.  Rows that end so go once more, adding up key by
-  // key what they see.
+  // key what they see.  So do rows of finite values whose sum leaves fp32, as the weights' sum divides it only at the
+  // end: `share` makes the weights so small that all of them together are less than one.
   auto walk = [&](auto exact_c) {
     for (int kt = kt0; kt < kt1; ++kt) {
       const int buf = BUFS == 2 ? (kt - kt0) & 1 : 0, j0 = kt * KT;

@@ -13,7 +13,7 @@ if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
 import paper_2410_08300_amd as cs  # noqa: E402
-from test_gpu_lm_more import DEV, DT, close, ints  # noqa: E402
+from test_gpu_lm_more import DEV, DT, check_prompt, close, gen, heads_of, ints  # noqa: E402
 
 
 # ---- prompt attention -------------------------------------------------------------
@@ -30,6 +30,22 @@ def test_prompt_holds_its_weights_in_24_bits(dtype, dim, seqs, n):
     y = cs.prompt_attention(q.to(DEV), k.to(DEV), v.to(DEV), ints(offsets), causal=False, scale=1.0)
     every = lambda t: t[:, None].expand(-1, n, -1, -1).reshape(seqs * n, 8, dim).repeat_interleave(2, 1)  # noqa: E731
     close(y, every(want), every(bits.bound(want, mag, DT[dtype])), "bits")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim", [32, 128, 256])
+@pytest.mark.parametrize("counts", [[2, 1, 5], [400, 150], [300] * 16], ids=str)
+def test_prompt_averages_values_near_the_largest_number(dtype, dim, counts):
+    """An average lies among its values; their sum leaves fp32 from the second one on."""
+    say("case prompt large values", dtype, dim, counts)
+    q, k, v = heads_of(gen(dim), sum(counts), 4, 2, dim, DT[dtype], fused=False)
+    v = (torch.sign(v.float()) * 3.2e38 * (0.5 + torch.sigmoid(v.float()) / 2)).to(DT[dtype])
+    v[:, 0] = v[:, 0].abs()
+    y = check_prompt(q, k, v, counts)
+    assert bool(torch.isfinite(y).all())
+    check_prompt(q, k, v, counts, True, 40)
+    v[counts[0] - 1, 0, 3] = float("-inf")  # reaches the rows that see it, which is one
+    check_prompt(q, k, v, counts)
 
 
 # ---- codes ------------------------------------------------------------------------
