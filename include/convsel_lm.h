@@ -227,7 +227,7 @@ typedef struct convsel_prompt_desc {
   int32_t dtype;             /* of q, k, v and y */
   int32_t causal;
   int32_t window; /* 0: none */
-  float scale;    /* finite */
+  float scale;    /* of magnitude 2^127 at most */
   int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
   int64_t v_token_stride, v_head_stride, y_token_stride, y_head_stride;
 } convsel_prompt_desc_t;

@@ -202,7 +202,9 @@ conv_status_t prompt_sizes(const convsel_prompt_desc_t* d) {
   if (d->kv_heads < 1 || d->kv_heads > 32767 || d->q_heads < 1 || d->q_heads > 65535 || d->q_heads % d->kv_heads != 0)
     return CONV_ERR_INVALID_ARG;
   if (d->head_dim < 1 || d->head_dim > 256 || d->tokens > kAttentionRowsMax / d->q_heads) return CONV_ERR_INVALID_ARG;
-  if (!dtype_ok(d->dtype) || !flag_ok(d->causal) || d->window < 0 || !isfinite(d->scale)) return CONV_ERR_INVALID_ARG;
+  // The scale times log2 e stays within fp32.
+  if (!dtype_ok(d->dtype) || !flag_ok(d->causal) || d->window < 0 || !(fabsf(d->scale) <= 0x1p127f))
+    return CONV_ERR_INVALID_ARG;
   const int64_t t = d->tokens;
   if (!stride_ok(d->q_token_stride, t) || !stride_ok(d->q_head_stride, d->q_heads) ||
       !stride_ok(d->k_token_stride, t) || !stride_ok(d->k_head_stride, d->kv_heads) ||

@@ -205,8 +205,8 @@ __global__ __launch_bounds__(64 * kWaves, (Shape<T, NC, R>::PER_CU)) void prompt
         for (int x = 0; x < 4; ++x) qf[u].d[x] ^= ES == 2 ? 0x80008000u : 0x80000000u;
     }
   }
-  // Never zero: a masked score of -inf times it stays -inf.
-  const float cs = fmaxf(fabsf(a.scale), 0x1p-126f);
+  // Never zero: a masked score of -inf times it stays -inf.  The largest score times the least number is 2^-21.
+  const float cs = fmaxf(fabsf(a.scale), 0x1p-149f);
   const float share = __builtin_amdgcn_ldexpf(1.f, __builtin_clz(sp.count) - 32);
   f32x16_t o[NC];
 #pragma unroll

@@ -48,6 +48,21 @@ def test_prompt_averages_values_near_the_largest_number(dtype, dim, counts):
     check_prompt(q, k, v, counts)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.0, 2.0 ** -133, -2.0 ** -130, 2.0 ** -126])
+def test_prompt_scales_below_the_least_normal_number(dtype, scale):
+    """Scores of up to 2^126 times such scales are small, and at a scale of zero all weights are alike."""
+    q, k, v = heads_of(gen(7), 200, 4, 2, 16, DT[dtype], fused=False)
+    q = torch.full_like(q, 2.0 ** 60)
+    k = (2.0 ** 62 * torch.sigmoid(k.float())).to(DT[dtype])
+    check_prompt(q, k, v, [120, 80], True, 0, scale)
+
+
+def test_prompt_scale_of_the_largest_size():
+    q, k, v = heads_of(gen(8), 60, 2, 1, 32, torch.float32, fused=False)
+    check_prompt(q * 2.0 ** -60, k * 2.0 ** -68, v, [60], True, 0, 2.0 ** 127)
+
+
 # ---- codes ------------------------------------------------------------------------
 
 def powers(g, n, low, high):

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import ref_prompt_bits as bits
+from test_lm_more_host import INVALID, prompt, prompt_bytes, prompt_desc
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=str)
@@ -17,3 +18,10 @@ def test_bound_of_cancelling_values_tells_16_bits_of_a_weight_from_24(dtype):
     high = w.bfloat16().float()
     two = high.double() + (w - high).bfloat16().double()
     assert bool(((bits.result(v, two, places, 3)[0] - want).abs() > limit).any())
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 127 * (1 + 2.0 ** -23), -2.5e38, 3.4e38])
+def test_prompt_scales_beyond_their_range_are_refused(scale):
+    """In powers of two they would be infinite: a score of zero times them is NaN."""
+    assert prompt(prompt_desc(scale=scale)) == INVALID and prompt_bytes(prompt_desc(scale=scale))[0] == INVALID
+    assert prompt_bytes(prompt_desc(scale=2.0 ** 127))[0] == prompt_bytes(prompt_desc(scale=-2.0 ** 127))[0] == 0
