@@ -87,7 +87,7 @@ struct Shape {
   static constexpr int ES = elem<T>::bytes, UE = elem<T>::per16;
   static constexpr int G = kWaves / R, ROWS = 32 * R;
   static constexpr int SB = ES == 2 && G == 1 ? 2 : 1;        // blocks of 32 keys of a wave
-  static constexpr int KT = 32 * SB * G;                      // keys
+  static constexpr int KT = 32 * SB * G;                      // keys; prompt_attention_describe() says them too
   static constexpr int RB = 32 * NC * ES, U = RB / 16;        // bytes and units of a row
   static constexpr int QU = U / 2;                            // units of a lane's half of a row
   static constexpr int TILE = KT * RB, NDMA = TILE / 1024 / kWaves;
@@ -780,9 +780,11 @@ hipError_t launch_prompt_attention(const PromptArgs& a, void* workspace, hipStre
 }
 
 void prompt_attention_describe(const PromptArgs& a, char* buf, size_t len) {
-  snprintf(buf, len, "prompt_attention kernels=%sprompt_attention_kernel rows=%d workspace=%zu",
-           prompt_attention_workspace(a) ? "prompt_pack_kernel;" : "", 32 * blocks_for(a),
-           prompt_attention_workspace(a));
+  const int blocks = blocks_for(a);
+  const int keys = blocks == 4 ? (a.dtype == CONV_F32 ? 32 : 64) : 128 / blocks;  // Shape::KT
+  const size_t workspace = prompt_attention_workspace(a);
+  snprintf(buf, len, "prompt_attention kernels=%sprompt_attention_kernel rows=%d keys=%d workspace=%zu",
+           workspace ? "prompt_pack_kernel;" : "", 32 * blocks, keys, workspace);
 }
 
 }  // namespace convsel

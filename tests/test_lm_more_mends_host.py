@@ -4,6 +4,7 @@ there to refuse.  No GPU."""
 import pytest
 import torch
 
+import paper_2410_08300_amd as cs
 import ref_prompt_bits as bits
 from test_lm_more_host import INVALID, prompt, prompt_bytes, prompt_desc
 
@@ -25,3 +26,11 @@ def test_prompt_scales_beyond_their_range_are_refused(scale):
     """In powers of two they would be infinite: a score of zero times them is NaN."""
     assert prompt(prompt_desc(scale=scale)) == INVALID and prompt_bytes(prompt_desc(scale=scale))[0] == INVALID
     assert prompt_bytes(prompt_desc(scale=2.0 ** 127))[0] == prompt_bytes(prompt_desc(scale=-2.0 ** 127))[0] == 0
+
+
+@pytest.mark.parametrize("dtype,seqs,tokens,rows,keys", [
+    (torch.bfloat16, 14, 14 * 301, 128, 64), (torch.float32, 14, 14 * 301, 128, 32), (torch.bfloat16, 5, 1850, 64, 64),
+    (torch.float32, 64, 192, 64, 64), (torch.bfloat16, 2, 850, 32, 128), (torch.float32, 2, 850, 32, 128)], ids=str)
+def test_prompt_is_described_by_rows_and_keys(dtype, seqs, tokens, rows, keys):
+    text = cs.describe_prompt_attention(seqs, tokens, 16, 8, 64, dtype)
+    assert "rows=%d keys=%d " % (rows, keys) in text, text
