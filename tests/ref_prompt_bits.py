@@ -49,3 +49,48 @@ def bound(y, mag, dtype):
     rather than rounded (18).  Zeros add nothing, the largest score is zero, and sum and quotient are errors of the
     small result itself.  With them and the output's rounding: 22, and half a step of the type."""
     return ref.half_ulp(dtype) * y.abs() + 22 * 2.0 ** -24 * mag
+
+
+def cut(t, bits):
+    """fp32 values rounded to so many bits."""
+    m, e = torch.frexp(t.double())
+    return torch.ldexp(torch.round(m * 2.0 ** bits), e - bits).float()
+
+
+def plain_f32(q, k, v, causal, window, scale, weights=lambda w: w):
+    """One sequence in fp32 steps throughout, each product and each addition rounded: scores summed over the columns one
+    by one, results over the keys."""
+    n, hq, dim = q.shape
+    i, j = torch.arange(n)[:, None], torch.arange(n)[None, :]
+    seen = (j <= i) if causal else torch.ones(n, n, dtype=torch.bool)
+    if window:
+        seen = seen & (j > i - window)
+    y = torch.zeros(n, hq, v.shape[2])
+    for h in range(hq):
+        a = h // (hq // k.shape[1])
+        s = torch.zeros(n, n)
+        for d in range(dim):
+            s += q[:, h, d, None] * k[None, :, a, d]
+        s = torch.where(seen, s * scale, -float("inf"))
+        w = weights(torch.exp(s - s.max(1, keepdim=True).values))
+        for r in range(n):
+            y[:, h] += w[:, r, None] * v[r, a]
+        y[:, h] /= w.sum(1, keepdim=True)
+    return y
+
+
+def far(y, want):
+    """Root of the mean squared error, for each head."""
+    return (ref.f64(y) - want).pow(2).mean((0, 2)).sqrt()
+
+
+# fp32 calls round as plain_f32() does, but for fused products (half its roundings) and the exponent in powers of two
+# (one more): twice its error is a bound.
+F32_CASES = [(513, 64, True, 0), (450, 128, True, 0), (300, 200, False, 0), (700, 80, True, 257), (100, 128, True, 0)]
+
+
+def f32_case(n, dim):
+    g = torch.Generator().manual_seed(n + dim)
+    sharp = 1 + 2 * torch.rand(4, 1, generator=g)
+    return (torch.randn(n, 4, dim, generator=g) * sharp, torch.randn(n, 2, dim, generator=g),
+            torch.randn(n, 2, dim, generator=g))

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+import ref_lm_more as more
 import ref_prompt_bits as bits
 from gpu_util import say
 
@@ -61,6 +62,78 @@ def test_prompt_scales_below_the_least_normal_number(dtype, scale):
 def test_prompt_scale_of_the_largest_size():
     q, k, v = heads_of(gen(8), 60, 2, 1, 32, torch.float32, fused=False)
     check_prompt(q * 2.0 ** -60, k * 2.0 ** -68, v, [60], True, 0, 2.0 ** 127)
+
+
+@pytest.mark.parametrize("n,dim,causal,window", bits.F32_CASES)
+def test_prompt_in_fp32_is_as_near_as_fp32_steps(n, dim, causal, window):
+    say("case prompt fp32", n, dim, causal, window)
+    q, k, v = bits.f32_case(n, dim)
+    want = more.prompt(q, k, v, [0, n], causal, window, dim ** -0.5)[0]
+    limit = 2 * bits.far(bits.plain_f32(q, k, v, causal, window, dim ** -0.5), want)
+    for copies in (1, 2, 14):  # 32 to 128 rows a workgroup
+        y = cs.prompt_attention(*(t.repeat(copies, 1, 1).to(DEV) for t in (q, k, v)),
+                                ints([n * i for i in range(copies + 1)]), causal=causal, window=window)
+        for part in y.split(n):
+            found = bits.far(part, want)
+            assert bool((found <= limit).all()), (found, limit)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("offsets,like", [
+    ([0, 100], [0, 64]), ([-5, 30, 64], [0, 30, 64]), ([0, 20, 2 ** 31 - 1], [0, 20, 64]), ([70, 80], None),
+    ([-2 ** 31, -1], None), ([0, 50, 20, 64], []), ([2 ** 31 - 1, -2 ** 31, 5], []), ([64, 0], [])], ids=str)
+def test_prompt_offsets_outside_the_tokens(offsets, like, dtype):
+    """Clamped to the tokens; nothing beside the result is written, and what does not rise may give anything there."""
+    say("case prompt offsets", offsets, dtype)
+    q, k, v = heads_of(gen(6), 64, 4, 2, 32, DT[dtype], fused=False)
+    held = torch.full((64 + 2 * 200, 4, 32), 7.0, dtype=DT[dtype], device=DEV)
+    out = held[200:264]
+    cs.prompt_attention(q, k, v, ints(offsets), out=out)
+    assert bool((held[:200] == 7).all()) and bool((held[264:] == 7).all())
+    if like is None:
+        assert bool((out == 7).all())
+    elif like:
+        assert torch.equal(out, cs.prompt_attention(q, k, v, ints(like)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("counts,dim,window", [([5003], 64, 0), ([4097, 1000], 128, 3000), ([6000], 32, 5500)], ids=str)
+def test_prompt_of_thousands_of_tokens(dtype, counts, dim, window):
+    say("case prompt long", dtype, counts, dim, window)
+    q, k, v = heads_of(gen(sum(counts)), sum(counts), 2, 1, dim, DT[dtype])
+    check_prompt(q, k, v, counts, True, window)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prompts_beyond_one_launch(dtype):
+    """More sequences than a launch's third axis holds: one token each, whose result is its value, to three roundings in
+    fp32: of the value times a weight near one, of one over that weight (their only sum), and of the product of both.
+    bf16's own rounding takes them back."""
+    say("case prompt launches", dtype)
+    n = 140001
+    q, k, v = heads_of(gen(1), n + 90, 2, 1, 32, DT[dtype])
+    offsets = torch.arange(n + 2, device=DEV, dtype=torch.int32)
+    offsets[-1] = n + 90
+    y = cs.prompt_attention(q, k, v, offsets)
+    off = (y[:n].double() - v[:n].double()).abs()
+    assert bool((off <= (3.01 * 2.0 ** -24 if dtype == "f32" else 0) * v[:n].double().abs()).all())
+    want, mag, smag = more.prompt(q[n:], k[n:], v[n:], [0, 90], True, 0, 32 ** -0.5)
+    close(y[n:], want, more.prompt_bound(want, mag, smag, 90, 32, DT[dtype]), "last")
+
+
+@pytest.mark.parametrize("dtype,es", [("bf16", 2), ("f32", 4)])
+def test_prompt_rows_as_far_apart_as_a_tile_reaches(dtype, es):
+    """The last rows of a tile lie 2 GiB behind its first; rows further apart are copied."""
+    say("case prompt strides", dtype)
+    near = 2 ** 31 // 128 // es - 256
+    q, k, v = heads_of(gen(2), 150, 4, 2, 64, DT[dtype], fused=False)
+    for step in (near, near + 256):
+        held = torch.empty(149 * step + 2 * 128, dtype=DT[dtype], device=DEV)
+        kk = torch.as_strided(held, (150, 2, 64), (step, 128, 1))
+        vv = torch.as_strided(held, (150, 2, 64), (step, 128, 1), 64)
+        kk.copy_(k), vv.copy_(v)
+        check_prompt(q, kk, vv, [150])
+        check_prompt(q, kk, vv, [21, 129], False)
 
 
 # ---- codes ------------------------------------------------------------------------

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2410_08300_amd as cs
+import ref_lm_more as more
 import ref_prompt_bits as bits
 from test_lm_more_host import INVALID, prompt, prompt_bytes, prompt_desc
 
@@ -34,3 +35,13 @@ def test_prompt_scales_beyond_their_range_are_refused(scale):
 def test_prompt_is_described_by_rows_and_keys(dtype, seqs, tokens, rows, keys):
     text = cs.describe_prompt_attention(seqs, tokens, 16, 8, 64, dtype)
     assert "rows=%d keys=%d " % (rows, keys) in text, text
+
+
+@pytest.mark.parametrize("n,dim,causal,window", bits.F32_CASES)
+def test_bound_of_fp32_prompts_refuses_16_bits(n, dim, causal, window):
+    q, k, v = bits.f32_case(n, dim)
+    want = more.prompt(q, k, v, [0, n], causal, window, dim ** -0.5)[0]
+    limit = 2 * bits.far(bits.plain_f32(q, k, v, causal, window, dim ** -0.5), want)
+    weights = bits.plain_f32(q, k, v, causal, window, dim ** -0.5, lambda w: bits.cut(w, 16))
+    scores = bits.plain_f32(bits.cut(q, 16), bits.cut(k, 16), v, causal, window, dim ** -0.5)
+    assert bool((bits.far(weights, want) > limit).all()) and bool((bits.far(scores, want) > limit).all())
