@@ -3,9 +3,10 @@
 // A workgroup owns 8 THREADS STEPS neighbouring tokens of a row, eight at a time
 // a thread, whose logits are on their way while it counts in LDS how often its row's
 // history holds each of them (whole numbers, in any order).  What bounds it:
-// traffic (256 rows of 128000 in fp32 without a history: 52 us, 5.0 TB/s, a copy's
-// rate), and the history, which every workgroup of a row reads from the caches (in
-// bf16 with histories of 2000: 34 us, 3.9 TB/s).
+// traffic (256 rows of 128000 in fp32 without a history: 51 us, 5.1 TB/s, a copy's
+// rate; in bf16, whose results stay in the caches, 28 us, 4.7 TB/s), and the
+// history, which every workgroup of a row reads from the caches (in bf16 with
+// histories of 2000: 44 us, 3.0 TB/s).
 #include "lm_common.hpp"
 #include "lm_kernels.hpp"
 
@@ -29,8 +30,10 @@ __device__ __forceinline__ void get8(const T* p, float (&z)[8]) {
     for (int e = 0; e < UE; ++e) z[u * UE + e] = elem<T>::to_f32(vec16_get<T>(v, e));
   }
 }
-// Stored past the caches where there is more than they hold: what a call reads then stays in them (256 rows of 128000
-// in bf16 with histories of 2000: 44 us, 34 so; in fp32, 64 and 61).
+// Stored past the caches where they would not keep it: what a call reads then stays in them, and what it wrote does not.
+// us of the call and an argmax of its results, past the caches and not, histories of 600: bf16, 16 MB 61.8 and 52.0, 66
+// MB 89.5 and 79.9, 98 MB 110.5 and 110.8, 131 MB 127.7 and 129.7; fp32, 16 MB 60.8 and 49.2, 98 MB 93.8 and 95.3, 131
+// MB 105.7 and 109.9, 164 MB 121.2 and 124.9.
 typedef uint32_t words_t __attribute__((ext_vector_type(4), aligned(2)));
 template <bool PAST>
 __device__ __forceinline__ void put16(void* p, const words_t& w) {
@@ -154,6 +157,12 @@ __global__ __launch_bounds__(THREADS) void adjust_logits_kernel(LogitsArgs a, in
   }
 }
 
+// More bytes of results than the caches keep for who reads them next.
+template <typename T>
+bool past_caches(const LogitsArgs& a) {
+  return a.rows * a.vocab * (int64_t)sizeof(T) > (int64_t)96 << 20;
+}
+
 template <typename T, int THREADS, int STEPS, bool PAST>
 hipError_t launch(const LogitsArgs& a, hipStream_t st) {
   constexpr int chunk = THREADS * kEach * STEPS;
@@ -163,21 +172,30 @@ hipError_t launch(const LogitsArgs& a, hipStream_t st) {
                      a.history ? chunk * 4 : 0, st, a, chunks);
   return hipGetLastError();
 }
+template <typename T, int THREADS, int STEPS>
+hipError_t launch(const LogitsArgs& a, hipStream_t st) {
+  return past_caches<T>(a) ? launch<T, THREADS, STEPS, true>(a, st) : launch<T, THREADS, STEPS, false>(a, st);
+}
 
 template <typename T>
 hipError_t launch_steps(const LogitsArgs& a, hipStream_t st) {
-  // Threads and steps, in us with 256 x 1, 256 x 4, 512 x 2 and 1024 x 4:
-  //   bf16, 8 rows of 128000, histories of 2000 and 1 of 8000    5.4 8.7 6.0 9.1 | 7.2 12.1 6.8 10.1
-  //         32 and 256 of 128000, 2000                           9.7 10.1 8.1 10.4 | 46.9 47.5 43.6 44.6
-  //         64 of 128000, 8000                                   24.3 18.7 16.6 13.5
-  //   fp32, 256 of 128000, 600, and with a bias and a mask       62.0 63.9 64.9 71.5 | 71.3 68.7 70.9 75.1
-  //         16 of 200000, 8000                                   15.0 15.1 12.2 14.4
+  // Threads and steps, in us of the call alone with 256 x 1, 512 x 2 and 1024 x 4:
+  //   bf16, 512 rows of 500, 8 of 128000, histories of 200, 2000    4.9 5.2 9.6 | 5.3 5.8 9.2
+  //         32, 64 and 256 of 128000, 2000                          9.9 8.0 10.5 | 14.2 12.7 11.9 | 47.2 43.8 44.9
+  //         1, 64 and 256 of 128000, 8000                           7.2 6.8 10.1 | 24.4 16.6 13.9 | 82.6 54.3 51.5
+  //   fp32, 64 and 256 of 128000, 1000 (the last past the caches)   16.2 16.8 15.7 | 53.0 58.7 67.2
+  //         256 of 128000, 600, bias and mask; 8000                 57.9 60.0 63.8 | 88.2 70.9 70.9
+  //         16 of 200000, 8000                                      14.0 11.1 12.8
   // Few logits need many workgroups, long histories few readers of them.
-  const int64_t units = a.rows * ((a.vocab + 8191) / 8192);
-  const bool longs = a.tokens / a.rows >= 4000;
-  if (units < 256) return longs ? launch<T, 512, 2, false>(a, st) : launch<T, 256, 1, false>(a, st);
-  if (longs && units >= 1024) return launch<T, 1024, 4, true>(a, st);
-  return sizeof(T) == 4 && !longs ? launch<T, 256, 4, true>(a, st) : launch<T, 512, 2, true>(a, st);
+  const int64_t logits = a.rows * a.vocab;
+  const bool few = logits < 256 * 8192, longs = a.tokens / a.rows >= 4000;
+  if constexpr (sizeof(T) == 4) {
+    if (!longs) return launch<T, 256, 1>(a, st);
+  } else {
+    if (few && !longs) return launch<T, 256, 1, false>(a, st);
+  }
+  if (few) return launch<T, 512, 2, false>(a, st);
+  return longs && logits >= 6000000 ? launch<T, 1024, 4>(a, st) : launch<T, 512, 2>(a, st);
 }
 
 }  // namespace

@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+import ref_lm as ref
 import ref_lm_more as more
 import ref_prompt_bits as bits
 from gpu_util import say
@@ -164,3 +165,26 @@ def test_int8_results_of_scales_far_apart(m, i, o, low, high):
     want = torch.where(near, 0.0, torch.where(want.abs() > most, want * np.inf, want))
     y = torch.where(near, 0.0, y.cpu())
     close(y, want, 3.01 * 2.0 ** -24 * want.abs() + 2.0 ** -149, "scales")
+
+
+# ---- logits -----------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,n,vocab", [("bf16", 260, 200003), ("f32", 130, 200003), ("bf16", 120, 70001),
+                                           ("f32", 120, 70001), ("bf16", 512, 500)])
+@pytest.mark.parametrize("seen", [40, 4100])
+def test_logits_of_every_width_and_store(dtype, n, vocab, seen):
+    """Results of more than 96 MiB go past the caches; rows are those of one alone, on any alignment."""
+    say("case logits stores", dtype, n, vocab, seen)
+    x = torch.randn(n, vocab, generator=gen(n), device=DEV).to(DT[dtype])
+    h = torch.randint(0, vocab, (n * seen,), generator=gen(1), device=DEV, dtype=torch.int32)
+    off = torch.arange(n + 1, device=DEV, dtype=torch.int32) * seen
+    p = [0.5 + torch.rand(n, generator=gen(2 + i), device=DEV) for i in range(3)]
+    mask = torch.randint(-2 ** 31, 2 ** 31, (n, (vocab + 31) // 32), generator=gen(9), device=DEV).to(torch.int32)
+    whole = cs.adjust_logits(x, h, off, None, *p, mask=mask)
+    for b in (0, 1, n // 2, n - 1):
+        one = cs.adjust_logits(x[b:b + 1], h[b * seen:(b + 1) * seen], ints([0, seen]), None, *(t[b:b + 1] for t in p),
+                               mask=mask[b:b + 1])
+        assert torch.equal(whole[b], one[0])
+    want, mag = more.logits(x[n - 1:], h[-seen:].tolist(), [0, seen], None, *(t[n - 1:] for t in p), None, mask[n - 1:])
+    size = torch.where(torch.isfinite(want), want.abs(), 0.0)
+    close(whole[n - 1:], want, 6 * 2.0 ** -24 * mag + 1.01 * ref.half_ulp(x.dtype) * size + 1e-37, "stores")
