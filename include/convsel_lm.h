@@ -270,7 +270,8 @@ conv_status_t convsel_quantize_rows(const void* x, int8_t* codes, float* scales,
  * less where ldw is, can be read; what they hold does not matter), sw their O scales.  x is
  * codes with m scales sx (x_dtype CONVSEL_CODES) or numbers (CONV_F32, CONV_BF16;
  * sx NULL), which are coded by rows as above within the call.  The sum is exact;
- * scales, bias, activation and residual are fp32, and y is rounded once. */
+ * scales (any: their product may leave fp32 where the result does not), bias,
+ * activation and residual are fp32, and y is rounded once. */
 #define CONVSEL_CODES (-1)
 typedef struct convsel_linear_int8_desc {
   int64_t m, in_features, out_features; /* in < 2^17, out < 2^26, m * out <= 2^35 */

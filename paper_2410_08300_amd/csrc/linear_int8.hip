@@ -5,13 +5,14 @@
 // Many rows go in the tiles of linear_tiles.hip, whose walk of 16-byte units is
 // the same for codes, sixteen a unit; few stream the weights through registers
 // (here).  Rows of x that come as numbers are coded by a kernel before the
-// product (4096 rows of 4096 in bf16: 13 us, 3.8 TB/s), one or two of them by the
+// product (4096 rows of 4096 in bf16: 13.6 us, 3.7 TB/s), one or two of them by the
 // product's own.
 //
 // What bounds it: few rows, the weights' way from memory (1 row, 4096 -> 4096:
 // 6.5 us in the kernel, 2.6 TB/s, of which launch and first loads are half); many,
 // the matrix cores at the clock that the card's power leaves (4096 rows, 4096 ->
-// 16384: 231 us, 2380 TOP/s; a large library product reaches 2130).
+// 16384: 231 us, 2380 TOP/s, 251 on a card of lower clock; a large library product
+// reaches 2130).
 #include <stdio.h>
 
 #include <type_traits>
@@ -89,7 +90,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(CodeArgs a, int vec)
   const T* x = reinterpret_cast<const T*>(a.x) + row * a.ldx;
   int8_t* codes = a.codes + row * a.ldc;
   const bool whole = a.ldc % kCoded == 0 && reinterpret_cast<uintptr_t>(a.codes) % kCoded == 0;
-  // The first 8192 numbers of a row stay in registers (4096 rows of 4096 in bf16: 12 us, 16 when they are read again).
+  // The first 8192 numbers of a row stay in registers (4096 rows of 4096 in bf16: 13.6 us, 4 more when they are read again).
   constexpr int HELD = 4, STEP = 256 * kCoded;
   const int64_t k0 = threadIdx.x * kCoded;
   float top = 0.f, held[HELD][kCoded], z[kCoded];

@@ -364,8 +364,8 @@ constexpr Place place_of(int n) {
   return k <= r ? Place{r, k} : Place{k - r - 1, r};
 }
 
-// Tiles of 256 in bf16 and of codes: four waves, one to each SIMD, of 128 x 128.  (Eight waves of 128 x 64 read half as much again
-// from LDS, which took a quarter longer.)  Products of 16 x 16 x 32: alone, on random operands, they reach 2065
+// Tiles of 256 in bf16 and of codes: four waves, one to each SIMD, of 128 x 128.  (Eight waves of 128 x 64 read half as
+// much again from LDS, which took a quarter longer.)  Products of 16 x 16 x 32: alone, on random operands, they reach 2065
 // TFLOP/s, those of 32 x 32 x 16 1810, because the card's power bounds both (5 % less time here).  The ring holds five
 // units of one operand's 256 rows and one k-tile, in the order w, x, w, x ...; a wave reads all of a k-tile's operands
 // in its first half, so that a unit is on its way for three quarters of a k-tile at least.
@@ -614,15 +614,15 @@ hipError_t launch_all(const LinearArgs& a0, const LinearTiles& p, void* workspac
   char* ws = (char*)workspace;
   if constexpr (!operand<T>::codes) {
     if (p.pack) {
-    const int64_t per = elem<T>::per16, padded = (a0.in + per - 1) / per * per;
-    const int64_t units = (a0.m + a0.out) * (padded / per);
-    const int64_t blocks = (units + 255) / 256;
-    hipLaunchKernelGGL(linear_pack_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, st, a0,
-                       (T*)ws, padded);
-    a.g.x = ws;
-    a.g.w = ws + a0.m * padded * sizeof(T);
-    a.g.in = a.g.ldx = padded;
-    ws += p.pack_bytes;
+      const int64_t per = elem<T>::per16, padded = (a0.in + per - 1) / per * per;
+      const int64_t units = (a0.m + a0.out) * (padded / per);
+      const int64_t blocks = (units + 255) / 256;
+      hipLaunchKernelGGL(linear_pack_kernel<T>, dim3((unsigned)(blocks < 16384 ? blocks : 16384)), dim3(256), 0, st,
+                         a0, (T*)ws, padded);
+      a.g.x = ws;
+      a.g.w = ws + a0.m * padded * sizeof(T);
+      a.g.in = a.g.ldx = padded;
+      ws += p.pack_bytes;
     }
   }
   const int side = kSide[p.config];
@@ -649,7 +649,8 @@ hipError_t launch_all(const LinearArgs& a0, const LinearTiles& p, void* workspac
   }
   if (e != hipSuccess || p.splits == 1) return e;
   const int64_t quads = (a0.out + 3) / 4 * a0.m;
-  hipLaunchKernelGGL((linear_join_kernel<Y, operand<T>::codes>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((linear_join_kernel<Y, operand<T>::codes>), dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st,
+                     a);
   return hipGetLastError();
 }
 

@@ -23,14 +23,14 @@
 // rounded one, where fp32 steps throughout leave 0.08 and three numbers 0.06.
 // fp32 calls use the fp32 matrix instructions.
 //
-// What bounds it.  Heads of 128 and more, long: the matrix cores, two thirds of
-// whose work with values is the weights' second and third numbers, at the clock
-// that the card's power leaves (8192 tokens of 32 heads on 8, causal: 900 us, 611
-// TFLOP/s, 1220 with those numbers).  Heads of 64: the vector unit beside them
-// (8192 tokens of 16 on 4: 295 us, 466 TFLOP/s); a weight costs a fused product, a
-// transcendental (four slots), an addition, seven halves of an operation for its
-// three numbers and half a maximum.  fp32: the
-// fp32 products (2048 tokens of 12 heads of 128 on 4: 162 us, 80 TFLOP/s).
+// What bounds it.  Heads of 128 and more, long: the matrix cores (64 % busy at 1.84
+// GHz), two thirds of whose work with values is the weights' second and third
+// numbers, and the vector unit beside them (50 %): 8192 tokens of 32 heads on 8,
+// causal: 917 us, 600 TFLOP/s, 1200 with those numbers (980 on a card of lower
+// clock).  Heads of 64: the vector unit (75 % busy; 8192 tokens of 16 on 4: 300 us,
+// 458 TFLOP/s); a weight costs a fused product, a transcendental (four slots), an
+// addition, seven halves of an operation for its three numbers and half a maximum.
+// fp32: the fp32 products (2048 tokens of 12 heads of 128 on 4: 160 us, 81 TFLOP/s).
 #include <stdio.h>
 
 #include <type_traits>
@@ -703,18 +703,20 @@ UnitRow units_for(const PromptArgs& g, int blocks) {
 }
 
 // Blocks of 32 rows a workgroup: four, or, where that gives few workgroups, two or one, whose keys the waves share out.
-// us of a call (and 8 of a graph's launch) with four, two and one:
-//   bf16, 32/8 heads of 128, 700, 1024, 2048 tokens   27 24 36 | 36 30 53 | 72 74 137
-//         8/8 heads of 128, 1024, 2048, 4096          32 25 22 | 55 40 38 | 104 81 106
-//         16/4 heads of 64, 1024, 2048, 4096          25 21 17 | 41 32 32 | 86 75 85
-//         8/2 heads of 256, 4096, 8192                170 125 | 389 460
-//   fp32, 8/8 heads of 64, 300, 1024, 2048            34 22 18 | 88 51 33 | 167 92 62
-//         12/4 heads of 80, 300, 1024, 2048           44 28 24 | 122 70 47 | 233 135 143
-//         32/8 heads of 128, 300, 701                 56 36 30 | 114 67 81
-// One block has most to join, so sequences are to be long enough for it.  us of the kernel alone:
-//   bf16, 8/8 heads of 128, 64, 200, 400 tokens        6 7 8 | 11 9 9 | 15 12 11
-//         16/4 heads of 64, 64, 200, 400               6 5 6 | 8 7 6 | 11 9 8
-//   fp32, 12/4 heads of 80, 37, 100                    12 9 10 | 19 13 10
+// us of the kernel with four, two and one:
+//   bf16, 32/8 heads of 128, 512, 700, 1024, 2048 tokens   21 16 20 | 28 21 32 | 37 29 49 | 82 78 141
+//         8/8 heads of 128, 400, 1024, 2048, 4096          18 13 12 | 36 24 19 | 64 43 38 | 122 91 115
+//         16/4 heads of 64, 400, 1024, 2048, 4096          13 10 8 | 25 17 13 | 44 31 31 | 94 82 95
+//         8/2 heads of 256, 4096, 8192                     211 154 | 478 546
+//   fp32, 8/8 heads of 64, 300, 1024, 2048                 29 18 13 | 85 47 29 | 165 88 58
+//         12/4 heads of 80, 300, 1024, 2048                40 24 18 | 118 64 40 | 230 123 129
+//         32/8 heads of 128, 300, 701                      50 31 25 | 106 61 72
+// One block has most to join, so sequences are to be long enough for it:
+//   bf16, 8/8 heads of 128, 64, 200 tokens                 6.8 6.9 8.3 | 12.5 9.8 9.4
+//         16/4 heads of 64, 64, 200                        6.0 5.3 5.6 | 9.0 7.3 6.4
+//   fp32, 12/4 heads of 80, 37, 100                        11.7 8.8 9.7 | 18.5 12.4 9.7
+// Every sequence counts as a workgroup of each head at least, so many short ones beside a long one lead to four blocks
+// too early (2048 tokens of 8/8 heads of 128 and 60 prompts of one token: 65, 42 with two).
 int blocks_for(const PromptArgs& g) {
   const bool f32 = g.dtype == CONV_F32;
   // Workgroups that are enough, of four blocks and of two.

@@ -384,7 +384,8 @@ def prompt_attention(q, k, v, offsets, causal=True, window=0, scale=None, out=No
     ``offsets`` (int32, [sequences + 1]) divides the tokens among the sequences.
     Head h reads key/value head h // (q_heads // kv_heads).  ``causal`` hides
     later tokens, ``window`` > 0 all but the last ``window`` up to the query;
-    what they hide has no influence.  ``scale`` is 1/sqrt(head_dim) by default.
+    what they hide has no influence.  ``scale`` is 1/sqrt(head_dim) by default
+    (2**127 at most in magnitude).
     Rows of ``out`` behind the last sequence are left as they were.
     """
     dt = _dtype_of("prompt_attention", q, k, v, out)
