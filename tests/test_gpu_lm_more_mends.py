@@ -188,3 +188,49 @@ def test_logits_of_every_width_and_store(dtype, n, vocab, seen):
     want, mag = more.logits(x[n - 1:], h[-seen:].tolist(), [0, seen], None, *(t[n - 1:] for t in p), None, mask[n - 1:])
     size = torch.where(torch.isfinite(want), want.abs(), 0.0)
     close(whole[n - 1:], want, 6 * 2.0 ** -24 * mag + 1.01 * ref.half_ulp(x.dtype) * size + 1e-37, "stores")
+
+
+# ---- more than 2^31 values ----------------------------------------------------------
+
+def test_prompt_of_more_than_32_bits_of_values():
+    say("case prompt beyond 2^31 values")
+    n, count = 530000, 265
+    q = torch.randn(n, 32, 128, generator=gen(3), device=DEV, dtype=torch.bfloat16)
+    k, v = q.roll(1, 1), q.roll(2, 1)
+    offsets = torch.arange(n // count + 1, device=DEV, dtype=torch.int32) * count
+    y = cs.prompt_attention(q, k, v, offsets)
+    for at in (0, n // 2 // count * count, n - count):
+        part = [t[at:at + count, 30:].clone() for t in (q, k, v)]
+        want, mag, smag = more.prompt(*part, [0, count], True, 0, 128 ** -0.5)
+        close(y[at:at + count, 30:], want, more.prompt_bound(want, mag, smag, count, 128, torch.bfloat16), "far")
+
+
+@pytest.mark.parametrize("m,i,o", [(70000, 64, 32768), (40000, 64, 60002)])
+def test_int8_of_more_than_32_bits_of_values(m, i, o):
+    say("case int8 beyond 2^31 values", m, i, o)
+    g = gen(4)
+    x = torch.randint(-128, 128, (m, i), generator=g, device=DEV, dtype=torch.int8)
+    w = torch.randint(-128, 128, (o, i), generator=g, device=DEV, dtype=torch.int8)
+    xs, ws = torch.rand(m, generator=g, device=DEV), torch.rand(o, generator=g, device=DEV) * 1e-3
+    y = cs.linear_int8(x, w, ws, x_scale=xs)
+    for rows in (slice(0, 3), slice(m // 2, m // 2 + 3), slice(m - 3, m)):  # sums are whole numbers: the same bits
+        assert torch.equal(y[rows], cs.linear_int8(x[rows], w, ws, x_scale=xs[rows]))
+    codes, scales = cs.quantize_rows(y)
+    for rows in (slice(0, 3), slice(m - 3, m)):
+        want, wanted = more.quantize(y[rows])
+        assert np.array_equal(codes[rows].cpu().numpy(), want) and np.array_equal(scales[rows].cpu().numpy(), wanted)
+
+
+def test_logits_of_more_than_32_bits_of_values():
+    say("case logits beyond 2^31 values")
+    n, vocab = 17000, 128001
+    x = torch.randn(n, vocab, generator=gen(5), device=DEV, dtype=torch.bfloat16)
+    h = torch.randint(0, vocab, (n * 20,), generator=gen(6), device=DEV, dtype=torch.int32)
+    off = torch.arange(n + 1, device=DEV, dtype=torch.int32) * 20
+    p = [0.5 + torch.rand(n, generator=gen(7 + i), device=DEV) for i in range(3)]
+    mask = torch.randint(-2 ** 31, 2 ** 31, (n, (vocab + 31) // 32), generator=gen(9), device=DEV).to(torch.int32)
+    y = cs.adjust_logits(x, h, off, None, *p, mask=mask)
+    for b in (0, n // 2, n - 1):
+        one = cs.adjust_logits(x[b:b + 1], h[b * 20:b * 20 + 20], ints([0, 20]), None, *(t[b:b + 1] for t in p),
+                               mask=mask[b:b + 1])
+        assert torch.equal(y[b], one[0])
